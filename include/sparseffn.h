@@ -309,6 +309,79 @@ SF_API int sf_ffn_step_host(const sf_ffn_desc* desc, int dense, const void* host
                      size_t fwd_ctx_bytes, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * The gated feed-forward block: three matrices, the form behind the paper's FLOP count of 18 B T D F (Section 5.1).
+ *
+ *     G = X Wg^T,  U = X Wu^T,  H = act(G) * U,  Y = H Wd^T           X, Y [T,D];  Wg, Wu [F,D];  Wd [D,F]; all bf16
+ *
+ * T >= 0 of any size (a single token and a training batch take the same call); D and F positive multiples of 8; each size at most
+ * 2^28. Tensors are contiguous. One rounding each: H (an operand of the second product) and Y; G and U stay in float32.
+ *
+ * sf_gated_ffn_fwd:  fwd_ctx NULL: inference, H lies in the workspace. Otherwise fwd_ctx receives what the backward pass needs: H in
+ *     bf16, act(G) and U act'(G) in float32 (10 bytes per token and feature). Y is the same either way.
+ * sf_gated_ffn_bwd:  dH = dY Wd;  dU = dH act(G);  dG = dH U act'(G);  dX = dG Wg + dU Wu;  dWg = dG^T X;  dWu = dU^T X;  dWd = dY^T H.
+ *     dG and dU are rounded to bf16 once. Any of the four outputs may be NULL and is then left out. With T == 0 the weights'
+ *     gradients are zero. The context is only read: the call may be repeated.
+ *     act'(0) of ReLU is 0.
+ * sf_gated_ffn_workspace_size: bytes of the context and of the workspace (the most that a call of this descriptor needs; the
+ *     forward call with a context needs the first 256 bytes only, without one 256 + 2 T F rounded up to 256). As for the
+ *     step above, the workspace's first 256 bytes are the status word: zero them once, read them with sf_check_status. Calls that may
+ *     overlap on the GPU need workspaces of their own. */
+typedef enum sf_gate_act {
+  SF_ACT_SILU = 0,       /* g / (1 + e^-g) */
+  SF_ACT_GELU = 1,       /* g Phi(g) */
+  SF_ACT_GELU_TANH = 2,  /* g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2 */
+  SF_ACT_RELU = 3,
+  SF_ACT_SQRELU = 4      /* max(g, 0)^2 */
+} sf_gate_act;
+typedef struct sf_gated_ffn_desc {
+  int64_t T, D, F;
+  int32_t act;           /* sf_gate_act; others are refused with SF_ERR_UNSUPPORTED */
+  int32_t reserved;
+} sf_gated_ffn_desc;
+SF_API int sf_gated_ffn_workspace_size(const sf_gated_ffn_desc* desc, size_t* fwd_ctx_bytes, size_t* workspace_bytes);
+SF_API int sf_gated_ffn_fwd(const sf_gated_ffn_desc* desc, const void* X, const void* Wg, const void* Wu, const void* Wd,
+                            void* Y, void* fwd_ctx, size_t fwd_ctx_bytes, void* workspace, size_t workspace_bytes,
+                            void* stream);
+SF_API int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* X, const void* Wg, const void* Wu,
+                            const void* Wd, const void* fwd_ctx, size_t fwd_ctx_bytes, void* dX, void* dWg, void* dWu,
+                            void* dWd, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Microscaled 4-bit operands (beside the E4M3 ones above): E2M1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign), two to a byte, the even
+ * column in the low nibble, and a scale sf to every block of a row. x scale, the float32 product, is quantised:
+ *
+ *     SF_FP4_NV  blocks of 16:  sf = e4m3(amax / 6), amax the block's largest |x scale|           (float32 quotient)
+ *     SF_FP4_MX  blocks of 32:  sf = 2^max(floor(log2 amax) - 2, -127)
+ *     code = e2m1(x scale / sf)   to nearest, ties to the even code, clamped at 6                  (float32 quotient)
+ *
+ * A block whose sf is 0 has codes of 0 (with the signs of x). Infinities clamp to 6 sf; a NaN makes its block's scale, and so the whole block, NaN.
+ * Scale bytes (E4M3 bits, or the exponent + 127) lie in tiles of 128 rows x 4 blocks, 512 bytes each: block c of row r is byte
+ * 16 (r % 32) + 4 (r % 128 / 32) + c % 4 of tile (r / 128) * ceil(blocks / 4) + c / 4. Of a ragged last tile the blocks beyond the
+ * row are written as 0 and must be; the rows beyond the last are neither written nor used.
+ *
+ * sf_fp4_sizes:       bytes of codes and scales of a [rows, cols] matrix.
+ * sf_fp4_quantize:    X bf16 [rows, cols] (ld >= cols, ld % 8 == 0) -> codes uint8 [rows, cols/2], scales.
+ * sf_fp4_dequantize:  Y[r, c] = bf16(code * sf * alpha), alpha normally 1 / scale (ld as above).
+ * sf_gemm_fp4:        C[Mr,Nc] = bf16(alpha * A B^T), A [Mr,K] and B [Nc,K] of one format, alpha normally 1 / (scale_A scale_B);
+ *                     float32 accumulation. With few rows of A (tokens) the other operand is streamed once.
+ * sf_gemm_fp4_gated:  H[Mr,Nc] = bf16(act(alpha_g A Bg^T) * (alpha_u A Bu^T)): the first half of the gated block on 4-bit operands.
+ * Any Mr and rows; cols and K multiples of 32; Nc a multiple of 8; sizes at most 2^28.
+ * `workspace`: sf_gemm_fp4_workspace_size() bytes, the first 256 the status word as everywhere. */
+typedef enum sf_fp4_format { SF_FP4_NV = 0, SF_FP4_MX = 1 } sf_fp4_format;
+SF_API int sf_fp4_sizes(int64_t rows, int64_t cols, int format, size_t* codes_bytes, size_t* scales_bytes);
+SF_API int sf_fp4_quantize(const void* X, int64_t rows, int64_t cols, int64_t ld, int format, float scale, void* codes,
+                           void* scales, void* stream);
+SF_API int sf_fp4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, int format, float alpha,
+                             void* Y, int64_t ld, void* stream);
+SF_API int sf_gemm_fp4_workspace_size(int64_t Mr, int64_t Nc, int64_t K, size_t* bytes);
+SF_API int sf_gemm_fp4(const void* A, const void* a_scales, const void* B, const void* b_scales, int format, void* C,
+                       int64_t Mr, int64_t Nc, int64_t K, float alpha, void* workspace, size_t workspace_bytes,
+                       void* stream);
+SF_API int sf_gemm_fp4_gated(const void* A, const void* a_scales, const void* Bg, const void* bg_scales, const void* Bu,
+                             const void* bu_scales, int format, int act, void* H, int64_t Mr, int64_t Nc, int64_t K,
+                             float alpha_g, float alpha_u, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Sparse/dense step schedule (Section 5.3.2) and speed-up arithmetic (Sections 3.1 and 5.1).
  * Host-side logic; nothing here touches the GPU except the two dispatchers.
  *

@@ -45,6 +45,14 @@ class sf_router_desc(C.Structure):
  SF_RCTX_RELU_VALS, SF_RCTX_META, SF_RCTX_Y1, SF_RCTX_DY1_VALS) = range(10)
 
 
+class sf_gated_ffn_desc(C.Structure):
+    _fields_ = [("T", C.c_int64), ("D", C.c_int64), ("F", C.c_int64), ("act", C.c_int32), ("reserved", C.c_int32)]
+
+
+SF_ACT_SILU, SF_ACT_GELU, SF_ACT_GELU_TANH, SF_ACT_RELU, SF_ACT_SQRELU = range(5)
+SF_FP4_NV, SF_FP4_MX = range(2)
+
+
 class sf_schedule(C.Structure):
     _fields_ = [("warmup_steps", C.c_int64), ("sparse_steps", C.c_int64), ("total_steps", C.c_int64)]
 
@@ -90,6 +98,17 @@ _SIGNATURES = {
     "sf_ffn_host_staging_size": (_i32, [C.POINTER(sf_ffn_desc), C.POINTER(_sz)]),
     "sf_ffn_step_host": (_i32, [C.POINTER(sf_ffn_desc), _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp,
                                 _sz, _vp]),
+    "sf_gated_ffn_workspace_size": (_i32, [C.POINTER(sf_gated_ffn_desc), C.POINTER(_sz), C.POINTER(_sz)]),
+    "sf_gated_ffn_fwd": (_i32, [C.POINTER(sf_gated_ffn_desc), _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _sz, _vp]),
+    "sf_gated_ffn_bwd": (_i32, [C.POINTER(sf_gated_ffn_desc), _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _sz,
+                                _vp]),
+    "sf_fp4_sizes": (_i32, [_i64, _i64, _i32, C.POINTER(_sz), C.POINTER(_sz)]),
+    "sf_fp4_quantize": (_i32, [_vp, _i64, _i64, _i64, _i32, C.c_float, _vp, _vp, _vp]),
+    "sf_fp4_dequantize": (_i32, [_vp, _vp, _i64, _i64, _i32, C.c_float, _vp, _i64, _vp]),
+    "sf_gemm_fp4_workspace_size": (_i32, [_i64, _i64, _i64, C.POINTER(_sz)]),
+    "sf_gemm_fp4": (_i32, [_vp, _vp, _vp, _vp, _i32, _vp, _i64, _i64, _i64, C.c_float, _vp, _sz, _vp]),
+    "sf_gemm_fp4_gated": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i64, C.c_float, C.c_float, _vp,
+                                 _sz, _vp]),
     "sf_schedule_step_kind": (_i32, [C.POINTER(sf_schedule), _i64, C.POINTER(_i32)]),
     "sf_schedule_speedup": (_i32, [C.POINTER(sf_schedule), C.c_double, C.POINTER(C.c_double)]),
     "sf_ffn_flop_fraction": (_i32, [_i64, _i64, _i64, _i64, _i64, C.POINTER(C.c_double)]),
@@ -499,6 +518,175 @@ def sf_routed_ctx_view(desc, buf: torch.Tensor, field: int) -> torch.Tensor:
     _check(lib().sf_routed_ctx_view(C.byref(desc), _ptr(buf), field, C.byref(p), C.byref(n)), "sf_routed_ctx_view")
     off = p.value - buf.data_ptr()
     return buf[off:off + n.value].view(_RCTX_DTYPES[field])
+
+
+# ---- gated feed-forward block and 4-bit operands -------------------------------------------------------
+# These calls take any number of tokens, so a tensor of another shape, type, layout or device would be read as something else
+# without a trace: they are checked here, where the sizes are still known.
+
+def _current_device() -> int:
+    return torch.cuda.current_device() if torch.cuda.is_available() else -1
+
+
+def _refuse(ok: bool, status: int, where: str, what: str) -> None:
+    if not ok:
+        raise SparseFFNError(status, f"{where}: {what}")
+
+
+def _expect(where: str, dev: int, **tensors) -> None:
+    """name=(tensor, dtype, shape): contiguous, of that type and shape, on device `dev`; a tensor of None passes."""
+    for name, (t, dtype, shape) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype is not dtype or tuple(t.shape) != shape:
+            raise SparseFFNError(SF_ERR_SHAPE, f"{where}: {name} is {t.dtype} {tuple(t.shape)}, wanted {dtype} {shape}")
+        if not t.is_contiguous():
+            raise SparseFFNError(SF_ERR_ALIGN, f"{where}: {name} is not contiguous")
+        if t.get_device() != dev:
+            raise SparseFFNError(SF_ERR_UNSUPPORTED, f"{where}: {name} is on {t.device}, the current device is {dev}")
+
+
+def make_gated_desc(T, D, F, act=SF_ACT_SILU) -> sf_gated_ffn_desc:
+    return sf_gated_ffn_desc(T, D, F, act, 0)
+
+
+def sf_gated_ffn_workspace_size(desc: sf_gated_ffn_desc):
+    a, b = _sz(), _sz()
+    _check(lib().sf_gated_ffn_workspace_size(C.byref(desc), C.byref(a), C.byref(b)), "sf_gated_ffn_workspace_size")
+    return a.value, b.value
+
+
+def alloc_gated_ffn_buffers(desc: sf_gated_ffn_desc, device="cuda", training: bool = True):
+    """(fwd_ctx, workspace); without training the context is None. The context is not initialised, the workspace is zero."""
+    c, w = sf_gated_ffn_workspace_size(desc)
+    return torch.empty((c,), dtype=torch.uint8, device=device) if training else None, _workspace(w, device)
+
+
+def _bytes_or_none(t):
+    return 0 if t is None else _nbytes(t)
+
+
+def sf_gated_ffn_fwd(desc, X, Wg, Wu, Wd, Y, fwd_ctx, workspace, stream=None):
+    """Y = (act(X Wg^T) * (X Wu^T)) Wd^T. fwd_ctx None: nothing is kept for a backward pass."""
+    T, D, F, bf = desc.T, desc.D, desc.F, torch.bfloat16
+    dev = _current_device()
+    _expect("sf_gated_ffn_fwd", dev, X=(X, bf, (T, D)), Wg=(Wg, bf, (F, D)), Wu=(Wu, bf, (F, D)), Wd=(Wd, bf, (D, F)),
+            Y=(Y, bf, (T, D)))
+    _expect_buffers("sf_gated_ffn_fwd", dev, fwd_ctx, workspace)
+    _check(lib().sf_gated_ffn_fwd(C.byref(desc), _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(Y), _ptr(fwd_ctx),
+                                  _bytes_or_none(fwd_ctx), _ptr(workspace), _bytes_or_none(workspace), _stream(stream)),
+           "sf_gated_ffn_fwd")
+
+
+def _expect_buffers(where, dev, *bufs):
+    for b in bufs:
+        if b is not None:
+            _refuse(b.is_contiguous(), SF_ERR_ALIGN, where, "a context or workspace is not contiguous")
+            _refuse(b.get_device() == dev, SF_ERR_UNSUPPORTED, where, f"a context or workspace is on {b.device}, the current device is {dev}")
+
+
+def sf_gated_ffn_bwd(desc, dY, X, Wg, Wu, Wd, fwd_ctx, dX, dWg, dWu, dWd, workspace, stream=None):
+    """Gradients of sf_gated_ffn_fwd with the context that it filled. An output of None is left out."""
+    T, D, F, bf = desc.T, desc.D, desc.F, torch.bfloat16
+    dev = _current_device()
+    _expect("sf_gated_ffn_bwd", dev, dY=(dY, bf, (T, D)), X=(X, bf, (T, D)), Wg=(Wg, bf, (F, D)), Wu=(Wu, bf, (F, D)),
+            Wd=(Wd, bf, (D, F)), dX=(dX, bf, (T, D)), dWg=(dWg, bf, (F, D)), dWu=(dWu, bf, (F, D)), dWd=(dWd, bf, (D, F)))
+    _expect_buffers("sf_gated_ffn_bwd", dev, fwd_ctx, workspace)
+    _check(lib().sf_gated_ffn_bwd(C.byref(desc), _ptr(dY), _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(fwd_ctx),
+                                  _bytes_or_none(fwd_ctx), _ptr(dX), _ptr(dWg), _ptr(dWu), _ptr(dWd), _ptr(workspace),
+                                  _bytes_or_none(workspace), _stream(stream)), "sf_gated_ffn_bwd")
+
+
+def sf_fp4_sizes(rows: int, cols: int, fmt: int):
+    a, b = _sz(), _sz()
+    _check(lib().sf_fp4_sizes(rows, cols, fmt, C.byref(a), C.byref(b)), "sf_fp4_sizes")
+    return a.value, b.value
+
+
+def _row_stride(where, name, t):
+    _refuse(t.dim() == 2 and t.dtype is torch.bfloat16, SF_ERR_SHAPE, where, f"{name} must be a bfloat16 matrix")
+    _refuse(t.shape[1] <= 1 or t.stride(1) == 1, SF_ERR_ALIGN, where, f"{name}'s rows are not contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def sf_fp4_quantize(X, fmt: int, scale: float, out=None, stream=None):
+    """(codes uint8 [rows, cols/2], scales uint8 tiles) of bf16 X, which may be a strided row view; ``out`` = a previous result
+    to write into."""
+    where, dev = "sf_fp4_quantize", _current_device()
+    ld = _row_stride(where, "X", X)
+    rows, cols = X.shape
+    _, n = sf_fp4_sizes(rows, cols, fmt)
+    codes, scales = out if out is not None else (torch.empty((rows, cols // 2), dtype=torch.uint8, device=X.device),
+                                                 torch.empty((n,), dtype=torch.uint8, device=X.device))
+    _refuse(X.get_device() == dev, SF_ERR_UNSUPPORTED, where, f"X is on {X.device}, the current device is {dev}")
+    _expect(where, dev, codes=(codes, torch.uint8, (rows, cols // 2)), scales=(scales, torch.uint8, (n,)))
+    _check(lib().sf_fp4_quantize(_ptr(X), rows, cols, ld, fmt, float(scale), _ptr(codes), _ptr(scales), _stream(stream)), where)
+    return codes, scales
+
+
+def sf_fp4_dequantize(codes, scales, fmt: int, alpha: float, out=None, stream=None):
+    """bf16 [rows, cols] = code * sf * alpha; ``out`` may be a strided row view."""
+    where, dev = "sf_fp4_dequantize", _current_device()
+    _refuse(codes.dim() == 2, SF_ERR_SHAPE, where, "codes must be a matrix")
+    rows, cols = codes.shape[0], 2 * codes.shape[1]
+    _, n = sf_fp4_sizes(rows, cols, fmt)
+    if out is None:
+        out = torch.empty((rows, cols), dtype=torch.bfloat16, device=codes.device)
+    ld = _row_stride(where, "out", out)
+    _refuse(tuple(out.shape) == (rows, cols), SF_ERR_SHAPE, where, f"out is {tuple(out.shape)}, wanted {(rows, cols)}")
+    _refuse(out.get_device() == dev, SF_ERR_UNSUPPORTED, where, f"out is on {out.device}, the current device is {dev}")
+    _expect(where, dev, codes=(codes, torch.uint8, (rows, cols // 2)), scales=(scales, torch.uint8, (n,)))
+    _check(lib().sf_fp4_dequantize(_ptr(codes), _ptr(scales), rows, cols, fmt, float(alpha), _ptr(out), ld, _stream(stream)), where)
+    return out
+
+
+def sf_gemm_fp4_workspace_size(Mr: int, Nc: int, K: int) -> int:
+    a = _sz()
+    _check(lib().sf_gemm_fp4_workspace_size(Mr, Nc, K, C.byref(a)), "sf_gemm_fp4_workspace_size")
+    return a.value
+
+
+def _fp4_operands(where, dev, fmt, K, **ops):
+    u8 = torch.uint8
+    for name, (codes, scales) in ops.items():
+        _refuse(codes.dim() == 2, SF_ERR_SHAPE, where, f"{name} must be a matrix of codes")
+        rows = codes.shape[0]
+        _expect(where, dev, **{name: (codes, u8, (rows, K // 2)), name + "_scales": (scales, u8, (sf_fp4_sizes(rows, K, fmt)[1],))})
+
+
+def sf_gemm_fp4(A, a_scales, B, b_scales, fmt: int, alpha: float, C_out=None, workspace=None, stream=None):
+    """C[Mr,Nc] = bf16(alpha * A B^T) of two 4-bit operands, codes [Mr,K/2] and [Nc,K/2] with their scales."""
+    where, dev = "sf_gemm_fp4", _current_device()
+    Mr, Nc, K = A.shape[0], B.shape[0], 2 * A.shape[1]
+    _fp4_operands(where, dev, fmt, K, A=(A, a_scales), B=(B, b_scales))
+    if C_out is None:
+        C_out = torch.empty((Mr, Nc), dtype=torch.bfloat16, device=A.device)
+    if workspace is None:
+        workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device)
+    _expect(where, dev, C_out=(C_out, torch.bfloat16, (Mr, Nc)))
+    _expect_buffers(where, dev, workspace)
+    _check(lib().sf_gemm_fp4(_ptr(A), _ptr(a_scales), _ptr(B), _ptr(b_scales), fmt, _ptr(C_out), Mr, Nc, K, float(alpha),
+                             _ptr(workspace), _nbytes(workspace), _stream(stream)), where)
+    return C_out
+
+
+def sf_gemm_fp4_gated(A, a_scales, Bg, bg_scales, Bu, bu_scales, fmt: int, act: int, alpha_g: float, alpha_u: float, H_out=None,
+                      workspace=None, stream=None):
+    """H[Mr,Nc] = bf16(act(alpha_g * A Bg^T) * (alpha_u * A Bu^T)) of 4-bit operands."""
+    where, dev = "sf_gemm_fp4_gated", _current_device()
+    Mr, Nc, K = A.shape[0], Bg.shape[0], 2 * A.shape[1]
+    _fp4_operands(where, dev, fmt, K, A=(A, a_scales), Bg=(Bg, bg_scales), Bu=(Bu, bu_scales))
+    _refuse(Bu.shape[0] == Nc, SF_ERR_SHAPE, where, f"Bg has {Nc} rows, Bu {Bu.shape[0]}")
+    if H_out is None:
+        H_out = torch.empty((Mr, Nc), dtype=torch.bfloat16, device=A.device)
+    if workspace is None:
+        workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device)
+    _expect(where, dev, H_out=(H_out, torch.bfloat16, (Mr, Nc)))
+    _expect_buffers(where, dev, workspace)
+    _check(lib().sf_gemm_fp4_gated(_ptr(A), _ptr(a_scales), _ptr(Bg), _ptr(bg_scales), _ptr(Bu), _ptr(bu_scales), fmt, act,
+                                   _ptr(H_out), Mr, Nc, K, float(alpha_g), float(alpha_u), _ptr(workspace), _nbytes(workspace),
+                                   _stream(stream)), where)
+    return H_out
 
 
 def make_schedule(warmup_steps: int, sparse_steps: int, total_steps: int) -> sf_schedule:

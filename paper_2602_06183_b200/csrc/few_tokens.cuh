@@ -1,0 +1,287 @@
+// Products of few tokens with whole weight matrices: C[T, N] = alpha A[T, K] W[N, K]^T, or the gated pair of such products, with T
+// at most kN. What bounds them is reading the weights once, so the weights are the instruction's 128 rows and the tokens its
+// few columns, and the reduction is split over the CTAs of a cluster until every SM has weights to read: each computes
+// a partial sum of its own K range in TMEM, leaves it in its shared memory, and the cluster adds the partial sums up in the order
+// of the ranges (the same every time) through distributed shared memory.
+//
+// CTA = 6 warps: TMA producer, MMA issuer, four warps that read the accumulator out. Every wait is bounded (see gemm_tc.cu); the
+// cluster barriers are reached by every warp because their own waits are.
+#pragma once
+
+#include "gated.cuh"
+
+namespace sf {
+namespace {
+
+using namespace ptx;
+
+constexpr int kFewThreads = 192;
+
+constexpr uint32_t pow2_cols(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
+
+template <int kFmt, bool kGated, int kN>
+struct FewCfg {
+  static constexpr bool kFp4 = kFmt != FMT_BF16;
+  static constexpr int kMats = kGated ? 2 : 1;
+  static constexpr int kTiles = kFmt == FMT_NV ? 4 : kFmt == FMT_MX ? 2 : 0;
+  static constexpr int kWBytes = 16384, kXBytes = kN * 128;
+  static constexpr int kScaleBytes = kTiles * 512 * (kMats + 1);
+  static constexpr int kStageBytes = kMats * kWBytes + kXBytes + kScaleBytes;
+  static constexpr int kPartBytes = kMats * kN * 128 * 4;
+  static constexpr uint32_t kScaleCol = kMats * kN, kScaleCols = kTiles * 4 * (kMats + 1);
+  static constexpr uint32_t kTmem = pow2_cols(kScaleCol + 2 * kScaleCols);
+  // two CTAs to an SM while their columns and their partial sums fit: one sets up and adds up while the other streams
+  static constexpr int kPerSm = kN <= 32 && kTmem <= 256 ? 2 : 1;
+  static constexpr int kRoom = ((kPerSm == 2 ? 115712 : 232448) - 2048) / kStageBytes;
+  static constexpr int kStages = kRoom < 8 ? kRoom : 8;
+  static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024;
+  static_assert(kStages >= 2 && kPartBytes <= kStages * kStageBytes, "shared memory");
+};
+
+struct FewArgs {
+  int T, N, nkb;                     // tokens, output columns, k-blocks (64 K of bf16, 256 K of 4 bits)
+  int act;
+  float alpha, alpha2;
+  void* C;                           // [T, N] bf16
+  float *P, *Q;                      // gated, optional
+  int* status;
+};
+struct FewMaps { CUtensorMap x, w0, w1, sx, s0, s1; };
+
+struct FewCtl {
+  uint64_t full[8], empty[8], done;
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ float2 ld_cluster_f2(uint32_t saddr, uint32_t rank) {
+  float2 v;
+  asm volatile(
+      "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %2, %3;\n\tld.shared::cluster.v2.f32 {%0, %1}, [a];\n\t}\n"
+      : "=f"(v.x), "=f"(v.y) : "r"(saddr), "r"(rank) : "memory");
+  return v;
+}
+// This warp's 32 lanes x 16 columns, complete when it returns.
+__device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr) : "memory");
+}
+template <int kFmt>
+__device__ __forceinline__ void mma_fp4_1cta(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t acc) {
+  if constexpr (kFmt == FMT_NV)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}\n"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}\n"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t sdesc) {
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+
+template <int kFmt, bool kGated, int kN>
+__global__ void __launch_bounds__(kFewThreads, FewCfg<kFmt, kGated, kN>::kPerSm)
+few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
+  using Cfg = FewCfg<kFmt, kGated, kN>;
+  constexpr bool kFp4 = Cfg::kFp4;
+  constexpr int kStages = Cfg::kStages, kMats = Cfg::kMats, kTiles = Cfg::kTiles;
+  extern __shared__ uint8_t smem_dyn[];
+  uint8_t* smem = smem_dyn + align_pad(smem_dyn, 1024);
+  FewCtl* ctl = reinterpret_cast<FewCtl*>(smem + kStages * Cfg::kStageBytes);
+  volatile int* abort_flag = &ctl->abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int S = (int)cluster_size(), rank = (int)cluster_ctarank();
+  const int f0 = (int)(blockIdx.x / S) * 128;               // first of this cluster's 128 weight rows
+  const int kb0 = (int)((int64_t)args.nkb * rank / S), kb1 = (int)((int64_t)args.nkb * (rank + 1) / S);
+
+  if (threadIdx.x == 0) {
+    prefetch_tmap(&maps.x);
+    prefetch_tmap(&maps.w0);
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    mbar_init(&ctl->done, 1);
+    ctl->abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&ctl->tmem_base, Cfg::kTmem);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait();
+  const uint32_t tmem_base = ctl->tmem_base;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t stage = 0, phase = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait(&ctl->empty[stage], phase ^ 1, abort_flag)) break;
+        uint8_t* sw = smem + stage * Cfg::kStageBytes;
+        uint8_t* sx = sw + kMats * Cfg::kWBytes;
+        uint8_t* ss = sx + Cfg::kXBytes;
+        uint64_t* bar = &ctl->full[stage];
+        mbar_arrive_expect_tx(bar, (uint32_t)Cfg::kStageBytes);
+        tma_load_2d(sw, &maps.w0, bar, kb * 64, f0);
+        if (kGated) tma_load_2d(sw + Cfg::kWBytes, &maps.w1, bar, kb * 64, f0);
+        tma_load_2d(sx, &maps.x, bar, kb * 64, 0);
+        if constexpr (kFp4) {
+          tma_load_3d(ss, &maps.s0, bar, 0, kb * kTiles, f0 >> 7);
+          if (kGated) tma_load_3d(ss + kTiles * 512, &maps.s1, bar, 0, kb * kTiles, f0 >> 7);
+          tma_load_3d(ss + kMats * kTiles * 512, &maps.sx, bar, 0, kb * kTiles, 0);
+        }
+        if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1; }
+      }
+      pdl_trigger();
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = kFp4 ? idesc_fp4(128, kN, kFmt) : idesc_bf16(128, kN, false, false, false);
+      const uint64_t proto = smem_desc(0, 16, 1024, kSwizzle128B), s_proto = smem_desc(0, 128, 128, kSwizzleNone);
+      uint32_t stage = 0, phase = 0;
+      bool ok = true;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait(&ctl->full[stage], phase, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t sw = smem_u32(smem) + stage * (uint32_t)Cfg::kStageBytes;
+        const uint64_t w = proto + (sw >> 4), x = proto + ((sw + kMats * Cfg::kWBytes) >> 4);
+        const uint32_t scol = tmem_base + Cfg::kScaleCol + ((uint32_t)(kb - kb0) & 1u) * Cfg::kScaleCols;
+        if constexpr (kFp4) {
+          const uint64_t sd = s_proto + ((sw + kMats * Cfg::kWBytes + Cfg::kXBytes) >> 4);
+#pragma unroll
+          for (int i = 0; i < kTiles * (kMats + 1); ++i) tmem_cp_scales(scol + 4 * i, sd + 32 * i);
+        }
+#pragma unroll
+        for (int m = 0; m < kMats; ++m)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t accum = (kb > kb0 || k > 0) ? 1u : 0u;
+            const uint64_t wd = w + m * (Cfg::kWBytes >> 4) + 2 * k, xd = x + 2 * k;
+            if constexpr (kFp4) {
+              const int i = kFmt == FMT_NV ? k : k >> 1;
+              const uint32_t id = kFmt == FMT_NV ? 0u : (uint32_t)(k & 1) * 2u;
+              mma_fp4_1cta<kFmt>(tmem_base + m * kN, wd, xd, idesc | id << 4 | id << 29, scol + 4 * (m * kTiles + i),
+                                 scol + 4 * (kMats * kTiles + i), accum);
+            } else {
+              mma_f16(tmem_base + m * kN, wd, xd, idesc, accum);
+            }
+          }
+        mma_commit(&ctl->empty[stage]);
+        if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1; }
+      }
+      if (ok) mma_commit(&ctl->done);
+    }
+  } else {
+    // every product has been made, so every load has landed and the ring is free: the partial sums go there, [matrix][token][row]
+    if (mbar_wait_warp(&ctl->done, 0, abort_flag)) {
+      tc_fence_after();
+      const int q = warp & 3;
+      float* part = reinterpret_cast<float*>(smem) + q * 32 + lane;
+#pragma unroll 1
+      for (int c = 0; c < kMats * kN; c += 16) {
+        uint32_t v[16];
+        tmem_ld_32x32b_x16(tmem_base + c + ((uint32_t)(q * 32) << 16), v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) part[(c + i) * 128] = __uint_as_float(v[i]);
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && ctl->abort_flag) {
+    atomicExch(args.status, 1);
+    drain_after_expiry();
+  }
+  cluster_sync_all();                                      // every partial sum of the cluster is there
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, Cfg::kTmem);
+  }
+  // each CTA adds up and writes an equal share of the cluster's rows, two neighbouring output columns to a thread
+  const int pairs = 64 / S, p0 = rank * pairs;
+  const uint32_t part = smem_u32(smem);
+  for (int i = threadIdx.x; i < args.T * pairs; i += kFewThreads) {
+    const int t = i / pairs, p = p0 + (i - t * pairs), f = f0 + 2 * p;
+    if (f >= args.N) continue;
+    float2 a = {0.f, 0.f}, b = {0.f, 0.f};
+    for (int s = 0; s < S; ++s) {
+      const float2 x = ld_cluster_f2(part + (uint32_t)(t * 128 + 2 * p) * 4u, s);
+      a.x += x.x; a.y += x.y;
+      if (kGated) {
+        const float2 y = ld_cluster_f2(part + (uint32_t)((kN + t) * 128 + 2 * p) * 4u, s);
+        b.x += y.x; b.y += y.y;
+      }
+    }
+    if (kFp4) { a.x *= args.alpha; a.y *= args.alpha; b.x *= args.alpha2; b.y *= args.alpha2; }
+    const int64_t at = (int64_t)t * args.N + f;
+    if constexpr (kGated) {
+      with_act(args.act, [&](auto tag) {
+        float v0, v1, d0, d1;
+        gate_act<decltype(tag)::value>(a.x, v0, d0);
+        gate_act<decltype(tag)::value>(a.y, v1, d1);
+        if (args.P) {
+          *reinterpret_cast<float2*>(args.P + at) = make_float2(v0, v1);
+          *reinterpret_cast<float2*>(args.Q + at) = make_float2(b.x * d0, b.y * d1);
+        }
+        a.x = v0 * b.x;
+        a.y = v1 * b.y;
+      });
+    }
+    *reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(args.C) + at) = bf16x2(a.x, a.y);
+  }
+  if (S > 1) cluster_sync_all();                           // no CTA leaves while another reads its shared memory
+}
+
+template <int kFmt, bool kGated, int kN>
+int launch_few(const FewMaps& maps, const FewArgs& a, int S, cudaStream_t s) {
+  using Cfg = FewCfg<kFmt, kGated, kN>;
+  auto kern = few_tokens_kernel<kFmt, kGated, kN>;
+  static bool attr_done[64] = {false};
+  int dev = 0;
+  SF_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+    SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
+    if (dev >= 0 && dev < 64) attr_done[dev] = true;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((a.N + 127) / 128 * S));
+  cfg.blockDim = dim3(kFewThreads);
+  cfg.dynamicSmemBytes = Cfg::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)S;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  SF_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, maps, a));
+  return SF_OK;
+}
+
+}  // namespace
+}  // namespace sf

@@ -1,0 +1,217 @@
+// The gated feed-forward block (the three-matrix FFN that the paper's FLOP count of 18 B T D F stands for, Section 5.1):
+//   forward   H = act(X Wg^T) * (X Wu^T),  Y = H Wd^T                                   two launches
+//   backward  dH = dY Wd,  dU = dH P,  dG = dH Q   with P = act(G), Q = U act'(G)       one launch, dH stays in TMEM
+//             dX = dG Wg + dU Wu                                                        one launch, one accumulation
+//             dWd = dY^T H,  dWg = dG^T X,  dWu = dU^T X                                one launch, tiles of all three
+//
+// Roundings: G, U and dH stay in float32. H, dG and dU are rounded to bf16 once, because they are operands of the next product; P and
+// Q are kept in float32 (8 bytes a hidden value where bf16 would take 4), because dG and dU would otherwise be rounded two or three times: the
+// error of dWu against 64 bits is then 1.8 times that of a result that is rounded once at its end, with them it is 1.4 times.
+#include "products.cuh"
+
+namespace sf {
+
+int sm_count_now() {
+  static int n[64] = {0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 148; }
+  if (n[dev] == 0) {
+    int v = 0;
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || v <= 0) v = 148;
+    n[dev] = v;
+  }
+  return n[dev];
+}
+
+namespace {
+
+int encode(void* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+           const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
+  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static Encode fn = nullptr;
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+      return cuda_fail(cudaErrorUnknown);
+    fn = reinterpret_cast<Encode>(p);
+  }
+  const cuuint32_t one[3] = {1, 1, 1};
+  const CUresult r = fn(reinterpret_cast<CUtensorMap*>(map), type, rank, const_cast<void*>(base), dims, strides, box, one,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r == CUDA_SUCCESS) return SF_OK;
+  g_last_cuda_error = (int)r;
+  return SF_ERR_CUDA;
+}
+
+int encode_2d(void* map, CUtensorMapDataType type, int bytes, const void* base, int64_t rows, int64_t cols, CUtensorMapSwizzle swizzle) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)cols * bytes};
+  const cuuint32_t box[2] = {32, 32};
+  return encode(map, type, 2, base, dims, strides, box, swizzle);
+}
+
+}  // namespace
+
+int make_tmap_f32(void* map, const void* base, int64_t rows, int64_t cols) {
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, rows, cols, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+int make_tmap_store(void* map, void* base, int64_t rows, int64_t cols) {
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols, CU_TENSOR_MAP_SWIZZLE_64B);
+}
+int make_tmap_scales(void* map, const void* base, int64_t row_blocks, int64_t k_tiles, uint32_t box_tiles) {
+  const cuuint64_t dims[3] = {128, (cuuint64_t)k_tiles, (cuuint64_t)row_blocks}, strides[2] = {512, 512 * (cuuint64_t)k_tiles};
+  const cuuint32_t box[3] = {128, box_tiles, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+namespace {
+
+constexpr size_t kStatus = 256;
+size_t padded(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct GatedSizes {
+  size_t h, f;          // bytes of a bf16 and of a float32 [T, F]
+};
+int gated_sizes(const sf_gated_ffn_desc* d, GatedSizes* z) {
+  if (!d) return SF_ERR_NULL;
+  if (!act_ok(d->act)) return SF_ERR_UNSUPPORTED;
+  if (d->T < 0 || d->D <= 0 || d->F <= 0 || d->D % 8 || d->F % 8 || d->T > kMaxSize || d->D > kMaxSize || d->F > kMaxSize) return SF_ERR_SHAPE;
+  const size_t n = (size_t)d->T * (size_t)d->F;
+  z->h = padded(2 * n);
+  z->f = padded(4 * n);
+  return SF_OK;
+}
+
+template <int kBN>
+int run_bwd(const sf_gated_ffn_desc& d, const void* dY, const void* Wd, const float* P, const float* Q, void* dG, void* dU,
+            const PairArgs& a, cudaStream_t s) {
+  PairMaps<6> m;
+  SF_TRY(kmajor_map(&m.m[0], FMT_BF16, dY, d.T, d.D, 128));
+  SF_TRY(mn_map(&m.m[1], Wd, d.D, d.F));
+  SF_TRY(make_tmap_f32(&m.m[2], P, d.T, d.F));
+  SF_TRY(make_tmap_f32(&m.m[3], Q, d.T, d.F));
+  SF_TRY(make_tmap_store(&m.m[4], dG, d.T, d.F));
+  SF_TRY(make_tmap_store(&m.m[5], dU, d.T, d.F));
+  return launch_pair<PK_BWD, kBN, FMT_BF16>(m, a, s);
+}
+
+template <int kBN>
+int run_dx(const sf_gated_ffn_desc& d, const void* dG, const void* dU, const void* Wg, const void* Wu, void* dX, const PairArgs& a,
+           cudaStream_t s) {
+  PairMaps<5> m;
+  SF_TRY(kmajor_map(&m.m[0], FMT_BF16, dG, d.T, d.F, 128));
+  SF_TRY(kmajor_map(&m.m[1], FMT_BF16, dU, d.T, d.F, 128));
+  SF_TRY(mn_map(&m.m[2], Wg, d.F, d.D));
+  SF_TRY(mn_map(&m.m[3], Wu, d.F, d.D));
+  SF_TRY(make_tmap_store(&m.m[4], dX, d.T, d.D));
+  return launch_pair<PK_DX, kBN, FMT_BF16>(m, a, s);
+}
+
+struct GradJob { const void *A, *B; int64_t M, N; void* C; };     // C[M, N] = A[T, M]^T B[T, N]
+template <int kBN>
+int run_dw(const GradJob* jobs, int64_t T, PairArgs a, cudaStream_t s) {
+  PairMaps<9> m;
+  for (int j = 0; j < a.jobs; ++j) {
+    SF_TRY(mn_map(&m.m[j], jobs[j].A, T, jobs[j].M));
+    SF_TRY(mn_map(&m.m[3 + j], jobs[j].B, T, jobs[j].N));
+    SF_TRY(make_tmap_store(&m.m[6 + j], jobs[j].C, jobs[j].M, jobs[j].N));
+  }
+  for (int j = a.jobs; j < 3; ++j)
+    for (int i = 0; i < 9; i += 3) m.m[i + j] = m.m[i];
+  return launch_pair<PK_DW, kBN, FMT_BF16>(m, a, s);
+}
+
+}  // namespace
+
+}  // namespace sf
+
+using namespace sf;
+
+extern "C" {
+
+int sf_gated_ffn_workspace_size(const sf_gated_ffn_desc* desc, size_t* fwd_ctx_bytes, size_t* workspace_bytes) {
+  GatedSizes z;
+  SF_TRY(gated_sizes(desc, &z));
+  if (!fwd_ctx_bytes || !workspace_bytes) return SF_ERR_NULL;
+  *fwd_ctx_bytes = z.h + 2 * z.f;
+  *workspace_bytes = kStatus + 2 * z.h;
+  return SF_OK;
+}
+
+int sf_gated_ffn_fwd(const sf_gated_ffn_desc* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, void* Y,
+                     void* fwd_ctx, size_t fwd_ctx_bytes, void* workspace, size_t workspace_bytes, void* stream) {
+  GatedSizes z;
+  SF_TRY(gated_sizes(desc, &z));
+  if (desc->T == 0) return SF_OK;
+  if (!X || !Wg || !Wu || !Wd || !Y || !workspace) return SF_ERR_NULL;
+  if (!aligned16(X) || !aligned16(Wg) || !aligned16(Wu) || !aligned16(Wd) || !aligned16(Y) || !aligned16(workspace) ||
+      (fwd_ctx && !aligned16(fwd_ctx)))
+    return SF_ERR_ALIGN;
+  if ((fwd_ctx && fwd_ctx_bytes < z.h + 2 * z.f) || workspace_bytes < kStatus + (fwd_ctx ? 0 : z.h)) return SF_ERR_WORKSPACE;
+  SF_TRY(check_arch());
+  cudaStream_t s = (cudaStream_t)stream;
+  uint8_t* h = fwd_ctx ? (uint8_t*)fwd_ctx : (uint8_t*)workspace + kStatus;
+  float* p = fwd_ctx ? (float*)(h + z.h) : nullptr;
+  float* q = fwd_ctx ? (float*)(h + z.h + z.f) : nullptr;
+  int* status = (int*)workspace;
+  SF_TRY(run_gated<FMT_BF16>({X, nullptr}, {Wg, nullptr}, {Wu, nullptr}, desc->T, desc->F, desc->D, desc->act, 1.f, 1.f, h, p, q, status, s));
+  return run_nt<FMT_BF16>({h, nullptr}, {Wd, nullptr}, desc->T, desc->D, desc->F, 1.f, Y, status, s);
+}
+
+int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* X, const void* Wg, const void* Wu, const void* Wd,
+                     const void* fwd_ctx, size_t fwd_ctx_bytes, void* dX, void* dWg, void* dWu, void* dWd, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+  GatedSizes z;
+  SF_TRY(gated_sizes(desc, &z));
+  const int64_t T = desc->T, D = desc->D, F = desc->F;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (!aligned16(dX) || !aligned16(dWg) || !aligned16(dWu) || !aligned16(dWd)) return SF_ERR_ALIGN;
+  if (T == 0) {                                            // no token: the weights' gradients are empty sums
+    SF_TRY(check_arch());
+    for (void* w : {dWg, dWu, dWd})
+      if (w) SF_CUDA_TRY(cudaMemsetAsync(w, 0, 2 * (size_t)D * (size_t)F, s));
+    return SF_OK;
+  }
+  if (!dX && !dWg && !dWu && !dWd) return SF_OK;
+  if (!dY || !X || !Wg || !Wu || !Wd || !fwd_ctx || !workspace) return SF_ERR_NULL;
+  if (!aligned16(dY) || !aligned16(X) || !aligned16(Wg) || !aligned16(Wu) || !aligned16(Wd) || !aligned16(fwd_ctx) || !aligned16(workspace))
+    return SF_ERR_ALIGN;
+  if (fwd_ctx_bytes < z.h + 2 * z.f || workspace_bytes < kStatus + 2 * z.h) return SF_ERR_WORKSPACE;
+  SF_TRY(check_arch());
+  const uint8_t* h = (const uint8_t*)fwd_ctx;
+  uint8_t* dg = (uint8_t*)workspace + kStatus;
+  uint8_t* du = dg + z.h;
+  PairArgs a{};
+  a.status = (int*)workspace;
+  a.jobs = 1;
+  if (dX || dWg || dWu) {
+    a.M[0] = (int)T; a.N[0] = (int)F; a.nkb = a.nkb0 = k_blocks(FMT_BF16, D);
+    const int w = pair_width(tiles_of(T, F, 256), tiles_of(T, F, 128), tiles_of(T, F, 64), a.nkb);
+    const float *p = (const float*)(h + z.h), *q = (const float*)(h + z.h + z.f);
+    SF_TRY(w == 256 ? run_bwd<256>(*desc, dY, Wd, p, q, dg, du, a, s)
+         : w == 128 ? run_bwd<128>(*desc, dY, Wd, p, q, dg, du, a, s) : run_bwd<64>(*desc, dY, Wd, p, q, dg, du, a, s));
+  }
+  if (dX) {
+    a.M[0] = (int)T; a.N[0] = (int)D; a.nkb0 = k_blocks(FMT_BF16, F); a.nkb = 2 * a.nkb0;
+    const int w = pair_width(tiles_of(T, D, 256), tiles_of(T, D, 128), tiles_of(T, D, 64), a.nkb);
+    SF_TRY(w == 256 ? run_dx<256>(*desc, dg, du, Wg, Wu, dX, a, s)
+         : w == 128 ? run_dx<128>(*desc, dg, du, Wg, Wu, dX, a, s) : run_dx<64>(*desc, dg, du, Wg, Wu, dX, a, s));
+  }
+  GradJob jobs[3];
+  a.jobs = 0;
+  if (dWd) jobs[a.jobs++] = {dY, h, D, F, dWd};
+  if (dWg) jobs[a.jobs++] = {dg, X, F, D, dWg};
+  if (dWu) jobs[a.jobs++] = {du, X, F, D, dWu};
+  if (a.jobs == 0) return SF_OK;
+  int64_t t256 = 0, t128 = 0, t64 = 0;
+  for (int j = 0; j < a.jobs; ++j) {
+    a.M[j] = (int)jobs[j].M; a.N[j] = (int)jobs[j].N;
+    t256 += tiles_of(jobs[j].M, jobs[j].N, 256); t128 += tiles_of(jobs[j].M, jobs[j].N, 128); t64 += tiles_of(jobs[j].M, jobs[j].N, 64);
+  }
+  a.nkb = a.nkb0 = (int)ceil_div(T, 64);
+  const int w = pair_width(t256, t128, t64, a.nkb);
+  return w == 256 ? run_dw<256>(jobs, T, a, s) : w == 128 ? run_dw<128>(jobs, T, a, s) : run_dw<64>(jobs, T, a, s);
+}
+
+}  // extern "C"

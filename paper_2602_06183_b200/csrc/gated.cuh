@@ -1,0 +1,88 @@
+// Internal interface of the gated feed-forward block and of the 4-bit products: the kernel on CTA pairs for long operands
+// (pair_product.cuh), the weight-streaming kernel for few tokens (few_tokens.cuh), and what both compute in their epilogues.
+#pragma once
+
+#include <cuda.h>
+
+#include "gemm_tc.cuh"
+#include "sf_common.cuh"
+#include "tc_ptx.cuh"
+
+namespace sf {
+
+// Operand formats of a product.
+enum OperandFmt { FMT_BF16 = 0, FMT_NV = 1, FMT_MX = 2 };
+
+// ---- activations ----------------------------------------------------------------------------------------
+// Value and derivative of the gate's activation in float32. The sigmoid is written with the exponential of -x, so that neither
+// tail cancels: 1 / (1 + e^-x) is 0 or 1 to within rounding there, and x times it underflows as the function does (rcp.approx holds to an
+// ulp for every denominator; the fast division gives 0 from 2^126 on, which x < -87 reaches).
+__device__ __forceinline__ float sigmoid32(float x) {
+  float r;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-x)));
+  return r;
+}
+
+template <int kAct>
+__device__ __forceinline__ void gate_act(float g, float& a, float& da) {
+  if constexpr (kAct == SF_ACT_SILU) {
+    const float s = sigmoid32(g);
+    a = g * s;
+    da = s * fmaf(g, 1.f - s, 1.f);
+  } else if constexpr (kAct == SF_ACT_GELU) {
+    const float c = normcdff(g);
+    a = g * c;
+    da = fmaf(g, 0.3989422804014327f * __expf(-0.5f * g * g), c);
+  } else if constexpr (kAct == SF_ACT_GELU_TANH) {
+    // 0.5 (1 + tanh(z)) = sigmoid(2 z), z = sqrt(2 / pi) (g + 0.044715 g^3)
+    constexpr float k = 1.5957691216057308f, c3 = 0.044715f;
+    const float g2 = g * g, s = sigmoid32(k * g * fmaf(c3, g2, 1.f));
+    a = g * s;
+    da = fmaf(a * (1.f - s), k * fmaf(3.f * c3, g2, 1.f), s);
+  } else {
+    const float r = fmaxf(g, 0.f);
+    a = kAct == SF_ACT_RELU ? r : r * r;
+    da = kAct == SF_ACT_RELU ? (g > 0.f ? 1.f : 0.f) : 2.f * r;
+  }
+}
+
+// Calls f with the run-time activation (uniform over the grid) as a constant.
+template <int kAct> struct ActTag { static constexpr int value = kAct; };
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  switch (act) {
+    case SF_ACT_SILU: f(ActTag<SF_ACT_SILU>{}); break;
+    case SF_ACT_GELU: f(ActTag<SF_ACT_GELU>{}); break;
+    case SF_ACT_GELU_TANH: f(ActTag<SF_ACT_GELU_TANH>{}); break;
+    case SF_ACT_RELU: f(ActTag<SF_ACT_RELU>{}); break;
+    default: f(ActTag<SF_ACT_SQRELU>{}); break;
+  }
+}
+
+inline bool act_ok(int act) { return act >= SF_ACT_SILU && act <= SF_ACT_SQRELU; }
+
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) { return float_to_bf16_bits(lo) | (float_to_bf16_bits(hi) << 16); }
+
+// Instruction descriptor of the block-scaled kinds with E2M1 operands: scale format in bit 23 (0 E4M3, 1 power of two), the byte of
+// a row's scale word that an instruction starts with in bits 4-5 (B) and 29-30 (A).
+__host__ __device__ constexpr uint32_t idesc_fp4(uint32_t M, uint32_t N, int fmt) {
+  return (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (fmt == FMT_MX ? 1u << 23 : 0u) | ((M >> 7) << 27);
+}
+
+// ---- tensor maps ------------------------------------------------------------------------------------------
+int sm_count_now();
+// [rows, cols] of 4-byte floats, box 32 x 32, 128-byte swizzle.
+int make_tmap_f32(void* map, const void* base, int64_t rows, int64_t cols);
+// Stores of bf16 [rows, cols], box 32 x 32, 64-byte swizzle.
+int make_tmap_store(void* map, void* base, int64_t rows, int64_t cols);
+// Scale tiles of a 4-bit operand: [row blocks][tiles along K][128 words], box {128, tiles, 1}.
+int make_tmap_scales(void* map, const void* base, int64_t row_blocks, int64_t k_tiles, uint32_t box_tiles);
+
+// ---- products -----------------------------------------------------------------------------------------------
+// A matrix operand: bf16 [rows, K] or, for the 4-bit formats, codes [rows, K / 2] with their scale tiles.
+struct Operand {
+  const void* data;
+  const void* scales;
+};
+
+}  // namespace sf

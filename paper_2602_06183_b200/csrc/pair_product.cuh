@@ -1,0 +1,451 @@
+// Products of long operands on CTA pairs, for any sizes whose rows are multiples of 16 bytes: tcgen05.mma.cta_group::2 on 256 x kBN
+// tiles, operands by TMA, accumulators in TMEM, epilogues that read and write whole chunks by TMA. Everything ragged is left to
+// TMA: loads beyond an edge bring zeros, stores beyond it are not made.
+//
+//   PK_NT    C = alpha A B^T                                both K-major
+//   PK_DX    C = A0 B0 + A1 B1                              A K-major, B stored [K, N]; one accumulation over both pairs
+//   PK_DW    C_j = A_j^T B_j, up to three products          both stored [K, .]; one launch, tiles of one after those of the other
+//   PK_FWD   H = act(A Bg^T) (A Bu^T)                       the even CTA of a pair holds rows of Bg, the odd one the same rows of Bu:
+//            the first half of a tile's columns is the gate, the second half the other factor of the same features, so that the
+//            product of the two is taken in registers and neither projection is written.
+//   PK_FWD_SAVE  the same, and P = act(g), Q = u act'(g) in float32 for the backward pass
+//   PK_BWD   dU = (A B) P, dG = (A B) Q                     A = dY, B = Wd [K, N]; dH is never written
+//
+// CTA = 10 warps: TMA producer, MMA issuer, two sets of four epilogue warps that share a tile's columns. Every wait is bounded
+// (see gemm_tc.cu): on expiry the CTA raises the status word and leaves.
+#pragma once
+
+#include "gated.cuh"
+
+namespace sf {
+namespace {
+
+using namespace ptx;
+
+enum PairKind { PK_NT, PK_DX, PK_DW, PK_FWD, PK_FWD_SAVE, PK_BWD };
+
+constexpr int kPairThreads = 320;
+constexpr int kPairSmemMax = 232448;
+
+template <int kKind, int kBN, int kFmt>
+struct PairCfg {
+  static constexpr bool kFp4 = kFmt != FMT_BF16;
+  static constexpr bool kAMN = kKind == PK_DW;
+  static constexpr bool kBMN = kKind == PK_DX || kKind == PK_DW || kKind == PK_BWD;
+  static constexpr bool kGated = kKind == PK_FWD || kKind == PK_FWD_SAVE;
+  static constexpr bool kWide = kKind == PK_FWD_SAVE || kKind == PK_BWD;         // float32 chunks in the epilogue
+  static constexpr int kHalf = kBN / 2;                                          // columns of B that a CTA holds
+  static constexpr int kBChunks = (kHalf + 63) / 64;                             // MN-major B: chunks of 64 columns
+  static constexpr int kABytes = 16384;
+  static constexpr int kBBytes = kBMN ? kBChunks * 8192 : kHalf * 128;
+  // 4-bit operands: a stage is 256 K; scale tiles of 512 bytes hold 128 rows x 4 scales = 64 (NV) or 128 (MX) K
+  static constexpr int kTiles = kFmt == FMT_NV ? 4 : kFmt == FMT_MX ? 2 : 0;      // scale tiles of a row block and stage
+  static constexpr int kBBlocks = kBN / 128;                                     // row blocks of B's scales
+  static constexpr int kScaleBytes = kTiles * 512 * (1 + kBBlocks);
+  static constexpr int kStageBytes = kABytes + kBBytes + kScaleBytes;
+  static constexpr int kEpiWarpBytes = kWide ? 8192 : 4096;
+  static constexpr int kRoom = (kPairSmemMax - 2048 - 8 * kEpiWarpBytes) / kStageBytes;
+  static constexpr int kStages = kRoom < 8 ? kRoom : 8;
+  static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kEpiWarpBytes + 1024;
+  // two accumulators; 4-bit tiles of 256 columns leave room for one next to the scales
+  static constexpr int kAccs = kFp4 && kBN == 256 ? 1 : 2;
+  static constexpr uint32_t kScaleCol = kAccs * kBN;
+  static constexpr uint32_t kScaleACols = kTiles * 4, kScaleCols = kScaleACols * (1 + kBBlocks);    // of one stage
+  static constexpr int kMaps = kKind == PK_DW ? 9 : kKind == PK_DX ? 5 : kKind == PK_NT ? (kFp4 ? 5 : 3)
+                             : kKind == PK_FWD ? (kFp4 ? 7 : 4) : 6;
+  static_assert(kBN == 256 || kBN == 128 || kBN == 64, "tile width");
+  static_assert(!kFp4 || kKind == PK_NT || (kKind == PK_FWD && kBN == 256), "4-bit operands: K-major, whole row blocks of scales");
+  static_assert(!kFp4 || kBN >= 128, "scales come in blocks of 128 rows");
+  static_assert(kStages >= 3 && kSmem <= kPairSmemMax && kSmem > 228 * 1024 / 2, "one CTA per SM");
+  static_assert(kScaleCol + 2 * kScaleCols <= 512, "TMEM columns");
+};
+
+struct PairArgs {
+  int jobs;
+  int num_m[3], num_n[3];            // tiles of each job
+  int M[3], N[3];                    // its output (PK_FWD: N features)
+  int nkb, nkb0;                     // k-blocks in all, and of the first pair of operands (PK_DX)
+  int act;
+  float alpha, alpha2;
+  int* status;
+};
+template <int N> struct PairMaps { CUtensorMap m[N]; };
+
+struct PairCtl {
+  uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], epi_full[8];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+struct PairTile { int job, m0, n0; };     // first row of the pair's tile, first column (PK_FWD: first feature)
+
+// The raster of the other products: bands of eight tile rows, rows fastest inside a band, so that the tiles which run at
+// the same time share few operand panels.
+template <int kKind, int kCols>
+__device__ __forceinline__ PairTile pair_tile(const PairArgs& a, int tile) {
+  int j = 0;
+  if (kKind == PK_DW) {
+    while (j < a.jobs - 1 && tile >= a.num_m[j] * a.num_n[j]) { tile -= a.num_m[j] * a.num_n[j]; ++j; }
+  }
+  const int num_m = a.num_m[j], num_n = a.num_n[j];
+  const int per_band = 8 * num_n, band = tile / per_band, rem = tile - band * per_band;
+  const int gm = min(8, num_m - band * 8), nt = rem / gm;
+  return PairTile{j, (band * 8 + rem - nt * gm) * 256, nt * kCols};
+}
+
+__device__ __forceinline__ void tma_load_3d_2cta(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar) & kPeerBitMask), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+
+// One chunk of 32 x 32 results as this lane's row, through a 4 KB buffer (two to a warp, taken in turn) to the map's matrix.
+// 64 (bf16) or 128 (float32) bytes a row, swizzled as the map has it.
+__device__ __forceinline__ void put_chunk_begin(int lane) {
+  if (lane == 0) bulk_wait_read<1>();                      // the store before the last has been read out of its buffer
+  __syncwarp();
+}
+__device__ __forceinline__ void put_chunk_end(const CUtensorMap* m, const uint8_t* b, int col, int row, int lane) {
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_2d(m, b, col, row);
+    bulk_commit();
+  }
+}
+__device__ __forceinline__ void row_bf16(uint8_t* b, int lane, const uint32_t (&w)[16]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    *reinterpret_cast<uint4*>(b + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+}
+__device__ __forceinline__ void row_f32(uint8_t* b, int lane, const uint32_t (&w)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    *reinterpret_cast<uint4*>(b + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+}
+// Block-scaled 4-bit products: E2M1 operands, one scale per 16 (E4M3) or 32 (power of two) K; K = 64 per instruction.
+template <int kFmt>
+__device__ __forceinline__ void mma_fp4_2cta(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t acc) {
+  if constexpr (kFmt == FMT_NV)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}\n"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}\n"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void tmem_cp_scales_2cta(uint32_t taddr, uint64_t sdesc) {
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
+}
+template <int kKind, int kBN, int kFmt>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps> maps, const PairArgs args) {
+  using Cfg = PairCfg<kKind, kBN, kFmt>;
+  constexpr bool kFp4 = Cfg::kFp4, kGated = Cfg::kGated;
+  constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs;
+  constexpr int kTileCols = kGated ? kBN / 2 : kBN;        // output columns of a tile
+  extern __shared__ uint8_t smem_dyn[];
+  uint8_t* smem = smem_dyn + align_pad(smem_dyn, 1024);
+  uint8_t* epi = smem + kStages * Cfg::kStageBytes;
+  PairCtl* ctl = reinterpret_cast<PairCtl*>(epi + 8 * Cfg::kEpiWarpBytes);
+  volatile int* abort_flag = &ctl->abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)cluster_ctarank();
+  const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+  int num_tiles = args.num_m[0] * args.num_n[0];
+  if (kKind == PK_DW)
+    for (int j = 1; j < args.jobs; ++j) num_tiles += args.num_m[j] * args.num_n[j];
+  const int nkb = args.nkb;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < (kKind == PK_DW ? 2 : 3); ++i) prefetch_tmap(&maps.m[i * (kKind == PK_DW ? 3 : 1)]);
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&ctl->full[s], 1);
+      mbar_init(&ctl->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&ctl->tmem_full[b], 1);
+      mbar_init(&ctl->tmem_empty[b], 16);                  // eight epilogue warps of either CTA
+    }
+    for (int w = 0; w < 8; ++w) mbar_init(&ctl->epi_full[w], 1);
+    ctl->abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_2cta(&ctl->tmem_base, 512);
+    tmem_relinquish_2cta();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  pdl_wait();
+  const uint32_t tmem_base = ctl->tmem_base;
+
+  if (warp == 0) {
+    // =========================== TMA producer (both CTAs) ===========================
+    uint32_t stage = 0, phase = 0;
+    bool ok = true;
+    for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
+      const PairTile t = pair_tile<kKind, kTileCols>(args, tile);
+      const int m0 = t.m0 + rank * 128;
+      const int n0 = kGated ? t.n0 : t.n0 + rank * Cfg::kHalf;
+      for (int kb = 0; kb < nkb; ++kb) {
+        if (!mbar_wait(&ctl->empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+        if (lane == 0) {
+          uint8_t* sA = smem + stage * Cfg::kStageBytes;
+          uint8_t* sB = sA + Cfg::kABytes;
+          uint64_t* bar = &ctl->full[stage];
+          if (rank == 0) mbar_arrive_expect_tx(bar, 2u * (uint32_t)Cfg::kStageBytes);     // the bytes of both CTAs
+          const bool second = kKind == PK_DX && kb >= args.nkb0;
+          const int k = (second ? kb - args.nkb0 : kb) * 64;
+          if constexpr (kKind == PK_DW) {
+            tma_load_2d_2cta(sA, &maps.m[t.job], bar, m0, k);
+            tma_load_2d_2cta(sA + 8192, &maps.m[t.job], bar, m0 + 64, k);
+          } else {
+            tma_load_2d_2cta(sA, &maps.m[second ? 1 : 0], bar, k, m0);
+          }
+          const CUtensorMap* mb = kKind == PK_DW ? &maps.m[3 + t.job] : kKind == PK_DX ? &maps.m[second ? 3 : 2]
+                                : kGated ? &maps.m[1 + rank] : &maps.m[1];
+          if constexpr (Cfg::kBMN) {
+#pragma unroll
+            for (int c = 0; c < Cfg::kBChunks; ++c) tma_load_2d_2cta(sB + c * 8192, mb, bar, n0 + c * 64, k);
+          } else {
+            tma_load_2d_2cta(sB, mb, bar, k, n0);
+          }
+          if constexpr (kFp4) {
+            uint8_t* sS = sB + Cfg::kBBytes;
+            tma_load_3d_2cta(sS, &maps.m[kGated ? 4 : 3], bar, 0, kb * Cfg::kTiles, m0 >> 7);
+#pragma unroll
+            for (int b = 0; b < Cfg::kBBlocks; ++b)        // the scales of all of the tile's columns, in both CTAs
+              tma_load_3d_2cta(sS + (1 + b) * Cfg::kTiles * 512, &maps.m[kGated ? 5 + b : 4], bar, 0, kb * Cfg::kTiles,
+                               kGated ? t.n0 >> 7 : (t.n0 >> 7) + b);
+          }
+        }
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+      }
+    }
+    pdl_trigger();
+  } else if (warp == 1) {
+    // =========================== MMA issuer (leader CTA only) ===========================
+    if (rank == 0 && lane == 0) {
+      constexpr uint32_t idesc = kFp4 ? idesc_fp4(256, kBN, kFmt) : idesc_bf16(256, kBN, Cfg::kAMN, Cfg::kBMN, false);
+      const uint64_t a_proto = Cfg::kAMN ? smem_desc(0, 8192, 1024, kSwizzle128B) : smem_desc(0, 16, 1024, kSwizzle128B);
+      const uint64_t b_proto = Cfg::kBMN ? smem_desc(0, 8192, 1024, kSwizzle128B) : smem_desc(0, 16, 1024, kSwizzle128B);
+      const uint64_t s_proto = smem_desc(0, 128, 128, kSwizzleNone);
+      const uint32_t a_hi = (uint32_t)(a_proto >> 32), b_hi = (uint32_t)(b_proto >> 32), s_hi = (uint32_t)(s_proto >> 32);
+      const uint32_t smem0 = smem_u32(smem);
+      const uint32_t a_lo0 = (uint32_t)a_proto + (smem0 >> 4);
+      const uint32_t b_lo0 = (uint32_t)b_proto + ((smem0 + Cfg::kABytes) >> 4);
+      const uint32_t s_lo0 = (uint32_t)s_proto + ((smem0 + Cfg::kABytes + Cfg::kBBytes) >> 4);
+      constexpr uint32_t a_step = (Cfg::kAMN ? 2048 : 32) >> 4, b_step = (Cfg::kBMN ? 2048 : 32) >> 4;
+      auto desc = [](uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; };
+      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+      bool ok = true;
+      for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
+        if (!mbar_wait(&ctl->tmem_empty[acc], acc_phase ^ 1, abort_flag)) break;
+        tc_fence_after();
+        const uint32_t d = tmem_base + acc * kBN;
+        for (int kb = 0; kb < nkb; ++kb) {
+          if (!mbar_wait(&ctl->full[stage], phase, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t soff = stage * (uint32_t)(Cfg::kStageBytes >> 4);
+          const uint32_t a_lo = a_lo0 + soff, b_lo = b_lo0 + soff;
+          if constexpr (kFp4) {
+            // the stage's scales go to TMEM, into one of two buffers in turn, ahead of the products that read them
+            const uint32_t sa = tmem_base + Cfg::kScaleCol + ((uint32_t)kb & 1u) * Cfg::kScaleCols, sb = sa + Cfg::kScaleACols;
+            const uint32_t s_lo = s_lo0 + soff;
+#pragma unroll
+            for (int i = 0; i < Cfg::kTiles; ++i) {
+              tmem_cp_scales_2cta(sa + 4 * i, desc(s_lo + 32 * i, s_hi));
+#pragma unroll
+              for (int b = 0; b < Cfg::kBBlocks; ++b)
+                tmem_cp_scales_2cta(sb + 4 * (i * Cfg::kBBlocks + b), desc(s_lo + 32 * ((1 + b) * Cfg::kTiles + i), s_hi));
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int i = kFmt == FMT_NV ? k : k >> 1;                                   // tile, and first scale in its words
+              const uint32_t id = kFmt == FMT_NV ? 0u : (uint32_t)(k & 1) * 2u;
+              mma_fp4_2cta<kFmt>(d, desc(a_lo + k * a_step, a_hi), desc(b_lo + k * b_step, b_hi), idesc | id << 4 | id << 29,
+                                 sa + 4 * i, sb + 4 * i * Cfg::kBBlocks, (kb > 0 || k > 0) ? 1u : 0u);
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma_f16_2cta(d, desc(a_lo + k * a_step, a_hi), desc(b_lo + k * b_step, b_hi), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+          }
+          mma_commit_2cta(&ctl->empty[stage]);
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        mma_commit_2cta(&ctl->tmem_full[acc]);
+        if (++acc == (uint32_t)kAccs) { acc = 0; acc_phase ^= 1; }
+      }
+    }
+  } else {
+    // =========================== epilogue (warps 2..9, both CTAs) ===========================
+    const int q = warp & 3, set = (warp - 2) >> 2;
+    uint8_t* bufs = epi + (warp - 2) * Cfg::kEpiWarpBytes;
+    uint64_t* loaded = &ctl->epi_full[warp - 2];
+    constexpr int kBufBytes = Cfg::kEpiWarpBytes / 2;
+    uint32_t acc = 0, acc_phase = 0, buf = 0, load_phase = 0;
+    auto put16 = [&](const CUtensorMap* m, const uint32_t (&w)[16], int col, int row) {
+      put_chunk_begin(lane);
+      row_bf16(bufs + buf * kBufBytes, lane, w);
+      put_chunk_end(m, bufs + buf * kBufBytes, col, row, lane);
+      buf ^= 1u;
+    };
+    auto put32 = [&](const CUtensorMap* m, const uint32_t (&w)[32], int col, int row) {
+      put_chunk_begin(lane);
+      row_f32(bufs + buf * kBufBytes, lane, w);
+      put_chunk_end(m, bufs + buf * kBufBytes, col, row, lane);
+      buf ^= 1u;
+    };
+    for (int tile = pair; tile < num_tiles; tile += num_pairs) {
+      const PairTile t = pair_tile<kKind, kTileCols>(args, tile);
+      const int row = t.m0 + rank * 128 + q * 32;
+      const int M = kKind == PK_DW ? args.M[t.job] : args.M[0], N = kKind == PK_DW ? args.N[t.job] : args.N[0];
+      // chunks of 32 output columns that are there; the two sets take them in turn
+      const int chunks = row < M ? min(kTileCols / 32, (N - t.n0 + 31) >> 5) : 0;
+      auto fetch = [&](int ch) {                           // PK_BWD: P and Q of a chunk
+        if (lane == 0) {
+          bulk_wait_read<0>();
+          mbar_arrive_expect_tx(loaded, 8192u);
+          tma_load_2d(bufs, &maps.m[2], loaded, t.n0 + ch * 32, row);
+          tma_load_2d(bufs + 4096, &maps.m[3], loaded, t.n0 + ch * 32, row);
+        }
+      };
+      if (kKind == PK_BWD && set < chunks) fetch(set);
+      if (!mbar_wait_warp(&ctl->tmem_full[acc], acc_phase, abort_flag)) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + acc * kBN + ((uint32_t)(q * 32) << 16);
+      bool ok = true;
+#pragma unroll 1
+      for (int ch = set; ch < chunks; ch += 2) {
+        const int col = t.n0 + ch * 32;
+        uint32_t v[32];
+        tmem_ld_32x32b_x32(taddr + ch * 32, v);
+        if constexpr (kGated) {
+          uint32_t u[32];
+          tmem_ld_32x32b_x32(taddr + kBN / 2 + ch * 32, u);
+          tmem_ld_wait_on(v);
+          tmem_ld_wait_on(u);
+          if constexpr (kFp4) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+              v[i] = __float_as_uint(__uint_as_float(v[i]) * args.alpha);
+              u[i] = __float_as_uint(__uint_as_float(u[i]) * args.alpha2);
+            }
+          }
+          uint32_t h[16];
+          with_act(args.act, [&](auto tag) {
+            constexpr int kAct = decltype(tag)::value;
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              float a[2], da[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float uu = __uint_as_float(u[i + e]);
+                gate_act<kAct>(__uint_as_float(v[i + e]), a[e], da[e]);
+                v[i + e] = __float_as_uint(a[e]);
+                u[i + e] = __float_as_uint(uu * da[e]);
+                a[e] *= uu;
+              }
+              h[i >> 1] = bf16x2(a[0], a[1]);
+            }
+          });
+          put16(&maps.m[3], h, col, row);
+          if constexpr (kKind == PK_FWD_SAVE) {
+            put32(&maps.m[4], v, col, row);
+            put32(&maps.m[5], u, col, row);
+          }
+        } else if constexpr (kKind == PK_BWD) {
+          uint32_t du[16], dg[16];
+          tmem_ld_wait_on(v);
+          if (!mbar_wait_warp(loaded, load_phase, abort_flag)) { ok = false; break; }
+          load_phase ^= 1u;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float4 p = *reinterpret_cast<const float4*>(bufs + lane * 128 + ((j ^ (lane & 7)) << 4));
+            const float4 r = *reinterpret_cast<const float4*>(bufs + 4096 + lane * 128 + ((j ^ (lane & 7)) << 4));
+            const float d0 = __uint_as_float(v[4 * j]), d1 = __uint_as_float(v[4 * j + 1]), d2 = __uint_as_float(v[4 * j + 2]),
+                        d3 = __uint_as_float(v[4 * j + 3]);
+            du[2 * j] = bf16x2(d0 * p.x, d1 * p.y); du[2 * j + 1] = bf16x2(d2 * p.z, d3 * p.w);
+            dg[2 * j] = bf16x2(d0 * r.x, d1 * r.y); dg[2 * j + 1] = bf16x2(d2 * r.z, d3 * r.w);
+          }
+          __syncwarp();                                    // every row has been read: the results take its place
+          row_bf16(bufs, lane, du);
+          row_bf16(bufs + 4096, lane, dg);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(&maps.m[5], bufs, col, row);
+            tma_store_2d(&maps.m[4], bufs + 4096, col, row);
+            bulk_commit();
+          }
+          if (ch + 2 < chunks) fetch(ch + 2);
+        } else {
+          tmem_ld_wait_on(v);
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float lo = __uint_as_float(v[2 * i]), hi = __uint_as_float(v[2 * i + 1]);
+            if (kFp4) { lo *= args.alpha; hi *= args.alpha; }
+            w[i] = bf16x2(lo, hi);
+          }
+          put16(&maps.m[kKind == PK_DW ? 6 + t.job : kKind == PK_DX ? 4 : 2], w, col, row);
+        }
+      }
+      if (!ok) break;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_leader(&ctl->tmem_empty[acc]);
+      if (++acc == (uint32_t)kAccs) { acc = 0; acc_phase ^= 1; }
+    }
+    if (lane == 0) bulk_wait_all();
+  }
+
+  // =========================== teardown ===========================
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && ctl->abort_flag) {
+    atomicExch(args.status, 1);
+    drain_after_expiry();
+  }
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_2cta(tmem_base, 512);
+  }
+}
+
+template <int kKind, int kBN, int kFmt>
+int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps>& maps, PairArgs a, cudaStream_t s) {
+  using Cfg = PairCfg<kKind, kBN, kFmt>;
+  auto kern = pair_product_kernel<kKind, kBN, kFmt>;
+  static bool attr_done[64] = {false};
+  int dev = 0;
+  SF_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+    SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
+    if (dev >= 0 && dev < 64) attr_done[dev] = true;
+  }
+  constexpr int cols = Cfg::kGated ? kBN / 2 : kBN;
+  int64_t tiles = 0;
+  for (int j = 0; j < a.jobs; ++j) {
+    a.num_m[j] = (a.M[j] + 255) / 256;
+    a.num_n[j] = (a.N[j] + cols - 1) / cols;
+    tiles += (int64_t)a.num_m[j] * a.num_n[j];
+  }
+  if (tiles > 0x7FFFFFFF - 1024) return SF_ERR_SHAPE;
+  const int64_t pairs = tiles < sm_count_now() / 2 ? tiles : sm_count_now() / 2;
+  return launch_pdl(kern, dim3((unsigned)(2 * pairs)), kPairThreads, Cfg::kSmem, s, maps, a);
+}
+
+}  // namespace
+}  // namespace sf

@@ -1,0 +1,230 @@
+"""The gated feed-forward block through the C ABI: exact on small integers at every edge of the tiles, within derived bounds for every
+activation, captured and replayed, on another stream, and with everything around its buffers left alone."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import f32_to_bf16, gated
+from paper_2602_06183_b200 import binding
+from util import Guarded, bits, f32, to_dev
+
+pytestmark = pytest.mark.gpu
+
+GRADS = ("dX", "dWg", "dWu", "dWd")
+
+
+def _ints(shape, r, lo=-2, hi=2, keep=0.3):
+    """Small integers, most of them zero: sums stay exact in float32."""
+    return (r.integers(lo, hi + 1, size=shape) * (r.random(shape) < keep)).astype(np.float64)
+
+
+def _dev(a):
+    return to_dev(f32_to_bf16(a.astype(np.float32)).reshape(a.shape))
+
+
+class Block:
+    """A block's tensors on the device, every buffer between guards."""
+
+    def __init__(self, T, D, F, act, X, Wg, Wu, Wd, dY=None, training=True):
+        self.desc = binding.make_gated_desc(T, D, F, binding.__dict__["SF_ACT_" + act.upper()])
+        c, w = binding.sf_gated_ffn_workspace_size(self.desc)
+        self.ctx = Guarded(c) if training else None
+        self.ws = Guarded(w)
+        self.ws.t[:256].zero_()
+        self.X, self.Wg, self.Wu, self.Wd = map(_dev, (X, Wg, Wu, Wd))
+        self.Y = Guarded((T, D), torch.bfloat16)
+        if dY is not None:
+            self.dY = _dev(dY)
+            self.out = {k: Guarded(tuple(getattr(self, k[1:]).shape), torch.bfloat16) for k in GRADS}
+
+    def fwd(self, stream=None):
+        binding.sf_gated_ffn_fwd(self.desc, self.X, self.Wg, self.Wu, self.Wd, self.Y.t, self.ctx.t if self.ctx else None, self.ws.t, stream=stream)
+
+    def bwd(self, only=GRADS, stream=None):
+        o = [self.out[k].t if k in only else None for k in GRADS]
+        binding.sf_gated_ffn_bwd(self.desc, self.dY, self.X, self.Wg, self.Wu, self.Wd, self.ctx.t, *o, self.ws.t, stream=stream)
+
+    def check(self):
+        assert binding.sf_check_status(self.ws.t) == binding.SF_OK
+        for g in [self.ctx, self.ws, self.Y, *getattr(self, "out", {}).values()]:
+            if g is not None:
+                g.check()
+
+
+def _same(got, ref, what):
+    g = bits(got)
+    r = f32_to_bf16(ref.astype(np.float32)).reshape(ref.shape)
+    bad = (g != r) & ~((g & 0x7FFF == 0) & (r & 0x7FFF == 0))
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} differ, first at {tuple(np.argwhere(bad)[0])}"
+
+
+def _within(got, ref, tol, what):
+    d = np.abs(f32(got).astype(np.float64) - ref)
+    assert np.all(d <= tol), f"{what}: {(d > tol).sum()} of {d.size} outside, worst {np.max(d / np.maximum(tol, 1e-300)):.3g} of the bound"
+
+
+# one token to more than a tile of 256; D and F: one 16-byte unit, below and above a block of 64, odd multiples of 8, several tiles
+SHAPES = [(1, 8, 8), (1, 264, 520), (2, 72, 136), (7, 1000, 328), (16, 64, 128), (17, 128, 64), (33, 520, 1032), (64, 256, 256),
+          (65, 136, 392), (128, 200, 776), (129, 8, 16), (129, 264, 520), (200, 584, 72), (256, 256, 512), (257, 392, 1160), (513, 136, 264)]
+
+
+@pytest.mark.parametrize("T,D,F", SHAPES)
+def test_step_is_exact_on_small_integers(T, D, F):
+    r = np.random.default_rng(T * 7 + D + F)
+    X, Wg, Wu, Wd, dY = _ints((T, D), r), _ints((F, D), r, -1, 1), _ints((F, D), r, -1, 1), _ints((D, F), r, -1, 1, 0.1), _ints((T, D), r, -1, 1)
+    ref = gated.exact_step(X, Wg, Wu, Wd, dY)
+    b = Block(T, D, F, "relu", X, Wg, Wu, Wd, dY)
+    b.fwd()
+    b.bwd()
+    b.check()
+    _same(b.Y.t, ref["Y"], "Y")
+    for k in GRADS:
+        _same(b.out[k].t, ref[k], k)
+    # without a context: the same Y, bit for bit
+    i = Block(T, D, F, "relu", X, Wg, Wu, Wd, training=False)
+    i.fwd()
+    i.check()
+    assert np.array_equal(bits(i.Y.t), bits(b.Y.t))
+
+
+def _normals(T, D, F, seed):
+    r = np.random.default_rng(seed)
+    def n(shape, s):
+        return gated.rne_bf16(r.normal(size=shape) * s)
+    return n((T, D), 1.0), n((F, D), 1.5 / D ** 0.5), n((F, D), 1 / D ** 0.5), n((D, F), 1 / F ** 0.5), n((T, D), 1.0)
+
+
+@pytest.mark.parametrize("act", gated.ACTS)
+@pytest.mark.parametrize("T,D,F", [(3, 264, 200), (40, 72, 136), (100, 128, 264), (300, 200, 392)])
+def test_step_within_the_bounds(act, T, D, F):
+    X, Wg, Wu, Wd, dY = _normals(T, D, F, T + len(act))
+    b = Block(T, D, F, act, X, Wg, Wu, Wd, dY)
+    b.fwd()
+    b.bwd()
+    b.check()
+    f = gated.forward(X, Wg, Wu, Wd, act)
+    _within(b.Y.t, f.Y, f.err_Y, "Y")
+    for k, (v, e) in gated.backward(X, Wg, Wu, Wd, dY, act).items():
+        _within(b.out[k].t, v, e, k)
+
+
+@pytest.mark.parametrize("act", gated.ACTS)
+def test_activation_in_its_tails(act):
+    """One column of X drives the gate from far below to far above 0: H = act(g), read through Wd = 1."""
+    g = np.concatenate([np.linspace(-60, 60, 121), [-1e4, -300.0, -88.0, 0.0, 88.0, 300.0, 1e4]])
+    g = gated.rne_bf16(g)
+    T = len(g)
+    X = np.zeros((T, 8)); X[:, 0] = g; X[:, 1] = 1.0   # noqa: E702
+    Wg, Wu, Wd = np.zeros((8, 8)), np.zeros((8, 8)), np.zeros((8, 8))
+    Wg[0, 0] = Wu[0, 1] = Wd[0, 0] = 1.0
+    for rows in (slice(0, T), slice(0, 40)):            # the kernel for long operands and the one for few tokens
+        x = X[rows]
+        b = Block(len(x), 8, 8, act, x, Wg, Wu, Wd, training=False)
+        b.fwd()
+        b.check()
+        ref = gated.act(act, x[:, 0])[0]
+        # evaluation in float32, one rounding for H (Y = H); results below float32's smallest normal may be flushed
+        tol = gated.U16 * np.abs(ref) + gated.ELEM * (1 + np.abs(x[:, 0])) * np.abs(ref) + 2.0 ** -125
+        _within(b.Y.t[:, 0], ref, tol, act)
+        assert not f32(b.Y.t)[:, 1:].any()
+
+
+def test_left_out_outputs():
+    T, D, F = 70, 72, 136
+    b = Block(T, D, F, "silu", *_normals(T, D, F, 5))
+    b.fwd()
+    b.bwd()
+    whole = {k: bits(b.out[k].t) for k in GRADS}
+    for only in [("dX",), ("dWg",), ("dWu", "dX"), ("dWd",), ("dWg", "dWd"), ()]:
+        for k in GRADS:
+            b.out[k].t.fill_(7.0)
+        b.bwd(only)
+        for k in GRADS:
+            if k in only:
+                assert np.array_equal(bits(b.out[k].t), whole[k]), (only, k)
+            else:
+                assert bool((b.out[k].t == 7.0).all()), (only, k)
+    b.check()
+
+
+def test_no_tokens():
+    D, F = 64, 72
+    z = np.zeros
+    b = Block(0, D, F, "silu", z((0, D)), z((F, D)), z((F, D)), z((D, F)), z((0, D)))
+    b.fwd()
+    for k in GRADS[1:]:
+        b.out[k].t.fill_(3.0)
+    b.bwd()
+    b.check()
+    for k in GRADS[1:]:
+        assert not bool(b.out[k].t.any())
+
+
+def test_non_finite_rows_stay_in_their_rows():
+    for T in (9, 140):
+        D, F = 72, 136
+        X, Wg, Wu, Wd, dY = _normals(T, D, F, 9)
+        clean = Block(T, D, F, "silu", X, Wg, Wu, Wd, dY)
+        clean.fwd()
+        X[4, 3], X[6, 5] = np.nan, np.inf
+        b = Block(T, D, F, "silu", X, Wg, Wu, Wd, dY)
+        b.fwd()
+        b.check()
+        y, c = f32(b.Y.t), f32(clean.Y.t)
+        ok = np.ones(T, bool)
+        ok[[4, 6]] = False
+        assert np.array_equal(y[ok], c[ok]) and not np.isfinite(y[~ok]).any()
+
+
+@pytest.mark.parametrize("T", [5, 200])
+def test_captured_replayed_and_on_another_stream(T):
+    D, F = 136, 264
+    a, c = _normals(T, D, F, 11), _normals(T, D, F, 12)
+    want = []
+    for x in (a, c):
+        b = Block(T, D, F, "gelu_tanh", *x)
+        b.fwd()
+        b.bwd()
+        want.append({"Y": bits(b.Y.t), **{k: bits(b.out[k].t) for k in GRADS}})
+    s = torch.cuda.Stream()
+    b = Block(T, D, F, "gelu_tanh", *a)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        b.fwd()
+        b.bwd()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            b.fwd()
+            b.bwd()
+    s.synchronize()
+    for i, x in ((0, a), (1, c), (0, a)):
+        for t, v in zip((b.X, b.Wg, b.Wu, b.Wd, b.dY), x):
+            t.copy_(_dev(v))
+        for g in (b.Y, *b.out.values()):
+            g.t.fill_(9.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        b.check()
+        assert np.array_equal(bits(b.Y.t), want[i]["Y"])
+        for k in GRADS:
+            assert np.array_equal(bits(b.out[k].t), want[i][k]), k
+    # the stream handed over instead of made current
+    b.Y.t.zero_()
+    torch.cuda.synchronize()
+    b.fwd(stream=s)
+    s.synchronize()
+    assert np.array_equal(bits(b.Y.t), want[0]["Y"])
+
+
+def test_repeated_calls_give_the_same_bits():
+    for T, D, F in [(1, 4096, 520), (3, 520, 4096), (100, 1024, 1032), (300, 264, 2048)]:
+        b = Block(T, D, F, "silu", *_normals(T, D, F, 3))
+        got = []
+        for _ in range(3):
+            b.fwd()
+            b.bwd()
+            got.append([bits(b.Y.t)] + [bits(b.out[k].t) for k in GRADS])
+        b.check()
+        for g in got[1:]:
+            assert all(np.array_equal(x, y) for x, y in zip(g, got[0]))
