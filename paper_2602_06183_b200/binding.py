@@ -173,9 +173,13 @@ try:
 
     def _current_stream() -> int:
         return _cuda_getCurrentRawStream(_cuda_getDevice())
+
+    _current_device = _cuda_getDevice
 except ImportError:
     def _current_stream() -> int:
         return torch.cuda.current_stream().cuda_stream
+
+    _current_device = torch.cuda.current_device
 
 
 def _stream(stream: Optional[torch.cuda.Stream] = None):
@@ -522,28 +526,36 @@ def sf_routed_ctx_view(desc, buf: torch.Tensor, field: int) -> torch.Tensor:
 
 # ---- gated feed-forward block and 4-bit operands -------------------------------------------------------
 # These calls take any number of tokens, so a tensor of another shape, type, layout or device would be read as something else
-# without a trace: they are checked here, where the sizes are still known.
+# without a trace: they are checked here, where the sizes are still known. A call on a single token is host-bound, so what passes is found
+# in one expression (0.4 us a tensor) and only what does not is looked at closely. `dev` is the device of the call's first tensor;
+# _launch_stream, the last argument of every call, refuses it unless it is the current one.
 
-def _current_device() -> int:
-    return torch.cuda.current_device() if torch.cuda.is_available() else -1
+def _refused(where: str, name: str, t, dtype, shape):
+    if t.dtype is not dtype or tuple(t.shape) != shape:
+        return SparseFFNError(SF_ERR_SHAPE, f"{where}: {name} is {t.dtype} {tuple(t.shape)}, wanted {dtype} {shape}")
+    if not t.is_contiguous():
+        return SparseFFNError(SF_ERR_ALIGN, f"{where}: {name} is not contiguous")
+    return SparseFFNError(SF_ERR_UNSUPPORTED, f"{where}: {name} is on {t.device}, another device than the first tensor")
 
 
-def _refuse(ok: bool, status: int, where: str, what: str) -> None:
-    if not ok:
-        raise SparseFFNError(status, f"{where}: {what}")
+def _tensor(where: str, name: str, t, dtype, shape, dev: int):
+    """The address of a contiguous tensor of that type and shape on device `dev`."""
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    raise _refused(where, name, t, dtype, shape)
 
 
-def _expect(where: str, dev: int, **tensors) -> None:
-    """name=(tensor, dtype, shape): contiguous, of that type and shape, on device `dev`; a tensor of None passes."""
-    for name, (t, dtype, shape) in tensors.items():
-        if t is None:
-            continue
-        if t.dtype is not dtype or tuple(t.shape) != shape:
-            raise SparseFFNError(SF_ERR_SHAPE, f"{where}: {name} is {t.dtype} {tuple(t.shape)}, wanted {dtype} {shape}")
-        if not t.is_contiguous():
-            raise SparseFFNError(SF_ERR_ALIGN, f"{where}: {name} is not contiguous")
-        if t.get_device() != dev:
-            raise SparseFFNError(SF_ERR_UNSUPPORTED, f"{where}: {name} is on {t.device}, the current device is {dev}")
+def _buffer(where: str, name: str, t, dev: int):
+    """(address, bytes) of a context or workspace; (None, 0) of None."""
+    if t is None:
+        return None, 0
+    return _tensor(where, name, t, t.dtype, t.shape, dev), t.numel() * t.element_size()
+
+
+def _launch_stream(where: str, dev: int, stream):
+    if dev < 0 or dev != _current_device():
+        raise SparseFFNError(SF_ERR_UNSUPPORTED, f"{where}: the tensors are on {'the CPU' if dev < 0 else f'device {dev}'}, not on the current device")
+    return _current_stream() if stream is None else stream.cuda_stream
 
 
 def make_gated_desc(T, D, F, act=SF_ACT_SILU) -> sf_gated_ffn_desc:
@@ -562,39 +574,26 @@ def alloc_gated_ffn_buffers(desc: sf_gated_ffn_desc, device="cuda", training: bo
     return torch.empty((c,), dtype=torch.uint8, device=device) if training else None, _workspace(w, device)
 
 
-def _bytes_or_none(t):
-    return 0 if t is None else _nbytes(t)
-
-
 def sf_gated_ffn_fwd(desc, X, Wg, Wu, Wd, Y, fwd_ctx, workspace, stream=None):
     """Y = (act(X Wg^T) * (X Wu^T)) Wd^T. fwd_ctx None: nothing is kept for a backward pass."""
-    T, D, F, bf = desc.T, desc.D, desc.F, torch.bfloat16
-    dev = _current_device()
-    _expect("sf_gated_ffn_fwd", dev, X=(X, bf, (T, D)), Wg=(Wg, bf, (F, D)), Wu=(Wu, bf, (F, D)), Wd=(Wd, bf, (D, F)),
-            Y=(Y, bf, (T, D)))
-    _expect_buffers("sf_gated_ffn_fwd", dev, fwd_ctx, workspace)
-    _check(lib().sf_gated_ffn_fwd(C.byref(desc), _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(Y), _ptr(fwd_ctx),
-                                  _bytes_or_none(fwd_ctx), _ptr(workspace), _bytes_or_none(workspace), _stream(stream)),
-           "sf_gated_ffn_fwd")
-
-
-def _expect_buffers(where, dev, *bufs):
-    for b in bufs:
-        if b is not None:
-            _refuse(b.is_contiguous(), SF_ERR_ALIGN, where, "a context or workspace is not contiguous")
-            _refuse(b.get_device() == dev, SF_ERR_UNSUPPORTED, where, f"a context or workspace is on {b.device}, the current device is {dev}")
+    w, bf, dev = "sf_gated_ffn_fwd", torch.bfloat16, X.get_device()
+    td, fd, df = (desc.T, desc.D), (desc.F, desc.D), (desc.D, desc.F)
+    _check(lib().sf_gated_ffn_fwd(
+        C.byref(desc), _tensor(w, "X", X, bf, td, dev), _tensor(w, "Wg", Wg, bf, fd, dev), _tensor(w, "Wu", Wu, bf, fd, dev),
+        _tensor(w, "Wd", Wd, bf, df, dev), _tensor(w, "Y", Y, bf, td, dev), *_buffer(w, "fwd_ctx", fwd_ctx, dev),
+        *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
 
 
 def sf_gated_ffn_bwd(desc, dY, X, Wg, Wu, Wd, fwd_ctx, dX, dWg, dWu, dWd, workspace, stream=None):
     """Gradients of sf_gated_ffn_fwd with the context that it filled. An output of None is left out."""
-    T, D, F, bf = desc.T, desc.D, desc.F, torch.bfloat16
-    dev = _current_device()
-    _expect("sf_gated_ffn_bwd", dev, dY=(dY, bf, (T, D)), X=(X, bf, (T, D)), Wg=(Wg, bf, (F, D)), Wu=(Wu, bf, (F, D)),
-            Wd=(Wd, bf, (D, F)), dX=(dX, bf, (T, D)), dWg=(dWg, bf, (F, D)), dWu=(dWu, bf, (F, D)), dWd=(dWd, bf, (D, F)))
-    _expect_buffers("sf_gated_ffn_bwd", dev, fwd_ctx, workspace)
-    _check(lib().sf_gated_ffn_bwd(C.byref(desc), _ptr(dY), _ptr(X), _ptr(Wg), _ptr(Wu), _ptr(Wd), _ptr(fwd_ctx),
-                                  _bytes_or_none(fwd_ctx), _ptr(dX), _ptr(dWg), _ptr(dWu), _ptr(dWd), _ptr(workspace),
-                                  _bytes_or_none(workspace), _stream(stream)), "sf_gated_ffn_bwd")
+    w, bf, dev = "sf_gated_ffn_bwd", torch.bfloat16, X.get_device()
+    td, fd, df = (desc.T, desc.D), (desc.F, desc.D), (desc.D, desc.F)
+    _check(lib().sf_gated_ffn_bwd(
+        C.byref(desc), _tensor(w, "dY", dY, bf, td, dev), _tensor(w, "X", X, bf, td, dev), _tensor(w, "Wg", Wg, bf, fd, dev),
+        _tensor(w, "Wu", Wu, bf, fd, dev), _tensor(w, "Wd", Wd, bf, df, dev), *_buffer(w, "fwd_ctx", fwd_ctx, dev),
+        None if dX is None else _tensor(w, "dX", dX, bf, td, dev), None if dWg is None else _tensor(w, "dWg", dWg, bf, fd, dev),
+        None if dWu is None else _tensor(w, "dWu", dWu, bf, fd, dev), None if dWd is None else _tensor(w, "dWd", dWd, bf, df, dev),
+        *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
 
 
 def sf_fp4_sizes(rows: int, cols: int, fmt: int):
@@ -603,40 +602,57 @@ def sf_fp4_sizes(rows: int, cols: int, fmt: int):
     return a.value, b.value
 
 
-def _row_stride(where, name, t):
-    _refuse(t.dim() == 2 and t.dtype is torch.bfloat16, SF_ERR_SHAPE, where, f"{name} must be a bfloat16 matrix")
-    _refuse(t.shape[1] <= 1 or t.stride(1) == 1, SF_ERR_ALIGN, where, f"{name}'s rows are not contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _scale_bytes(rows: int, cols: int, fmt: int) -> int:
+    """Bytes of the scale tiles, as sf_fp4_sizes has them."""
+    if cols % 32 or (fmt != SF_FP4_NV and fmt != SF_FP4_MX):
+        return sf_fp4_sizes(rows, cols, fmt)[1]                  # refuses
+    return -(-rows // 128) * -(-cols // (64 if fmt == SF_FP4_NV else 128)) * 512
+
+
+def _row_stride(where: str, name: str, t) -> int:
+    """Leading dimension of a bfloat16 matrix with contiguous rows."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 2:
+        raise SparseFFNError(SF_ERR_SHAPE, f"{where}: {name} must be a bfloat16 matrix")
+    if t.stride(1) != 1 and t.size(1) > 1:
+        raise SparseFFNError(SF_ERR_ALIGN, f"{where}: {name}'s rows are not contiguous")
+    return t.stride(0) if t.size(0) > 1 else t.size(1)
+
+
+def _codes_shape(where: str, *codes):
+    for t in codes:
+        if t.dim() != 2:
+            raise SparseFFNError(SF_ERR_SHAPE, f"{where}: codes must be a matrix")
+    return codes[0].shape
 
 
 def sf_fp4_quantize(X, fmt: int, scale: float, out=None, stream=None):
     """(codes uint8 [rows, cols/2], scales uint8 tiles) of bf16 X, which may be a strided row view; ``out`` = a previous result
     to write into."""
-    where, dev = "sf_fp4_quantize", _current_device()
-    ld = _row_stride(where, "X", X)
+    w, u8, dev = "sf_fp4_quantize", torch.uint8, X.get_device()
+    ld = _row_stride(w, "X", X)
     rows, cols = X.shape
-    _, n = sf_fp4_sizes(rows, cols, fmt)
-    codes, scales = out if out is not None else (torch.empty((rows, cols // 2), dtype=torch.uint8, device=X.device),
-                                                 torch.empty((n,), dtype=torch.uint8, device=X.device))
-    _refuse(X.get_device() == dev, SF_ERR_UNSUPPORTED, where, f"X is on {X.device}, the current device is {dev}")
-    _expect(where, dev, codes=(codes, torch.uint8, (rows, cols // 2)), scales=(scales, torch.uint8, (n,)))
-    _check(lib().sf_fp4_quantize(_ptr(X), rows, cols, ld, fmt, float(scale), _ptr(codes), _ptr(scales), _stream(stream)), where)
-    return codes, scales
+    n = _scale_bytes(rows, cols, fmt)
+    if out is None:
+        out = torch.empty((rows, cols // 2), dtype=u8, device=X.device), torch.empty((n,), dtype=u8, device=X.device)
+    codes, scales = out
+    _check(lib().sf_fp4_quantize(X.data_ptr(), rows, cols, ld, fmt, scale, _tensor(w, "codes", codes, u8, (rows, cols // 2), dev),
+                                 _tensor(w, "scales", scales, u8, (n,), dev), _launch_stream(w, dev, stream)), w)
+    return out
 
 
 def sf_fp4_dequantize(codes, scales, fmt: int, alpha: float, out=None, stream=None):
     """bf16 [rows, cols] = code * sf * alpha; ``out`` may be a strided row view."""
-    where, dev = "sf_fp4_dequantize", _current_device()
-    _refuse(codes.dim() == 2, SF_ERR_SHAPE, where, "codes must be a matrix")
-    rows, cols = codes.shape[0], 2 * codes.shape[1]
-    _, n = sf_fp4_sizes(rows, cols, fmt)
+    w, u8, dev = "sf_fp4_dequantize", torch.uint8, codes.get_device()
+    rows, half = _codes_shape(w, codes)
+    cols = 2 * half
     if out is None:
         out = torch.empty((rows, cols), dtype=torch.bfloat16, device=codes.device)
-    ld = _row_stride(where, "out", out)
-    _refuse(tuple(out.shape) == (rows, cols), SF_ERR_SHAPE, where, f"out is {tuple(out.shape)}, wanted {(rows, cols)}")
-    _refuse(out.get_device() == dev, SF_ERR_UNSUPPORTED, where, f"out is on {out.device}, the current device is {dev}")
-    _expect(where, dev, codes=(codes, torch.uint8, (rows, cols // 2)), scales=(scales, torch.uint8, (n,)))
-    _check(lib().sf_fp4_dequantize(_ptr(codes), _ptr(scales), rows, cols, fmt, float(alpha), _ptr(out), ld, _stream(stream)), where)
+    ld = _row_stride(w, "out", out)
+    if out.shape != (rows, cols) or out.get_device() != dev:
+        raise _refused(w, "out", out, torch.bfloat16, (rows, cols))
+    _check(lib().sf_fp4_dequantize(_tensor(w, "codes", codes, u8, (rows, half), dev),
+                                   _tensor(w, "scales", scales, u8, (_scale_bytes(rows, cols, fmt),), dev), rows, cols, fmt, alpha,
+                                   out.data_ptr(), ld, _launch_stream(w, dev, stream)), w)
     return out
 
 
@@ -646,46 +662,38 @@ def sf_gemm_fp4_workspace_size(Mr: int, Nc: int, K: int) -> int:
     return a.value
 
 
-def _fp4_operands(where, dev, fmt, K, **ops):
-    u8 = torch.uint8
-    for name, (codes, scales) in ops.items():
-        _refuse(codes.dim() == 2, SF_ERR_SHAPE, where, f"{name} must be a matrix of codes")
-        rows = codes.shape[0]
-        _expect(where, dev, **{name: (codes, u8, (rows, K // 2)), name + "_scales": (scales, u8, (sf_fp4_sizes(rows, K, fmt)[1],))})
-
-
 def sf_gemm_fp4(A, a_scales, B, b_scales, fmt: int, alpha: float, C_out=None, workspace=None, stream=None):
     """C[Mr,Nc] = bf16(alpha * A B^T) of two 4-bit operands, codes [Mr,K/2] and [Nc,K/2] with their scales."""
-    where, dev = "sf_gemm_fp4", _current_device()
-    Mr, Nc, K = A.shape[0], B.shape[0], 2 * A.shape[1]
-    _fp4_operands(where, dev, fmt, K, A=(A, a_scales), B=(B, b_scales))
+    w, u8, dev = "sf_gemm_fp4", torch.uint8, A.get_device()
+    Mr, half = _codes_shape(w, A, B)
+    Nc, K = B.size(0), 2 * half
+    a, a_s = _tensor(w, "A", A, u8, (Mr, half), dev), _tensor(w, "a_scales", a_scales, u8, (_scale_bytes(Mr, K, fmt),), dev)
+    b, b_s = _tensor(w, "B", B, u8, (Nc, half), dev), _tensor(w, "b_scales", b_scales, u8, (_scale_bytes(Nc, K, fmt),), dev)
     if C_out is None:
         C_out = torch.empty((Mr, Nc), dtype=torch.bfloat16, device=A.device)
     if workspace is None:
         workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device)
-    _expect(where, dev, C_out=(C_out, torch.bfloat16, (Mr, Nc)))
-    _expect_buffers(where, dev, workspace)
-    _check(lib().sf_gemm_fp4(_ptr(A), _ptr(a_scales), _ptr(B), _ptr(b_scales), fmt, _ptr(C_out), Mr, Nc, K, float(alpha),
-                             _ptr(workspace), _nbytes(workspace), _stream(stream)), where)
+    _check(lib().sf_gemm_fp4(a, a_s, b, b_s, fmt, _tensor(w, "C_out", C_out, torch.bfloat16, (Mr, Nc), dev), Mr, Nc, K, alpha,
+                             *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
     return C_out
 
 
 def sf_gemm_fp4_gated(A, a_scales, Bg, bg_scales, Bu, bu_scales, fmt: int, act: int, alpha_g: float, alpha_u: float, H_out=None,
                       workspace=None, stream=None):
     """H[Mr,Nc] = bf16(act(alpha_g * A Bg^T) * (alpha_u * A Bu^T)) of 4-bit operands."""
-    where, dev = "sf_gemm_fp4_gated", _current_device()
-    Mr, Nc, K = A.shape[0], Bg.shape[0], 2 * A.shape[1]
-    _fp4_operands(where, dev, fmt, K, A=(A, a_scales), Bg=(Bg, bg_scales), Bu=(Bu, bu_scales))
-    _refuse(Bu.shape[0] == Nc, SF_ERR_SHAPE, where, f"Bg has {Nc} rows, Bu {Bu.shape[0]}")
+    w, u8, dev = "sf_gemm_fp4_gated", torch.uint8, A.get_device()
+    Mr, half = _codes_shape(w, A, Bg, Bu)
+    Nc, K = Bg.size(0), 2 * half
+    shape, tiles = (Nc, half), (_scale_bytes(Nc, K, fmt),)
+    a, a_s = _tensor(w, "A", A, u8, (Mr, half), dev), _tensor(w, "a_scales", a_scales, u8, (_scale_bytes(Mr, K, fmt),), dev)
+    g, g_s = _tensor(w, "Bg", Bg, u8, shape, dev), _tensor(w, "bg_scales", bg_scales, u8, tiles, dev)
+    u, u_s = _tensor(w, "Bu", Bu, u8, shape, dev), _tensor(w, "bu_scales", bu_scales, u8, tiles, dev)
     if H_out is None:
         H_out = torch.empty((Mr, Nc), dtype=torch.bfloat16, device=A.device)
     if workspace is None:
         workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device)
-    _expect(where, dev, H_out=(H_out, torch.bfloat16, (Mr, Nc)))
-    _expect_buffers(where, dev, workspace)
-    _check(lib().sf_gemm_fp4_gated(_ptr(A), _ptr(a_scales), _ptr(Bg), _ptr(bg_scales), _ptr(Bu), _ptr(bu_scales), fmt, act,
-                                   _ptr(H_out), Mr, Nc, K, float(alpha_g), float(alpha_u), _ptr(workspace), _nbytes(workspace),
-                                   _stream(stream)), where)
+    _check(lib().sf_gemm_fp4_gated(a, a_s, g, g_s, u, u_s, fmt, act, _tensor(w, "H_out", H_out, torch.bfloat16, (Mr, Nc), dev), Mr, Nc, K,
+                                   alpha_g, alpha_u, *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
     return H_out
 
 

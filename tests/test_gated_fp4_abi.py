@@ -86,7 +86,7 @@ def test_binding_refuses_tensors_that_would_be_read_as_something_else(lib):
     assert _status(lambda: fwd(x=X.float())) == SF_ERR_SHAPE
     assert _status(lambda: fwd(wd=Wd.T)) == SF_ERR_SHAPE
     assert _status(lambda: fwd(w=torch.zeros(24, 32, dtype=bf)[:, ::2])) == SF_ERR_ALIGN
-    codes, scales = torch.zeros(4, 32, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8)
+    codes, scales = torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8)
     gemm = lambda A=codes, sa=scales, B=codes, fmt=0: binding.sf_gemm_fp4(A, sa, B, scales, fmt, 1.0)   # noqa: E731
     assert _status(lambda: gemm(B=codes[:, :16])) == SF_ERR_SHAPE
     assert _status(lambda: gemm(sa=scales[:256])) == SF_ERR_SHAPE
