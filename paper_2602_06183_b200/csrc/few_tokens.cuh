@@ -169,6 +169,11 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
         const uint64_t w = proto + (sw >> 4), x = proto + ((sw + kMats * Cfg::kWBytes) >> 4);
         const uint32_t scol = tmem_base + Cfg::kScaleCol + ((uint32_t)(kb - kb0) & 1u) * Cfg::kScaleCols;
         if constexpr (kFp4) {
+          // one of two buffers in turn; the products of two blocks ago, which read this one, have signalled their end with their stage
+          if (kb - kb0 >= 2) {
+            const uint32_t back = stage >= 2 ? stage - 2 : stage + kStages - 2;
+            if (!mbar_wait(&ctl->empty[back], stage >= 2 ? phase : phase ^ 1u, abort_flag)) { ok = false; break; }
+          }
           const uint64_t sd = s_proto + ((sw + kMats * Cfg::kWBytes + Cfg::kXBytes) >> 4);
 #pragma unroll
           for (int i = 0; i < kTiles * (kMats + 1); ++i) tmem_cp_scales(scol + 4 * i, sd + 32 * i);

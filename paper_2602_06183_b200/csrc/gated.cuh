@@ -17,10 +17,32 @@ enum OperandFmt { FMT_BF16 = 0, FMT_NV = 1, FMT_MX = 2 };
 // Value and derivative of the gate's activation in float32. The sigmoid is written with the exponential of -x, so that neither
 // tail cancels: 1 / (1 + e^-x) is 0 or 1 to within rounding there, and x times it underflows as the function does (rcp.approx holds to an
 // ulp for every denominator; the fast division gives 0 from 2^126 on, which x < -87 reaches).
-__device__ __forceinline__ float sigmoid32(float x) {
+__device__ __forceinline__ float rcp32(float x) {
   float r;
-  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.f + __expf(-x)));
+  asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+__device__ __forceinline__ float sigmoid32(float x) { return rcp32(1.f + __expf(-x)); }
+
+// The normal distribution from its tail, Phi(-x) = e^(-x^2 / 2) p(1 / (1 + 0.3 x)) for x >= 0: the tail over its exponential is smooth in that
+// variable, and a polynomial of degree 8 (weighted least squares over 0 <= x <= 14, the weights raised where the relative error was
+// largest until it was level) is within 6e-8 of it, 4e-7 in float32 arithmetic, at every x where the exponential is not zero. A library call
+// that is as exact took the epilogue of the 1999 x 5504 x 1408 product 9600 issue cycles a tile, next to 11 300 of its main loop.
+// e: the exponential, which the density shares.
+__device__ __forceinline__ float normal_cdf(float g, float& e) {
+  const float x = fabsf(g), t = rcp32(fmaf(0.3f, x, 1.f));
+  float p = 0.038378290832042694f;
+  p = fmaf(p, t, -0.16916611790657043f);
+  p = fmaf(p, t, 0.22866007685661316f);
+  p = fmaf(p, t, -0.07650648057460785f);
+  p = fmaf(p, t, 0.1425355225801468f);
+  p = fmaf(p, t, 0.09468352049589157f);
+  p = fmaf(p, t, 0.12192033976316452f);
+  p = fmaf(p, t, 0.1194876879453659f);
+  p = fmaf(p, t, 7.168875981733436e-06f);
+  e = __expf(-0.5f * g * g);
+  const float tail = e * p;
+  return g < 0.f ? tail : 1.f - tail;
 }
 
 template <int kAct>
@@ -30,9 +52,10 @@ __device__ __forceinline__ void gate_act(float g, float& a, float& da) {
     a = g * s;
     da = s * fmaf(g, 1.f - s, 1.f);
   } else if constexpr (kAct == SF_ACT_GELU) {
-    const float c = normcdff(g);
+    float e;
+    const float c = normal_cdf(g, e);
     a = g * c;
-    da = fmaf(g, 0.3989422804014327f * __expf(-0.5f * g * g), c);
+    da = fmaf(g, 0.3989422804014327f * e, c);
   } else if constexpr (kAct == SF_ACT_GELU_TANH) {
     // 0.5 (1 + tanh(z)) = sigmoid(2 z), z = sqrt(2 / pi) (g + 0.044715 g^3)
     constexpr float k = 1.5957691216057308f, c3 = 0.044715f;

@@ -67,6 +67,7 @@ struct PairArgs {
   int nkb, nkb0;                     // k-blocks in all, and of the first pair of operands (PK_DX)
   int act;
   float alpha, alpha2;
+  int early_next;                    // several rounds of tiles: the next launch is let in at the start (see long_dense in gemm_tc.cu)
   int* status;
 };
 template <int N> struct PairMaps { CUtensorMap m[N]; };
@@ -184,6 +185,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
   cluster_sync_all();
   tc_fence_after();
   pdl_wait();
+  if (args.early_next) pdl_trigger();
   const uint32_t tmem_base = ctl->tmem_base;
 
   if (warp == 0) {
@@ -244,7 +246,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
       const uint32_t s_lo0 = (uint32_t)s_proto + ((smem0 + Cfg::kABytes + Cfg::kBBytes) >> 4);
       constexpr uint32_t a_step = (Cfg::kAMN ? 2048 : 32) >> 4, b_step = (Cfg::kBMN ? 2048 : 32) >> 4;
       auto desc = [](uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; };
-      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, blocks = 0;
       bool ok = true;
       for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
         if (!mbar_wait(&ctl->tmem_empty[acc], acc_phase ^ 1, abort_flag)) break;
@@ -256,8 +258,13 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
           const uint32_t soff = stage * (uint32_t)(Cfg::kStageBytes >> 4);
           const uint32_t a_lo = a_lo0 + soff, b_lo = b_lo0 + soff;
           if constexpr (kFp4) {
-            // the stage's scales go to TMEM, into one of two buffers in turn, ahead of the products that read them
-            const uint32_t sa = tmem_base + Cfg::kScaleCol + ((uint32_t)kb & 1u) * Cfg::kScaleCols, sb = sa + Cfg::kScaleACols;
+            // The stage's scales go to TMEM, into one of two buffers in turn, ahead of the products that read them. The products that read
+            // this buffer last are those of two blocks ago: their end has been signalled with their stage.
+            if (blocks >= 2) {
+              const uint32_t back = stage >= 2 ? stage - 2 : stage + kStages - 2;
+              if (!mbar_wait(&ctl->empty[back], stage >= 2 ? phase : phase ^ 1u, abort_flag)) { ok = false; break; }
+            }
+            const uint32_t sa = tmem_base + Cfg::kScaleCol + (blocks & 1u) * Cfg::kScaleCols, sb = sa + Cfg::kScaleACols;
             const uint32_t s_lo = s_lo0 + soff;
 #pragma unroll
             for (int i = 0; i < Cfg::kTiles; ++i) {
@@ -279,6 +286,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
               mma_f16_2cta(d, desc(a_lo + k * a_step, a_hi), desc(b_lo + k * b_step, b_hi), idesc, (kb > 0 || k > 0) ? 1u : 0u);
           }
           mma_commit_2cta(&ctl->empty[stage]);
+          ++blocks;
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
         if (!ok) break;
@@ -324,86 +332,123 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
       tc_fence_after();
       const uint32_t taddr = tmem_base + acc * kBN + ((uint32_t)(q * 32) << 16);
       bool ok = true;
-#pragma unroll 1
-      for (int ch = set; ch < chunks; ch += 2) {
-        const int col = t.n0 + ch * 32;
-        uint32_t v[32];
-        tmem_ld_32x32b_x32(taddr + ch * 32, v);
-        if constexpr (kGated) {
-          uint32_t u[32];
-          tmem_ld_32x32b_x32(taddr + kBN / 2 + ch * 32, u);
-          tmem_ld_wait_on(v);
-          tmem_ld_wait_on(u);
-          if constexpr (kFp4) {
+      auto release = [&]() {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_leader(&ctl->tmem_empty[acc]);
+      };
+      // gate (v) and other factor (u) of a chunk to H and, where they are kept, P and Q
+      auto gated_chunk = [&](uint32_t (&v)[32], uint32_t (&u)[32], int col) {
+        uint32_t h[16];
+        with_act(args.act, [&](auto tag) {
+          constexpr int kAct = decltype(tag)::value;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              v[i] = __float_as_uint(__uint_as_float(v[i]) * args.alpha);
-              u[i] = __float_as_uint(__uint_as_float(u[i]) * args.alpha2);
+          for (int i = 0; i < 32; i += 2) {
+            float a[2], da[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float g = __uint_as_float(v[i + e]), uu = __uint_as_float(u[i + e]);
+              if (kFp4) { g *= args.alpha; uu *= args.alpha2; }
+              gate_act<kAct>(g, a[e], da[e]);
+              v[i + e] = __float_as_uint(a[e]);
+              u[i + e] = __float_as_uint(uu * da[e]);
+              a[e] *= uu;
             }
+            h[i >> 1] = bf16x2(a[0], a[1]);
           }
-          uint32_t h[16];
-          with_act(args.act, [&](auto tag) {
-            constexpr int kAct = decltype(tag)::value;
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              float a[2], da[2];
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float uu = __uint_as_float(u[i + e]);
-                gate_act<kAct>(__uint_as_float(v[i + e]), a[e], da[e]);
-                v[i + e] = __float_as_uint(a[e]);
-                u[i + e] = __float_as_uint(uu * da[e]);
-                a[e] *= uu;
-              }
-              h[i >> 1] = bf16x2(a[0], a[1]);
-            }
-          });
-          put16(&maps.m[3], h, col, row);
-          if constexpr (kKind == PK_FWD_SAVE) {
-            put32(&maps.m[4], v, col, row);
-            put32(&maps.m[5], u, col, row);
-          }
-        } else if constexpr (kKind == PK_BWD) {
-          uint32_t du[16], dg[16];
-          tmem_ld_wait_on(v);
-          if (!mbar_wait_warp(loaded, load_phase, abort_flag)) { ok = false; break; }
-          load_phase ^= 1u;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float4 p = *reinterpret_cast<const float4*>(bufs + lane * 128 + ((j ^ (lane & 7)) << 4));
-            const float4 r = *reinterpret_cast<const float4*>(bufs + 4096 + lane * 128 + ((j ^ (lane & 7)) << 4));
-            const float d0 = __uint_as_float(v[4 * j]), d1 = __uint_as_float(v[4 * j + 1]), d2 = __uint_as_float(v[4 * j + 2]),
-                        d3 = __uint_as_float(v[4 * j + 3]);
-            du[2 * j] = bf16x2(d0 * p.x, d1 * p.y); du[2 * j + 1] = bf16x2(d2 * p.z, d3 * p.w);
-            dg[2 * j] = bf16x2(d0 * r.x, d1 * r.y); dg[2 * j + 1] = bf16x2(d2 * r.z, d3 * r.w);
-          }
-          __syncwarp();                                    // every row has been read: the results take its place
-          row_bf16(bufs, lane, du);
-          row_bf16(bufs + 4096, lane, dg);
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store_2d(&maps.m[5], bufs, col, row);
-            tma_store_2d(&maps.m[4], bufs + 4096, col, row);
-            bulk_commit();
-          }
-          if (ch + 2 < chunks) fetch(ch + 2);
-        } else {
-          tmem_ld_wait_on(v);
-          uint32_t w[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float lo = __uint_as_float(v[2 * i]), hi = __uint_as_float(v[2 * i + 1]);
-            if (kFp4) { lo *= args.alpha; hi *= args.alpha; }
-            w[i] = bf16x2(lo, hi);
-          }
-          put16(&maps.m[kKind == PK_DW ? 6 + t.job : kKind == PK_DX ? 4 : 2], w, col, row);
+        });
+        put16(&maps.m[3], h, col, row);
+        if constexpr (kKind == PK_FWD_SAVE) {
+          put32(&maps.m[4], v, col, row);
+          put32(&maps.m[5], u, col, row);
         }
+      };
+      auto plain_chunk = [&](const uint32_t (&v)[32], uint32_t (&w)[16]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float lo = __uint_as_float(v[2 * i]), hi = __uint_as_float(v[2 * i + 1]);
+          if (kFp4) { lo *= args.alpha; hi *= args.alpha; }
+          w[i] = bf16x2(lo, hi);
+        }
+      };
+      if constexpr (kAccs == 1) {
+        // One accumulator: the next main loop waits for it, so all of it is read into registers and handed back before anything
+        // is made of it (4099 x 8192 x 2048 gated, blocks of 16: 133 -> 112 us; 16384 x 4096 x 4096, blocks of 32: 161 -> 158).
+        if constexpr (kGated) {
+          uint32_t v[2][32], u[2][32];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            tmem_ld_32x32b_x32(taddr + (set + 2 * i) * 32, v[i]);
+            tmem_ld_32x32b_x32(taddr + kBN / 2 + (set + 2 * i) * 32, u[i]);
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) { tmem_ld_wait_on(v[i]); tmem_ld_wait_on(u[i]); }
+          release();
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            if (set + 2 * i < chunks) gated_chunk(v[i], u[i], t.n0 + (set + 2 * i) * 32);
+        } else {
+          constexpr int kMine = kBN / 64;
+          uint32_t w[kMine][16], v[2][32];
+          tmem_ld_32x32b_x32(taddr + set * 32, v[0]);
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) {
+            tmem_ld_wait_on(v[i & 1]);
+            if (i + 1 < kMine) tmem_ld_32x32b_x32(taddr + (set + 2 * i + 2) * 32, v[(i + 1) & 1]);
+            plain_chunk(v[i & 1], w[i]);
+          }
+          release();
+#pragma unroll
+          for (int i = 0; i < kMine; ++i)
+            if (set + 2 * i < chunks) put16(&maps.m[2], w[i], t.n0 + (set + 2 * i) * 32, row);
+        }
+      } else {
+#pragma unroll 1
+        for (int ch = set; ch < chunks; ch += 2) {
+          const int col = t.n0 + ch * 32;
+          uint32_t v[32];
+          tmem_ld_32x32b_x32(taddr + ch * 32, v);
+          if constexpr (kGated) {
+            uint32_t u[32];
+            tmem_ld_32x32b_x32(taddr + kBN / 2 + ch * 32, u);
+            tmem_ld_wait_on(v);
+            tmem_ld_wait_on(u);
+            gated_chunk(v, u, col);
+          } else if constexpr (kKind == PK_BWD) {
+            uint32_t du[16], dg[16];
+            tmem_ld_wait_on(v);
+            if (!mbar_wait_warp(loaded, load_phase, abort_flag)) { ok = false; break; }
+            load_phase ^= 1u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float4 p = *reinterpret_cast<const float4*>(bufs + lane * 128 + ((j ^ (lane & 7)) << 4));
+              const float4 r = *reinterpret_cast<const float4*>(bufs + 4096 + lane * 128 + ((j ^ (lane & 7)) << 4));
+              const float d0 = __uint_as_float(v[4 * j]), d1 = __uint_as_float(v[4 * j + 1]), d2 = __uint_as_float(v[4 * j + 2]),
+                          d3 = __uint_as_float(v[4 * j + 3]);
+              du[2 * j] = bf16x2(d0 * p.x, d1 * p.y); du[2 * j + 1] = bf16x2(d2 * p.z, d3 * p.w);
+              dg[2 * j] = bf16x2(d0 * r.x, d1 * r.y); dg[2 * j + 1] = bf16x2(d2 * r.z, d3 * r.w);
+            }
+            __syncwarp();                                  // every row has been read: the results take its place
+            row_bf16(bufs, lane, du);
+            row_bf16(bufs + 4096, lane, dg);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              tma_store_2d(&maps.m[5], bufs, col, row);
+              tma_store_2d(&maps.m[4], bufs + 4096, col, row);
+              bulk_commit();
+            }
+            if (ch + 2 < chunks) fetch(ch + 2);
+          } else {
+            tmem_ld_wait_on(v);
+            uint32_t w[16];
+            plain_chunk(v, w);
+            put16(&maps.m[kKind == PK_DW ? 6 + t.job : kKind == PK_DX ? 4 : 2], w, col, row);
+          }
+        }
+        if (!ok) break;
+        release();
       }
-      if (!ok) break;
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_leader(&ctl->tmem_empty[acc]);
       if (++acc == (uint32_t)kAccs) { acc = 0; acc_phase ^= 1; }
     }
     if (lane == 0) bulk_wait_all();
@@ -443,6 +488,7 @@ int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps>& maps, PairArgs
     tiles += (int64_t)a.num_m[j] * a.num_n[j];
   }
   if (tiles > 0x7FFFFFFF - 1024) return SF_ERR_SHAPE;
+  a.early_next = tiles > sm_count_now() / 2 && (tiles * 2 / sm_count_now() + 1) * a.nkb >= 128;
   const int64_t pairs = tiles < sm_count_now() / 2 ? tiles : sm_count_now() / 2;
   return launch_pdl(kern, dim3((unsigned)(2 * pairs)), kPairThreads, Cfg::kSmem, s, maps, a);
 }
