@@ -142,6 +142,17 @@ __device__ __forceinline__ void mma_fp4_2cta(uint32_t d, uint64_t a, uint64_t b,
 __device__ __forceinline__ void tmem_cp_scales_2cta(uint32_t taddr, uint64_t sdesc) {
   asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
 }
+// True in one lane of the (converged) warp.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}\n" : "=r"(r));
+  return r != 0;
+}
+// smem_desc at address 0, as a constant: the address (in 16-byte units) is added.
+__host__ __device__ constexpr uint64_t desc_proto(uint32_t lbo, uint32_t sbo, uint32_t swizzle) {
+  return (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 | 1ull << 46 | (uint64_t)swizzle << 61;
+}
+
 template <int kKind, int kBN, int kFmt>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps> maps, const PairArgs args) {
@@ -234,63 +245,66 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
     pdl_trigger();
   } else if (warp == 1) {
     // =========================== MMA issuer (leader CTA only) ===========================
-    if (rank == 0 && lane == 0) {
+    // The whole warp walks the loop and one lane issues: with control flow and addresses the same for every lane, the compiler keeps the
+    // descriptors in uniform registers, where the instructions want them.
+    if (rank == 0) {
       constexpr uint32_t idesc = kFp4 ? idesc_fp4(256, kBN, kFmt) : idesc_bf16(256, kBN, Cfg::kAMN, Cfg::kBMN, false);
-      const uint64_t a_proto = Cfg::kAMN ? smem_desc(0, 8192, 1024, kSwizzle128B) : smem_desc(0, 16, 1024, kSwizzle128B);
-      const uint64_t b_proto = Cfg::kBMN ? smem_desc(0, 8192, 1024, kSwizzle128B) : smem_desc(0, 16, 1024, kSwizzle128B);
-      const uint64_t s_proto = smem_desc(0, 128, 128, kSwizzleNone);
-      const uint32_t a_hi = (uint32_t)(a_proto >> 32), b_hi = (uint32_t)(b_proto >> 32), s_hi = (uint32_t)(s_proto >> 32);
-      const uint32_t smem0 = smem_u32(smem);
-      const uint32_t a_lo0 = (uint32_t)a_proto + (smem0 >> 4);
-      const uint32_t b_lo0 = (uint32_t)b_proto + ((smem0 + Cfg::kABytes) >> 4);
-      const uint32_t s_lo0 = (uint32_t)s_proto + ((smem0 + Cfg::kABytes + Cfg::kBBytes) >> 4);
+      constexpr uint64_t a_proto = desc_proto(Cfg::kAMN ? 8192 : 16, 1024, kSwizzle128B);
+      constexpr uint64_t b_proto = desc_proto(Cfg::kBMN ? 8192 : 16, 1024, kSwizzle128B);
+      constexpr uint64_t s_proto = desc_proto(128, 128, kSwizzleNone);
+      const uint32_t smem16 = smem_u32(smem) >> 4, tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
       constexpr uint32_t a_step = (Cfg::kAMN ? 2048 : 32) >> 4, b_step = (Cfg::kBMN ? 2048 : 32) >> 4;
-      auto desc = [](uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; };
+      const bool issues = elect_one();
       uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, blocks = 0;
       bool ok = true;
       for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
-        if (!mbar_wait(&ctl->tmem_empty[acc], acc_phase ^ 1, abort_flag)) break;
+        if (!mbar_wait_warp(&ctl->tmem_empty[acc], acc_phase ^ 1, abort_flag)) break;
         tc_fence_after();
-        const uint32_t d = tmem_base + acc * kBN;
+        const uint32_t d = tmem + acc * kBN;
         for (int kb = 0; kb < nkb; ++kb) {
-          if (!mbar_wait(&ctl->full[stage], phase, abort_flag)) { ok = false; break; }
+          if (!mbar_wait_warp(&ctl->full[stage], phase, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t soff = stage * (uint32_t)(Cfg::kStageBytes >> 4);
-          const uint32_t a_lo = a_lo0 + soff, b_lo = b_lo0 + soff;
+          const uint32_t s16 = smem16 + stage * (uint32_t)(Cfg::kStageBytes >> 4);
+          const uint64_t a = a_proto + s16, b = b_proto + (s16 + (Cfg::kABytes >> 4));
+          const uint32_t more = kb > 0 ? 1u : 0u;
           if constexpr (kFp4) {
             // The stage's scales go to TMEM, into one of two buffers in turn, ahead of the products that read them. The products that read
             // this buffer last are those of two blocks ago: their end has been signalled with their stage.
             if (blocks >= 2) {
               const uint32_t back = stage >= 2 ? stage - 2 : stage + kStages - 2;
-              if (!mbar_wait(&ctl->empty[back], stage >= 2 ? phase : phase ^ 1u, abort_flag)) { ok = false; break; }
+              if (!mbar_wait_warp(&ctl->empty[back], stage >= 2 ? phase : phase ^ 1u, abort_flag)) { ok = false; break; }
             }
-            const uint32_t sa = tmem_base + Cfg::kScaleCol + (blocks & 1u) * Cfg::kScaleCols, sb = sa + Cfg::kScaleACols;
-            const uint32_t s_lo = s_lo0 + soff;
+            const uint32_t sa = tmem + Cfg::kScaleCol + (blocks & 1u) * Cfg::kScaleCols, sb = sa + Cfg::kScaleACols;
+            const uint64_t sd = s_proto + (s16 + ((Cfg::kABytes + Cfg::kBBytes) >> 4));
+            if (issues) {
 #pragma unroll
-            for (int i = 0; i < Cfg::kTiles; ++i) {
-              tmem_cp_scales_2cta(sa + 4 * i, desc(s_lo + 32 * i, s_hi));
+              for (int i = 0; i < Cfg::kTiles; ++i) {
+                tmem_cp_scales_2cta(sa + 4 * i, sd + 32 * i);
 #pragma unroll
-              for (int b = 0; b < Cfg::kBBlocks; ++b)
-                tmem_cp_scales_2cta(sb + 4 * (i * Cfg::kBBlocks + b), desc(s_lo + 32 * ((1 + b) * Cfg::kTiles + i), s_hi));
+                for (int j = 0; j < Cfg::kBBlocks; ++j)
+                  tmem_cp_scales_2cta(sb + 4 * (i * Cfg::kBBlocks + j), sd + 32 * ((1 + j) * Cfg::kTiles + i));
+              }
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const int i = kFmt == FMT_NV ? k : k >> 1;                                 // tile, and first scale in its words
+                const uint32_t id = kFmt == FMT_NV ? 0u : (uint32_t)(k & 1) * 2u;
+                mma_fp4_2cta<kFmt>(d, a + k * a_step, b + k * b_step, idesc | id << 4 | id << 29, sa + 4 * i, sb + 4 * i * Cfg::kBBlocks,
+                                   k > 0 ? 1u : more);
+              }
+              mma_commit_2cta(&ctl->empty[stage]);
             }
+          } else if (issues) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int i = kFmt == FMT_NV ? k : k >> 1;                                   // tile, and first scale in its words
-              const uint32_t id = kFmt == FMT_NV ? 0u : (uint32_t)(k & 1) * 2u;
-              mma_fp4_2cta<kFmt>(d, desc(a_lo + k * a_step, a_hi), desc(b_lo + k * b_step, b_hi), idesc | id << 4 | id << 29,
-                                 sa + 4 * i, sb + 4 * i * Cfg::kBBlocks, (kb > 0 || k > 0) ? 1u : 0u);
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              mma_f16_2cta(d, desc(a_lo + k * a_step, a_hi), desc(b_lo + k * b_step, b_hi), idesc, (kb > 0 || k > 0) ? 1u : 0u);
+            for (int k = 0; k < 4; ++k) mma_f16_2cta(d, a + k * a_step, b + k * b_step, idesc, k > 0 ? 1u : more);
+            mma_commit_2cta(&ctl->empty[stage]);
           }
-          mma_commit_2cta(&ctl->empty[stage]);
+          __syncwarp();
           ++blocks;
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
         if (!ok) break;
-        mma_commit_2cta(&ctl->tmem_full[acc]);
+        if (issues) mma_commit_2cta(&ctl->tmem_full[acc]);
+        __syncwarp();
         if (++acc == (uint32_t)kAccs) { acc = 0; acc_phase ^= 1; }
       }
     }
