@@ -135,10 +135,11 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
   const uint32_t tmem_base = ctl->tmem_base;
 
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t stage = 0, phase = 0;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!mbar_wait(&ctl->empty[stage], phase ^ 1, abort_flag)) break;
+    const bool issues = elect_one();
+    uint32_t stage = 0, phase = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag)) break;
+      if (issues) {
         uint8_t* sw = smem + stage * Cfg::kStageBytes;
         uint8_t* sx = sw + kMats * Cfg::kWBytes;
         uint8_t* ss = sx + Cfg::kXBytes;
@@ -152,29 +153,32 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
           if (kGated) tma_load_3d(ss + kTiles * 512, &maps.s1, bar, 0, kb * kTiles, f0 >> 7);
           tma_load_3d(ss + kMats * kTiles * 512, &maps.sx, bar, 0, kb * kTiles, 0);
         }
-        if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1; }
       }
-      pdl_trigger();
+      if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1; }
     }
+    pdl_trigger();
   } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = kFp4 ? idesc_fp4(128, kN, kFmt) : idesc_bf16(128, kN, false, false, false);
-      const uint64_t proto = smem_desc(0, 16, 1024, kSwizzle128B), s_proto = smem_desc(0, 128, 128, kSwizzleNone);
-      uint32_t stage = 0, phase = 0;
-      bool ok = true;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        if (!mbar_wait(&ctl->full[stage], phase, abort_flag)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t sw = smem_u32(smem) + stage * (uint32_t)Cfg::kStageBytes;
-        const uint64_t w = proto + (sw >> 4), x = proto + ((sw + kMats * Cfg::kWBytes) >> 4);
-        const uint32_t scol = tmem_base + Cfg::kScaleCol + ((uint32_t)(kb - kb0) & 1u) * Cfg::kScaleCols;
+    constexpr uint32_t idesc = kFp4 ? idesc_fp4(128, kN, kFmt) : idesc_bf16(128, kN, false, false, false);
+    constexpr uint64_t proto = desc_proto(16, 1024, kSwizzle128B), s_proto = desc_proto(128, 128, kSwizzleNone);
+    const uint32_t smem16 = smem_u32(smem) >> 4, tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
+    const bool issues = elect_one();
+    uint32_t stage = 0, phase = 0;
+    bool ok = true;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait_warp(&ctl->full[stage], phase, abort_flag)) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t s16 = smem16 + stage * (uint32_t)(Cfg::kStageBytes >> 4);
+      const uint64_t w = proto + s16, x = proto + (s16 + (kMats * Cfg::kWBytes >> 4));
+      const uint32_t scol = tmem + Cfg::kScaleCol + ((uint32_t)(kb - kb0) & 1u) * Cfg::kScaleCols;
+      const uint32_t more = kb > kb0 ? 1u : 0u;
+      // scales: one of two buffers in turn; the products of two blocks ago, which read this one, have signalled their end with their stage
+      if (kFp4 && kb - kb0 >= 2) {
+        const uint32_t back = stage >= 2 ? stage - 2 : stage + kStages - 2;
+        if (!mbar_wait_warp(&ctl->empty[back], stage >= 2 ? phase : phase ^ 1u, abort_flag)) { ok = false; break; }
+      }
+      if (issues) {
         if constexpr (kFp4) {
-          // one of two buffers in turn; the products of two blocks ago, which read this one, have signalled their end with their stage
-          if (kb - kb0 >= 2) {
-            const uint32_t back = stage >= 2 ? stage - 2 : stage + kStages - 2;
-            if (!mbar_wait(&ctl->empty[back], stage >= 2 ? phase : phase ^ 1u, abort_flag)) { ok = false; break; }
-          }
-          const uint64_t sd = s_proto + ((sw + kMats * Cfg::kWBytes + Cfg::kXBytes) >> 4);
+          const uint64_t sd = s_proto + (s16 + ((kMats * Cfg::kWBytes + Cfg::kXBytes) >> 4));
 #pragma unroll
           for (int i = 0; i < kTiles * (kMats + 1); ++i) tmem_cp_scales(scol + 4 * i, sd + 32 * i);
         }
@@ -182,22 +186,22 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
         for (int m = 0; m < kMats; ++m)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint32_t accum = (kb > kb0 || k > 0) ? 1u : 0u;
-            const uint64_t wd = w + m * (Cfg::kWBytes >> 4) + 2 * k, xd = x + 2 * k;
+            const uint64_t wd = w + (m * (Cfg::kWBytes >> 4) + 2 * k), xd = x + 2 * k;
             if constexpr (kFp4) {
               const int i = kFmt == FMT_NV ? k : k >> 1;
               const uint32_t id = kFmt == FMT_NV ? 0u : (uint32_t)(k & 1) * 2u;
-              mma_fp4_1cta<kFmt>(tmem_base + m * kN, wd, xd, idesc | id << 4 | id << 29, scol + 4 * (m * kTiles + i),
-                                 scol + 4 * (kMats * kTiles + i), accum);
+              mma_fp4_1cta<kFmt>(tmem + m * kN, wd, xd, idesc | id << 4 | id << 29, scol + 4 * (m * kTiles + i),
+                                 scol + 4 * (kMats * kTiles + i), k > 0 ? 1u : more);
             } else {
-              mma_f16(tmem_base + m * kN, wd, xd, idesc, accum);
+              mma_f16(tmem + m * kN, wd, xd, idesc, k > 0 ? 1u : more);
             }
           }
         mma_commit(&ctl->empty[stage]);
-        if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1; }
       }
-      if (ok) mma_commit(&ctl->done);
+      __syncwarp();
+      if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1; }
     }
+    if (ok && issues) mma_commit(&ctl->done);
   } else {
     // every product has been made, so every load has landed and the ring is free: the partial sums go there, [matrix][token][row]
     if (mbar_wait_warp(&ctl->done, 0, abort_flag)) {
@@ -225,11 +229,10 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
     tc_fence_after();
     tmem_dealloc(tmem_base, Cfg::kTmem);
   }
-  // each CTA adds up and writes an equal share of the cluster's rows, two neighbouring output columns to a thread
-  const int pairs = 64 / S, p0 = rank * pairs;
+  // the cluster's threads share the sums, two neighbouring output columns to a thread
   const uint32_t part = smem_u32(smem);
-  for (int i = threadIdx.x; i < args.T * pairs; i += kFewThreads) {
-    const int t = i / pairs, p = p0 + (i - t * pairs), f = f0 + 2 * p;
+  for (int i = rank * kFewThreads + threadIdx.x; i < args.T * 64; i += S * kFewThreads) {
+    const int t = i >> 6, p = i & 63, f = f0 + 2 * p;
     if (f >= args.N) continue;
     float2 a = {0.f, 0.f}, b = {0.f, 0.f};
     for (int s = 0; s < S; ++s) {

@@ -142,17 +142,6 @@ __device__ __forceinline__ void mma_fp4_2cta(uint32_t d, uint64_t a, uint64_t b,
 __device__ __forceinline__ void tmem_cp_scales_2cta(uint32_t taddr, uint64_t sdesc) {
   asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
 }
-// True in one lane of the (converged) warp.
-__device__ __forceinline__ bool elect_one() {
-  uint32_t r;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}\n" : "=r"(r));
-  return r != 0;
-}
-// smem_desc at address 0, as a constant: the address (in 16-byte units) is added.
-__host__ __device__ constexpr uint64_t desc_proto(uint32_t lbo, uint32_t sbo, uint32_t swizzle) {
-  return (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 | 1ull << 46 | (uint64_t)swizzle << 61;
-}
-
 template <int kKind, int kBN, int kFmt>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps> maps, const PairArgs args) {
@@ -201,6 +190,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
 
   if (warp == 0) {
     // =========================== TMA producer (both CTAs) ===========================
+    const bool issues = elect_one();
     uint32_t stage = 0, phase = 0;
     bool ok = true;
     for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
@@ -208,8 +198,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
       const int m0 = t.m0 + rank * 128;
       const int n0 = kGated ? t.n0 : t.n0 + rank * Cfg::kHalf;
       for (int kb = 0; kb < nkb; ++kb) {
-        if (!mbar_wait(&ctl->empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
-        if (lane == 0) {
+        if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
+        if (issues) {
           uint8_t* sA = smem + stage * Cfg::kStageBytes;
           uint8_t* sB = sA + Cfg::kABytes;
           uint64_t* bar = &ctl->full[stage];
@@ -245,8 +235,6 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
     pdl_trigger();
   } else if (warp == 1) {
     // =========================== MMA issuer (leader CTA only) ===========================
-    // The whole warp walks the loop and one lane issues: with control flow and addresses the same for every lane, the compiler keeps the
-    // descriptors in uniform registers, where the instructions want them.
     if (rank == 0) {
       constexpr uint32_t idesc = kFp4 ? idesc_fp4(256, kBN, kFmt) : idesc_bf16(256, kBN, Cfg::kAMN, Cfg::kBMN, false);
       constexpr uint64_t a_proto = desc_proto(Cfg::kAMN ? 8192 : 16, 1024, kSwizzle128B);

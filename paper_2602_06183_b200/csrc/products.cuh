@@ -52,13 +52,21 @@ inline int pair_width(int64_t tiles256, int64_t tiles128, int64_t tiles64, int64
 }
 inline int64_t tiles_of(int64_t M, int64_t N, int64_t cols) { return ceil_div(M, 256) * ceil_div(N, cols); }
 
-// Over how many CTAs of a cluster the reduction of a few-token product is split: until there are weights to read for every SM, as long
-// as a CTA keeps some blocks of its own.
-inline int few_split(int64_t N, int nkb, int per_sm) {
-  const int64_t units = ceil_div(N, 128), want = (int64_t)sm_count_now() * per_sm;
-  int S = 1;
-  while (S < 8 && units * S < want && nkb >= 2 * S * 2) S *= 2;
-  return S;
+// Over how many CTAs of a cluster the reduction of a few-token product is split, by its estimated time: rounds of CTAs, each at its
+// share of the memory's rate, or at what one SM takes in where they are few, and what a round costs beside its loads.
+inline int few_split(int64_t N, int nkb, int per_sm, int stage_bytes) {
+  const int64_t units = ceil_div(N, 128);
+  const double slots = (double)sm_count_now() * per_sm;
+  int best = 1;
+  double least = 0;
+  for (int S = 1; S <= 8 && S <= nkb; ++S) {
+    const double ctas = (double)(units * S), rounds = (double)ceil_div((int64_t)ctas, (int64_t)slots);
+    const double at_once = ctas < slots ? ctas : slots;
+    const double share = at_once / 6.5e6, alone = per_sm / 0.1e6;            // us per byte: all of the memory, 100 GB/s to an SM
+    const double us = rounds * ((double)ceil_div(nkb, S) * stage_bytes * (share > alone ? share : alone) + 2.0);
+    if (S == 1 || us < 0.97 * least) { best = S; least = us; }
+  }
+  return best;
 }
 
 template <int kFmt, bool kGated, int kN>
@@ -75,13 +83,14 @@ int run_few_n(const Operand& X, const Operand& W0, const Operand& W1, int64_t N,
     SF_TRY(scale_map(&m.s0, kFmt, W0.scales, N, K));
     if (kGated) SF_TRY(scale_map(&m.s1, kFmt, W1.scales, N, K));
   }
-  return launch_few<kFmt, kGated, kN>(m, a, few_split(N, a.nkb, Cfg::kPerSm), s);
+  return launch_few<kFmt, kGated, kN>(m, a, few_split(N, a.nkb, Cfg::kPerSm, Cfg::kStageBytes), s);
 }
 template <int kFmt, bool kGated>
 int run_few(const Operand& X, const Operand& W0, const Operand& W1, int64_t N, int64_t K, const FewArgs& a, cudaStream_t s) {
   if (a.T <= 16) return run_few_n<kFmt, kGated, 16>(X, W0, W1, N, K, a, s);
   if (a.T <= 32) return run_few_n<kFmt, kGated, 32>(X, W0, W1, N, K, a, s);
   if (a.T <= 64) return run_few_n<kFmt, kGated, 64>(X, W0, W1, N, K, a, s);
+  if (a.T <= 96) return run_few_n<kFmt, kGated, 96>(X, W0, W1, N, K, a, s);
   return run_few_n<kFmt, kGated, 128>(X, W0, W1, N, K, a, s);
 }
 
