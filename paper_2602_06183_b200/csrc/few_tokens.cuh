@@ -16,6 +16,7 @@ namespace {
 using namespace ptx;
 
 constexpr int kFewThreads = 192;
+constexpr int kFewStages = 10;       // of the ring, at most
 
 constexpr uint32_t pow2_cols(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
 
@@ -30,17 +31,21 @@ struct FewCfg {
   static constexpr int kPartBytes = kMats * kN * 128 * 4;
   static constexpr uint32_t kScaleCol = kMats * kN, kScaleCols = kTiles * 4 * (kMats + 1);
   static constexpr uint32_t kTmem = pow2_cols(kScaleCol + 2 * kScaleCols);
-  // two CTAs to an SM while their columns and their partial sums fit: one sets up and adds up while the other streams
-  static constexpr int kPerSm = kN <= 32 && kTmem <= 256 ? 2 : 1;
-  static constexpr int kRoom = ((kPerSm == 2 ? 115712 : 232448) - 2048) / kStageBytes;
-  static constexpr int kStages = kRoom < 8 ? kRoom : 8;
-  static constexpr int kSmem = 1024 + kStages * kStageBytes + 1024;
-  static_assert(kStages >= 2 && kPartBytes <= kStages * kStageBytes, "shared memory");
+  // one CTA to an SM, or two (one sets up and adds up while the other streams) while their columns and partial sums fit
+  static constexpr int stages(int per_sm) {
+    const int n = ((per_sm == 2 ? 115712 : 232448) - 2048) / kStageBytes;
+    return n < kFewStages ? n : kFewStages;
+  }
+  static constexpr int smem(int per_sm) { return 2048 + stages(per_sm) * kStageBytes; }
+  static constexpr int kMostPerSm = kTmem <= 256 && stages(2) >= 2 && kPartBytes <= stages(2) * kStageBytes ? 2 : 1;
+  static_assert(stages(1) >= 2 && kPartBytes <= stages(1) * kStageBytes, "shared memory");
 };
 
 struct FewArgs {
   int T, N, nkb;                     // tokens, output columns, k-blocks (64 K of bf16, 256 K of 4 bits)
   int act;
+  int stages;                        // of the ring
+  int early_weights;                 // the launch before this one does not write the weights, and waited for those that may have
   float alpha, alpha2;
   void* C;                           // [T, N] bf16
   float *P, *Q;                      // gated, optional
@@ -49,7 +54,7 @@ struct FewArgs {
 struct FewMaps { CUtensorMap x, w0, w1, sx, s0, s1; };
 
 struct FewCtl {
-  uint64_t full[8], empty[8], done;
+  uint64_t full[kFewStages], empty[kFewStages], done;
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -65,11 +70,11 @@ __device__ __forceinline__ uint32_t cluster_size() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ float2 ld_cluster_f2(uint32_t saddr, uint32_t rank) {
-  float2 v;
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t saddr, uint32_t rank) {
+  float4 v;
   asm volatile(
-      "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %2, %3;\n\tld.shared::cluster.v2.f32 {%0, %1}, [a];\n\t}\n"
-      : "=f"(v.x), "=f"(v.y) : "r"(saddr), "r"(rank) : "memory");
+      "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}\n"
+      : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(saddr), "r"(rank) : "memory");
   return v;
 }
 // This warp's 32 lanes x 16 columns, complete when it returns.
@@ -98,15 +103,37 @@ __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t sdesc) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
 }
 
+// The weights' part of a stage, and the tokens'.
 template <int kFmt, bool kGated, int kN>
-__global__ void __launch_bounds__(kFewThreads, FewCfg<kFmt, kGated, kN>::kPerSm)
+__device__ __forceinline__ void load_weights(const FewMaps& maps, uint8_t* sw, uint64_t* bar, int kb, int f0) {
+  using Cfg = FewCfg<kFmt, kGated, kN>;
+  mbar_arrive_expect_tx(bar, (uint32_t)Cfg::kStageBytes);
+  tma_load_2d(sw, &maps.w0, bar, kb * 64, f0);
+  if (kGated) tma_load_2d(sw + Cfg::kWBytes, &maps.w1, bar, kb * 64, f0);
+  if constexpr (Cfg::kFp4) {
+    uint8_t* ss = sw + Cfg::kMats * Cfg::kWBytes + Cfg::kXBytes;
+    tma_load_3d(ss, &maps.s0, bar, 0, kb * Cfg::kTiles, f0 >> 7);
+    if (kGated) tma_load_3d(ss + Cfg::kTiles * 512, &maps.s1, bar, 0, kb * Cfg::kTiles, f0 >> 7);
+  }
+}
+template <int kFmt, bool kGated, int kN>
+__device__ __forceinline__ void load_tokens(const FewMaps& maps, uint8_t* sw, uint64_t* bar, int kb) {
+  using Cfg = FewCfg<kFmt, kGated, kN>;
+  uint8_t* sx = sw + Cfg::kMats * Cfg::kWBytes;
+  tma_load_2d(sx, &maps.x, bar, kb * 64, 0);
+  if constexpr (Cfg::kFp4) tma_load_3d(sx + Cfg::kXBytes + Cfg::kMats * Cfg::kTiles * 512, &maps.sx, bar, 0, kb * Cfg::kTiles, 0);
+}
+
+template <int kFmt, bool kGated, int kN>
+__global__ void __launch_bounds__(kFewThreads, FewCfg<kFmt, kGated, kN>::kMostPerSm)
 few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
   using Cfg = FewCfg<kFmt, kGated, kN>;
   constexpr bool kFp4 = Cfg::kFp4;
-  constexpr int kStages = Cfg::kStages, kMats = Cfg::kMats, kTiles = Cfg::kTiles;
+  constexpr int kMats = Cfg::kMats, kTiles = Cfg::kTiles;
+  const uint32_t stages = (uint32_t)args.stages;
   extern __shared__ uint8_t smem_dyn[];
   uint8_t* smem = smem_dyn + align_pad(smem_dyn, 1024);
-  FewCtl* ctl = reinterpret_cast<FewCtl*>(smem + kStages * Cfg::kStageBytes);
+  FewCtl* ctl = reinterpret_cast<FewCtl*>(smem + stages * Cfg::kStageBytes);
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int S = (int)cluster_size(), rank = (int)cluster_ctarank();
@@ -114,9 +141,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
   const int kb0 = (int)((int64_t)args.nkb * rank / S), kb1 = (int)((int64_t)args.nkb * (rank + 1) / S);
 
   if (threadIdx.x == 0) {
-    prefetch_tmap(&maps.x);
-    prefetch_tmap(&maps.w0);
-    for (int s = 0; s < kStages; ++s) {
+    for (uint32_t s = 0; s < stages; ++s) {
       mbar_init(&ctl->full[s], 1);
       mbar_init(&ctl->empty[s], 1);
     }
@@ -124,6 +149,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
     ctl->abort_flag = 0;
     fence_mbar_init();
   }
+  if (threadIdx.x >= 64 && threadIdx.x < 70) prefetch_tmap(&maps.x + (threadIdx.x - 64));
   if (warp == 1) {
     tmem_alloc(&ctl->tmem_base, Cfg::kTmem);
     tmem_relinquish();
@@ -131,30 +157,25 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  pdl_wait();
   const uint32_t tmem_base = ctl->tmem_base;
 
   if (warp == 0) {
     const bool issues = elect_one();
+    // what fits the ring of weights that are known to be there is fetched while the launch before this one ends
+    const int early = args.early_weights ? min((int)stages, kb1 - kb0) : 0;
+    if (issues)
+      for (int i = 0; i < early; ++i) load_weights<kFmt, kGated, kN>(maps, smem + i * Cfg::kStageBytes, &ctl->full[i], kb0 + i, f0);
+    __syncwarp();
+    pdl_wait();
     uint32_t stage = 0, phase = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
       if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag)) break;
       if (issues) {
         uint8_t* sw = smem + stage * Cfg::kStageBytes;
-        uint8_t* sx = sw + kMats * Cfg::kWBytes;
-        uint8_t* ss = sx + Cfg::kXBytes;
-        uint64_t* bar = &ctl->full[stage];
-        mbar_arrive_expect_tx(bar, (uint32_t)Cfg::kStageBytes);
-        tma_load_2d(sw, &maps.w0, bar, kb * 64, f0);
-        if (kGated) tma_load_2d(sw + Cfg::kWBytes, &maps.w1, bar, kb * 64, f0);
-        tma_load_2d(sx, &maps.x, bar, kb * 64, 0);
-        if constexpr (kFp4) {
-          tma_load_3d(ss, &maps.s0, bar, 0, kb * kTiles, f0 >> 7);
-          if (kGated) tma_load_3d(ss + kTiles * 512, &maps.s1, bar, 0, kb * kTiles, f0 >> 7);
-          tma_load_3d(ss + kMats * kTiles * 512, &maps.sx, bar, 0, kb * kTiles, 0);
-        }
+        if (kb - kb0 >= early) load_weights<kFmt, kGated, kN>(maps, sw, &ctl->full[stage], kb, f0);
+        load_tokens<kFmt, kGated, kN>(maps, sw, &ctl->full[stage], kb);
       }
-      if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1; }
+      if (++stage == stages) { stage = 0; phase ^= 1; }
     }
     pdl_trigger();
   } else if (warp == 1) {
@@ -173,7 +194,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
       const uint32_t more = kb > kb0 ? 1u : 0u;
       // scales: one of two buffers in turn; the products of two blocks ago, which read this one, have signalled their end with their stage
       if (kFp4 && kb - kb0 >= 2) {
-        const uint32_t back = stage >= 2 ? stage - 2 : stage + kStages - 2;
+        const uint32_t back = stage >= 2 ? stage - 2 : stage + stages - 2;
         if (!mbar_wait_warp(&ctl->empty[back], stage >= 2 ? phase : phase ^ 1u, abort_flag)) { ok = false; break; }
       }
       if (issues) {
@@ -199,7 +220,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
         mma_commit(&ctl->empty[stage]);
       }
       __syncwarp();
-      if (++stage == (uint32_t)kStages) { stage = 0; phase ^= 1; }
+      if (++stage == stages) { stage = 0; phase ^= 1; }
     }
     if (ok && issues) mma_commit(&ctl->done);
   } else {
@@ -209,12 +230,14 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
       const int q = warp & 3;
       float* part = reinterpret_cast<float*>(smem) + q * 32 + lane;
 #pragma unroll 1
-      for (int c = 0; c < kMats * kN; c += 16) {
-        uint32_t v[16];
-        tmem_ld_32x32b_x16(tmem_base + c + ((uint32_t)(q * 32) << 16), v);
+      for (int m = 0; m < kMats; ++m)
+#pragma unroll 1
+        for (int c = m * kN; c < m * kN + args.T; c += 16) {
+          uint32_t v[16];
+          tmem_ld_32x32b_x16(tmem_base + c + ((uint32_t)(q * 32) << 16), v);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) part[(c + i) * 128] = __uint_as_float(v[i]);
-      }
+          for (int i = 0; i < 16; ++i) part[(c + i) * 128] = __uint_as_float(v[i]);
+        }
     }
   }
   __syncwarp();
@@ -229,55 +252,66 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
     tc_fence_after();
     tmem_dealloc(tmem_base, Cfg::kTmem);
   }
-  // the cluster's threads share the sums, two neighbouring output columns to a thread
+  pdl_wait();                                              // (the producer has waited; the output may be read by the launch before)
+  // the cluster's threads share the sums, four neighbouring output columns to a thread; all partial sums of a value are fetched at once
   const uint32_t part = smem_u32(smem);
-  for (int i = rank * kFewThreads + threadIdx.x; i < args.T * 64; i += S * kFewThreads) {
-    const int t = i >> 6, p = i & 63, f = f0 + 2 * p;
+  for (int i = rank * kFewThreads + threadIdx.x; i < args.T * 32; i += S * kFewThreads) {
+    const int t = i >> 5, p = (i & 31) * 4, f = f0 + p;
     if (f >= args.N) continue;
-    float2 a = {0.f, 0.f}, b = {0.f, 0.f};
-    for (int s = 0; s < S; ++s) {
-      const float2 x = ld_cluster_f2(part + (uint32_t)(t * 128 + 2 * p) * 4u, s);
-      a.x += x.x; a.y += x.y;
-      if (kGated) {
-        const float2 y = ld_cluster_f2(part + (uint32_t)((kN + t) * 128 + 2 * p) * 4u, s);
-        b.x += y.x; b.y += y.y;
-      }
-    }
-    if (kFp4) { a.x *= args.alpha; a.y *= args.alpha; b.x *= args.alpha2; b.y *= args.alpha2; }
+    float4 x[kMats][8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int m = 0; m < kMats; ++m)
+        if (s < S) x[m][s] = ld_cluster_f4(part + (uint32_t)((m * kN + t) * 128 + p) * 4u, s);
+#pragma unroll
+    for (int s = 1; s < 8; ++s)
+#pragma unroll
+      for (int m = 0; m < kMats; ++m)
+        if (s < S) { x[m][0].x += x[m][s].x; x[m][0].y += x[m][s].y; x[m][0].z += x[m][s].z; x[m][0].w += x[m][s].w; }
+    float a[4] = {x[0][0].x, x[0][0].y, x[0][0].z, x[0][0].w};
+    if (kFp4)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] *= args.alpha;
     const int64_t at = (int64_t)t * args.N + f;
     if constexpr (kGated) {
+      const float4 y = x[kMats - 1][0];
+      float b[4] = {y.x, y.y, y.z, y.w}, d[4];
+      if (kFp4)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] *= args.alpha2;
       with_act(args.act, [&](auto tag) {
-        float v0, v1, d0, d1;
-        gate_act<decltype(tag)::value>(a.x, v0, d0);
-        gate_act<decltype(tag)::value>(a.y, v1, d1);
-        if (args.P) {
-          *reinterpret_cast<float2*>(args.P + at) = make_float2(v0, v1);
-          *reinterpret_cast<float2*>(args.Q + at) = make_float2(b.x * d0, b.y * d1);
-        }
-        a.x = v0 * b.x;
-        a.y = v1 * b.y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) gate_act<decltype(tag)::value>(a[e], a[e], d[e]);
       });
+      if (args.P) {
+        *reinterpret_cast<float4*>(args.P + at) = make_float4(a[0], a[1], a[2], a[3]);
+        *reinterpret_cast<float4*>(args.Q + at) = make_float4(b[0] * d[0], b[1] * d[1], b[2] * d[2], b[3] * d[3]);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] *= b[e];
     }
-    *reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(args.C) + at) = bf16x2(a.x, a.y);
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(args.C) + at) = make_uint2(bf16x2(a[0], a[1]), bf16x2(a[2], a[3]));
   }
   if (S > 1) cluster_sync_all();                           // no CTA leaves while another reads its shared memory
 }
 
 template <int kFmt, bool kGated, int kN>
-int launch_few(const FewMaps& maps, const FewArgs& a, int S, cudaStream_t s) {
+int launch_few(const FewMaps& maps, FewArgs a, int S, int per_sm, cudaStream_t s) {
   using Cfg = FewCfg<kFmt, kGated, kN>;
   auto kern = few_tokens_kernel<kFmt, kGated, kN>;
   static bool attr_done[64] = {false};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_done[dev]) {
-    SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
+    SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::smem(1)));
     if (dev >= 0 && dev < 64) attr_done[dev] = true;
   }
+  a.stages = Cfg::stages(per_sm);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((a.N + 127) / 128 * S));
   cfg.blockDim = dim3(kFewThreads);
-  cfg.dynamicSmemBytes = Cfg::kSmem;
+  cfg.dynamicSmemBytes = Cfg::smem(per_sm);
   cfg.stream = s;
   cudaLaunchAttribute attr[2] = {};
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -156,7 +156,7 @@ int sf_gated_ffn_fwd(const sf_gated_ffn_desc* desc, const void* X, const void* W
   float* q = fwd_ctx ? (float*)(h + z.h + z.f) : nullptr;
   int* status = (int*)workspace;
   SF_TRY(run_gated<FMT_BF16>({X, nullptr}, {Wg, nullptr}, {Wu, nullptr}, desc->T, desc->F, desc->D, desc->act, 1.f, 1.f, h, p, q, status, s));
-  return run_nt<FMT_BF16>({h, nullptr}, {Wd, nullptr}, desc->T, desc->D, desc->F, 1.f, Y, status, s);
+  return run_nt<FMT_BF16>({h, nullptr}, {Wd, nullptr}, desc->T, desc->D, desc->F, 1.f, Y, status, s, true);
 }
 
 int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* X, const void* Wg, const void* Wu, const void* Wd,

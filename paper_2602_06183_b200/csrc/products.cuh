@@ -52,20 +52,27 @@ inline int pair_width(int64_t tiles256, int64_t tiles128, int64_t tiles64, int64
 }
 inline int64_t tiles_of(int64_t M, int64_t N, int64_t cols) { return ceil_div(M, 256) * ceil_div(N, cols); }
 
-// Over how many CTAs of a cluster the reduction of a few-token product is split, by its estimated time: rounds of CTAs, each at its
-// share of the memory's rate, or at what one SM takes in where they are few, and what a round costs beside its loads.
-inline int few_split(int64_t N, int nkb, int per_sm, int stage_bytes) {
+// Over how many CTAs of a cluster the reduction of a few-token product is split and how many CTAs share an SM, by the estimated time:
+// rounds of CTAs, each at its share of the memory's rate, at what one SM takes in where they are few, or at what its ring holds in
+// flight; and what a round costs beside its loads.
+struct FewPlan { int S, per_sm; };
+template <typename Cfg>
+FewPlan few_plan(int64_t N, int nkb) {
   const int64_t units = ceil_div(N, 128);
-  const double slots = (double)sm_count_now() * per_sm;
-  int best = 1;
+  FewPlan best{1, 1};
   double least = 0;
-  for (int S = 1; S <= 8 && S <= nkb; ++S) {
-    const double ctas = (double)(units * S), rounds = (double)ceil_div((int64_t)ctas, (int64_t)slots);
-    const double at_once = ctas < slots ? ctas : slots;
-    const double share = at_once / 6.5e6, alone = per_sm / 0.1e6;            // us per byte: all of the memory, 100 GB/s to an SM
-    const double us = rounds * ((double)ceil_div(nkb, S) * stage_bytes * (share > alone ? share : alone) + 2.0);
-    if (S == 1 || us < 0.97 * least) { best = S; least = us; }
-  }
+  for (int per_sm = 1; per_sm <= Cfg::kMostPerSm; ++per_sm)
+    for (int S = 1; S <= 8 && S <= nkb; ++S) {
+      const double slots = (double)sm_count_now() * per_sm, ctas = (double)(units * S);
+      const double at_once = ctas < slots ? ctas : slots, rounds = (double)ceil_div((int64_t)ctas, (int64_t)slots);
+      const int ring = Cfg::stages(per_sm) < nkb / S + 1 ? Cfg::stages(per_sm) : nkb / S + 1;
+      double us = Cfg::kStageBytes * at_once / 6.5e6;                                              // a stage's time
+      const double sm = Cfg::kStageBytes * (ctas <= sm_count_now() ? 1 : per_sm) / 0.1e6, flight = 1.8 / ring;
+      us = us > sm ? us : sm;
+      us = us > flight ? us : flight;
+      us = rounds * (us * (double)ceil_div(nkb, S) + 1.5) + (S > 1 ? 0.3 : 0.0);
+      if (least == 0 || us < 0.98 * least) { best = FewPlan{S, per_sm}; least = us; }
+    }
   return best;
 }
 
@@ -83,7 +90,8 @@ int run_few_n(const Operand& X, const Operand& W0, const Operand& W1, int64_t N,
     SF_TRY(scale_map(&m.s0, kFmt, W0.scales, N, K));
     if (kGated) SF_TRY(scale_map(&m.s1, kFmt, W1.scales, N, K));
   }
-  return launch_few<kFmt, kGated, kN>(m, a, few_split(N, a.nkb, Cfg::kPerSm, Cfg::kStageBytes), s);
+  const FewPlan plan = few_plan<Cfg>(N, a.nkb);
+  return launch_few<kFmt, kGated, kN>(m, a, plan.S, plan.per_sm, s);
 }
 template <int kFmt, bool kGated>
 int run_few(const Operand& X, const Operand& W0, const Operand& W1, int64_t N, int64_t K, const FewArgs& a, cudaStream_t s) {
@@ -107,13 +115,16 @@ int run_nt_pair(const Operand& A, const Operand& B, int64_t K, void* C, const Pa
   return launch_pair<PK_NT, kBN, kFmt>(m, a, s);
 }
 
-// C[M, N] = alpha A B^T; M, N, K > 0.
+// C[M, N] = alpha A B^T; M, N, K > 0. early_weights: the launch before this one is another product of the same call, which does not
+// write B.
 template <int kFmt>
-int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, float alpha, void* C, int* status, cudaStream_t s) {
+int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, float alpha, void* C, int* status, cudaStream_t s,
+           bool early_weights = false) {
   const int nkb = k_blocks(kFmt, K);
   if (M <= kFewTokens) {
     FewArgs a{};
     a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.alpha = a.alpha2 = alpha; a.C = C; a.status = status;
+    a.early_weights = early_weights;
     return run_few<kFmt, false>(A, B, B, N, K, a, s);
   }
   PairArgs a{};
