@@ -297,31 +297,60 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
 }
 
 template <int kFmt, bool kGated, int kN>
-int launch_few(const FewMaps& maps, FewArgs a, int S, int per_sm, cudaStream_t s) {
-  using Cfg = FewCfg<kFmt, kGated, kN>;
-  auto kern = few_tokens_kernel<kFmt, kGated, kN>;
-  static bool attr_done[64] = {false};
-  int dev = 0;
-  SF_CUDA_TRY(cudaGetDevice(&dev));
-  if (dev < 0 || dev >= 64 || !attr_done[dev]) {
-    SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::smem(1)));
-    if (dev >= 0 && dev < 64) attr_done[dev] = true;
-  }
-  a.stages = Cfg::stages(per_sm);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((a.N + 127) / 128 * S));
+void few_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int64_t N, int S, int per_sm, cudaStream_t s) {
+  cfg = {};
+  cfg.gridDim = dim3((unsigned)((N + 127) / 128 * S));
   cfg.blockDim = dim3(kFewThreads);
-  cfg.dynamicSmemBytes = Cfg::smem(per_sm);
+  cfg.dynamicSmemBytes = FewCfg<kFmt, kGated, kN>::smem(per_sm);
   cfg.stream = s;
-  cudaLaunchAttribute attr[2] = {};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)S;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  attr[0] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)S;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1] = {};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  SF_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, maps, a));
+}
+
+// How many clusters of 1 to 8 CTAs a device holds at once with one CTA to an SM (a cluster stays within one of the chip's groups of
+// SMs, whose size is no multiple of most numbers); with two it is taken for twice as many. Asked once; every thread that asks
+// gets the same answer.
+struct FewRoom { int clusters[8]; int set; };
+template <int kFmt, bool kGated, int kN>
+int few_room(const FewRoom** room) {
+  using Cfg = FewCfg<kFmt, kGated, kN>;
+  static FewRoom rooms[64];
+  static FewRoom other;
+  int dev = 0;
+  SF_CUDA_TRY(cudaGetDevice(&dev));
+  FewRoom& r = dev >= 0 && dev < 64 ? rooms[dev] : other;
+  *room = &r;
+  if (r.set && &r != &other) return SF_OK;
+  auto kern = few_tokens_kernel<kFmt, kGated, kN>;
+  SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::smem(1)));
+  SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
+  for (int S = 1; S <= 8; ++S) {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    few_config<kFmt, kGated, kN>(cfg, attr, 128 * 1024, S, 1, nullptr);
+    cfg.numAttrs = 1;
+    int n = 0;
+    SF_CUDA_TRY(cudaOccupancyMaxActiveClusters(&n, kern, &cfg));
+    r.clusters[S - 1] = n;
+  }
+  r.set = 1;
+  return SF_OK;
+}
+
+template <int kFmt, bool kGated, int kN>
+int launch_few(const FewMaps& maps, FewArgs a, int S, int per_sm, cudaStream_t s) {
+  a.stages = FewCfg<kFmt, kGated, kN>::stages(per_sm);
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attr[2];
+  few_config<kFmt, kGated, kN>(cfg, attr, a.N, S, per_sm, s);
+  SF_CUDA_TRY(cudaLaunchKernelEx(&cfg, few_tokens_kernel<kFmt, kGated, kN>, maps, a));
   return SF_OK;
 }
 

@@ -1,6 +1,8 @@
 // Host side of the products of the gated block and of 4-bit operands: tensor maps, choice of kernel and tile, launches.
 #pragma once
 
+#include <cmath>
+
 #include "few_tokens.cuh"
 #include "pair_product.cuh"
 
@@ -53,24 +55,28 @@ inline int pair_width(int64_t tiles256, int64_t tiles128, int64_t tiles64, int64
 inline int64_t tiles_of(int64_t M, int64_t N, int64_t cols) { return ceil_div(M, 256) * ceil_div(N, cols); }
 
 // Over how many CTAs of a cluster the reduction of a few-token product is split and how many CTAs share an SM, by the estimated time:
-// rounds of CTAs, each at its share of the memory's rate, at what one SM takes in where they are few, or at what its ring holds in
-// flight; and what a round costs beside its loads.
+// rounds of clusters; the time of a stage at its share of the memory's rate (which a part of the SMs does not reach: the 134 MB of the
+// 4096 x 16384 down projection took 3 us more on 128 of them than on all), at what one SM takes in, or at what its ring holds in
+// flight; what a round costs beside; and the sums, which grow with the CTAs that a value comes from (128 tokens, 2048 x 8192 of 4
+// bits: 8.2 us over 4, 9.9 over 8).
 struct FewPlan { int S, per_sm; };
 template <typename Cfg>
-FewPlan few_plan(int64_t N, int nkb) {
+FewPlan few_plan(int64_t N, int nkb, const FewRoom& room) {
   const int64_t units = ceil_div(N, 128);
   FewPlan best{1, 1};
   double least = 0;
   for (int per_sm = 1; per_sm <= Cfg::kMostPerSm; ++per_sm)
     for (int S = 1; S <= 8 && S <= nkb; ++S) {
-      const double slots = (double)sm_count_now() * per_sm, ctas = (double)(units * S);
-      const double at_once = ctas < slots ? ctas : slots, rounds = (double)ceil_div((int64_t)ctas, (int64_t)slots);
+      const int64_t slots = (int64_t)room.clusters[S - 1] * per_sm;
+      if (slots <= 0) continue;
+      const double at_once = (double)((units < slots ? units : slots) * S), rounds = (double)ceil_div(units, slots);
       const int ring = Cfg::stages(per_sm) < nkb / S + 1 ? Cfg::stages(per_sm) : nkb / S + 1;
-      double us = Cfg::kStageBytes * at_once / 6.5e6;                                              // a stage's time
-      const double sm = Cfg::kStageBytes * (ctas <= sm_count_now() ? 1 : per_sm) / 0.1e6, flight = 1.8 / ring;
+      const double part = at_once / sm_count_now();
+      double us = Cfg::kStageBytes * at_once / (6.5e6 * (part < 1 ? std::sqrt(part) : 1.0));
+      const double sm = Cfg::kStageBytes * (part <= 1 ? 1 : per_sm) / 0.075e6, flight = 1.8 / ring;
       us = us > sm ? us : sm;
       us = us > flight ? us : flight;
-      us = rounds * (us * (double)ceil_div(nkb, S) + 1.5) + (S > 1 ? 0.3 : 0.0);
+      us = rounds * (us * (double)ceil_div(nkb, S) + (per_sm == 2 ? 1.0 : 1.5)) + (S > 1 ? 0.3 + 0.05 * S * Cfg::kPartBytes / 8192 : 0.0);
       if (least == 0 || us < 0.98 * least) { best = FewPlan{S, per_sm}; least = us; }
     }
   return best;
@@ -90,7 +96,9 @@ int run_few_n(const Operand& X, const Operand& W0, const Operand& W1, int64_t N,
     SF_TRY(scale_map(&m.s0, kFmt, W0.scales, N, K));
     if (kGated) SF_TRY(scale_map(&m.s1, kFmt, W1.scales, N, K));
   }
-  const FewPlan plan = few_plan<Cfg>(N, a.nkb);
+  const FewRoom* room;
+  SF_TRY((few_room<kFmt, kGated, kN>(&room)));
+  const FewPlan plan = few_plan<Cfg>(N, a.nkb, *room);
   return launch_few<kFmt, kGated, kN>(m, a, plan.S, plan.per_sm, s);
 }
 template <int kFmt, bool kGated>
