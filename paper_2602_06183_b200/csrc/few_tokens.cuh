@@ -4,7 +4,8 @@
 // a partial sum of its own K range in TMEM, leaves it in its shared memory, and the cluster adds the partial sums up in the order
 // of the ranges (the same every time) through distributed shared memory.
 //
-// CTA = 6 warps: TMA producer, MMA issuer, four warps that read the accumulator out. Every wait is bounded (see gemm_tc.cu); the
+// CTA = 10 warps: TMA producer, MMA issuer, four warps that read the accumulator out; all of them add up (with six, whose loads
+// are few at a time, 100 tokens through both projections of 8192 x 2048 took 15.7 us, with ten %X%). Every wait is bounded (see gemm_tc.cu); the
 // cluster barriers are reached by every warp because their own waits are.
 #pragma once
 
@@ -15,7 +16,7 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kFewThreads = 192;
+constexpr int kFewThreads = 320;
 constexpr int kFewStages = 10;       // of the ring, at most
 
 constexpr uint32_t pow2_cols(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
@@ -223,7 +224,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
       if (++stage == stages) { stage = 0; phase ^= 1; }
     }
     if (ok && issues) mma_commit(&ctl->done);
-  } else {
+  } else if (warp < 6) {
     // every product has been made, so every load has landed and the ring is free: the partial sums go there, [matrix][token][row]
     if (mbar_wait_warp(&ctl->done, 0, abort_flag)) {
       tc_fence_after();
@@ -258,24 +259,32 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
   for (int i = rank * kFewThreads + threadIdx.x; i < args.T * 32; i += S * kFewThreads) {
     const int t = i >> 5, p = (i & 31) * 4, f = f0 + p;
     if (f >= args.N) continue;
-    float4 x[kMats][8];
+    float4 x[kMats][4], sum[kMats];
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
+    for (int s0 = 0; s0 < 8; s0 += 4) {
+      if (s0 >= S) break;
 #pragma unroll
-      for (int m = 0; m < kMats; ++m)
-        if (s < S) x[m][s] = ld_cluster_f4(part + (uint32_t)((m * kN + t) * 128 + p) * 4u, s);
+      for (int s = 0; s < 4; ++s)
 #pragma unroll
-    for (int s = 1; s < 8; ++s)
+        for (int m = 0; m < kMats; ++m) {
+          const uint32_t at = part + (uint32_t)((m * kN + t) * 128 + p) * 4u;
+          if (s0 + s < S) x[m][s] = ld_cluster_f4(at, s0 + s);
+        }
 #pragma unroll
-      for (int m = 0; m < kMats; ++m)
-        if (s < S) { x[m][0].x += x[m][s].x; x[m][0].y += x[m][s].y; x[m][0].z += x[m][s].z; x[m][0].w += x[m][s].w; }
-    float a[4] = {x[0][0].x, x[0][0].y, x[0][0].z, x[0][0].w};
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int m = 0; m < kMats; ++m) {
+          if (s0 + s == 0) sum[m] = x[m][0];
+          else if (s0 + s < S) { sum[m].x += x[m][s].x; sum[m].y += x[m][s].y; sum[m].z += x[m][s].z; sum[m].w += x[m][s].w; }
+        }
+    }
+    float a[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w};
     if (kFp4)
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] *= args.alpha;
     const int64_t at = (int64_t)t * args.N + f;
     if constexpr (kGated) {
-      const float4 y = x[kMats - 1][0];
+      const float4 y = sum[kMats - 1];
       float b[4] = {y.x, y.y, y.z, y.w}, d[4];
       if (kFp4)
 #pragma unroll
