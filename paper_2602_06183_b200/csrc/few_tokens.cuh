@@ -71,13 +71,6 @@ __device__ __forceinline__ uint32_t cluster_size() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
-__device__ __forceinline__ float4 ld_cluster_f4(uint32_t saddr, uint32_t rank) {
-  float4 v;
-  asm volatile(
-      "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}\n"
-      : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(saddr), "r"(rank) : "memory");
-  return v;
-}
 // This warp's 32 lanes x 16 columns, complete when it returns.
 __device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t (&v)[16]) {
   asm volatile(
@@ -182,7 +175,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
   } else if (warp == 1) {
     constexpr uint32_t idesc = kFp4 ? idesc_fp4(128, kN, kFmt) : idesc_bf16(128, kN, false, false, false);
     constexpr uint64_t proto = desc_proto(16, 1024, kSwizzle128B), s_proto = desc_proto(128, 128, kSwizzleNone);
-    const uint32_t smem16 = smem_u32(smem) >> 4, tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
+    const uint32_t smem16 = desc_address(smem), tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
     const bool issues = elect_one();
     uint32_t stage = 0, phase = 0;
     bool ok = true;

@@ -83,44 +83,7 @@ int gated_sizes(const sf_gated_ffn_desc* d, GatedSizes* z) {
   return SF_OK;
 }
 
-template <int kBN>
-int run_bwd(const sf_gated_ffn_desc& d, const void* dY, const void* Wd, const float* P, const float* Q, void* dG, void* dU,
-            const PairArgs& a, cudaStream_t s) {
-  PairMaps<6> m;
-  SF_TRY(kmajor_map(&m.m[0], FMT_BF16, dY, d.T, d.D, 128));
-  SF_TRY(mn_map(&m.m[1], Wd, d.D, d.F));
-  SF_TRY(make_tmap_f32(&m.m[2], P, d.T, d.F));
-  SF_TRY(make_tmap_f32(&m.m[3], Q, d.T, d.F));
-  SF_TRY(make_tmap_store(&m.m[4], dG, d.T, d.F));
-  SF_TRY(make_tmap_store(&m.m[5], dU, d.T, d.F));
-  return launch_pair<PK_BWD, kBN, FMT_BF16>(m, a, s);
-}
-
-template <int kBN>
-int run_dx(const sf_gated_ffn_desc& d, const void* dG, const void* dU, const void* Wg, const void* Wu, void* dX, const PairArgs& a,
-           cudaStream_t s) {
-  PairMaps<5> m;
-  SF_TRY(kmajor_map(&m.m[0], FMT_BF16, dG, d.T, d.F, 128));
-  SF_TRY(kmajor_map(&m.m[1], FMT_BF16, dU, d.T, d.F, 128));
-  SF_TRY(mn_map(&m.m[2], Wg, d.F, d.D));
-  SF_TRY(mn_map(&m.m[3], Wu, d.F, d.D));
-  SF_TRY(make_tmap_store(&m.m[4], dX, d.T, d.D));
-  return launch_pair<PK_DX, kBN, FMT_BF16>(m, a, s);
-}
-
 struct GradJob { const void *A, *B; int64_t M, N; void* C; };     // C[M, N] = A[T, M]^T B[T, N]
-template <int kBN>
-int run_dw(const GradJob* jobs, int64_t T, PairArgs a, cudaStream_t s) {
-  PairMaps<9> m;
-  for (int j = 0; j < a.jobs; ++j) {
-    SF_TRY(mn_map(&m.m[j], jobs[j].A, T, jobs[j].M));
-    SF_TRY(mn_map(&m.m[3 + j], jobs[j].B, T, jobs[j].N));
-    SF_TRY(make_tmap_store(&m.m[6 + j], jobs[j].C, jobs[j].M, jobs[j].N));
-  }
-  for (int j = a.jobs; j < 3; ++j)
-    for (int i = 0; i < 9; i += 3) m.m[i + j] = m.m[i];
-  return launch_pair<PK_DW, kBN, FMT_BF16>(m, a, s);
-}
 
 }  // namespace
 
@@ -187,16 +150,24 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
   a.jobs = 1;
   if (dX || dWg || dWu) {
     a.M[0] = (int)T; a.N[0] = (int)F; a.nkb = a.nkb0 = k_blocks(FMT_BF16, D);
-    const int w = pair_width(tiles_of(T, F, 256), tiles_of(T, F, 128), tiles_of(T, F, 64), a.nkb);
-    const float *p = (const float*)(h + z.h), *q = (const float*)(h + z.h + z.f);
-    SF_TRY(w == 256 ? run_bwd<256>(*desc, dY, Wd, p, q, dg, du, a, s)
-         : w == 128 ? run_bwd<128>(*desc, dY, Wd, p, q, dg, du, a, s) : run_bwd<64>(*desc, dY, Wd, p, q, dg, du, a, s));
+    SF_TRY(launch_best<PK_BWD>(a, s, [&](CUtensorMap* m, int) {
+      SF_TRY(kmajor_map(&m[0], FMT_BF16, dY, T, D, 128));
+      SF_TRY(mn_map(&m[1], Wd, D, F));
+      SF_TRY(make_tmap_f32(&m[2], h + z.h, T, F));
+      SF_TRY(make_tmap_f32(&m[3], h + z.h + z.f, T, F));
+      SF_TRY(make_tmap_store(&m[4], dg, T, F));
+      return make_tmap_store(&m[5], du, T, F);
+    }));
   }
   if (dX) {
     a.M[0] = (int)T; a.N[0] = (int)D; a.nkb0 = k_blocks(FMT_BF16, F); a.nkb = 2 * a.nkb0;
-    const int w = pair_width(tiles_of(T, D, 256), tiles_of(T, D, 128), tiles_of(T, D, 64), a.nkb);
-    SF_TRY(w == 256 ? run_dx<256>(*desc, dg, du, Wg, Wu, dX, a, s)
-         : w == 128 ? run_dx<128>(*desc, dg, du, Wg, Wu, dX, a, s) : run_dx<64>(*desc, dg, du, Wg, Wu, dX, a, s));
+    SF_TRY(launch_best<PK_DX>(a, s, [&](CUtensorMap* m, int) {
+      SF_TRY(kmajor_map(&m[0], FMT_BF16, dg, T, F, 128));
+      SF_TRY(kmajor_map(&m[1], FMT_BF16, du, T, F, 128));
+      SF_TRY(mn_map(&m[2], Wg, F, D));
+      SF_TRY(mn_map(&m[3], Wu, F, D));
+      return make_tmap_store(&m[4], dX, T, D);
+    }));
   }
   GradJob jobs[3];
   a.jobs = 0;
@@ -204,14 +175,18 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
   if (dWg) jobs[a.jobs++] = {dg, X, F, D, dWg};
   if (dWu) jobs[a.jobs++] = {du, X, F, D, dWu};
   if (a.jobs == 0) return SF_OK;
-  int64_t t256 = 0, t128 = 0, t64 = 0;
-  for (int j = 0; j < a.jobs; ++j) {
-    a.M[j] = (int)jobs[j].M; a.N[j] = (int)jobs[j].N;
-    t256 += tiles_of(jobs[j].M, jobs[j].N, 256); t128 += tiles_of(jobs[j].M, jobs[j].N, 128); t64 += tiles_of(jobs[j].M, jobs[j].N, 64);
-  }
+  for (int j = 0; j < a.jobs; ++j) { a.M[j] = (int)jobs[j].M; a.N[j] = (int)jobs[j].N; }
   a.nkb = a.nkb0 = (int)ceil_div(T, 64);
-  const int w = pair_width(t256, t128, t64, a.nkb);
-  return w == 256 ? run_dw<256>(jobs, T, a, s) : w == 128 ? run_dw<128>(jobs, T, a, s) : run_dw<64>(jobs, T, a, s);
+  return launch_best<PK_DW>(a, s, [&](CUtensorMap* m, int) {
+    for (int j = 0; j < a.jobs; ++j) {
+      SF_TRY(mn_map(&m[j], jobs[j].A, T, jobs[j].M));
+      SF_TRY(mn_map(&m[3 + j], jobs[j].B, T, jobs[j].N));
+      SF_TRY(make_tmap_store(&m[6 + j], jobs[j].C, jobs[j].M, jobs[j].N));
+    }
+    for (int j = a.jobs; j < 3; ++j)
+      for (int i = 0; i < 9; i += 3) m[i + j] = m[i];
+    return (int)SF_OK;
+  });
 }
 
 }  // extern "C"

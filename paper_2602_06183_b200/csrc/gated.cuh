@@ -92,10 +92,20 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}\n" : "=r"(r));
   return r != 0;
 }
-// ptx::smem_desc at address 0, as a constant: the address (in 16-byte units) is added.
+// Four floats of the shared memory of a CTA of the cluster, at this CTA's own address of the same place.
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t saddr, uint32_t rank) {
+  float4 v;
+  asm volatile(
+      "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}\n"
+      : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(saddr), "r"(rank) : "memory");
+  return v;
+}
+// ptx::smem_desc at address 0, as a constant, and the address that is added to it: in units of 16 bytes, without the bits above that name the
+// CTA of the cluster and would run into the descriptor's next field.
 __host__ __device__ constexpr uint64_t desc_proto(uint32_t lbo, uint32_t sbo, uint32_t swizzle) {
   return (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 | 1ull << 46 | (uint64_t)swizzle << 61;
 }
+__device__ __forceinline__ uint32_t desc_address(const void* p) { return (ptx::smem_u32(p) >> 4) & 0x3FFFu; }
 
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi) { return float_to_bf16_bits(lo) | (float_to_bf16_bits(hi) << 16); }
 

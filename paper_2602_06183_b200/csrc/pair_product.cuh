@@ -27,7 +27,12 @@ enum PairKind { PK_NT, PK_DX, PK_DW, PK_FWD, PK_FWD_SAVE, PK_BWD };
 constexpr int kPairThreads = 320;
 constexpr int kPairSmemMax = 232448;
 
-template <int kKind, int kBN, int kFmt>
+// Full-width tiles; tiles of a width that the launch says (a multiple of 32; PK_FWD, whose two halves are, of 64), for products that
+// fill the pairs better with it; and such tiles with the reduction split over the pairs of a cluster, one tile to a cluster, for
+// long reductions of few tiles.
+enum PairMode { PM_FULL, PM_WIDTH, PM_SPLIT };
+
+template <int kKind, int kBN, int kFmt, int kMode>
 struct PairCfg {
   static constexpr bool kFp4 = kFmt != FMT_BF16;
   static constexpr bool kAMN = kKind == PK_DW;
@@ -53,9 +58,9 @@ struct PairCfg {
   static constexpr uint32_t kScaleACols = kTiles * 4, kScaleCols = kScaleACols * (1 + kBBlocks);    // of one stage
   static constexpr int kMaps = kKind == PK_DW ? 9 : kKind == PK_DX ? 5 : kKind == PK_NT ? (kFp4 ? 5 : 3)
                              : kKind == PK_FWD ? (kFp4 ? 7 : 4) : 6;
-  static_assert(kBN == 256 || kBN == 128 || kBN == 64, "tile width");
+  static_assert(kBN == 256 || (kFp4 && kBN == 128), "tile width");
+  static_assert(kMode == PM_FULL || !kFp4, "4-bit operands: widths of whole row blocks of scales");
   static_assert(!kFp4 || kKind == PK_NT || (kKind == PK_FWD && kBN == 256), "4-bit operands: K-major, whole row blocks of scales");
-  static_assert(!kFp4 || kBN >= 128, "scales come in blocks of 128 rows");
   static_assert(kStages >= 3 && kSmem <= kPairSmemMax && kSmem > 228 * 1024 / 2, "one CTA per SM");
   static_assert(kScaleCol + 2 * kScaleCols <= 512, "TMEM columns");
 };
@@ -66,6 +71,8 @@ struct PairArgs {
   int M[3], N[3];                    // its output (PK_FWD: N features)
   int nkb, nkb0;                     // k-blocks in all, and of the first pair of operands (PK_DX)
   int act;
+  int bn;                            // tile width (PM_WIDTH, PM_SPLIT)
+  int parts;                         // pairs of a cluster (PM_SPLIT)
   float alpha, alpha2;
   int early_next;                    // several rounds of tiles: the next launch is let in at the start (see long_dense in gemm_tc.cu)
   int* status;
@@ -82,8 +89,8 @@ struct PairTile { int job, m0, n0; };     // first row of the pair's tile, first
 
 // The raster of the other products: bands of eight tile rows, rows fastest inside a band, so that the tiles which run at
 // the same time share few operand panels.
-template <int kKind, int kCols>
-__device__ __forceinline__ PairTile pair_tile(const PairArgs& a, int tile) {
+template <int kKind>
+__device__ __forceinline__ PairTile pair_tile(const PairArgs& a, int tile, int cols) {
   int j = 0;
   if (kKind == PK_DW) {
     while (j < a.jobs - 1 && tile >= a.num_m[j] * a.num_n[j]) { tile -= a.num_m[j] * a.num_n[j]; ++j; }
@@ -91,7 +98,7 @@ __device__ __forceinline__ PairTile pair_tile(const PairArgs& a, int tile) {
   const int num_m = a.num_m[j], num_n = a.num_n[j];
   const int per_band = 8 * num_n, band = tile / per_band, rem = tile - band * per_band;
   const int gm = min(8, num_m - band * 8), nt = rem / gm;
-  return PairTile{j, (band * 8 + rem - nt * gm) * 256, nt * kCols};
+  return PairTile{j, (band * 8 + rem - nt * gm) * 256, nt * cols};
 }
 
 __device__ __forceinline__ void tma_load_3d_2cta(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z) {
@@ -142,25 +149,59 @@ __device__ __forceinline__ void mma_fp4_2cta(uint32_t d, uint64_t a, uint64_t b,
 __device__ __forceinline__ void tmem_cp_scales_2cta(uint32_t taddr, uint64_t sdesc) {
   asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(sdesc) : "memory");
 }
-template <int kKind, int kBN, int kFmt>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
-pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps> maps, const PairArgs args) {
-  using Cfg = PairCfg<kKind, kBN, kFmt>;
-  constexpr bool kFp4 = Cfg::kFp4, kGated = Cfg::kGated;
+// 32 columns of this lane's row, added up over the parts of a cluster in their order; four parts' loads are under way at once.
+__device__ __forceinline__ void sum_parts(uint32_t (&v)[32], uint32_t from, int rank, int parts) {
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    float4 x[4][2];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (s < parts) x[s][j] = ld_cluster_f4(from + (uint32_t)(2 * h + j) * 2048u, (uint32_t)(2 * s + rank));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float4 a = x[0][j];
+#pragma unroll
+      for (int s = 1; s < 4; ++s)
+        if (s < parts) { a.x += x[s][j].x; a.y += x[s][j].y; a.z += x[s][j].z; a.w += x[s][j].w; }
+      v[8 * h + 4 * j] = __float_as_uint(a.x); v[8 * h + 4 * j + 1] = __float_as_uint(a.y);
+      v[8 * h + 4 * j + 2] = __float_as_uint(a.z); v[8 * h + 4 * j + 3] = __float_as_uint(a.w);
+    }
+  }
+}
+// mma_commit_2cta for any pair of a cluster: `pair` its number.
+__device__ __forceinline__ void commit_pair(uint64_t* bar, int pair) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+      ::"r"(smem_u32(bar)), "h"((uint16_t)(3 << (2 * pair)))
+      : "memory");
+}
+
+template <int kKind, int kBN, int kFmt, int kMode>
+__global__ void __launch_bounds__(kPairThreads, 1)
+pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps> maps, const PairArgs args) {
+  using Cfg = PairCfg<kKind, kBN, kFmt, kMode>;
+  constexpr bool kFp4 = Cfg::kFp4, kGated = Cfg::kGated, kVar = kMode != PM_FULL, kSplit = kMode == PM_SPLIT;
   constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs;
-  constexpr int kTileCols = kGated ? kBN / 2 : kBN;        // output columns of a tile
+  const int bn = kVar ? args.bn : kBN, half = bn / 2;      // this CTA's columns of B
+  const int tile_cols = kGated ? half : bn;                // output columns of a tile
   extern __shared__ uint8_t smem_dyn[];
   uint8_t* smem = smem_dyn + align_pad(smem_dyn, 1024);
   uint8_t* epi = smem + kStages * Cfg::kStageBytes;
   PairCtl* ctl = reinterpret_cast<PairCtl*>(epi + 8 * Cfg::kEpiWarpBytes);
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = (int)cluster_ctarank();
-  const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+  const int cta = (int)cluster_ctarank(), rank = cta & 1, part = kSplit ? cta >> 1 : 0;
+  // the tiles of this pair (of this cluster, where pairs share one), and its k-blocks
+  const int parts = kSplit ? args.parts : 1;
+  const int pair = kSplit ? (int)blockIdx.x / (2 * parts) : blockIdx.x >> 1, num_pairs = kSplit ? 0x3FFFFFFF : gridDim.x >> 1;
+  const int kb0 = kSplit ? args.nkb * part / parts : 0, kb1 = kSplit ? args.nkb * (part + 1) / parts : args.nkb;
+  const int b_chunks = (half + 63) >> 6;                   // MN-major B: chunks of 64 columns
+  const uint32_t stage_tx = kVar ? 2u * (uint32_t)(Cfg::kABytes + (Cfg::kBMN ? b_chunks * 8192 : half * 128)) : 2u * Cfg::kStageBytes;
   int num_tiles = args.num_m[0] * args.num_n[0];
   if (kKind == PK_DW)
     for (int j = 1; j < args.jobs; ++j) num_tiles += args.num_m[j] * args.num_n[j];
-  const int nkb = args.nkb;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < (kKind == PK_DW ? 2 : 3); ++i) prefetch_tmap(&maps.m[i * (kKind == PK_DW ? 3 : 1)]);
@@ -194,16 +235,16 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
     uint32_t stage = 0, phase = 0;
     bool ok = true;
     for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
-      const PairTile t = pair_tile<kKind, kTileCols>(args, tile);
+      const PairTile t = pair_tile<kKind>(args, tile, tile_cols);
       const int m0 = t.m0 + rank * 128;
-      const int n0 = kGated ? t.n0 : t.n0 + rank * Cfg::kHalf;
-      for (int kb = 0; kb < nkb; ++kb) {
+      const int n0 = kGated ? t.n0 : t.n0 + rank * half;
+      for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag)) { ok = false; break; }
         if (issues) {
           uint8_t* sA = smem + stage * Cfg::kStageBytes;
           uint8_t* sB = sA + Cfg::kABytes;
           uint64_t* bar = &ctl->full[stage];
-          if (rank == 0) mbar_arrive_expect_tx(bar, 2u * (uint32_t)Cfg::kStageBytes);     // the bytes of both CTAs
+          if (rank == 0) mbar_arrive_expect_tx(bar, stage_tx);                            // the bytes of both CTAs
           const bool second = kKind == PK_DX && kb >= args.nkb0;
           const int k = (second ? kb - args.nkb0 : kb) * 64;
           if constexpr (kKind == PK_DW) {
@@ -216,7 +257,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
                                 : kGated ? &maps.m[1 + rank] : &maps.m[1];
           if constexpr (Cfg::kBMN) {
 #pragma unroll
-            for (int c = 0; c < Cfg::kBChunks; ++c) tma_load_2d_2cta(sB + c * 8192, mb, bar, n0 + c * 64, k);
+            for (int c = 0; c < Cfg::kBChunks; ++c)
+              if (!kVar || c < b_chunks) tma_load_2d_2cta(sB + c * 8192, mb, bar, n0 + c * 64, k);
           } else {
             tma_load_2d_2cta(sB, mb, bar, k, n0);
           }
@@ -236,11 +278,12 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
   } else if (warp == 1) {
     // =========================== MMA issuer (leader CTA only) ===========================
     if (rank == 0) {
-      constexpr uint32_t idesc = kFp4 ? idesc_fp4(256, kBN, kFmt) : idesc_bf16(256, kBN, Cfg::kAMN, Cfg::kBMN, false);
+      constexpr uint32_t idesc_full = kFp4 ? idesc_fp4(256, kBN, kFmt) : idesc_bf16(256, kBN, Cfg::kAMN, Cfg::kBMN, false);
+      const uint32_t idesc = kVar ? idesc_full - ((uint32_t)(kBN - bn) >> 3 << 17) : idesc_full;
       constexpr uint64_t a_proto = desc_proto(Cfg::kAMN ? 8192 : 16, 1024, kSwizzle128B);
       constexpr uint64_t b_proto = desc_proto(Cfg::kBMN ? 8192 : 16, 1024, kSwizzle128B);
       constexpr uint64_t s_proto = desc_proto(128, 128, kSwizzleNone);
-      const uint32_t smem16 = smem_u32(smem) >> 4, tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
+      const uint32_t smem16 = desc_address(smem), tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
       constexpr uint32_t a_step = (Cfg::kAMN ? 2048 : 32) >> 4, b_step = (Cfg::kBMN ? 2048 : 32) >> 4;
       const bool issues = elect_one();
       uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, blocks = 0;
@@ -249,12 +292,12 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
         if (!mbar_wait_warp(&ctl->tmem_empty[acc], acc_phase ^ 1, abort_flag)) break;
         tc_fence_after();
         const uint32_t d = tmem + acc * kBN;
-        for (int kb = 0; kb < nkb; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait_warp(&ctl->full[stage], phase, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t s16 = smem16 + stage * (uint32_t)(Cfg::kStageBytes >> 4);
           const uint64_t a = a_proto + s16, b = b_proto + (s16 + (Cfg::kABytes >> 4));
-          const uint32_t more = kb > 0 ? 1u : 0u;
+          const uint32_t more = kb > kb0 ? 1u : 0u;
           if constexpr (kFp4) {
             // The stage's scales go to TMEM, into one of two buffers in turn, ahead of the products that read them. The products that read
             // this buffer last are those of two blocks ago: their end has been signalled with their stage.
@@ -279,19 +322,19 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
                 mma_fp4_2cta<kFmt>(d, a + k * a_step, b + k * b_step, idesc | id << 4 | id << 29, sa + 4 * i, sb + 4 * i * Cfg::kBBlocks,
                                    k > 0 ? 1u : more);
               }
-              mma_commit_2cta(&ctl->empty[stage]);
+              commit_pair(&ctl->empty[stage], part);
             }
           } else if (issues) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) mma_f16_2cta(d, a + k * a_step, b + k * b_step, idesc, k > 0 ? 1u : more);
-            mma_commit_2cta(&ctl->empty[stage]);
+            commit_pair(&ctl->empty[stage], part);
           }
           __syncwarp();
           ++blocks;
           if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
         if (!ok) break;
-        if (issues) mma_commit_2cta(&ctl->tmem_full[acc]);
+        if (issues) commit_pair(&ctl->tmem_full[acc], part);
         __syncwarp();
         if (++acc == (uint32_t)kAccs) { acc = 0; acc_phase ^= 1; }
       }
@@ -316,11 +359,11 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
       buf ^= 1u;
     };
     for (int tile = pair; tile < num_tiles; tile += num_pairs) {
-      const PairTile t = pair_tile<kKind, kTileCols>(args, tile);
+      const PairTile t = pair_tile<kKind>(args, tile, tile_cols);
       const int row = t.m0 + rank * 128 + q * 32;
       const int M = kKind == PK_DW ? args.M[t.job] : args.M[0], N = kKind == PK_DW ? args.N[t.job] : args.N[0];
       // chunks of 32 output columns that are there; the two sets take them in turn
-      const int chunks = row < M ? min(kTileCols / 32, (N - t.n0 + 31) >> 5) : 0;
+      const int chunks = row < M ? min(tile_cols >> 5, (N - t.n0 + 31) >> 5) : 0;
       auto fetch = [&](int ch) {                           // PK_BWD: P and Q of a chunk
         if (lane == 0) {
           bulk_wait_read<0>();
@@ -329,8 +372,10 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
           tma_load_2d(bufs + 4096, &maps.m[3], loaded, t.n0 + ch * 32, row);
         }
       };
-      if (kKind == PK_BWD && set < chunks) fetch(set);
-      if (!mbar_wait_warp(&ctl->tmem_full[acc], acc_phase, abort_flag)) break;
+      if (kKind == PK_BWD && part * 2 + set < chunks) fetch(part * 2 + set);
+      if (!mbar_wait_warp(&ctl->tmem_full[acc], acc_phase, abort_flag)) {
+        if constexpr (!kSplit) break;
+      }
       tc_fence_after();
       const uint32_t taddr = tmem_base + acc * kBN + ((uint32_t)(q * 32) << 16);
       bool ok = true;
@@ -373,6 +418,41 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
           w[i] = bf16x2(lo, hi);
         }
       };
+      // a chunk's accumulator columns to its outputs
+      auto chunk = [&](uint32_t (&v)[32], uint32_t (&u)[32], int ch) {
+        const int col = t.n0 + ch * 32;
+        if constexpr (kGated) {
+          gated_chunk(v, u, col);
+        } else if constexpr (kKind == PK_BWD) {
+          uint32_t du[16], dg[16];
+          if (!mbar_wait_warp(loaded, load_phase, abort_flag)) return false;
+          load_phase ^= 1u;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float4 p = *reinterpret_cast<const float4*>(bufs + lane * 128 + ((j ^ (lane & 7)) << 4));
+            const float4 r = *reinterpret_cast<const float4*>(bufs + 4096 + lane * 128 + ((j ^ (lane & 7)) << 4));
+            const float d0 = __uint_as_float(v[4 * j]), d1 = __uint_as_float(v[4 * j + 1]), d2 = __uint_as_float(v[4 * j + 2]),
+                        d3 = __uint_as_float(v[4 * j + 3]);
+            du[2 * j] = bf16x2(d0 * p.x, d1 * p.y); du[2 * j + 1] = bf16x2(d2 * p.z, d3 * p.w);
+            dg[2 * j] = bf16x2(d0 * r.x, d1 * r.y); dg[2 * j + 1] = bf16x2(d2 * r.z, d3 * r.w);
+          }
+          __syncwarp();                                    // every row has been read: the results take its place
+          row_bf16(bufs, lane, du);
+          row_bf16(bufs + 4096, lane, dg);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            tma_store_2d(&maps.m[5], bufs, col, row);
+            tma_store_2d(&maps.m[4], bufs + 4096, col, row);
+            bulk_commit();
+          }
+        } else {
+          uint32_t w[16];
+          plain_chunk(v, w);
+          put16(&maps.m[kKind == PK_DW ? 6 + t.job : kKind == PK_DX ? 4 : 2], w, col, row);
+        }
+        return true;
+      };
       if constexpr (kAccs == 1) {
         // One accumulator: the next main loop waits for it, so all of it is read into registers and handed back before anything
         // is made of it (4099 x 8192 x 2048 gated, blocks of 16: 133 -> 112 us; 16384 x 4096 x 4096, blocks of 32: 161 -> 158).
@@ -404,58 +484,59 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
           for (int i = 0; i < kMine; ++i)
             if (set + 2 * i < chunks) put16(&maps.m[2], w[i], t.n0 + (set + 2 * i) * 32, row);
         }
+      } else if constexpr (kSplit) {
+        // this pair's sum over its part of K, [four columns][row][4], where the ring was: every product has been made
+        if (chunks > 0) {
+          float4* mine = reinterpret_cast<float4*>(smem) + q * 32 + lane;
+#pragma unroll 1
+          for (int ch = set; ch < bn >> 5; ch += 2) {
+            uint32_t v[32];
+            tmem_ld_32x32b_x32(taddr + ch * 32, v);
+            tmem_ld_wait_on(v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              mine[(ch * 8 + j) * 128] = make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]),
+                                                     __uint_as_float(v[4 * j + 3]));
+          }
+        }
       } else {
 #pragma unroll 1
         for (int ch = set; ch < chunks; ch += 2) {
-          const int col = t.n0 + ch * 32;
-          uint32_t v[32];
+          uint32_t v[32], u[32];
           tmem_ld_32x32b_x32(taddr + ch * 32, v);
-          if constexpr (kGated) {
-            uint32_t u[32];
-            tmem_ld_32x32b_x32(taddr + kBN / 2 + ch * 32, u);
-            tmem_ld_wait_on(v);
-            tmem_ld_wait_on(u);
-            gated_chunk(v, u, col);
-          } else if constexpr (kKind == PK_BWD) {
-            uint32_t du[16], dg[16];
-            tmem_ld_wait_on(v);
-            if (!mbar_wait_warp(loaded, load_phase, abort_flag)) { ok = false; break; }
-            load_phase ^= 1u;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-              const float4 p = *reinterpret_cast<const float4*>(bufs + lane * 128 + ((j ^ (lane & 7)) << 4));
-              const float4 r = *reinterpret_cast<const float4*>(bufs + 4096 + lane * 128 + ((j ^ (lane & 7)) << 4));
-              const float d0 = __uint_as_float(v[4 * j]), d1 = __uint_as_float(v[4 * j + 1]), d2 = __uint_as_float(v[4 * j + 2]),
-                          d3 = __uint_as_float(v[4 * j + 3]);
-              du[2 * j] = bf16x2(d0 * p.x, d1 * p.y); du[2 * j + 1] = bf16x2(d2 * p.z, d3 * p.w);
-              dg[2 * j] = bf16x2(d0 * r.x, d1 * r.y); dg[2 * j + 1] = bf16x2(d2 * r.z, d3 * r.w);
-            }
-            __syncwarp();                                  // every row has been read: the results take its place
-            row_bf16(bufs, lane, du);
-            row_bf16(bufs + 4096, lane, dg);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              tma_store_2d(&maps.m[5], bufs, col, row);
-              tma_store_2d(&maps.m[4], bufs + 4096, col, row);
-              bulk_commit();
-            }
-            if (ch + 2 < chunks) fetch(ch + 2);
-          } else {
-            tmem_ld_wait_on(v);
-            uint32_t w[16];
-            plain_chunk(v, w);
-            put16(&maps.m[kKind == PK_DW ? 6 + t.job : kKind == PK_DX ? 4 : 2], w, col, row);
-          }
+          if constexpr (kGated) tmem_ld_32x32b_x32(taddr + half + ch * 32, u);
+          tmem_ld_wait_on(v);
+          if constexpr (kGated) tmem_ld_wait_on(u);
+          if (!(ok = chunk(v, u, ch))) break;
+          if (kKind == PK_BWD && ch + 2 < chunks) fetch(ch + 2);
         }
         if (!ok) break;
         release();
       }
       if (++acc == (uint32_t)kAccs) { acc = 0; acc_phase ^= 1; }
+      if constexpr (kSplit) {
+        __syncwarp();
+        tc_fence_before();
+        cluster_sync_all();                                // every pair's sum is there
+        // the pairs share the tile's chunks, two to a pair at a time, and add them up in the order of the parts
+        const uint32_t from = smem_u32(smem) + (uint32_t)(q * 32 + lane) * 16u;
+#pragma unroll 1
+        for (int ch = part * 2 + set; ch < chunks; ch += 2 * parts) {
+          uint32_t v[32], u[32];
+          if (kKind == PK_BWD && ch != part * 2 + set) fetch(ch);
+          sum_parts(v, from + (uint32_t)ch * 16384u, rank, parts);
+          if constexpr (kGated) sum_parts(u, from + (uint32_t)(ch + (half >> 5)) * 16384u, rank, parts);
+          if (!chunk(v, u, ch)) break;
+        }
+      }
     }
     if (lane == 0) bulk_wait_all();
   }
 
+  if (kSplit && warp < 2) {
+    __syncwarp();
+    cluster_sync_all();                                    // with the epilogue warps, see there
+  }
   // =========================== teardown ===========================
   __syncwarp();
   tc_fence_before();
@@ -471,10 +552,10 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt>::
   }
 }
 
-template <int kKind, int kBN, int kFmt>
-int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps>& maps, PairArgs a, cudaStream_t s) {
-  using Cfg = PairCfg<kKind, kBN, kFmt>;
-  auto kern = pair_product_kernel<kKind, kBN, kFmt>;
+template <int kKind, int kBN, int kFmt, int kMode>
+int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps>& maps, PairArgs a, cudaStream_t s) {
+  using Cfg = PairCfg<kKind, kBN, kFmt, kMode>;
+  auto kern = pair_product_kernel<kKind, kBN, kFmt, kMode>;
   static bool attr_done[64] = {false};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
@@ -482,17 +563,31 @@ int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps>& maps, PairArgs
     SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::kSmem));
     if (dev >= 0 && dev < 64) attr_done[dev] = true;
   }
-  constexpr int cols = Cfg::kGated ? kBN / 2 : kBN;
+  const int bn = kMode == PM_FULL ? kBN : a.bn, cols = Cfg::kGated ? bn / 2 : bn, parts = kMode == PM_SPLIT ? a.parts : 1;
   int64_t tiles = 0;
   for (int j = 0; j < a.jobs; ++j) {
     a.num_m[j] = (a.M[j] + 255) / 256;
     a.num_n[j] = (a.N[j] + cols - 1) / cols;
     tiles += (int64_t)a.num_m[j] * a.num_n[j];
   }
-  if (tiles > 0x7FFFFFFF - 1024) return SF_ERR_SHAPE;
-  a.early_next = tiles > sm_count_now() / 2 && (tiles * 2 / sm_count_now() + 1) * a.nkb >= 128;
-  const int64_t pairs = tiles < sm_count_now() / 2 ? tiles : sm_count_now() / 2;
-  return launch_pdl(kern, dim3((unsigned)(2 * pairs)), kPairThreads, Cfg::kSmem, s, maps, a);
+  if (tiles > 0x3FFFFFFF / (2 * parts)) return SF_ERR_SHAPE;
+  const int64_t pairs = kMode == PM_SPLIT ? tiles * parts : tiles < sm_count_now() / 2 ? tiles : sm_count_now() / 2;
+  a.early_next = kMode != PM_SPLIT && tiles > sm_count_now() / 2 && (tiles * 2 / sm_count_now() + 1) * a.nkb >= 128;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * pairs));
+  cfg.blockDim = dim3(kPairThreads);
+  cfg.dynamicSmemBytes = Cfg::kSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)(2 * parts);
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  SF_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, maps, a));
+  return SF_OK;
 }
 
 }  // namespace

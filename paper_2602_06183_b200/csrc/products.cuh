@@ -38,21 +38,41 @@ inline int scale_map(void* m, int fmt, const void* p, int64_t rows, int64_t K) {
   return make_tmap_scales(m, p, ceil_div(rows, 128), scale_tiles(fmt, K), fmt == FMT_NV ? 4 : 2);
 }
 
-// Tile width of a product on CTA pairs by its estimated clocks: rounds of tiles, each of nkb stages and what a tile costs beside them. A
-// stage of 256 columns takes the tensor pipe 512 clocks; narrower ones are bounded by shared memory (operands written once, read
-// once, 128 bytes a clock).
-inline int pair_width(int64_t tiles256, int64_t tiles128, int64_t tiles64, int64_t nkb) {
-  const int64_t pairs = sm_count_now() / 2, tiles[3] = {tiles256, tiles128, tiles64};
-  const int width[3] = {256, 128, 64}, stage[3] = {512, 384, 320}, beside[3] = {900, 700, 600};
-  int best = 0;
-  double least = 0;
-  for (int i = 0; i < 3; ++i) {
-    const double c = (double)ceil_div(tiles[i], pairs) * (double)(nkb * stage[i] + beside[i]) + 4.0 * width[i];
-    if (i == 0 || c < 0.97 * least) { best = i; least = c; }
-  }
-  return width[best];
-}
 inline int64_t tiles_of(int64_t M, int64_t N, int64_t cols) { return ceil_div(M, 256) * ceil_div(N, cols); }
+
+// How a product on CTA pairs is cut, by its estimated clocks. Persistent tiles: rounds of nkb stages. Split: rounds of clusters, each with
+// its part of the stages, and with the sums through distributed shared memory and an epilogue that nothing runs beside.
+//   A stage of bn columns takes the tensor pipe 2 bn clocks, and shared memory the bytes that are written and read, 128 a clock
+//   (A 16 KB; B 64 bytes a column, MN-major B written in chunks of 64 columns).
+// Beside them: what a tile's epilogue takes on eight warps, which counts where it is longer than the main loop and after the last tile.
+struct PairPlan { int mode, bn, parts; };
+struct PairJob { int64_t M, N; };
+inline PairPlan pair_plan(int kind, const PairJob* jobs, int njobs, int64_t nkb, const FewRoom& room) {
+  const bool gated = kind == PK_FWD || kind == PK_FWD_SAVE, bmn = kind == PK_DX || kind == PK_DW || kind == PK_BWD;
+  const double chunk = kind == PK_FWD ? 900 : kind == PK_FWD_SAVE ? 1800 : kind == PK_BWD ? 1800 : 450;     // 32 output columns of a warp
+  PairPlan best{PM_FULL, 256, 1};
+  double least = 0;
+  for (int bn = 256; bn >= 64; bn -= gated ? 64 : 32) {
+    const int cols = gated ? bn / 2 : bn;
+    int64_t tiles = 0;
+    for (int j = 0; j < njobs; ++j) tiles += tiles_of(jobs[j].M, jobs[j].N, cols);
+    const double smem = bmn ? 256 + 64 * ceil_div(bn, 128) + bn / 2 : 256 + bn, stage = smem > 2 * bn ? smem : 2 * bn;
+    const double epilogue = chunk * (double)ceil_div(cols, 64);
+    for (int S = 1; S <= 4 && S <= nkb; ++S) {
+      const int64_t at_once = S == 1 ? sm_count_now() / 2 : room.clusters[2 * S - 1];
+      if (at_once <= 0) continue;
+      const double rounds = (double)ceil_div(tiles, at_once), loop = (double)ceil_div(nkb, S) * stage;
+      double c;
+      if (S == 1) c = rounds * (loop + 200 > epilogue ? loop + 200 : epilogue) + epilogue;
+      else c = rounds * (loop + 2500 + bn * 3 + ((double)ceil_div(cols, 64 * S)) * (chunk + 250 * S * (gated ? 2 : 1)));
+      if (least == 0 || c < 0.97 * least) {
+        best = PairPlan{S > 1 ? PM_SPLIT : bn == 256 ? PM_FULL : PM_WIDTH, bn, S};
+        least = c;
+      }
+    }
+  }
+  return best;
+}
 
 // Over how many CTAs of a cluster the reduction of a few-token product is split and how many CTAs share an SM, by the estimated time:
 // rounds of clusters; the time of a stage at its share of the memory's rate (which a part of the SMs does not reach: the 134 MB of the
@@ -110,17 +130,36 @@ int run_few(const Operand& X, const Operand& W0, const Operand& W1, int64_t N, i
   return run_few_n<kFmt, kGated, 128>(X, W0, W1, N, K, a, s);
 }
 
+// Launches the kernel of a plan: make(maps, bn) fills the tensor maps for tiles of that width.
+template <int kKind, typename F>
+int launch_plan(const PairPlan& plan, PairArgs a, cudaStream_t s, F&& make) {
+  PairMaps<PairCfg<kKind, 256, FMT_BF16, PM_FULL>::kMaps> maps;
+  SF_TRY(make(maps.m, plan.bn));
+  a.bn = plan.bn;
+  a.parts = plan.parts;
+  return plan.mode == PM_FULL    ? launch_pair<kKind, 256, FMT_BF16, PM_FULL>(maps, a, s)
+         : plan.mode == PM_WIDTH ? launch_pair<kKind, 256, FMT_BF16, PM_WIDTH>(maps, a, s)
+                                 : launch_pair<kKind, 256, FMT_BF16, PM_SPLIT>(maps, a, s);
+}
+// The same from the sizes.
+template <int kKind, typename F>
+int launch_best(const PairArgs& a, cudaStream_t s, F&& make) {
+  const FewRoom* room;
+  SF_TRY((few_room<FMT_BF16, false, 16>(&room)));          // (one CTA to an SM, like the pairs')
+  PairJob jobs[3];
+  for (int j = 0; j < a.jobs; ++j) jobs[j] = PairJob{a.M[j], a.N[j]};
+  return launch_plan<kKind>(pair_plan(kKind, jobs, a.jobs, a.nkb, *room), a, s, make);
+}
+
 template <int kFmt, int kBN>
-int run_nt_pair(const Operand& A, const Operand& B, int64_t K, void* C, const PairArgs& a, cudaStream_t s) {
-  PairMaps<PairCfg<PK_NT, kBN, kFmt>::kMaps> m;
+int run_nt_fp4(const Operand& A, const Operand& B, int64_t K, void* C, const PairArgs& a, cudaStream_t s) {
+  PairMaps<5> m;
   SF_TRY(kmajor_map(&m.m[0], kFmt, A.data, a.M[0], K, 128));
   SF_TRY(kmajor_map(&m.m[1], kFmt, B.data, a.N[0], K, kBN / 2));
   SF_TRY(make_tmap_store(&m.m[2], C, a.M[0], a.N[0]));
-  if constexpr (kFmt != FMT_BF16) {
-    SF_TRY(scale_map(&m.m[3], kFmt, A.scales, a.M[0], K));
-    SF_TRY(scale_map(&m.m[4], kFmt, B.scales, a.N[0], K));
-  }
-  return launch_pair<PK_NT, kBN, kFmt>(m, a, s);
+  SF_TRY(scale_map(&m.m[3], kFmt, A.scales, a.M[0], K));
+  SF_TRY(scale_map(&m.m[4], kFmt, B.scales, a.N[0], K));
+  return launch_pair<PK_NT, kBN, kFmt, PM_FULL>(m, a, s);
 }
 
 // C[M, N] = alpha A B^T; M, N, K > 0. early_weights: the launch before this one is another product of the same call, which does not
@@ -137,31 +176,18 @@ int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, 
   }
   PairArgs a{};
   a.jobs = 1; a.M[0] = (int)M; a.N[0] = (int)N; a.nkb = a.nkb0 = nkb; a.alpha = alpha; a.status = status;
-  const int w = pair_width(tiles_of(M, N, 256), tiles_of(M, N, 128), kFmt == FMT_BF16 ? tiles_of(M, N, 64) : (int64_t)1 << 40, nkb);
-  if (w == 256) return run_nt_pair<kFmt, 256>(A, B, K, C, a, s);
-  if constexpr (kFmt == FMT_BF16)
-    if (w == 64) return run_nt_pair<kFmt, 64>(A, B, K, C, a, s);
-  return run_nt_pair<kFmt, 128>(A, B, K, C, a, s);
-}
-
-template <int kKind, int kFmt, int kBN>
-int run_gated_pair(const Operand& A, const Operand& Bg, const Operand& Bu, int64_t K, void* H, float* P, float* Q, const PairArgs& a,
-                   cudaStream_t s) {
-  PairMaps<PairCfg<kKind, kBN, kFmt>::kMaps> m;
-  SF_TRY(kmajor_map(&m.m[0], kFmt, A.data, a.M[0], K, 128));
-  SF_TRY(kmajor_map(&m.m[1], kFmt, Bg.data, a.N[0], K, kBN / 2));
-  SF_TRY(kmajor_map(&m.m[2], kFmt, Bu.data, a.N[0], K, kBN / 2));
-  SF_TRY(make_tmap_store(&m.m[3], H, a.M[0], a.N[0]));
-  if constexpr (kKind == PK_FWD_SAVE) {
-    SF_TRY(make_tmap_f32(&m.m[4], P, a.M[0], a.N[0]));
-    SF_TRY(make_tmap_f32(&m.m[5], Q, a.M[0], a.N[0]));
+  if constexpr (kFmt == FMT_BF16) {
+    return launch_best<PK_NT>(a, s, [&](CUtensorMap* m, int bn) {
+      SF_TRY(kmajor_map(&m[0], kFmt, A.data, M, K, 128));
+      SF_TRY(kmajor_map(&m[1], kFmt, B.data, N, K, bn / 2));
+      return make_tmap_store(&m[2], C, M, N);
+    });
+  } else {
+    // rounds of tiles, a stage of 256 or of 128 columns (bounded by shared memory), and what a tile costs beside
+    const int64_t pairs = sm_count_now() / 2;
+    const int64_t wide = ceil_div(tiles_of(M, N, 256), pairs) * (nkb * 600 + 900), narrow = ceil_div(tiles_of(M, N, 128), pairs) * (nkb * 450 + 200);
+    return wide <= narrow ? run_nt_fp4<kFmt, 256>(A, B, K, C, a, s) : run_nt_fp4<kFmt, 128>(A, B, K, C, a, s);
   }
-  if constexpr (kFmt != FMT_BF16) {
-    SF_TRY(scale_map(&m.m[4], kFmt, A.scales, a.M[0], K));
-    SF_TRY(scale_map(&m.m[5], kFmt, Bg.scales, a.N[0], K));
-    SF_TRY(scale_map(&m.m[6], kFmt, Bu.scales, a.N[0], K));
-  }
-  return launch_pair<kKind, kBN, kFmt>(m, a, s);
 }
 
 // H = act(alpha_g A Bg^T) (alpha_u A Bu^T); P, Q (bf16 operands; both or neither): act(g) and u act'(g) in float32. M, N, K > 0.
@@ -178,18 +204,27 @@ int run_gated(const Operand& A, const Operand& Bg, const Operand& Bu, int64_t M,
   PairArgs a{};
   a.jobs = 1; a.M[0] = (int)M; a.N[0] = (int)N; a.nkb = a.nkb0 = nkb; a.act = act; a.alpha = alpha_g; a.alpha2 = alpha_u;
   a.status = status;
+  auto operands = [&](CUtensorMap* m, int bn) {
+    SF_TRY(kmajor_map(&m[0], kFmt, A.data, M, K, 128));
+    SF_TRY(kmajor_map(&m[1], kFmt, Bg.data, N, K, bn / 2));
+    SF_TRY(kmajor_map(&m[2], kFmt, Bu.data, N, K, bn / 2));
+    return make_tmap_store(&m[3], H, M, N);
+  };
   if constexpr (kFmt != FMT_BF16) {
-    return run_gated_pair<PK_FWD, kFmt, 256>(A, Bg, Bu, K, H, nullptr, nullptr, a, s);
+    PairMaps<7> m;
+    SF_TRY(operands(m.m, 256));
+    SF_TRY(scale_map(&m.m[4], kFmt, A.scales, M, K));
+    SF_TRY(scale_map(&m.m[5], kFmt, Bg.scales, N, K));
+    SF_TRY(scale_map(&m.m[6], kFmt, Bu.scales, N, K));
+    return launch_pair<PK_FWD, 256, kFmt, PM_FULL>(m, a, s);
+  } else if (P) {
+    return launch_best<PK_FWD_SAVE>(a, s, [&](CUtensorMap* m, int bn) {
+      SF_TRY(operands(m, bn));
+      SF_TRY(make_tmap_f32(&m[4], P, M, N));
+      return make_tmap_f32(&m[5], Q, M, N);
+    });
   } else {
-    const int w = pair_width(tiles_of(M, N, 128), tiles_of(M, N, 64), tiles_of(M, N, 32), nkb);
-    if (P) {
-      if (w == 256) return run_gated_pair<PK_FWD_SAVE, kFmt, 256>(A, Bg, Bu, K, H, P, Q, a, s);
-      if (w == 128) return run_gated_pair<PK_FWD_SAVE, kFmt, 128>(A, Bg, Bu, K, H, P, Q, a, s);
-      return run_gated_pair<PK_FWD_SAVE, kFmt, 64>(A, Bg, Bu, K, H, P, Q, a, s);
-    }
-    if (w == 256) return run_gated_pair<PK_FWD, kFmt, 256>(A, Bg, Bu, K, H, P, Q, a, s);
-    if (w == 128) return run_gated_pair<PK_FWD, kFmt, 128>(A, Bg, Bu, K, H, P, Q, a, s);
-    return run_gated_pair<PK_FWD, kFmt, 64>(A, Bg, Bu, K, H, P, Q, a, s);
+    return launch_best<PK_FWD>(a, s, operands);
   }
 }
 
