@@ -471,18 +471,19 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
             if (set + 2 * i < chunks) gated_chunk(v[i], u[i], t.n0 + (set + 2 * i) * 32);
         } else {
           constexpr int kMine = kBN / 64;
-          uint32_t w[kMine][16], v[2][32];
-          tmem_ld_32x32b_x32(taddr + set * 32, v[0]);
+          uint32_t v[kMine][32];
 #pragma unroll
-          for (int i = 0; i < kMine; ++i) {
-            tmem_ld_wait_on(v[i & 1]);
-            if (i + 1 < kMine) tmem_ld_32x32b_x32(taddr + (set + 2 * i + 2) * 32, v[(i + 1) & 1]);
-            plain_chunk(v[i & 1], w[i]);
-          }
+          for (int i = 0; i < kMine; ++i) tmem_ld_32x32b_x32(taddr + (set + 2 * i) * 32, v[i]);
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) tmem_ld_wait_on(v[i]);
           release();
 #pragma unroll
           for (int i = 0; i < kMine; ++i)
-            if (set + 2 * i < chunks) put16(&maps.m[2], w[i], t.n0 + (set + 2 * i) * 32, row);
+            if (set + 2 * i < chunks) {
+              uint32_t w[16];
+              plain_chunk(v[i], w);
+              put16(&maps.m[2], w, t.n0 + (set + 2 * i) * 32, row);
+            }
         }
       } else if constexpr (kSplit) {
         // this pair's sum over its part of K, [four columns][row][4], where the ring was: every product has been made
