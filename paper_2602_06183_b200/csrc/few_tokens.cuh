@@ -5,7 +5,7 @@
 // of the ranges (the same every time) through distributed shared memory.
 //
 // CTA = 10 warps: TMA producer, MMA issuer, four warps that read the accumulator out; all of them add up (with six, whose loads
-// are few at a time, 100 tokens through both projections of 8192 x 2048 took 15.7 us, with ten %X%). Every wait is bounded (see gemm_tc.cu); the
+// are few at a time, 100 tokens through both projections of 8192 x 2048 took 15.7 us, with ten 12.1). Every wait is bounded (see gemm_tc.cu); the
 // cluster barriers are reached by every warp because their own waits are.
 #pragma once
 
