@@ -159,7 +159,9 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
       return make_tmap_store(&m[5], du, T, F);
     }));
   }
+  PairPlan dx_plan;
   if (dX) {
+    a.early_next = dWg || dWu || dWd;                      // they run beside it
     a.M[0] = (int)T; a.N[0] = (int)D; a.nkb0 = k_blocks(FMT_BF16, F); a.nkb = 2 * a.nkb0;
     SF_TRY(launch_best<PK_DX>(a, s, [&](CUtensorMap* m, int) {
       SF_TRY(kmajor_map(&m[0], FMT_BF16, dg, T, F, 128));
@@ -167,7 +169,8 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
       SF_TRY(mn_map(&m[2], Wg, F, D));
       SF_TRY(mn_map(&m[3], Wu, F, D));
       return make_tmap_store(&m[4], dX, T, D);
-    }));
+    }, &dx_plan));
+    a.early_next = 0;
   }
   GradJob jobs[3];
   a.jobs = 0;
@@ -186,7 +189,7 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
     for (int j = a.jobs; j < 3; ++j)
       for (int i = 0; i < 9; i += 3) m[i + j] = m[i];
     return (int)SF_OK;
-  });
+  }, nullptr, dX ? &dx_plan : nullptr);
 }
 
 }  // extern "C"

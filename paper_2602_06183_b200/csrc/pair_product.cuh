@@ -74,7 +74,10 @@ struct PairArgs {
   int bn;                            // tile width (PM_WIDTH, PM_SPLIT)
   int parts;                         // pairs of a cluster (PM_SPLIT)
   float alpha, alpha2;
-  int early_next;                    // several rounds of tiles: the next launch is let in at the start (see long_dense in gemm_tc.cu)
+  int early_next;                    // the next launch is let in at the start: several rounds of tiles (see long_dense in gemm_tc.cu), or it runs beside
+  // Beside the launch before it, whose results it does not read (they are waited for at the end): that one holds the pairs from `first_late` on for
+  // about `late_rounds` tiles of this one, which those pairs leave to the others.
+  int beside, first_late, late_rounds;
   int* status;
 };
 template <int N> struct PairMaps { CUtensorMap m[N]; };
@@ -89,6 +92,13 @@ struct PairTile { int job, m0, n0; };     // first row of the pair's tile, first
 
 // The raster of the other products: bands of eight tile rows, rows fastest inside a band, so that the tiles which run at
 // the same time share few operand panels.
+// The n-th tile of a pair: every num_pairs-th one; the first late_rounds rounds are shared by the pairs that are not late.
+__device__ __forceinline__ int nth_tile(const PairArgs& a, int n, int pair, int num_pairs) {
+  const int r = a.late_rounds, e = a.first_late;
+  if (r == 0) return pair + n * num_pairs;
+  return pair >= e ? r * e + n * num_pairs + pair : n < r ? n * e + pair : r * e + (n - r) * num_pairs + pair;
+}
+
 template <int kKind>
 __device__ __forceinline__ PairTile pair_tile(const PairArgs& a, int tile, int cols) {
   int j = 0;
@@ -225,7 +235,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
   __syncthreads();
   cluster_sync_all();
   tc_fence_after();
-  pdl_wait();
+  if (!args.beside) pdl_wait();
   if (args.early_next) pdl_trigger();
   const uint32_t tmem_base = ctl->tmem_base;
 
@@ -234,7 +244,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
     const bool issues = elect_one();
     uint32_t stage = 0, phase = 0;
     bool ok = true;
-    for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
+    for (int n = 0, tile; ok && (tile = nth_tile(args, n, pair, num_pairs)) < num_tiles; ++n) {
       const PairTile t = pair_tile<kKind>(args, tile, tile_cols);
       const int m0 = t.m0 + rank * 128;
       const int n0 = kGated ? t.n0 : t.n0 + rank * half;
@@ -288,7 +298,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       const bool issues = elect_one();
       uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0, blocks = 0;
       bool ok = true;
-      for (int tile = pair; tile < num_tiles && ok; tile += num_pairs) {
+      for (int n = 0, tile; ok && (tile = nth_tile(args, n, pair, num_pairs)) < num_tiles; ++n) {
         if (!mbar_wait_warp(&ctl->tmem_empty[acc], acc_phase ^ 1, abort_flag)) break;
         tc_fence_after();
         const uint32_t d = tmem + acc * kBN;
@@ -358,7 +368,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       put_chunk_end(m, bufs + buf * kBufBytes, col, row, lane);
       buf ^= 1u;
     };
-    for (int tile = pair; tile < num_tiles; tile += num_pairs) {
+    for (int n = 0, tile; (tile = nth_tile(args, n, pair, num_pairs)) < num_tiles; ++n) {
       const PairTile t = pair_tile<kKind>(args, tile, tile_cols);
       const int row = t.m0 + rank * 128 + q * 32;
       const int M = kKind == PK_DW ? args.M[t.job] : args.M[0], N = kKind == PK_DW ? args.N[t.job] : args.N[0];
@@ -546,6 +556,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
     atomicExch(args.status, 1);
     drain_after_expiry();
   }
+  if (args.beside) pdl_wait();                             // this launch ends after the one before it
   cluster_sync_all();
   if (warp == 1) {
     tc_fence_after();
@@ -573,7 +584,7 @@ int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps>& maps, P
   }
   if (tiles > 0x3FFFFFFF / (2 * parts)) return SF_ERR_SHAPE;
   const int64_t pairs = kMode == PM_SPLIT ? tiles * parts : tiles < sm_count_now() / 2 ? tiles : sm_count_now() / 2;
-  a.early_next = kMode != PM_SPLIT && tiles > sm_count_now() / 2 && (tiles * 2 / sm_count_now() + 1) * a.nkb >= 128;
+  a.early_next |= kMode != PM_SPLIT && tiles > sm_count_now() / 2 && (tiles * 2 / sm_count_now() + 1) * a.nkb >= 128;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
   cfg.blockDim = dim3(kPairThreads);

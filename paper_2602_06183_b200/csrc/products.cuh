@@ -45,12 +45,12 @@ inline int64_t tiles_of(int64_t M, int64_t N, int64_t cols) { return ceil_div(M,
 //   A stage of bn columns takes the tensor pipe 2 bn clocks, and shared memory the bytes that are written and read, 128 a clock
 //   (A 16 KB; B 64 bytes a column, MN-major B written in chunks of 64 columns).
 // Beside them: what a tile's epilogue takes on eight warps, which counts where it is longer than the main loop and after the last tile.
-struct PairPlan { int mode, bn, parts; };
+struct PairPlan { int mode, bn, parts; int64_t pairs; double clocks, per_tile; };      // pairs that it holds; estimates
 struct PairJob { int64_t M, N; };
 inline PairPlan pair_plan(int kind, const PairJob* jobs, int njobs, int64_t nkb, const FewRoom& room) {
   const bool gated = kind == PK_FWD || kind == PK_FWD_SAVE, bmn = kind == PK_DX || kind == PK_DW || kind == PK_BWD;
-  const double chunk = kind == PK_FWD ? 900 : kind == PK_FWD_SAVE ? 1800 : kind == PK_BWD ? 1800 : 450;     // 32 output columns of a warp
-  PairPlan best{PM_FULL, 256, 1};
+  const double chunk = kind == PK_FWD ? 1200 : kind == PK_FWD_SAVE ? 2400 : kind == PK_BWD ? 2200 : 1000;   // 32 output columns of a warp
+  PairPlan best{PM_FULL, 256, 1, 0, 0, 0};
   double least = 0;
   for (int bn = 256; bn >= 64; bn -= gated ? 64 : 32) {
     const int cols = gated ? bn / 2 : bn;
@@ -66,7 +66,8 @@ inline PairPlan pair_plan(int kind, const PairJob* jobs, int njobs, int64_t nkb,
       if (S == 1) c = rounds * (loop + 200 > epilogue ? loop + 200 : epilogue) + epilogue;
       else c = rounds * (loop + 2500 + bn * 3 + ((double)ceil_div(cols, 64 * S)) * (chunk + 250 * S * (gated ? 2 : 1)));
       if (least == 0 || c < 0.97 * least) {
-        best = PairPlan{S > 1 ? PM_SPLIT : bn == 256 ? PM_FULL : PM_WIDTH, bn, S};
+        best = PairPlan{S > 1 ? PM_SPLIT : bn == 256 ? PM_FULL : PM_WIDTH, bn, S, (tiles < at_once ? tiles : at_once) * S, c,
+                        loop + 200 > epilogue ? loop + 200 : epilogue};
         least = c;
       }
     }
@@ -143,12 +144,26 @@ int launch_plan(const PairPlan& plan, PairArgs a, cudaStream_t s, F&& make) {
 }
 // The same from the sizes.
 template <int kKind, typename F>
-int launch_best(const PairArgs& a, cudaStream_t s, F&& make) {
+int launch_best(const PairArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr, const PairPlan* beside = nullptr) {
   const FewRoom* room;
   SF_TRY((few_room<FMT_BF16, false, 16>(&room)));          // (one CTA to an SM, like the pairs')
   PairJob jobs[3];
   for (int j = 0; j < a.jobs; ++j) jobs[j] = PairJob{a.M[j], a.N[j]};
-  return launch_plan<kKind>(pair_plan(kKind, jobs, a.jobs, a.nkb, *room), a, s, make);
+  const PairPlan plan = pair_plan(kKind, jobs, a.jobs, a.nkb, *room);
+  if (taken) *taken = plan;
+  if (!beside) return launch_plan<kKind>(plan, a, s, make);
+  PairArgs b = a;
+  b.beside = 1;
+  const int64_t pairs = sm_count_now() / 2;
+  if (beside->pairs < pairs && plan.mode != PM_SPLIT) {
+    b.first_late = (int)(pairs - beside->pairs);
+    b.late_rounds = (int)(beside->clocks / plan.per_tile);
+    // (fewer tiles than pairs, or all of them made before the late ones come: the plain order)
+    int64_t tiles = 0;
+    for (int j = 0; j < a.jobs; ++j) tiles += tiles_of(a.M[j], a.N[j], plan.bn);
+    if (tiles <= b.first_late) b.late_rounds = 0;
+  }
+  return launch_plan<kKind>(plan, b, s, make);
 }
 
 template <int kFmt, int kBN>
