@@ -1,5 +1,9 @@
-// Products of few tokens with whole weight matrices: C[T, N] = alpha A[T, K] W[N, K]^T, or the gated pair of such products, with T
-// at most kN. What bounds them is reading the weights once, so the weights are the instruction's 128 rows and the tokens its
+// Products of few tokens with whole weight matrices, T at most kN:
+//   FK_NT     C[T, N] = alpha X[T, K] W[N, K]^T
+//   FK_GATED  H = act(alpha_g X Wg^T) (alpha_u X Wu^T), optionally P and Q
+//   FK_DX     C = X0 W0 + X1 W1, the weights stored [K, N]; one accumulation over both pairs
+//   FK_BWD    dU = (X W) P, dG = (X W) Q, the weights stored [K, N]
+// What bounds them is reading the weights once, so the weights are the instruction's 128 rows and the tokens its
 // few columns, and the reduction is split over the CTAs of a cluster until every SM has weights to read: each computes
 // a partial sum of its own K range in TMEM, leaves it in its shared memory, and the cluster adds the partial sums up in the order
 // of the ranges (the same every time) through distributed shared memory.
@@ -21,9 +25,11 @@ constexpr int kFewStages = 10;       // of the ring, at most
 
 constexpr uint32_t pow2_cols(uint32_t n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
 
-template <int kFmt, bool kGated, int kN>
+enum FewKind { FK_NT, FK_GATED, FK_DX, FK_BWD };
+
+template <int kFmt, int kKind, int kN>
 struct FewCfg {
-  static constexpr bool kFp4 = kFmt != FMT_BF16;
+  static constexpr bool kFp4 = kFmt != FMT_BF16, kGated = kKind == FK_GATED, kWMN = kKind == FK_DX || kKind == FK_BWD;
   static constexpr int kMats = kGated ? 2 : 1;
   static constexpr int kTiles = kFmt == FMT_NV ? 4 : kFmt == FMT_MX ? 2 : 0;
   static constexpr int kWBytes = 16384, kXBytes = kN * 128;
@@ -44,15 +50,18 @@ struct FewCfg {
 
 struct FewArgs {
   int T, N, nkb;                     // tokens, output columns, k-blocks (64 K of bf16, 256 K of 4 bits)
+  int nkb0;                          // FK_DX: those of the first pair
   int act;
   int stages;                        // of the ring
   int early_weights;                 // the launch before this one does not write the weights, and waited for those that may have
+  int early_next;                    // the next launch runs beside this one
   float alpha, alpha2;
-  void* C;                           // [T, N] bf16
-  float *P, *Q;                      // gated, optional
+  void* C;                           // [T, N] bf16 (FK_BWD: dU)
+  void* C2;                          // FK_BWD: dG
+  float *P, *Q;                      // FK_GATED: written, optional; FK_BWD: read
   int* status;
 };
-struct FewMaps { CUtensorMap x, w0, w1, sx, s0, s1; };
+struct FewMaps { CUtensorMap x, w0, w1, sx, s0, s1; };      // (FK_DX: the second pair is w1 and sx)
 
 struct FewCtl {
   uint64_t full[kFewStages], empty[kFewStages], done;
@@ -98,31 +107,40 @@ __device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t sdesc) {
 }
 
 // The weights' part of a stage, and the tokens'.
-template <int kFmt, bool kGated, int kN>
-__device__ __forceinline__ void load_weights(const FewMaps& maps, uint8_t* sw, uint64_t* bar, int kb, int f0) {
-  using Cfg = FewCfg<kFmt, kGated, kN>;
+template <int kFmt, int kKind, int kN>
+__device__ __forceinline__ void load_weights(const FewMaps& maps, uint8_t* sw, uint64_t* bar, int kb, int f0, int nkb0) {
+  using Cfg = FewCfg<kFmt, kKind, kN>;
   mbar_arrive_expect_tx(bar, (uint32_t)Cfg::kStageBytes);
+  if constexpr (Cfg::kWMN) {
+    const bool second = kKind == FK_DX && kb >= nkb0;
+    const CUtensorMap* w = second ? &maps.w1 : &maps.w0;
+    const int k = (second ? kb - nkb0 : kb) * 64;
+    tma_load_2d(sw, w, bar, f0, k);
+    tma_load_2d(sw + 8192, w, bar, f0 + 64, k);
+    return;
+  }
   tma_load_2d(sw, &maps.w0, bar, kb * 64, f0);
-  if (kGated) tma_load_2d(sw + Cfg::kWBytes, &maps.w1, bar, kb * 64, f0);
+  if (Cfg::kGated) tma_load_2d(sw + Cfg::kWBytes, &maps.w1, bar, kb * 64, f0);
   if constexpr (Cfg::kFp4) {
     uint8_t* ss = sw + Cfg::kMats * Cfg::kWBytes + Cfg::kXBytes;
     tma_load_3d(ss, &maps.s0, bar, 0, kb * Cfg::kTiles, f0 >> 7);
-    if (kGated) tma_load_3d(ss + Cfg::kTiles * 512, &maps.s1, bar, 0, kb * Cfg::kTiles, f0 >> 7);
+    if (Cfg::kGated) tma_load_3d(ss + Cfg::kTiles * 512, &maps.s1, bar, 0, kb * Cfg::kTiles, f0 >> 7);
   }
 }
-template <int kFmt, bool kGated, int kN>
-__device__ __forceinline__ void load_tokens(const FewMaps& maps, uint8_t* sw, uint64_t* bar, int kb) {
-  using Cfg = FewCfg<kFmt, kGated, kN>;
+template <int kFmt, int kKind, int kN>
+__device__ __forceinline__ void load_tokens(const FewMaps& maps, uint8_t* sw, uint64_t* bar, int kb, int nkb0) {
+  using Cfg = FewCfg<kFmt, kKind, kN>;
   uint8_t* sx = sw + Cfg::kMats * Cfg::kWBytes;
-  tma_load_2d(sx, &maps.x, bar, kb * 64, 0);
+  const bool second = kKind == FK_DX && kb >= nkb0;
+  tma_load_2d(sx, second ? &maps.sx : &maps.x, bar, (second ? kb - nkb0 : kb) * 64, 0);
   if constexpr (Cfg::kFp4) tma_load_3d(sx + Cfg::kXBytes + Cfg::kMats * Cfg::kTiles * 512, &maps.sx, bar, 0, kb * Cfg::kTiles, 0);
 }
 
-template <int kFmt, bool kGated, int kN>
-__global__ void __launch_bounds__(kFewThreads, FewCfg<kFmt, kGated, kN>::kMostPerSm)
+template <int kFmt, int kKind, int kN>
+__global__ void __launch_bounds__(kFewThreads, FewCfg<kFmt, kKind, kN>::kMostPerSm)
 few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
-  using Cfg = FewCfg<kFmt, kGated, kN>;
-  constexpr bool kFp4 = Cfg::kFp4;
+  using Cfg = FewCfg<kFmt, kKind, kN>;
+  constexpr bool kFp4 = Cfg::kFp4, kGated = Cfg::kGated;
   constexpr int kMats = Cfg::kMats, kTiles = Cfg::kTiles;
   const uint32_t stages = (uint32_t)args.stages;
   extern __shared__ uint8_t smem_dyn[];
@@ -158,23 +176,26 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
     // what fits the ring of weights that are known to be there is fetched while the launch before this one ends
     const int early = args.early_weights ? min((int)stages, kb1 - kb0) : 0;
     if (issues)
-      for (int i = 0; i < early; ++i) load_weights<kFmt, kGated, kN>(maps, smem + i * Cfg::kStageBytes, &ctl->full[i], kb0 + i, f0);
+      for (int i = 0; i < early; ++i) load_weights<kFmt, kKind, kN>(maps, smem + i * Cfg::kStageBytes, &ctl->full[i], kb0 + i, f0, args.nkb0);
     __syncwarp();
     pdl_wait();
+    if (args.early_next) pdl_trigger();
     uint32_t stage = 0, phase = 0;
     for (int kb = kb0; kb < kb1; ++kb) {
       if (!mbar_wait_warp(&ctl->empty[stage], phase ^ 1, abort_flag)) break;
       if (issues) {
         uint8_t* sw = smem + stage * Cfg::kStageBytes;
-        if (kb - kb0 >= early) load_weights<kFmt, kGated, kN>(maps, sw, &ctl->full[stage], kb, f0);
-        load_tokens<kFmt, kGated, kN>(maps, sw, &ctl->full[stage], kb);
+        if (kb - kb0 >= early) load_weights<kFmt, kKind, kN>(maps, sw, &ctl->full[stage], kb, f0, args.nkb0);
+        load_tokens<kFmt, kKind, kN>(maps, sw, &ctl->full[stage], kb, args.nkb0);
       }
       if (++stage == stages) { stage = 0; phase ^= 1; }
     }
     pdl_trigger();
   } else if (warp == 1) {
-    constexpr uint32_t idesc = kFp4 ? idesc_fp4(128, kN, kFmt) : idesc_bf16(128, kN, false, false, false);
-    constexpr uint64_t proto = desc_proto(16, 1024, kSwizzle128B), s_proto = desc_proto(128, 128, kSwizzleNone);
+    constexpr uint32_t idesc = kFp4 ? idesc_fp4(128, kN, kFmt) : idesc_bf16(128, kN, Cfg::kWMN, false, false);
+    constexpr uint64_t proto = desc_proto(16, 1024, kSwizzle128B), w_proto = desc_proto(Cfg::kWMN ? 8192 : 16, 1024, kSwizzle128B);
+    constexpr uint32_t w_step = (Cfg::kWMN ? 2048 : 32) >> 4;
+    constexpr uint64_t s_proto = desc_proto(128, 128, kSwizzleNone);
     const uint32_t smem16 = desc_address(smem), tmem = __shfl_sync(0xFFFFFFFFu, tmem_base, 0);
     const bool issues = elect_one();
     uint32_t stage = 0, phase = 0;
@@ -183,7 +204,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
       if (!mbar_wait_warp(&ctl->full[stage], phase, abort_flag)) { ok = false; break; }
       tc_fence_after();
       const uint32_t s16 = smem16 + stage * (uint32_t)(Cfg::kStageBytes >> 4);
-      const uint64_t w = proto + s16, x = proto + (s16 + (kMats * Cfg::kWBytes >> 4));
+      const uint64_t w = w_proto + s16, x = proto + (s16 + (kMats * Cfg::kWBytes >> 4));
       const uint32_t scol = tmem + Cfg::kScaleCol + ((uint32_t)(kb - kb0) & 1u) * Cfg::kScaleCols;
       const uint32_t more = kb > kb0 ? 1u : 0u;
       // scales: one of two buffers in turn; the products of two blocks ago, which read this one, have signalled their end with their stage
@@ -201,7 +222,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
         for (int m = 0; m < kMats; ++m)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const uint64_t wd = w + (m * (Cfg::kWBytes >> 4) + 2 * k), xd = x + 2 * k;
+            const uint64_t wd = w + (m * (Cfg::kWBytes >> 4) + k * w_step), xd = x + 2 * k;
             if constexpr (kFp4) {
               const int i = kFmt == FMT_NV ? k : k >> 1;
               const uint32_t id = kFmt == FMT_NV ? 0u : (uint32_t)(k & 1) * 2u;
@@ -293,17 +314,22 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] *= b[e];
     }
+    if constexpr (kKind == FK_BWD) {
+      const float4 p = __ldg(reinterpret_cast<const float4*>(args.P + at)), r = __ldg(reinterpret_cast<const float4*>(args.Q + at));
+      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(args.C2) + at) = make_uint2(bf16x2(a[0] * r.x, a[1] * r.y), bf16x2(a[2] * r.z, a[3] * r.w));
+      a[0] *= p.x; a[1] *= p.y; a[2] *= p.z; a[3] *= p.w;
+    }
     *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(args.C) + at) = make_uint2(bf16x2(a[0], a[1]), bf16x2(a[2], a[3]));
   }
   if (S > 1) cluster_sync_all();                           // no CTA leaves while another reads its shared memory
 }
 
-template <int kFmt, bool kGated, int kN>
+template <int kFmt, int kKind, int kN>
 void few_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int64_t N, int S, int per_sm, cudaStream_t s) {
   cfg = {};
   cfg.gridDim = dim3((unsigned)((N + 127) / 128 * S));
   cfg.blockDim = dim3(kFewThreads);
-  cfg.dynamicSmemBytes = FewCfg<kFmt, kGated, kN>::smem(per_sm);
+  cfg.dynamicSmemBytes = FewCfg<kFmt, kKind, kN>::smem(per_sm);
   cfg.stream = s;
   attr[0] = {};
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -320,9 +346,9 @@ void few_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int64_t
 // SMs, whose size is no multiple of most numbers); with two it is taken for twice as many. Asked once; every thread that asks
 // gets the same answer.
 struct FewRoom { int clusters[8]; int set; };
-template <int kFmt, bool kGated, int kN>
+template <int kFmt, int kKind, int kN>
 int few_room(const FewRoom** room) {
-  using Cfg = FewCfg<kFmt, kGated, kN>;
+  using Cfg = FewCfg<kFmt, kKind, kN>;
   static FewRoom rooms[64];
   static FewRoom other;
   int dev = 0;
@@ -330,13 +356,13 @@ int few_room(const FewRoom** room) {
   FewRoom& r = dev >= 0 && dev < 64 ? rooms[dev] : other;
   *room = &r;
   if (r.set && &r != &other) return SF_OK;
-  auto kern = few_tokens_kernel<kFmt, kGated, kN>;
+  auto kern = few_tokens_kernel<kFmt, kKind, kN>;
   SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::smem(1)));
   SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
   for (int S = 1; S <= 8; ++S) {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[2];
-    few_config<kFmt, kGated, kN>(cfg, attr, 128 * 1024, S, 1, nullptr);
+    few_config<kFmt, kKind, kN>(cfg, attr, 128 * 1024, S, 1, nullptr);
     cfg.numAttrs = 1;
     int n = 0;
     SF_CUDA_TRY(cudaOccupancyMaxActiveClusters(&n, kern, &cfg));
@@ -346,13 +372,13 @@ int few_room(const FewRoom** room) {
   return SF_OK;
 }
 
-template <int kFmt, bool kGated, int kN>
+template <int kFmt, int kKind, int kN>
 int launch_few(const FewMaps& maps, FewArgs a, int S, int per_sm, cudaStream_t s) {
-  a.stages = FewCfg<kFmt, kGated, kN>::stages(per_sm);
+  a.stages = FewCfg<kFmt, kKind, kN>::stages(per_sm);
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attr[2];
-  few_config<kFmt, kGated, kN>(cfg, attr, a.N, S, per_sm, s);
-  SF_CUDA_TRY(cudaLaunchKernelEx(&cfg, few_tokens_kernel<kFmt, kGated, kN>, maps, a));
+  few_config<kFmt, kKind, kN>(cfg, attr, a.N, S, per_sm, s);
+  SF_CUDA_TRY(cudaLaunchKernelEx(&cfg, few_tokens_kernel<kFmt, kKind, kN>, maps, a));
   return SF_OK;
 }
 

@@ -148,29 +148,59 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
   PairArgs a{};
   a.status = (int*)workspace;
   a.jobs = 1;
+  const bool few = T <= kFewTokens;
+  FewArgs f{};
+  f.T = (int)T; f.status = (int*)workspace;
   if (dX || dWg || dWu) {
-    a.M[0] = (int)T; a.N[0] = (int)F; a.nkb = a.nkb0 = k_blocks(FMT_BF16, D);
-    SF_TRY(launch_best<PK_BWD>(a, s, [&](CUtensorMap* m, int) {
-      SF_TRY(kmajor_map(&m[0], FMT_BF16, dY, T, D, 128));
-      SF_TRY(mn_map(&m[1], Wd, D, F));
-      SF_TRY(make_tmap_f32(&m[2], h + z.h, T, F));
-      SF_TRY(make_tmap_f32(&m[3], h + z.h + z.f, T, F));
-      SF_TRY(make_tmap_store(&m[4], dg, T, F));
-      return make_tmap_store(&m[5], du, T, F);
-    }));
+    const int nkb = k_blocks(FMT_BF16, D);
+    const float *p = (const float*)(h + z.h), *q = (const float*)(h + z.h + z.f);
+    if (few) {
+      f.N = (int)F; f.nkb = f.nkb0 = nkb; f.C = du; f.C2 = dg; f.P = const_cast<float*>(p); f.Q = const_cast<float*>(q);
+      SF_TRY((run_few<FMT_BF16, FK_BWD>(f, s, [&](FewMaps& m, int n) {
+        SF_TRY(kmajor_map(&m.x, FMT_BF16, dY, T, D, n));
+        SF_TRY(mn_map(&m.w0, Wd, D, F));
+        m.w1 = m.w0;
+        m.sx = m.s0 = m.s1 = m.x;
+        return (int)SF_OK;
+      })));
+    } else {
+      a.M[0] = (int)T; a.N[0] = (int)F; a.nkb = a.nkb0 = nkb;
+      SF_TRY(launch_best<PK_BWD>(a, s, [&](CUtensorMap* m, int) {
+        SF_TRY(kmajor_map(&m[0], FMT_BF16, dY, T, D, 128));
+        SF_TRY(mn_map(&m[1], Wd, D, F));
+        SF_TRY(make_tmap_f32(&m[2], p, T, F));
+        SF_TRY(make_tmap_f32(&m[3], q, T, F));
+        SF_TRY(make_tmap_store(&m[4], dg, T, F));
+        return make_tmap_store(&m[5], du, T, F);
+      }));
+    }
   }
   PairPlan dx_plan;
   if (dX) {
-    a.early_next = dWg || dWu || dWd;                      // they run beside it
-    a.M[0] = (int)T; a.N[0] = (int)D; a.nkb0 = k_blocks(FMT_BF16, F); a.nkb = 2 * a.nkb0;
-    SF_TRY(launch_best<PK_DX>(a, s, [&](CUtensorMap* m, int) {
-      SF_TRY(kmajor_map(&m[0], FMT_BF16, dg, T, F, 128));
-      SF_TRY(kmajor_map(&m[1], FMT_BF16, du, T, F, 128));
-      SF_TRY(mn_map(&m[2], Wg, F, D));
-      SF_TRY(mn_map(&m[3], Wu, F, D));
-      return make_tmap_store(&m[4], dX, T, D);
-    }, &dx_plan));
-    a.early_next = 0;
+    const int nkb = k_blocks(FMT_BF16, F);
+    const int beside = dWg || dWu || dWd;                  // they run beside it
+    if (few) {
+      f.N = (int)D; f.nkb0 = nkb; f.nkb = 2 * nkb; f.C = dX; f.early_weights = 1; f.early_next = beside;
+      SF_TRY((run_few<FMT_BF16, FK_DX>(f, s, [&](FewMaps& m, int n) {
+        SF_TRY(kmajor_map(&m.x, FMT_BF16, dg, T, F, n));
+        SF_TRY(kmajor_map(&m.sx, FMT_BF16, du, T, F, n));
+        SF_TRY(mn_map(&m.w0, Wg, F, D));
+        SF_TRY(mn_map(&m.w1, Wu, F, D));
+        m.s0 = m.s1 = m.x;
+        return (int)SF_OK;
+      }, &dx_plan)));
+    } else {
+      a.early_next = beside;
+      a.M[0] = (int)T; a.N[0] = (int)D; a.nkb0 = nkb; a.nkb = 2 * nkb;
+      SF_TRY(launch_best<PK_DX>(a, s, [&](CUtensorMap* m, int) {
+        SF_TRY(kmajor_map(&m[0], FMT_BF16, dg, T, F, 128));
+        SF_TRY(kmajor_map(&m[1], FMT_BF16, du, T, F, 128));
+        SF_TRY(mn_map(&m[2], Wg, F, D));
+        SF_TRY(mn_map(&m[3], Wu, F, D));
+        return make_tmap_store(&m[4], dX, T, D);
+      }, &dx_plan));
+      a.early_next = 0;
+    }
   }
   GradJob jobs[3];
   a.jobs = 0;

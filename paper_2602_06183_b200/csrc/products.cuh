@@ -80,11 +80,11 @@ inline PairPlan pair_plan(int kind, const PairJob* jobs, int njobs, int64_t nkb,
 // 4096 x 16384 down projection took 3 us more on 128 of them than on all), at what one SM takes in, or at what its ring holds in
 // flight; what a round costs beside; and the sums, which grow with the CTAs that a value comes from (128 tokens, 2048 x 8192 of 4
 // bits: 8.2 us over 4, 9.9 over 8).
-struct FewPlan { int S, per_sm; };
+struct FewPlan { int S, per_sm; double us; };
 template <typename Cfg>
 FewPlan few_plan(int64_t N, int nkb, const FewRoom& room) {
   const int64_t units = ceil_div(N, 128);
-  FewPlan best{1, 1};
+  FewPlan best{1, 1, 0};
   double least = 0;
   for (int per_sm = 1; per_sm <= Cfg::kMostPerSm; ++per_sm)
     for (int S = 1; S <= 8 && S <= nkb; ++S) {
@@ -98,37 +98,47 @@ FewPlan few_plan(int64_t N, int nkb, const FewRoom& room) {
       us = us > sm ? us : sm;
       us = us > flight ? us : flight;
       us = rounds * (us * (double)ceil_div(nkb, S) + (per_sm == 2 ? 1.0 : 1.5)) + (S > 1 ? 0.3 + 0.05 * S * Cfg::kPartBytes / 8192 : 0.0);
-      if (least == 0 || us < 0.98 * least) { best = FewPlan{S, per_sm}; least = us; }
+      if (least == 0 || us < 0.98 * least) { best = FewPlan{S, per_sm, us}; least = us; }
     }
   return best;
 }
 
-template <int kFmt, bool kGated, int kN>
-int run_few_n(const Operand& X, const Operand& W0, const Operand& W1, int64_t N, int64_t K, FewArgs a, cudaStream_t s) {
-  using Cfg = FewCfg<kFmt, kGated, kN>;
+// Of a few-token product: its operands by their maps (see FewMaps; the tokens' box is kN rows), then the launch.
+template <int kFmt, int kKind, int kN, typename F>
+int run_few_n(const FewArgs& a, cudaStream_t s, F& make, PairPlan* taken) {
+  using Cfg = FewCfg<kFmt, kKind, kN>;
   FewMaps m;
-  SF_TRY(kmajor_map(&m.x, kFmt, X.data, a.T, K, kN));
-  SF_TRY(kmajor_map(&m.w0, kFmt, W0.data, N, K, 128));
-  m.w1 = m.w0;
-  if (kGated) SF_TRY(kmajor_map(&m.w1, kFmt, W1.data, N, K, 128));
-  m.sx = m.s0 = m.s1 = m.x;
-  if (Cfg::kFp4) {
-    SF_TRY(scale_map(&m.sx, kFmt, X.scales, a.T, K));
-    SF_TRY(scale_map(&m.s0, kFmt, W0.scales, N, K));
-    if (kGated) SF_TRY(scale_map(&m.s1, kFmt, W1.scales, N, K));
-  }
+  SF_TRY(make(m, kN));
   const FewRoom* room;
-  SF_TRY((few_room<kFmt, kGated, kN>(&room)));
-  const FewPlan plan = few_plan<Cfg>(N, a.nkb, *room);
-  return launch_few<kFmt, kGated, kN>(m, a, plan.S, plan.per_sm, s);
+  SF_TRY((few_room<kFmt, kKind, kN>(&room)));
+  const FewPlan plan = few_plan<Cfg>(a.N, a.nkb, *room);
+  if (taken) *taken = PairPlan{PM_SPLIT, 0, plan.S, ceil_div(ceil_div(a.N, 128) * plan.S, 2 * plan.per_sm), plan.us * 1900, 0};
+  return launch_few<kFmt, kKind, kN>(m, a, plan.S, plan.per_sm, s);
 }
-template <int kFmt, bool kGated>
-int run_few(const Operand& X, const Operand& W0, const Operand& W1, int64_t N, int64_t K, const FewArgs& a, cudaStream_t s) {
-  if (a.T <= 16) return run_few_n<kFmt, kGated, 16>(X, W0, W1, N, K, a, s);
-  if (a.T <= 32) return run_few_n<kFmt, kGated, 32>(X, W0, W1, N, K, a, s);
-  if (a.T <= 64) return run_few_n<kFmt, kGated, 64>(X, W0, W1, N, K, a, s);
-  if (a.T <= 96) return run_few_n<kFmt, kGated, 96>(X, W0, W1, N, K, a, s);
-  return run_few_n<kFmt, kGated, 128>(X, W0, W1, N, K, a, s);
+template <int kFmt, int kKind, typename F>
+int run_few(const FewArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr) {
+  if (a.T <= 16) return run_few_n<kFmt, kKind, 16>(a, s, make, taken);
+  if (a.T <= 32) return run_few_n<kFmt, kKind, 32>(a, s, make, taken);
+  if (a.T <= 64) return run_few_n<kFmt, kKind, 64>(a, s, make, taken);
+  if (a.T <= 96) return run_few_n<kFmt, kKind, 96>(a, s, make, taken);
+  return run_few_n<kFmt, kKind, 128>(a, s, make, taken);
+}
+// X W^T with one matrix, or two of one shape.
+template <int kFmt, int kKind>
+int run_few_rows(const Operand& X, const Operand& W0, const Operand& W1, int64_t N, int64_t K, const FewArgs& a, cudaStream_t s) {
+  return run_few<kFmt, kKind>(a, s, [&](FewMaps& m, int n) {
+    SF_TRY(kmajor_map(&m.x, kFmt, X.data, a.T, K, n));
+    SF_TRY(kmajor_map(&m.w0, kFmt, W0.data, N, K, 128));
+    m.w1 = m.w0;
+    if (kKind == FK_GATED) SF_TRY(kmajor_map(&m.w1, kFmt, W1.data, N, K, 128));
+    m.sx = m.s0 = m.s1 = m.x;
+    if (kFmt != FMT_BF16) {
+      SF_TRY(scale_map(&m.sx, kFmt, X.scales, a.T, K));
+      SF_TRY(scale_map(&m.s0, kFmt, W0.scales, N, K));
+      if (kKind == FK_GATED) SF_TRY(scale_map(&m.s1, kFmt, W1.scales, N, K));
+    }
+    return (int)SF_OK;
+  });
 }
 
 // Launches the kernel of a plan: make(maps, bn) fills the tensor maps for tiles of that width.
@@ -146,7 +156,7 @@ int launch_plan(const PairPlan& plan, PairArgs a, cudaStream_t s, F&& make) {
 template <int kKind, typename F>
 int launch_best(const PairArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr, const PairPlan* beside = nullptr) {
   const FewRoom* room;
-  SF_TRY((few_room<FMT_BF16, false, 16>(&room)));          // (one CTA to an SM, like the pairs')
+  SF_TRY((few_room<FMT_BF16, FK_NT, 16>(&room)));          // (one CTA to an SM, like the pairs')
   PairJob jobs[3];
   for (int j = 0; j < a.jobs; ++j) jobs[j] = PairJob{a.M[j], a.N[j]};
   const PairPlan plan = pair_plan(kKind, jobs, a.jobs, a.nkb, *room);
@@ -187,7 +197,7 @@ int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, 
     FewArgs a{};
     a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.alpha = a.alpha2 = alpha; a.C = C; a.status = status;
     a.early_weights = early_weights;
-    return run_few<kFmt, false>(A, B, B, N, K, a, s);
+    return run_few_rows<kFmt, FK_NT>(A, B, B, N, K, a, s);
   }
   PairArgs a{};
   a.jobs = 1; a.M[0] = (int)M; a.N[0] = (int)N; a.nkb = a.nkb0 = nkb; a.alpha = alpha; a.status = status;
@@ -214,7 +224,7 @@ int run_gated(const Operand& A, const Operand& Bg, const Operand& Bu, int64_t M,
     FewArgs a{};
     a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.act = act; a.alpha = alpha_g; a.alpha2 = alpha_u; a.C = H; a.P = P; a.Q = Q;
     a.status = status;
-    return run_few<kFmt, true>(A, Bg, Bu, N, K, a, s);
+    return run_few_rows<kFmt, FK_GATED>(A, Bg, Bu, N, K, a, s);
   }
   PairArgs a{};
   a.jobs = 1; a.M[0] = (int)M; a.N[0] = (int)N; a.nkb = a.nkb0 = nkb; a.act = act; a.alpha = alpha_g; a.alpha2 = alpha_u;
