@@ -339,6 +339,22 @@ typedef struct sf_gated_ffn_desc {
   int32_t reserved;
 } sf_gated_ffn_desc;
 SF_API int sf_gated_ffn_workspace_size(const sf_gated_ffn_desc* desc, size_t* fwd_ctx_bytes, size_t* workspace_bytes);
+/* How the products of a descriptor run on the current device (a B200 is assumed where there is none): host arithmetic by the rules
+ * that the calls use, for tests and for accounts of a step's launches. Per product: its form, the columns of its tiles (SF_GATED_FEW:
+ * the tokens that the kernel is made for), and over how many CTAs (SF_GATED_FEW) or CTA pairs the reduction is split. */
+typedef enum sf_gated_product {
+  SF_GATED_H = 0,        /* H without a context */
+  SF_GATED_H_KEPT = 1,   /* H with one */
+  SF_GATED_Y = 2,
+  SF_GATED_DH = 3,       /* dH, as dG and dU */
+  SF_GATED_DX = 4,
+  SF_GATED_DW = 5        /* the three weight gradients */
+} sf_gated_product;
+typedef enum sf_gated_form { SF_GATED_NONE = 0, SF_GATED_FEW = 1, SF_GATED_TILES = 2, SF_GATED_SPLIT = 3 } sf_gated_form;
+typedef struct sf_gated_ffn_plan {
+  int32_t form[6], cols[6], parts[6];
+} sf_gated_ffn_plan;
+SF_API int sf_gated_ffn_step_plan(const sf_gated_ffn_desc* desc, sf_gated_ffn_plan* plan);
 SF_API int sf_gated_ffn_fwd(const sf_gated_ffn_desc* desc, const void* X, const void* Wg, const void* Wu, const void* Wd,
                             void* Y, void* fwd_ctx, size_t fwd_ctx_bytes, void* workspace, size_t workspace_bytes,
                             void* stream);

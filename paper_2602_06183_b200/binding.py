@@ -49,6 +49,12 @@ class sf_gated_ffn_desc(C.Structure):
     _fields_ = [("T", C.c_int64), ("D", C.c_int64), ("F", C.c_int64), ("act", C.c_int32), ("reserved", C.c_int32)]
 
 
+class sf_gated_ffn_plan(C.Structure):
+    _fields_ = [("form", C.c_int32 * 6), ("cols", C.c_int32 * 6), ("parts", C.c_int32 * 6)]
+
+
+SF_GATED_H, SF_GATED_H_KEPT, SF_GATED_Y, SF_GATED_DH, SF_GATED_DX, SF_GATED_DW = range(6)
+SF_GATED_NONE, SF_GATED_FEW, SF_GATED_TILES, SF_GATED_SPLIT = range(4)
 SF_ACT_SILU, SF_ACT_GELU, SF_ACT_GELU_TANH, SF_ACT_RELU, SF_ACT_SQRELU = range(5)
 SF_FP4_NV, SF_FP4_MX = range(2)
 
@@ -99,6 +105,7 @@ _SIGNATURES = {
     "sf_ffn_step_host": (_i32, [C.POINTER(sf_ffn_desc), _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp,
                                 _sz, _vp]),
     "sf_gated_ffn_workspace_size": (_i32, [C.POINTER(sf_gated_ffn_desc), C.POINTER(_sz), C.POINTER(_sz)]),
+    "sf_gated_ffn_step_plan": (_i32, [C.POINTER(sf_gated_ffn_desc), C.POINTER(sf_gated_ffn_plan)]),
     "sf_gated_ffn_fwd": (_i32, [C.POINTER(sf_gated_ffn_desc), _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _sz, _vp]),
     "sf_gated_ffn_bwd": (_i32, [C.POINTER(sf_gated_ffn_desc), _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp, _vp, _vp, _vp, _sz,
                                 _vp]),
@@ -566,6 +573,12 @@ def sf_gated_ffn_workspace_size(desc: sf_gated_ffn_desc):
     a, b = _sz(), _sz()
     _check(lib().sf_gated_ffn_workspace_size(C.byref(desc), C.byref(a), C.byref(b)), "sf_gated_ffn_workspace_size")
     return a.value, b.value
+
+
+def sf_gated_ffn_step_plan(desc: sf_gated_ffn_desc) -> sf_gated_ffn_plan:
+    plan = sf_gated_ffn_plan()
+    _check(lib().sf_gated_ffn_step_plan(C.byref(desc), C.byref(plan)), "sf_gated_ffn_step_plan")
+    return plan
 
 
 def alloc_gated_ffn_buffers(desc: sf_gated_ffn_desc, device="cuda", training: bool = True):

@@ -7,6 +7,8 @@
 // Roundings: G, U and dH stay in float32. H, dG and dU are rounded to bf16 once, because they are operands of the next product; P and
 // Q are kept in float32 (8 bytes a hidden value where bf16 would take 4), because dG and dU would otherwise be rounded two or three times: the
 // error of dWu against 64 bits is then 1.8 times that of a result that is rounded once at its end, with them it is 1.4 times.
+#include <initializer_list>
+
 #include "products.cuh"
 
 namespace sf {
@@ -100,6 +102,49 @@ int sf_gated_ffn_workspace_size(const sf_gated_ffn_desc* desc, size_t* fwd_ctx_b
   *fwd_ctx_bytes = z.h + 2 * z.f;
   *workspace_bytes = kStatus + 2 * z.h;
   return SF_OK;
+}
+
+int sf_gated_ffn_step_plan(const sf_gated_ffn_desc* desc, sf_gated_ffn_plan* plan) {
+  GatedSizes z;
+  SF_TRY(gated_sizes(desc, &z));
+  if (!plan) return SF_ERR_NULL;
+  *plan = sf_gated_ffn_plan{};
+  if (desc->T == 0) return SF_OK;
+  const int T = (int)desc->T, D = (int)desc->D, F = (int)desc->F;
+  const int kd = k_blocks(FMT_BF16, D), kf = k_blocks(FMT_BF16, F), kt = (int)ceil_div(T, 64);
+  auto few = [&](auto kind, int i, int N, int nkb) {
+    FewArgs a{};
+    a.T = T; a.N = N; a.nkb = nkb;
+    PairPlan p;
+    NoMaps none;
+    SF_TRY((run_few<FMT_BF16, decltype(kind)::value>(a, nullptr, none, &p)));
+    plan->form[i] = SF_GATED_FEW; plan->cols[i] = p.bn; plan->parts[i] = p.parts;
+    return (int)SF_OK;
+  };
+  auto pairs = [&](int kind, int i, std::initializer_list<PairJob> jobs, int nkb) {
+    PairArgs a{};
+    for (const PairJob& j : jobs) { a.M[a.jobs] = (int)j.M; a.N[a.jobs++] = (int)j.N; }
+    a.nkb = nkb;
+    PairPlan p;
+    SF_TRY(plan_pairs(kind, a, &p));
+    plan->form[i] = p.mode == PM_SPLIT ? SF_GATED_SPLIT : SF_GATED_TILES; plan->cols[i] = p.bn; plan->parts[i] = p.parts;
+    return (int)SF_OK;
+  };
+  if (T <= kFewTokens) {
+    SF_TRY(few(ActTag<FK_GATED>{}, SF_GATED_H, F, kd));
+    SF_TRY(few(ActTag<FK_NT>{}, SF_GATED_Y, D, kf));
+    SF_TRY(few(ActTag<FK_BWD>{}, SF_GATED_DH, F, kd));
+    SF_TRY(few(ActTag<FK_DX>{}, SF_GATED_DX, D, 2 * kf));
+    plan->form[SF_GATED_H_KEPT] = plan->form[SF_GATED_H]; plan->cols[SF_GATED_H_KEPT] = plan->cols[SF_GATED_H];
+    plan->parts[SF_GATED_H_KEPT] = plan->parts[SF_GATED_H];
+  } else {
+    SF_TRY(pairs(PK_FWD, SF_GATED_H, {{T, F}}, kd));
+    SF_TRY(pairs(PK_FWD_SAVE, SF_GATED_H_KEPT, {{T, F}}, kd));
+    SF_TRY(pairs(PK_NT, SF_GATED_Y, {{T, D}}, kf));
+    SF_TRY(pairs(PK_BWD, SF_GATED_DH, {{T, F}}, kd));
+    SF_TRY(pairs(PK_DX, SF_GATED_DX, {{T, D}}, 2 * kf));
+  }
+  return pairs(PK_DW, SF_GATED_DW, {{D, F}, {F, D}, {F, D}}, kt);
 }
 
 int sf_gated_ffn_fwd(const sf_gated_ffn_desc* desc, const void* X, const void* Wg, const void* Wu, const void* Wd, void* Y,

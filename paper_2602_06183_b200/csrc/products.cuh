@@ -2,6 +2,7 @@
 #pragma once
 
 #include <cmath>
+#include <type_traits>
 
 #include "few_tokens.cuh"
 #include "pair_product.cuh"
@@ -103,17 +104,21 @@ FewPlan few_plan(int64_t N, int nkb, const FewRoom& room) {
   return best;
 }
 
-// Of a few-token product: its operands by their maps (see FewMaps; the tokens' box is kN rows), then the launch.
+// Of a few-token product: its operands by their maps (see FewMaps; the tokens' box is kN rows), then the launch; without `make` the plan only.
+struct NoMaps {};
 template <int kFmt, int kKind, int kN, typename F>
 int run_few_n(const FewArgs& a, cudaStream_t s, F& make, PairPlan* taken) {
   using Cfg = FewCfg<kFmt, kKind, kN>;
-  FewMaps m;
-  SF_TRY(make(m, kN));
   const FewRoom* room;
   SF_TRY((few_room<kFmt, kKind, kN>(&room)));
   const FewPlan plan = few_plan<Cfg>(a.N, a.nkb, *room);
-  if (taken) *taken = PairPlan{PM_SPLIT, 0, plan.S, ceil_div(ceil_div(a.N, 128) * plan.S, 2 * plan.per_sm), plan.us * 1900, 0};
-  return launch_few<kFmt, kKind, kN>(m, a, plan.S, plan.per_sm, s);
+  if (taken) *taken = PairPlan{PM_SPLIT, kN, plan.S, ceil_div(ceil_div(a.N, 128) * plan.S, 2 * plan.per_sm), plan.us * 1900, 0};
+  if constexpr (!std::is_same_v<F, NoMaps>) {
+    FewMaps m;
+    SF_TRY(make(m, kN));
+    return launch_few<kFmt, kKind, kN>(m, a, plan.S, plan.per_sm, s);
+  }
+  return SF_OK;
 }
 template <int kFmt, int kKind, typename F>
 int run_few(const FewArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr) {
@@ -153,13 +158,18 @@ int launch_plan(const PairPlan& plan, PairArgs a, cudaStream_t s, F&& make) {
                                  : launch_pair<kKind, 256, FMT_BF16, PM_SPLIT>(maps, a, s);
 }
 // The same from the sizes.
-template <int kKind, typename F>
-int launch_best(const PairArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr, const PairPlan* beside = nullptr) {
+inline int plan_pairs(int kind, const PairArgs& a, PairPlan* plan) {
   const FewRoom* room;
   SF_TRY((few_room<FMT_BF16, FK_NT, 16>(&room)));          // (one CTA to an SM, like the pairs')
   PairJob jobs[3];
   for (int j = 0; j < a.jobs; ++j) jobs[j] = PairJob{a.M[j], a.N[j]};
-  const PairPlan plan = pair_plan(kKind, jobs, a.jobs, a.nkb, *room);
+  *plan = pair_plan(kind, jobs, a.jobs, a.nkb, *room);
+  return SF_OK;
+}
+template <int kKind, typename F>
+int launch_best(const PairArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr, const PairPlan* beside = nullptr) {
+  PairPlan plan;
+  SF_TRY(plan_pairs(kKind, a, &plan));
   if (taken) *taken = plan;
   if (!beside) return launch_plan<kKind>(plan, a, s, make);
   PairArgs b = a;

@@ -68,7 +68,14 @@ SHAPES = [(1, 8, 8), (1, 264, 520), (2, 72, 136), (7, 1000, 328), (16, 64, 128),
           (65, 136, 392), (128, 200, 776), (129, 8, 16), (129, 264, 520), (200, 584, 72), (256, 256, 512), (257, 392, 1160), (513, 136, 264)]
 
 
-@pytest.mark.parametrize("T,D,F", SHAPES)
+# every product of the step in every form that it has beyond the few tokens above (see test_gated_plan.py): persistent tiles of full and
+# of narrower width, and reductions split over two to four pairs
+FORM_SHAPES = [(130, 1408, 8), (130, 8, 1032), (257, 392, 1160), (513, 256, 2048), (513, 520, 2048), (513, 776, 1160), (513, 2048, 520),
+               (513, 1024, 1032), (513, 1408, 1032), (1000, 8, 8), (1500, 1032, 8), (1000, 4096, 520), (3000, 256, 2048),
+               (3000, 1024, 1160), (4096, 776, 264)]
+
+
+@pytest.mark.parametrize("T,D,F", SHAPES + FORM_SHAPES)
 def test_step_is_exact_on_small_integers(T, D, F):
     r = np.random.default_rng(T * 7 + D + F)
     X, Wg, Wu, Wd, dY = _ints((T, D), r), _ints((F, D), r, -1, 1), _ints((F, D), r, -1, 1), _ints((D, F), r, -1, 1, 0.1), _ints((T, D), r, -1, 1)
