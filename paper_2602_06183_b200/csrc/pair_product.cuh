@@ -583,8 +583,8 @@ int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps>& maps, P
     tiles += (int64_t)a.num_m[j] * a.num_n[j];
   }
   if (tiles > 0x3FFFFFFF / (2 * parts)) return SF_ERR_SHAPE;
-  const int64_t pairs = kMode == PM_SPLIT ? tiles * parts : tiles < sm_count_now() / 2 ? tiles : sm_count_now() / 2;
-  a.early_next |= kMode != PM_SPLIT && tiles > sm_count_now() / 2 && (tiles * 2 / sm_count_now() + 1) * a.nkb >= 128;
+  const int64_t most = sm_count_now() / 2, pairs = kMode == PM_SPLIT ? tiles * parts : tiles < most ? tiles : most;
+  a.early_next |= kMode != PM_SPLIT && tiles > most && (tiles / most + 1) * a.nkb >= 128;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * pairs));
   cfg.blockDim = dim3(kPairThreads);

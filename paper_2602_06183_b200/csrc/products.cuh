@@ -53,6 +53,7 @@ inline PairPlan pair_plan(int kind, const PairJob* jobs, int njobs, int64_t nkb,
   const double chunk = kind == PK_FWD ? 1200 : kind == PK_FWD_SAVE ? 2400 : kind == PK_BWD ? 2200 : 1000;   // 32 output columns of a warp
   PairPlan best{PM_FULL, 256, 1, 0, 0, 0};
   double least = 0;
+  const int64_t pairs = sm_count_now() / 2;
   for (int bn = 256; bn >= 64; bn -= gated ? 64 : 32) {
     const int cols = gated ? bn / 2 : bn;
     int64_t tiles = 0;
@@ -60,7 +61,7 @@ inline PairPlan pair_plan(int kind, const PairJob* jobs, int njobs, int64_t nkb,
     const double smem = bmn ? 256 + 64 * ceil_div(bn, 128) + bn / 2 : 256 + bn, stage = smem > 2 * bn ? smem : 2 * bn;
     const double epilogue = chunk * (double)ceil_div(cols, 64);
     for (int S = 1; S <= 4 && S <= nkb; ++S) {
-      const int64_t at_once = S == 1 ? sm_count_now() / 2 : room.clusters[2 * S - 1];
+      const int64_t at_once = S == 1 ? pairs : room.clusters[2 * S - 1];
       if (at_once <= 0) continue;
       const double rounds = (double)ceil_div(tiles, at_once), loop = (double)ceil_div(nkb, S) * stage;
       double c;
@@ -87,13 +88,14 @@ FewPlan few_plan(int64_t N, int nkb, const FewRoom& room) {
   const int64_t units = ceil_div(N, 128);
   FewPlan best{1, 1, 0};
   double least = 0;
+  const double sms = sm_count_now();
   for (int per_sm = 1; per_sm <= Cfg::kMostPerSm; ++per_sm)
     for (int S = 1; S <= 8 && S <= nkb; ++S) {
       const int64_t slots = (int64_t)room.clusters[S - 1] * per_sm;
       if (slots <= 0) continue;
       const double at_once = (double)((units < slots ? units : slots) * S), rounds = (double)ceil_div(units, slots);
       const int ring = Cfg::stages(per_sm) < nkb / S + 1 ? Cfg::stages(per_sm) : nkb / S + 1;
-      const double part = at_once / sm_count_now();
+      const double part = at_once / sms;
       double us = Cfg::kStageBytes * at_once / (6.5e6 * (part < 1 ? std::sqrt(part) : 1.0));
       const double sm = Cfg::kStageBytes * (part <= 1 ? 1 : per_sm) / 0.075e6, flight = 1.8 / ring;
       us = us > sm ? us : sm;
