@@ -531,6 +531,8 @@ SF_API int sf_selftest_wait_expiry(void* workspace, int64_t budget_clocks, void*
  *   dense fwd: 3 events, dense bwd: 5 events.
  *   routed fwd: 6 events (prune W1 | route | group + tile tables + gather X | y1 product | y3 product)
  *   routed bwd: 7 events (prune W2 | gather dY | dy1 product | dX product | dW2 product | dW1 product).
+ *   gated fwd: 3 events (H product | Y product); gated bwd: 4 events (dH product | dX product | the weights' gradients),
+ *              the intervals of what is left out empty. While tracing is on, the weights' gradients do not run beside dX.
  * sf_trace_count returns how many events have been recorded since sf_trace_set. Not thread-safe. */
 SF_API int sf_trace_set(void** events, int capacity);
 SF_API int sf_trace_count(void);

@@ -219,6 +219,7 @@ int weight_grads(const sf_ffn_desc& d, const void* dY, const void* h, const void
 
 }  // namespace
 
+bool trace_on() { return g_trace_events && g_trace_n < g_trace_cap; }
 void trace_mark(cudaStream_t s) {
   if (g_trace_events && g_trace_n < g_trace_cap) cudaEventRecord(g_trace_events[g_trace_n++], s);
 }

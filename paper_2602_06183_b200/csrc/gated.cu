@@ -163,8 +163,12 @@ int sf_gated_ffn_fwd(const sf_gated_ffn_desc* desc, const void* X, const void* W
   float* p = fwd_ctx ? (float*)(h + z.h) : nullptr;
   float* q = fwd_ctx ? (float*)(h + z.h + z.f) : nullptr;
   int* status = (int*)workspace;
+  trace_mark(s);
   SF_TRY(run_gated<FMT_BF16>({X, nullptr}, {Wg, nullptr}, {Wu, nullptr}, desc->T, desc->F, desc->D, desc->act, 1.f, 1.f, h, p, q, status, s));
-  return run_nt<FMT_BF16>({h, nullptr}, {Wd, nullptr}, desc->T, desc->D, desc->F, 1.f, Y, status, s, true);
+  trace_mark(s);
+  SF_TRY(run_nt<FMT_BF16>({h, nullptr}, {Wd, nullptr}, desc->T, desc->D, desc->F, 1.f, Y, status, s, true));
+  trace_mark(s);
+  return SF_OK;
 }
 
 int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* X, const void* Wg, const void* Wu, const void* Wd,
@@ -196,6 +200,7 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
   const bool few = T <= kFewTokens;
   FewArgs f{};
   f.T = (int)T; f.status = (int*)workspace;
+  trace_mark(s);
   if (dX || dWg || dWu) {
     const int nkb = k_blocks(FMT_BF16, D);
     const float *p = (const float*)(h + z.h), *q = (const float*)(h + z.h + z.f);
@@ -220,10 +225,11 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
       }));
     }
   }
+  trace_mark(s);
+  const bool beside = dX && (dWg || dWu || dWd) && !trace_on();      // the weights' gradients run beside dX
   PairPlan dx_plan;
   if (dX) {
     const int nkb = k_blocks(FMT_BF16, F);
-    const int beside = dWg || dWu || dWd;                  // they run beside it
     if (few) {
       f.N = (int)D; f.nkb0 = nkb; f.nkb = 2 * nkb; f.C = dX; f.early_weights = 1; f.early_next = beside;
       SF_TRY((run_few<FMT_BF16, FK_DX>(f, s, [&](FewMaps& m, int n) {
@@ -247,15 +253,19 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
       a.early_next = 0;
     }
   }
+  trace_mark(s);
   GradJob jobs[3];
   a.jobs = 0;
   if (dWd) jobs[a.jobs++] = {dY, h, D, F, dWd};
   if (dWg) jobs[a.jobs++] = {dg, X, F, D, dWg};
   if (dWu) jobs[a.jobs++] = {du, X, F, D, dWu};
-  if (a.jobs == 0) return SF_OK;
+  if (a.jobs == 0) {
+    trace_mark(s);
+    return SF_OK;
+  }
   for (int j = 0; j < a.jobs; ++j) { a.M[j] = (int)jobs[j].M; a.N[j] = (int)jobs[j].N; }
   a.nkb = a.nkb0 = (int)ceil_div(T, 64);
-  return launch_best<PK_DW>(a, s, [&](CUtensorMap* m, int) {
+  SF_TRY(launch_best<PK_DW>(a, s, [&](CUtensorMap* m, int) {
     for (int j = 0; j < a.jobs; ++j) {
       SF_TRY(mn_map(&m[j], jobs[j].A, T, jobs[j].M));
       SF_TRY(mn_map(&m[3 + j], jobs[j].B, T, jobs[j].N));
@@ -264,7 +274,9 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
     for (int j = a.jobs; j < 3; ++j)
       for (int i = 0; i < 9; i += 3) m[i + j] = m[i];
     return (int)SF_OK;
-  }, nullptr, dX ? &dx_plan : nullptr);
+  }, nullptr, beside ? &dx_plan : nullptr));
+  trace_mark(s);
+  return SF_OK;
 }
 
 }  // extern "C"

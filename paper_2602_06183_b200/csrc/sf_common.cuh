@@ -217,6 +217,7 @@ int launch_transpose(const void* in, void* out, int64_t rows, int64_t cols, cuda
 int noalloc_status_word(void** out);
 // Records the next caller-owned trace event on `s` while stage tracing is on (sf_trace_set); else a no-op.
 void trace_mark(cudaStream_t s);
+bool trace_on();
 
 // Byte offset of the metadata word (row m, 16-column word kw) inside the hardware-ordered
 // metadata tensor of a [R, K] 2:4 operand: 2 KB atoms of 128 rows x 128 columns, atoms of one

@@ -232,3 +232,20 @@ def test_trained_block_served_on_four_bits(T):
     assert np.all(np.abs(f32(Y4).astype(np.float64) - ref) <= tol + gated.U16 * (np.abs(ref) + tol))
 
 
+
+
+def test_offsets_beyond_32_bits():
+    """A matrix of 4.4e9 elements: its last rows come out as a matrix of their own."""
+    rows, cols, tail = 66_000, 66_560, 130
+    X = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    X[-tail:] = torch.randn((tail, cols), device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    last = rows - tail - (rows - tail) % 128                                # from the start of a tile of rows
+    for fmt in (binding.SF_FP4_NV, binding.SF_FP4_MX):
+        codes, scales = binding.sf_fp4_quantize(X, fmt, 2.0)
+        c, s = binding.sf_fp4_quantize(X[last:], fmt, 2.0)
+        assert torch.equal(codes[last:], c) and not bool(codes[:last].any())
+        whole = s.numel() // 512 - (cols // (64 if fmt == binding.SF_FP4_NV else 128))         # tiles of whole row blocks of the tail
+        assert torch.equal(scales[-s.numel():][:whole * 512], s[:whole * 512])
+        back = binding.sf_fp4_dequantize(codes, scales, fmt, 0.5)
+        assert torch.equal(back[last:], binding.sf_fp4_dequantize(c, s, fmt, 0.5)) and not bool(back[:last].any())
+        del codes, scales, back

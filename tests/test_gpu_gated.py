@@ -235,3 +235,46 @@ def test_repeated_calls_give_the_same_bits():
         b.check()
         for g in got[1:]:
             assert all(np.array_equal(x, y) for x, y in zip(g, got[0]))
+
+
+@pytest.mark.parametrize("T", [20, 300])
+def test_stage_trace(T):
+    D, F = 136, 264
+    b = Block(T, D, F, "silu", *_normals(T, D, F, 21))
+    b.fwd()
+    b.bwd()
+    want = [bits(b.Y.t)] + [bits(b.out[k].t) for k in GRADS]
+    with binding.StageTrace(16) as tr:
+        b.fwd()
+        b.bwd()
+    assert tr.count == 7 and all(ms >= 0 for ms in tr.durations_ms())
+    b.check()
+    assert all(np.array_equal(x, y) for x, y in zip([bits(b.Y.t)] + [bits(b.out[k].t) for k in GRADS], want))
+    with binding.StageTrace(16) as tr:
+        b.bwd(("dWg",))
+    assert tr.count == 4
+
+
+def test_offsets_beyond_32_bits():
+    """[T, F] of 2.3e9 elements: the last tokens' results are those of a batch of their own (small integers, exact in any order)."""
+    T, D, F, tail = 140_000, 64, 16384, 200
+    r = np.random.default_rng(4)
+    W = [_dev(_ints(s, r, -1, 1)) for s in ((F, D), (F, D))] + [_dev(_ints((D, F), r, -1, 1, 0.05))]
+    x, dy = _dev(_ints((tail, D), r)), _dev(_ints((tail, D), r, -1, 1))
+
+    def step(X, dY):
+        d = binding.make_gated_desc(len(X), D, F, binding.SF_ACT_RELU)
+        ctx, ws = binding.alloc_gated_ffn_buffers(d)
+        Y, dX = torch.empty_like(X), torch.empty_like(X)
+        g = [torch.empty_like(w) for w in W]
+        binding.sf_gated_ffn_fwd(d, X, *W, Y, ctx, ws)
+        binding.sf_gated_ffn_bwd(d, dY, X, *W, ctx, dX, *g, ws)
+        assert binding.sf_check_status(ws) == binding.SF_OK
+        return Y, dX, g
+    small = step(x, dy)
+    X, dY = torch.zeros((T, D), dtype=torch.bfloat16, device="cuda"), torch.zeros((T, D), dtype=torch.bfloat16, device="cuda")
+    X[-tail:], dY[-tail:] = x, dy
+    Y, dX, g = step(X, dY)
+    assert torch.equal(Y[-tail:], small[0]) and torch.equal(dX[-tail:], small[1])
+    assert not bool(Y[:-tail].any()) and not bool(dX[:-tail].any())
+    assert all(torch.equal(a, b) for a, b in zip(g, small[2]))          # every other token is zero
