@@ -100,7 +100,7 @@ FewPlan few_plan(int64_t N, int nkb, const FewRoom& room) {
       const double sm = Cfg::kStageBytes * (part <= 1 ? 1 : per_sm) / 0.075e6, flight = 1.8 / ring;
       us = us > sm ? us : sm;
       us = us > flight ? us : flight;
-      us = rounds * (us * (double)ceil_div(nkb, S) + (per_sm == 2 ? 1.0 : 1.5)) + (S > 1 ? 0.3 + 0.05 * S * Cfg::kPartBytes / 8192 : 0.0);
+      us = rounds * (us * (double)ceil_div(nkb, S) + (per_sm == 2 ? 1.0 : 1.5)) + (S > 1 ? 0.6 + 0.05 * S * Cfg::kPartBytes / 8192 : 0.0);
       if (least == 0 || us < 0.98 * least) { best = FewPlan{S, per_sm, us}; least = us; }
     }
   return best;
