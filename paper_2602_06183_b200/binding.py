@@ -556,7 +556,9 @@ def _buffer(where: str, name: str, t, dev: int):
     """(address, bytes) of a context or workspace; (None, 0) of None."""
     if t is None:
         return None, 0
-    return _tensor(where, name, t, t.dtype, t.shape, dev), t.numel() * t.element_size()
+    if t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr(), t.nbytes
+    raise _refused(where, name, t, t.dtype, tuple(t.shape))
 
 
 def _launch_stream(where: str, dev: int, stream):
@@ -589,7 +591,7 @@ def alloc_gated_ffn_buffers(desc: sf_gated_ffn_desc, device="cuda", training: bo
 
 def sf_gated_ffn_fwd(desc, X, Wg, Wu, Wd, Y, fwd_ctx, workspace, stream=None):
     """Y = (act(X Wg^T) * (X Wu^T)) Wd^T. fwd_ctx None: nothing is kept for a backward pass."""
-    w, bf, dev = "sf_gated_ffn_fwd", torch.bfloat16, X.get_device()
+    w, bf, dev = "sf_gated_ffn_fwd", _BF16, X.get_device()
     td, fd, df = (desc.T, desc.D), (desc.F, desc.D), (desc.D, desc.F)
     _check(lib().sf_gated_ffn_fwd(
         C.byref(desc), _tensor(w, "X", X, bf, td, dev), _tensor(w, "Wg", Wg, bf, fd, dev), _tensor(w, "Wu", Wu, bf, fd, dev),
@@ -599,7 +601,7 @@ def sf_gated_ffn_fwd(desc, X, Wg, Wu, Wd, Y, fwd_ctx, workspace, stream=None):
 
 def sf_gated_ffn_bwd(desc, dY, X, Wg, Wu, Wd, fwd_ctx, dX, dWg, dWu, dWd, workspace, stream=None):
     """Gradients of sf_gated_ffn_fwd with the context that it filled. An output of None is left out."""
-    w, bf, dev = "sf_gated_ffn_bwd", torch.bfloat16, X.get_device()
+    w, bf, dev = "sf_gated_ffn_bwd", _BF16, X.get_device()
     td, fd, df = (desc.T, desc.D), (desc.F, desc.D), (desc.D, desc.F)
     _check(lib().sf_gated_ffn_bwd(
         C.byref(desc), _tensor(w, "dY", dY, bf, td, dev), _tensor(w, "X", X, bf, td, dev), _tensor(w, "Wg", Wg, bf, fd, dev),
@@ -615,11 +617,22 @@ def sf_fp4_sizes(rows: int, cols: int, fmt: int):
     return a.value, b.value
 
 
+_BF16, _U8 = torch.bfloat16, torch.uint8
+_SCALE_TILE = {SF_FP4_NV: 6, SF_FP4_MX: 7}          # log2 of the columns of a tile of scales
+
+
 def _scale_bytes(rows: int, cols: int, fmt: int) -> int:
     """Bytes of the scale tiles, as sf_fp4_sizes has them."""
-    if cols % 32 or (fmt != SF_FP4_NV and fmt != SF_FP4_MX):
+    lg = _SCALE_TILE.get(fmt)
+    if lg is None or cols & 31:
         return sf_fp4_sizes(rows, cols, fmt)[1]                  # refuses
-    return -(-rows // 128) * -(-cols // (64 if fmt == SF_FP4_NV else 128)) * 512
+    return ((rows + 127 >> 7) * (cols + (1 << lg) - 1 >> lg)) << 9
+
+
+def _matrix_shape(where: str, t):
+    if t.dim() != 2:
+        raise SparseFFNError(SF_ERR_SHAPE, f"{where}: codes must be a matrix")
+    return t.shape
 
 
 def _row_stride(where: str, name: str, t) -> int:
@@ -631,17 +644,10 @@ def _row_stride(where: str, name: str, t) -> int:
     return t.stride(0) if t.size(0) > 1 else t.size(1)
 
 
-def _codes_shape(where: str, *codes):
-    for t in codes:
-        if t.dim() != 2:
-            raise SparseFFNError(SF_ERR_SHAPE, f"{where}: codes must be a matrix")
-    return codes[0].shape
-
-
 def sf_fp4_quantize(X, fmt: int, scale: float, out=None, stream=None):
     """(codes uint8 [rows, cols/2], scales uint8 tiles) of bf16 X, which may be a strided row view; ``out`` = a previous result
     to write into."""
-    w, u8, dev = "sf_fp4_quantize", torch.uint8, X.get_device()
+    w, u8, dev = "sf_fp4_quantize", _U8, X.get_device()
     ld = _row_stride(w, "X", X)
     rows, cols = X.shape
     n = _scale_bytes(rows, cols, fmt)
@@ -655,8 +661,8 @@ def sf_fp4_quantize(X, fmt: int, scale: float, out=None, stream=None):
 
 def sf_fp4_dequantize(codes, scales, fmt: int, alpha: float, out=None, stream=None):
     """bf16 [rows, cols] = code * sf * alpha; ``out`` may be a strided row view."""
-    w, u8, dev = "sf_fp4_dequantize", torch.uint8, codes.get_device()
-    rows, half = _codes_shape(w, codes)
+    w, u8, dev = "sf_fp4_dequantize", _U8, codes.get_device()
+    rows, half = _matrix_shape(w, codes)
     cols = 2 * half
     if out is None:
         out = torch.empty((rows, cols), dtype=torch.bfloat16, device=codes.device)
@@ -677,16 +683,16 @@ def sf_gemm_fp4_workspace_size(Mr: int, Nc: int, K: int) -> int:
 
 def sf_gemm_fp4(A, a_scales, B, b_scales, fmt: int, alpha: float, C_out=None, workspace=None, stream=None):
     """C[Mr,Nc] = bf16(alpha * A B^T) of two 4-bit operands, codes [Mr,K/2] and [Nc,K/2] with their scales."""
-    w, u8, dev = "sf_gemm_fp4", torch.uint8, A.get_device()
-    Mr, half = _codes_shape(w, A, B)
-    Nc, K = B.size(0), 2 * half
+    w, u8, dev = "sf_gemm_fp4", _U8, A.get_device()
+    Mr, half = _matrix_shape(w, A)
+    Nc, K = _matrix_shape(w, B)[0], 2 * half
     a, a_s = _tensor(w, "A", A, u8, (Mr, half), dev), _tensor(w, "a_scales", a_scales, u8, (_scale_bytes(Mr, K, fmt),), dev)
     b, b_s = _tensor(w, "B", B, u8, (Nc, half), dev), _tensor(w, "b_scales", b_scales, u8, (_scale_bytes(Nc, K, fmt),), dev)
     if C_out is None:
         C_out = torch.empty((Mr, Nc), dtype=torch.bfloat16, device=A.device)
     if workspace is None:
         workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device)
-    _check(lib().sf_gemm_fp4(a, a_s, b, b_s, fmt, _tensor(w, "C_out", C_out, torch.bfloat16, (Mr, Nc), dev), Mr, Nc, K, alpha,
+    _check(lib().sf_gemm_fp4(a, a_s, b, b_s, fmt, _tensor(w, "C_out", C_out, _BF16, (Mr, Nc), dev), Mr, Nc, K, alpha,
                              *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
     return C_out
 
@@ -694,9 +700,9 @@ def sf_gemm_fp4(A, a_scales, B, b_scales, fmt: int, alpha: float, C_out=None, wo
 def sf_gemm_fp4_gated(A, a_scales, Bg, bg_scales, Bu, bu_scales, fmt: int, act: int, alpha_g: float, alpha_u: float, H_out=None,
                       workspace=None, stream=None):
     """H[Mr,Nc] = bf16(act(alpha_g * A Bg^T) * (alpha_u * A Bu^T)) of 4-bit operands."""
-    w, u8, dev = "sf_gemm_fp4_gated", torch.uint8, A.get_device()
-    Mr, half = _codes_shape(w, A, Bg, Bu)
-    Nc, K = Bg.size(0), 2 * half
+    w, u8, dev = "sf_gemm_fp4_gated", _U8, A.get_device()
+    Mr, half = _matrix_shape(w, A)
+    Nc, K = _matrix_shape(w, Bg)[0], 2 * half
     shape, tiles = (Nc, half), (_scale_bytes(Nc, K, fmt),)
     a, a_s = _tensor(w, "A", A, u8, (Mr, half), dev), _tensor(w, "a_scales", a_scales, u8, (_scale_bytes(Mr, K, fmt),), dev)
     g, g_s = _tensor(w, "Bg", Bg, u8, shape, dev), _tensor(w, "bg_scales", bg_scales, u8, tiles, dev)
@@ -705,7 +711,7 @@ def sf_gemm_fp4_gated(A, a_scales, Bg, bg_scales, Bu, bu_scales, fmt: int, act: 
         H_out = torch.empty((Mr, Nc), dtype=torch.bfloat16, device=A.device)
     if workspace is None:
         workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device)
-    _check(lib().sf_gemm_fp4_gated(a, a_s, g, g_s, u, u_s, fmt, act, _tensor(w, "H_out", H_out, torch.bfloat16, (Mr, Nc), dev), Mr, Nc, K,
+    _check(lib().sf_gemm_fp4_gated(a, a_s, g, g_s, u, u_s, fmt, act, _tensor(w, "H_out", H_out, _BF16, (Mr, Nc), dev), Mr, Nc, K,
                                    alpha_g, alpha_u, *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
     return H_out
 
