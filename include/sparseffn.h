@@ -314,16 +314,17 @@ SF_API int sf_ffn_step_host(const sf_ffn_desc* desc, int dense, const void* host
  *     G = X Wg^T,  U = X Wu^T,  H = act(G) * U,  Y = H Wd^T           X, Y [T,D];  Wg, Wu [F,D];  Wd [D,F]; all bf16
  *
  * T >= 0 of any size (a single token and a training batch take the same call); D and F positive multiples of 8; each size at most
- * 2^28. Tensors are contiguous. One rounding each: H (an operand of the second product) and Y; G and U stay in float32.
+ * 2^28. Tensors are contiguous. One rounding each: H (an operand of the second product; with T <= 16 a sum of two bf16 numbers) and Y; G
+ * and U stay in float32. A non-finite value makes the results that it enters non-finite.
  *
  * sf_gated_ffn_fwd:  fwd_ctx NULL: inference, H lies in the workspace. Otherwise fwd_ctx receives what the backward pass needs: H in
- *     bf16, act(G) and U act'(G) in float32 (10 bytes per token and feature). Y is the same either way.
+ *     bf16, act(G) and U act'(G) in float32 (10 bytes per token and feature, 12 with T <= 16). Y is the same either way.
  * sf_gated_ffn_bwd:  dH = dY Wd;  dU = dH act(G);  dG = dH U act'(G);  dX = dG Wg + dU Wu;  dWg = dG^T X;  dWu = dU^T X;  dWd = dY^T H.
- *     dG and dU are rounded to bf16 once. Any of the four outputs may be NULL and is then left out. With T == 0 the weights'
+ *     dG and dU are rounded to bf16 once (sums of two with T <= 16). Any of the four outputs may be NULL and is then left out. With T == 0 the weights'
  *     gradients are zero. The context is only read: the call may be repeated.
  *     act'(0) of ReLU is 0.
  * sf_gated_ffn_workspace_size: bytes of the context and of the workspace (the most that a call of this descriptor needs; the
- *     forward call with a context needs the first 256 bytes only, without one 256 + 2 T F rounded up to 256). As for the
+ *     forward call with a context needs the first 256 bytes only, without one half of the rest too). As for the
  *     step above, the workspace's first 256 bytes are the status word: zero them once, read them with sf_check_status. Calls that may
  *     overlap on the GPU need workspaces of their own. */
 typedef enum sf_gate_act {

@@ -3,7 +3,7 @@
     G = X Wg^T,  U = X Wu^T,  H = act(G) * U,  Y = H Wd^T
 
 in float64, with the roundings of the product path where asked for: H, dG and dU are operands of products and are rounded to bf16
-once; everything else is not rounded before its end. With the forward values the bounds of their error are
+once (with up to 16 tokens, to the sum of two bf16 numbers); everything else is not rounded before its end. With the forward values the bounds of their error are
 returned too, from the arithmetic alone (see ``forward``).
 """
 import math
@@ -37,6 +37,17 @@ def act(name, g):
 def rne_bf16(x):
     """float64 -> nearest bf16 value as float64 (through float32; exact where x is a float32)."""
     return bf16_to_f32(f32_to_bf16(np.asarray(x, np.float64).astype(np.float32))).astype(np.float64)
+
+
+def two_terms(x):
+    """The sum of two bf16 numbers that stands for x: x rounded, and what that left, rounded."""
+    hi = rne_bf16(x)
+    return hi + rne_bf16(x - hi)
+
+
+def held(x, T):
+    """An operand in between (H, dG, dU): one bf16, or with up to 16 tokens the sum of two."""
+    return two_terms(x) if T <= 16 else rne_bf16(x)
 
 
 U16 = 2.0 ** -8          # a rounding to bf16, relative
@@ -75,10 +86,11 @@ def forward(X, Wg, Wu, Wd, name, round_h=True):
     Q = U * dP
     eq = (np.abs(dP) + edp) * eu + (np.abs(U) + eu) * edp
     H = P * U
-    eh = (np.abs(P) + ep) * eu + np.abs(U) * ep + U16 * np.abs(H)
+    u = U16 if X.shape[0] > 16 else U16 * U16        # of the operand in between
+    eh = (np.abs(P) + ep) * eu + np.abs(U) * ep + u * np.abs(H)
     if round_h:
-        H = rne_bf16(H)
-        eh = eh + U16 * np.abs(H)        # the reference is rounded too: a value next to a border may go either way
+        H = held(H, X.shape[0])
+        eh = eh + u * np.abs(H)          # the reference is rounded too: a value next to a border may go either way
     Y = H @ Wd.T
     ey = eh @ np.abs(Wd).T + F * ADD * (np.abs(H) @ np.abs(Wd).T)
     ey = ey + U16 * (np.abs(Y) + ey)
@@ -96,7 +108,8 @@ def backward(X, Wg, Wu, Wd, dY, name):
     dU, dG = dH * f.P, dH * f.Q
     edu = (a(f.P) + f.err_P) * edh + a(dH) * f.err_P
     edg = (a(f.Q) + f.err_Q) * edh + a(dH) * f.err_Q
-    edu, edg = edu + U16 * (a(dU) + edu), edg + U16 * (a(dG) + edg)
+    u = U16 if T > 16 else U16 * U16
+    edu, edg = edu + u * (a(dU) + edu), edg + u * (a(dG) + edg)
 
     def done(v, e):
         return v, e + U16 * (a(v) + e)
@@ -112,8 +125,9 @@ def exact_step(X, Wg, Wu, Wd, dY, name="relu"):
     any order of additions, with one rounding to bf16 where the path has one."""
     G, U = X @ Wg.T, X @ Wu.T
     P, dP = act(name, G)
-    H = rne_bf16(P * U)
+    T = X.shape[0]
+    H = held(P * U, T)
     dH = dY @ Wd
-    dU, dG = rne_bf16(dH * P), rne_bf16(dH * (U * dP))
+    dU, dG = held(dH * P, T), held(dH * (U * dP), T)
     return {"Y": rne_bf16(H @ Wd.T), "dX": rne_bf16(dG @ Wg + dU @ Wu), "dWg": rne_bf16(dG.T @ X), "dWu": rne_bf16(dU.T @ X),
             "dWd": rne_bf16(dY.T @ H)}

@@ -50,6 +50,7 @@ struct FewCfg {
 
 struct FewArgs {
   int T, N, nkb;                     // tokens, output columns, k-blocks (64 K of bf16, 256 K of 4 bits)
+  int in_terms, out_terms;           // 2: the tokens' operand, or the results, are sums of two bf16: rows t and T + t (see kTwoTerms)
   int nkb0;                          // FK_DX: those of the first pair
   int act;
   int stages;                        // of the ring
@@ -247,7 +248,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
 #pragma unroll 1
       for (int m = 0; m < kMats; ++m)
 #pragma unroll 1
-        for (int c = m * kN; c < m * kN + args.T; c += 16) {
+        for (int c = m * kN; c < m * kN + args.in_terms * args.T; c += 16) {
           uint32_t v[16];
           tmem_ld_32x32b_x16(tmem_base + c + ((uint32_t)(q * 32) << 16), v);
 #pragma unroll
@@ -274,24 +275,25 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
     const int t = i >> 5, p = (i & 31) * 4, f = f0 + p;
     if (f >= args.N) continue;
     float4 x[kMats][4], sum[kMats];
+    for (int term = 0; term < args.in_terms; ++term)
 #pragma unroll
-    for (int s0 = 0; s0 < 8; s0 += 4) {
-      if (s0 >= S) break;
+      for (int s0 = 0; s0 < 8; s0 += 4) {
+        if (s0 >= S) break;
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int m = 0; m < kMats; ++m) {
-          const uint32_t at = part + (uint32_t)((m * kN + t) * 128 + p) * 4u;
-          if (s0 + s < S) x[m][s] = ld_cluster_f4(at, s0 + s);
-        }
+          for (int m = 0; m < kMats; ++m) {
+            const uint32_t at = part + (uint32_t)((m * kN + term * args.T + t) * 128 + p) * 4u;
+            if (s0 + s < S) x[m][s] = ld_cluster_f4(at, s0 + s);
+          }
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
-        for (int m = 0; m < kMats; ++m) {
-          if (s0 + s == 0) sum[m] = x[m][0];
-          else if (s0 + s < S) { sum[m].x += x[m][s].x; sum[m].y += x[m][s].y; sum[m].z += x[m][s].z; sum[m].w += x[m][s].w; }
-        }
-    }
+          for (int m = 0; m < kMats; ++m) {
+            if (s0 + s == 0 && term == 0) sum[m] = x[m][0];
+            else if (s0 + s < S) { sum[m].x += x[m][s].x; sum[m].y += x[m][s].y; sum[m].z += x[m][s].z; sum[m].w += x[m][s].w; }
+          }
+      }
     float a[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w};
     if (kFp4)
 #pragma unroll
@@ -314,12 +316,29 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] *= b[e];
     }
+    // four results of a row: rounded, and where the row has a second term, what the rounding left
+    auto put = [&](void* C, const float (&v)[4]) {
+      uint16_t* c = reinterpret_cast<uint16_t*>(C) + at;
+      const uint32_t lo = bf16x2(v[0], v[1]), hi = bf16x2(v[2], v[3]);
+      *reinterpret_cast<uint2*>(c) = make_uint2(lo, hi);
+      if ((kKind == FK_GATED || kKind == FK_BWD) && args.out_terms == 2) {
+        const uint32_t w[2] = {lo, hi};
+        float rest[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float r = __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+          rest[e] = isfinite(r) ? v[e] - r : 0.f;
+        }
+        *reinterpret_cast<uint2*>(c + (int64_t)args.T * args.N) = make_uint2(bf16x2(rest[0], rest[1]), bf16x2(rest[2], rest[3]));
+      }
+    };
     if constexpr (kKind == FK_BWD) {
       const float4 p = __ldg(reinterpret_cast<const float4*>(args.P + at)), r = __ldg(reinterpret_cast<const float4*>(args.Q + at));
-      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(args.C2) + at) = make_uint2(bf16x2(a[0] * r.x, a[1] * r.y), bf16x2(a[2] * r.z, a[3] * r.w));
+      const float dg[4] = {a[0] * r.x, a[1] * r.y, a[2] * r.z, a[3] * r.w};
+      put(args.C2, dg);
       a[0] *= p.x; a[1] *= p.y; a[2] *= p.z; a[3] *= p.w;
     }
-    *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(args.C) + at) = make_uint2(bf16x2(a[0], a[1]), bf16x2(a[2], a[3]));
+    put(args.C, a);
   }
   if (S > 1) cluster_sync_all();                           // no CTA leaves while another reads its shared memory
 }

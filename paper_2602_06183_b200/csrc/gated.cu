@@ -4,7 +4,8 @@
 //             dX = dG Wg + dU Wu                                                        one launch, one accumulation
 //             dWd = dY^T H,  dWg = dG^T X,  dWu = dU^T X                                one launch, tiles of all three
 //
-// Roundings: G, U and dH stay in float32. H, dG and dU are rounded to bf16 once, because they are operands of the next product; P and
+// Roundings: G, U and dH stay in float32. H, dG and dU are rounded to bf16 once, because they are operands of the next product (with up to 16
+// tokens they are sums of two bf16 numbers, see kTwoTerms); P and
 // Q are kept in float32 (8 bytes a hidden value where bf16 would take 4), because dG and dU would otherwise be rounded two or three times: the
 // error of dWu against 64 bits is then 1.8 times that of a result that is rounded once at its end, with them it is 1.4 times.
 #include <initializer_list>
@@ -73,19 +74,19 @@ constexpr size_t kStatus = 256;
 size_t padded(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct GatedSizes {
-  size_t h, f;          // bytes of a bf16 and of a float32 [T, F]
+  size_t h, f;          // bytes of an operand in between (one or two bf16 [T, F]) and of a float32 [T, F]
 };
 int gated_sizes(const sf_gated_ffn_desc* d, GatedSizes* z) {
   if (!d) return SF_ERR_NULL;
   if (!act_ok(d->act)) return SF_ERR_UNSUPPORTED;
   if (d->T < 0 || d->D <= 0 || d->F <= 0 || d->D % 8 || d->F % 8 || d->T > kMaxSize || d->D > kMaxSize || d->F > kMaxSize) return SF_ERR_SHAPE;
   const size_t n = (size_t)d->T * (size_t)d->F;
-  z->h = padded(2 * n);
+  z->h = padded(2 * n * terms_of(d->T));
   z->f = padded(4 * n);
   return SF_OK;
 }
 
-struct GradJob { const void *A, *B; int64_t M, N; void* C; };     // C[M, N] = A[T, M]^T B[T, N]
+struct GradJob { const void *A, *B; int64_t M, N; void* C; int a_terms, b_terms; };     // C[M, N] = A[T, M]^T B[T, N]
 
 }  // namespace
 
@@ -112,9 +113,9 @@ int sf_gated_ffn_step_plan(const sf_gated_ffn_desc* desc, sf_gated_ffn_plan* pla
   if (desc->T == 0) return SF_OK;
   const int T = (int)desc->T, D = (int)desc->D, F = (int)desc->F;
   const int kd = k_blocks(FMT_BF16, D), kf = k_blocks(FMT_BF16, F), kt = (int)ceil_div(T, 64);
-  auto few = [&](auto kind, int i, int N, int nkb) {
+  auto few = [&](auto kind, int i, int N, int nkb, int terms) {
     FewArgs a{};
-    a.T = T; a.N = N; a.nkb = nkb;
+    a.T = T; a.N = N; a.nkb = nkb; a.in_terms = terms;
     PairPlan p;
     NoMaps none;
     SF_TRY((run_few<FMT_BF16, decltype(kind)::value>(a, nullptr, none, &p)));
@@ -131,10 +132,10 @@ int sf_gated_ffn_step_plan(const sf_gated_ffn_desc* desc, sf_gated_ffn_plan* pla
     return (int)SF_OK;
   };
   if (T <= kFewTokens) {
-    SF_TRY(few(ActTag<FK_GATED>{}, SF_GATED_H, F, kd));
-    SF_TRY(few(ActTag<FK_NT>{}, SF_GATED_Y, D, kf));
-    SF_TRY(few(ActTag<FK_BWD>{}, SF_GATED_DH, F, kd));
-    SF_TRY(few(ActTag<FK_DX>{}, SF_GATED_DX, D, 2 * kf));
+    SF_TRY(few(ActTag<FK_GATED>{}, SF_GATED_H, F, kd, 1));
+    SF_TRY(few(ActTag<FK_NT>{}, SF_GATED_Y, D, kf, terms_of(T)));
+    SF_TRY(few(ActTag<FK_BWD>{}, SF_GATED_DH, F, kd, 1));
+    SF_TRY(few(ActTag<FK_DX>{}, SF_GATED_DX, D, 2 * kf, terms_of(T)));
     plan->form[SF_GATED_H_KEPT] = plan->form[SF_GATED_H]; plan->cols[SF_GATED_H_KEPT] = plan->cols[SF_GATED_H];
     plan->parts[SF_GATED_H_KEPT] = plan->parts[SF_GATED_H];
   } else {
@@ -164,9 +165,11 @@ int sf_gated_ffn_fwd(const sf_gated_ffn_desc* desc, const void* X, const void* W
   float* q = fwd_ctx ? (float*)(h + z.h + z.f) : nullptr;
   int* status = (int*)workspace;
   trace_mark(s);
-  SF_TRY(run_gated<FMT_BF16>({X, nullptr}, {Wg, nullptr}, {Wu, nullptr}, desc->T, desc->F, desc->D, desc->act, 1.f, 1.f, h, p, q, status, s));
+  SF_TRY(run_gated<FMT_BF16>({X, nullptr}, {Wg, nullptr}, {Wu, nullptr}, desc->T, desc->F, desc->D, desc->act, 1.f, 1.f, h, p, q, status, s,
+                             terms_of(desc->T)));
   trace_mark(s);
-  SF_TRY(run_nt<FMT_BF16>({h, nullptr}, {Wd, nullptr}, desc->T, desc->D, desc->F, 1.f, Y, status, s, true));
+  SF_TRY(run_nt<FMT_BF16>({h, nullptr}, {Wd, nullptr}, desc->T, desc->D, desc->F, 1.f, Y, status, s, true,
+                          terms_of(desc->T)));
   trace_mark(s);
   return SF_OK;
 }
@@ -198,6 +201,7 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
   a.status = (int*)workspace;
   a.jobs = 1;
   const bool few = T <= kFewTokens;
+  const int terms = terms_of(T);
   FewArgs f{};
   f.T = (int)T; f.status = (int*)workspace;
   trace_mark(s);
@@ -205,7 +209,7 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
     const int nkb = k_blocks(FMT_BF16, D);
     const float *p = (const float*)(h + z.h), *q = (const float*)(h + z.h + z.f);
     if (few) {
-      f.N = (int)F; f.nkb = f.nkb0 = nkb; f.C = du; f.C2 = dg; f.P = const_cast<float*>(p); f.Q = const_cast<float*>(q);
+      f.N = (int)F; f.nkb = f.nkb0 = nkb; f.in_terms = 1; f.out_terms = terms; f.C = du; f.C2 = dg; f.P = const_cast<float*>(p); f.Q = const_cast<float*>(q);
       SF_TRY((run_few<FMT_BF16, FK_BWD>(f, s, [&](FewMaps& m, int n) {
         SF_TRY(kmajor_map(&m.x, FMT_BF16, dY, T, D, n));
         SF_TRY(mn_map(&m.w0, Wd, D, F));
@@ -232,9 +236,10 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
     const int nkb = k_blocks(FMT_BF16, F);
     if (few) {
       f.N = (int)D; f.nkb0 = nkb; f.nkb = 2 * nkb; f.C = dX; f.early_weights = 1; f.early_next = beside;
+      f.in_terms = terms; f.out_terms = 1;
       SF_TRY((run_few<FMT_BF16, FK_DX>(f, s, [&](FewMaps& m, int n) {
-        SF_TRY(kmajor_map(&m.x, FMT_BF16, dg, T, F, n));
-        SF_TRY(kmajor_map(&m.sx, FMT_BF16, du, T, F, n));
+        SF_TRY(kmajor_map(&m.x, FMT_BF16, dg, T * terms, F, n));
+        SF_TRY(kmajor_map(&m.sx, FMT_BF16, du, T * terms, F, n));
         SF_TRY(mn_map(&m.w0, Wg, F, D));
         SF_TRY(mn_map(&m.w1, Wu, F, D));
         m.s0 = m.s1 = m.x;
@@ -256,19 +261,23 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
   trace_mark(s);
   GradJob jobs[3];
   a.jobs = 0;
-  if (dWd) jobs[a.jobs++] = {dY, h, D, F, dWd};
-  if (dWg) jobs[a.jobs++] = {dg, X, F, D, dWg};
-  if (dWu) jobs[a.jobs++] = {du, X, F, D, dWu};
+  if (dWd) jobs[a.jobs++] = {dY, h, D, F, dWd, 1, terms};
+  if (dWg) jobs[a.jobs++] = {dg, X, F, D, dWg, terms, 1};
+  if (dWu) jobs[a.jobs++] = {du, X, F, D, dWu, terms, 1};
   if (a.jobs == 0) {
     trace_mark(s);
     return SF_OK;
   }
-  for (int j = 0; j < a.jobs; ++j) { a.M[j] = (int)jobs[j].M; a.N[j] = (int)jobs[j].N; }
+  for (int j = 0; j < a.jobs; ++j) {
+    a.M[j] = (int)jobs[j].M; a.N[j] = (int)jobs[j].N;
+    a.sums_in_a |= (jobs[j].a_terms == 2) << j;
+  }
   a.nkb = a.nkb0 = (int)ceil_div(T, 64);
+  a.term_rows = terms == 2 ? (int)T : 0;
   SF_TRY(launch_best<PK_DW>(a, s, [&](CUtensorMap* m, int) {
     for (int j = 0; j < a.jobs; ++j) {
-      SF_TRY(mn_map(&m[j], jobs[j].A, T, jobs[j].M));
-      SF_TRY(mn_map(&m[3 + j], jobs[j].B, T, jobs[j].N));
+      SF_TRY(mn_map(&m[j], jobs[j].A, T * jobs[j].a_terms, jobs[j].M, terms == 2 ? 16 : 64));
+      SF_TRY(mn_map(&m[3 + j], jobs[j].B, T * jobs[j].b_terms, jobs[j].N, terms == 2 ? 16 : 64));
       SF_TRY(make_tmap_store(&m[6 + j], jobs[j].C, jobs[j].M, jobs[j].N));
     }
     for (int j = a.jobs; j < 3; ++j)

@@ -73,6 +73,8 @@ struct PairArgs {
   int act;
   int bn;                            // tile width (PM_WIDTH, PM_SPLIT)
   int parts;                         // pairs of a cluster (PM_SPLIT)
+  // PK_DW of up to 16 tokens, whose sums of two (A's in the jobs of the mask, else B's) have their second terms from this row on: 0 otherwise
+  int term_rows, sums_in_a;
   float alpha, alpha2;
   int early_next;                    // the next launch is let in at the start: several rounds of tiles (see long_dense in gemm_tc.cu), or it runs beside
   // Beside the launch before it, whose results it does not read (they are waited for at the end): that one holds the pairs from `first_late` on for
@@ -208,7 +210,9 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
   const int pair = kSplit ? (int)blockIdx.x / (2 * parts) : blockIdx.x >> 1, num_pairs = kSplit ? 0x3FFFFFFF : gridDim.x >> 1;
   const int kb0 = kSplit ? args.nkb * part / parts : 0, kb1 = kSplit ? args.nkb * (part + 1) / parts : args.nkb;
   const int b_chunks = (half + 63) >> 6;                   // MN-major B: chunks of 64 columns
-  const uint32_t stage_tx = kVar ? 2u * (uint32_t)(Cfg::kABytes + (Cfg::kBMN ? b_chunks * 8192 : half * 128)) : 2u * Cfg::kStageBytes;
+  const bool sums = kKind == PK_DW && kMode != PM_SPLIT && args.term_rows > 0;
+  const uint32_t stage_tx = sums   ? 2u * (uint32_t)(8192 + b_chunks * 4096)
+                            : kVar ? 2u * (uint32_t)(Cfg::kABytes + (Cfg::kBMN ? b_chunks * 8192 : half * 128)) : 2u * Cfg::kStageBytes;
   int num_tiles = args.num_m[0] * args.num_n[0];
   if (kKind == PK_DW)
     for (int j = 1; j < args.jobs; ++j) num_tiles += args.num_m[j] * args.num_n[j];
@@ -257,28 +261,43 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
           if (rank == 0) mbar_arrive_expect_tx(bar, stage_tx);                            // the bytes of both CTAs
           const bool second = kKind == PK_DX && kb >= args.nkb0;
           const int k = (second ? kb - args.nkb0 : kb) * 64;
-          if constexpr (kKind == PK_DW) {
-            tma_load_2d_2cta(sA, &maps.m[t.job], bar, m0, k);
-            tma_load_2d_2cta(sA + 8192, &maps.m[t.job], bar, m0 + 64, k);
-          } else {
-            tma_load_2d_2cta(sA, &maps.m[second ? 1 : 0], bar, k, m0);
-          }
-          const CUtensorMap* mb = kKind == PK_DW ? &maps.m[3 + t.job] : kKind == PK_DX ? &maps.m[second ? 3 : 2]
-                                : kGated ? &maps.m[1 + rank] : &maps.m[1];
-          if constexpr (Cfg::kBMN) {
+          if (sums) {
+            // 16 rows of the first terms, then 16 of the second ones, each with the other operand's rows: two products instead of four (rows
+            // of second terms that meet the other operand's zeros are finite)
+            const bool in_a = args.sums_in_a >> t.job & 1;
 #pragma unroll
-            for (int c = 0; c < Cfg::kBChunks; ++c)
-              if (!kVar || c < b_chunks) tma_load_2d_2cta(sB + c * 8192, mb, bar, n0 + c * 64, k);
-          } else {
-            tma_load_2d_2cta(sB, mb, bar, k, n0);
-          }
-          if constexpr (kFp4) {
-            uint8_t* sS = sB + Cfg::kBBytes;
-            tma_load_3d_2cta(sS, &maps.m[kGated ? 4 : 3], bar, 0, kb * Cfg::kTiles, m0 >> 7);
+            for (int h = 0; h < 2; ++h) {
+              const int kA = in_a ? h * args.term_rows : 0, kB = in_a ? 0 : h * args.term_rows;
+              tma_load_2d_2cta(sA + h * 2048, &maps.m[t.job], bar, m0, kA);
+              tma_load_2d_2cta(sA + 8192 + h * 2048, &maps.m[t.job], bar, m0 + 64, kA);
 #pragma unroll
-            for (int b = 0; b < Cfg::kBBlocks; ++b)        // the scales of all of the tile's columns, in both CTAs
-              tma_load_3d_2cta(sS + (1 + b) * Cfg::kTiles * 512, &maps.m[kGated ? 5 + b : 4], bar, 0, kb * Cfg::kTiles,
-                               kGated ? t.n0 >> 7 : (t.n0 >> 7) + b);
+              for (int c = 0; c < Cfg::kBChunks; ++c)
+                if (!kVar || c < b_chunks) tma_load_2d_2cta(sB + c * 8192 + h * 2048, &maps.m[3 + t.job], bar, n0 + c * 64, kB);
+            }
+          } else {
+            if constexpr (kKind == PK_DW) {
+              tma_load_2d_2cta(sA, &maps.m[t.job], bar, m0, k);
+              tma_load_2d_2cta(sA + 8192, &maps.m[t.job], bar, m0 + 64, k);
+            } else {
+              tma_load_2d_2cta(sA, &maps.m[second ? 1 : 0], bar, k, m0);
+            }
+            const CUtensorMap* mb = kKind == PK_DW ? &maps.m[3 + t.job] : kKind == PK_DX ? &maps.m[second ? 3 : 2]
+                                  : kGated ? &maps.m[1 + rank] : &maps.m[1];
+            if constexpr (Cfg::kBMN) {
+#pragma unroll
+              for (int c = 0; c < Cfg::kBChunks; ++c)
+                if (!kVar || c < b_chunks) tma_load_2d_2cta(sB + c * 8192, mb, bar, n0 + c * 64, k);
+            } else {
+              tma_load_2d_2cta(sB, mb, bar, k, n0);
+            }
+            if constexpr (kFp4) {
+              uint8_t* sS = sB + Cfg::kBBytes;
+              tma_load_3d_2cta(sS, &maps.m[kGated ? 4 : 3], bar, 0, kb * Cfg::kTiles, m0 >> 7);
+#pragma unroll
+              for (int b = 0; b < Cfg::kBBlocks; ++b)        // the scales of all of the tile's columns, in both CTAs
+                tma_load_3d_2cta(sS + (1 + b) * Cfg::kTiles * 512, &maps.m[kGated ? 5 + b : 4], bar, 0, kb * Cfg::kTiles,
+                                 kGated ? t.n0 >> 7 : (t.n0 >> 7) + b);
+            }
           }
         }
         if (++stage == kStages) { stage = 0; phase ^= 1; }
@@ -336,7 +355,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
             }
           } else if (issues) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) mma_f16_2cta(d, a + k * a_step, b + k * b_step, idesc, k > 0 ? 1u : more);
+            for (int k = 0; k < 4; ++k)
+              if (kKind != PK_DW || k < 2 || !sums) mma_f16_2cta(d, a + k * a_step, b + k * b_step, idesc, k > 0 ? 1u : more);
             commit_pair(&ctl->empty[stage], part);
           }
           __syncwarp();

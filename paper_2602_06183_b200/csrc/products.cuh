@@ -22,6 +22,13 @@ namespace {
 #endif
 constexpr int64_t kFewTokens = SF_FEW_TOKENS;
 
+// Up to this many tokens the operands in between (H, dG, dU) are held as sums of two bf16 numbers, which the few-token products take as
+// twice the tokens: there is room for them in the instruction's columns, and the products wait for the weights. With so few tokens
+// a result rests on a handful of large hidden values, and rounding those once showed: the error of Y against 64 bits was 1.3 to 1.6 times
+// that of a result that is rounded at its end only (1 x 1480 x 600), now it is the same.
+constexpr int64_t kTwoTerms = 16;
+inline int terms_of(int64_t T) { return T <= kTwoTerms ? 2 : 1; }
+
 constexpr int64_t kMaxSize = (int64_t)1 << 28;      // of a dimension: coordinates and counts stay within 32 bits
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -34,7 +41,9 @@ inline int64_t scale_tiles(int fmt, int64_t K) { return ceil_div(K, fmt == FMT_N
 inline int kmajor_map(void* m, int fmt, const void* p, int64_t rows, int64_t K, uint32_t box_rows) {
   return make_tmap_2d(m, p, rows, row_units(fmt, K), row_units(fmt, K), 64, box_rows, true);
 }
-inline int mn_map(void* m, const void* p, int64_t K, int64_t cols) { return make_tmap_2d(m, p, K, cols, cols, 64, 64, true); }
+inline int mn_map(void* m, const void* p, int64_t K, int64_t cols, uint32_t box_rows = 64) {
+  return make_tmap_2d(m, p, K, cols, cols, 64, box_rows, true);
+}
 inline int scale_map(void* m, int fmt, const void* p, int64_t rows, int64_t K) {
   return make_tmap_scales(m, p, ceil_div(rows, 128), scale_tiles(fmt, K), fmt == FMT_NV ? 4 : 2);
 }
@@ -124,17 +133,18 @@ int run_few_n(const FewArgs& a, cudaStream_t s, F& make, PairPlan* taken) {
 }
 template <int kFmt, int kKind, typename F>
 int run_few(const FewArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr) {
-  if (a.T <= 16) return run_few_n<kFmt, kKind, 16>(a, s, make, taken);
-  if (a.T <= 32) return run_few_n<kFmt, kKind, 32>(a, s, make, taken);
-  if (a.T <= 64) return run_few_n<kFmt, kKind, 64>(a, s, make, taken);
-  if (a.T <= 96) return run_few_n<kFmt, kKind, 96>(a, s, make, taken);
+  const int columns = a.T * a.in_terms;
+  if (columns <= 16) return run_few_n<kFmt, kKind, 16>(a, s, make, taken);
+  if (columns <= 32) return run_few_n<kFmt, kKind, 32>(a, s, make, taken);
+  if (columns <= 64) return run_few_n<kFmt, kKind, 64>(a, s, make, taken);
+  if (columns <= 96) return run_few_n<kFmt, kKind, 96>(a, s, make, taken);
   return run_few_n<kFmt, kKind, 128>(a, s, make, taken);
 }
 // X W^T with one matrix, or two of one shape.
 template <int kFmt, int kKind>
 int run_few_rows(const Operand& X, const Operand& W0, const Operand& W1, int64_t N, int64_t K, const FewArgs& a, cudaStream_t s) {
   return run_few<kFmt, kKind>(a, s, [&](FewMaps& m, int n) {
-    SF_TRY(kmajor_map(&m.x, kFmt, X.data, a.T, K, n));
+    SF_TRY(kmajor_map(&m.x, kFmt, X.data, (int64_t)a.T * a.in_terms, K, n));
     SF_TRY(kmajor_map(&m.w0, kFmt, W0.data, N, K, 128));
     m.w1 = m.w0;
     if (kKind == FK_GATED) SF_TRY(kmajor_map(&m.w1, kFmt, W1.data, N, K, 128));
@@ -200,15 +210,15 @@ int run_nt_fp4(const Operand& A, const Operand& B, int64_t K, void* C, const Pai
 }
 
 // C[M, N] = alpha A B^T; M, N, K > 0. early_weights: the launch before this one is another product of the same call, which does not
-// write B.
+// write B. terms: 2 where A is a sum (few tokens).
 template <int kFmt>
 int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, float alpha, void* C, int* status, cudaStream_t s,
-           bool early_weights = false) {
+           bool early_weights = false, int terms = 1) {
   const int nkb = k_blocks(kFmt, K);
   if (M <= kFewTokens) {
     FewArgs a{};
     a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.alpha = a.alpha2 = alpha; a.C = C; a.status = status;
-    a.early_weights = early_weights;
+    a.early_weights = early_weights; a.in_terms = terms; a.out_terms = 1;
     return run_few_rows<kFmt, FK_NT>(A, B, B, N, K, a, s);
   }
   PairArgs a{};
@@ -227,15 +237,16 @@ int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, 
   }
 }
 
-// H = act(alpha_g A Bg^T) (alpha_u A Bu^T); P, Q (bf16 operands; both or neither): act(g) and u act'(g) in float32. M, N, K > 0.
+// H = act(alpha_g A Bg^T) (alpha_u A Bu^T); P, Q (bf16 operands; both or neither): act(g) and u act'(g) in float32. M, N, K > 0. terms: 2
+// where H is a sum (few tokens).
 template <int kFmt>
 int run_gated(const Operand& A, const Operand& Bg, const Operand& Bu, int64_t M, int64_t N, int64_t K, int act, float alpha_g,
-              float alpha_u, void* H, float* P, float* Q, int* status, cudaStream_t s) {
+              float alpha_u, void* H, float* P, float* Q, int* status, cudaStream_t s, int terms = 1) {
   const int nkb = k_blocks(kFmt, K);
   if (M <= kFewTokens) {
     FewArgs a{};
     a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.act = act; a.alpha = alpha_g; a.alpha2 = alpha_u; a.C = H; a.P = P; a.Q = Q;
-    a.status = status;
+    a.status = status; a.in_terms = 1; a.out_terms = terms;
     return run_few_rows<kFmt, FK_GATED>(A, Bg, Bu, N, K, a, s);
   }
   PairArgs a{};
