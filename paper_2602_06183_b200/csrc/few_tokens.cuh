@@ -13,6 +13,8 @@
 // cluster barriers are reached by every warp because their own waits are.
 #pragma once
 
+#include <atomic>
+
 #include "gated.cuh"
 
 namespace sf {
@@ -364,7 +366,10 @@ void few_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[2], int64_t
 // How many clusters of 1 to 8 CTAs a device holds at once with one CTA to an SM (a cluster stays within one of the chip's groups of
 // SMs, whose size is no multiple of most numbers); with two it is taken for twice as many. Asked once; every thread that asks
 // gets the same answer.
-struct FewRoom { int clusters[8]; int set; };
+struct FewRoom {
+  int clusters[8];
+  std::atomic<int> set;
+};
 template <int kFmt, int kKind, int kN>
 int few_room(const FewRoom** room) {
   using Cfg = FewCfg<kFmt, kKind, kN>;
@@ -372,14 +377,14 @@ int few_room(const FewRoom** room) {
   static FewRoom other;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) {                // no device: what the chip that this is written for answers
-    static const FewRoom usual = {{148, 74, 45, 33, 26, 22, 15, 15}, 1};
+    static const FewRoom usual{{148, 74, 45, 33, 26, 22, 15, 15}, {1}};
     cudaGetLastError();
     *room = &usual;
     return SF_OK;
   }
   FewRoom& r = dev >= 0 && dev < 64 ? rooms[dev] : other;
   *room = &r;
-  if (r.set && &r != &other) return SF_OK;
+  if (r.set.load(std::memory_order_acquire) && &r != &other) return SF_OK;
   auto kern = few_tokens_kernel<kFmt, kKind, kN>;
   SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::smem(1)));
   SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared));
@@ -392,7 +397,7 @@ int few_room(const FewRoom** room) {
     SF_CUDA_TRY(cudaOccupancyMaxActiveClusters(&n, kern, &cfg));
     r.clusters[S - 1] = n;
   }
-  r.set = 1;
+  r.set.store(1, std::memory_order_release);
   return SF_OK;
 }
 

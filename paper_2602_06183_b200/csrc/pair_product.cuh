@@ -77,8 +77,9 @@ struct PairArgs {
   int term_rows, sums_in_a;
   float alpha, alpha2;
   int early_next;                    // the next launch is let in at the start: several rounds of tiles (see long_dense in gemm_tc.cu), or it runs beside
-  // Beside the launch before it, whose results it does not read (they are waited for at the end): that one holds the pairs from `first_late` on for
-  // about `late_rounds` tiles of this one, which those pairs leave to the others.
+  // Beside the launch before it, which let it in behind its own wait and whose results it does not read (its end is waited for at the end, so that the
+  // order of the stream is kept; that launch does not wait for this one): that one holds the pairs from `first_late` on for about
+  // `late_rounds` tiles of this one, which those pairs leave to the others.
   int beside, first_late, late_rounds;
   int* status;
 };

@@ -224,6 +224,77 @@ def test_captured_replayed_and_on_another_stream(T):
     assert np.array_equal(bits(b.Y.t), want[0]["Y"])
 
 
+@pytest.mark.parametrize("T", [6, 300])
+def test_two_calls_at_once(T):
+    """Two streams, each with buffers of its own, forward and backward interleaved."""
+    D, F = 264, 520
+    data = [_normals(T, D, F, s) for s in (31, 32)]
+    want = []
+    for x in data:
+        b = Block(T, D, F, "silu", *x)
+        b.fwd()
+        b.bwd()
+        want.append([bits(b.Y.t)] + [bits(b.out[k].t) for k in GRADS])
+    blocks, streams = [Block(T, D, F, "silu", *x) for x in data], [torch.cuda.Stream() for _ in data]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for b, s in zip(blocks, streams):
+            b.fwd(stream=s)
+        for b, s in zip(blocks, streams):
+            b.bwd(stream=s)
+    torch.cuda.synchronize()
+    for b, w in zip(blocks, want):
+        b.check()
+        assert all(np.array_equal(x, y) for x, y in zip([bits(b.Y.t)] + [bits(b.out[k].t) for k in GRADS], w))
+
+
+def test_first_call_inside_a_capture():
+    """Nothing has run before in the process: what a first call looks up and sets is allowed while a stream is captured."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import torch
+from paper_2602_06183_b200 import binding as b
+bf = torch.bfloat16
+def block(T):
+    D, F = 136, 264
+    g = torch.Generator("cuda").manual_seed(T)
+    n = lambda *s: torch.randn(s, generator=g, device="cuda").to(bf)
+    d = b.make_gated_desc(T, D, F)
+    t = [n(T, D), n(T, D), n(F, D), n(F, D), n(D, F)]
+    out = [torch.zeros_like(x) for x in (t[1], t[1], t[2], t[3], t[4])]
+    ctx, ws = b.alloc_gated_ffn_buffers(d)
+    def run():
+        b.sf_gated_ffn_fwd(d, *t[1:], out[0], ctx, ws)
+        b.sf_gated_ffn_bwd(d, *t, ctx, *out[1:], ws)
+        q = b.sf_fp4_quantize(t[2][:, :128], b.SF_FP4_NV, 2.0, out=qw)
+        x = b.sf_fp4_quantize(t[1][:, :128], b.SF_FP4_NV, 2.0, out=qx)
+        b.sf_gemm_fp4(*x, *q, b.SF_FP4_NV, 0.25, C_out=C, workspace=ws4)
+    qw = torch.zeros((F, 64), dtype=torch.uint8, device="cuda"), torch.zeros((b.sf_fp4_sizes(F, 128, 0)[1],), dtype=torch.uint8, device="cuda")
+    qx = torch.zeros((T, 64), dtype=torch.uint8, device="cuda"), torch.zeros((b.sf_fp4_sizes(T, 128, 0)[1],), dtype=torch.uint8, device="cuda")
+    C, ws4 = torch.zeros((T, F), dtype=bf, device="cuda"), torch.zeros((256,), dtype=torch.uint8, device="cuda")
+    return run, out + [C]
+for T in (5, 200):
+    run, out = block(T)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    graph.replay()
+    torch.cuda.synchronize()
+    got = [x.clone() for x in out]
+    for x in out:
+        x.zero_()
+    run()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) and bool(x.any()) for x, y in zip(out, got)), T
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-3000:]
+
+
 def test_repeated_calls_give_the_same_bits():
     for T, D, F in [(1, 4096, 520), (3, 520, 4096), (100, 1024, 1032), (300, 264, 2048)]:
         b = Block(T, D, F, "silu", *_normals(T, D, F, 3))
