@@ -13,6 +13,13 @@
 //
 // CTA = 10 warps: TMA producer, MMA issuer, two sets of four epilogue warps that share a tile's columns. Every wait is bounded
 // (see gemm_tc.cu): on expiry the CTA raises the status word and leaves.
+//
+// 256 columns for two CTAs because a k-block of 64 then brings in 64 bytes a clock and SM next to 512 clocks of products, about what
+// the L2 delivers; narrower tiles are fed worse and are taken only where they fill the pairs better (pair_plan).
+// What bounds them, T 2048, D 4096, F 8192, each from cold caches: dW 255 us (1.62 PFLOP/s, tensor pipe 94 % of its active cycles), dX 187
+// (1.47, 95 %), H with P and Q 180 (1.53, 86 %: 173 MB of stores beside it), Y 97 (1.41, 91 %: one round and a part), dH 110 (1.25,
+// 77 %: reads 134 MB of P and Q in its epilogue). Repeated back to back they draw the power limit and the clock falls to 1.2-1.5 GHz.
+// Products of 4 bits, 4096 x 4096 x 8192, blocks of 16: 56 us (4.9 PFLOP/s, 78 %).
 #pragma once
 
 #include "gated.cuh"
@@ -486,7 +493,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       };
       if constexpr (kAccs == 1) {
         // One accumulator: the next main loop waits for it, so all of it is read into registers and handed back before anything
-        // is made of it (4099 x 8192 x 2048 gated, blocks of 16: 133 -> 112 us; 16384 x 4096 x 4096, blocks of 32: 161 -> 158).
+        // is made of it (4099 x 8192 x 2048 gated, blocks of 16: 133 -> 112 us; 16384 x 4096 x 4096, blocks of 32: 122 -> 98).
         if constexpr (kGated) {
           uint32_t v[2][32], u[2][32];
 #pragma unroll
