@@ -326,7 +326,9 @@ SF_API int sf_ffn_step_host(const sf_ffn_desc* desc, int dense, const void* host
  * sf_gated_ffn_workspace_size: bytes of the context and of the workspace (the most that a call of this descriptor needs; the
  *     forward call with a context needs the first 256 bytes only, without one half of the rest too). As for the
  *     step above, the workspace's first 256 bytes are the status word: zero them once, read them with sf_check_status. Calls that may
- *     overlap on the GPU need workspaces of their own. */
+ *     overlap on the GPU need workspaces of their own.
+ * What a call writes (outputs, workspace, in the forward call the context) must not share a byte with what it reads or with another of
+ *     them: SF_ERR_UNSUPPORTED. Inputs may be one another. */
 typedef enum sf_gate_act {
   SF_ACT_SILU = 0,       /* g / (1 + e^-g) */
   SF_ACT_GELU = 1,       /* g Phi(g) */
@@ -383,6 +385,7 @@ SF_API int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const
  *                     float32 accumulation. With few rows of A (tokens) the other operand is streamed once.
  * sf_gemm_fp4_gated:  H[Mr,Nc] = bf16(act(alpha_g A Bg^T) * (alpha_u A Bu^T)): the first half of the gated block on 4-bit operands.
  * Any Mr and rows; cols and K multiples of 32; Nc a multiple of 8; sizes at most 2^28.
+ * Outputs that share a byte with an input are refused (SF_ERR_UNSUPPORTED; rows with a stride count from the first to the last element).
  * `workspace`: sf_gemm_fp4_workspace_size() bytes, the first 256 the status word as everywhere. */
 typedef enum sf_fp4_format { SF_FP4_NV = 0, SF_FP4_MX = 1 } sf_fp4_format;
 SF_API int sf_fp4_sizes(int64_t rows, int64_t cols, int format, size_t* codes_bytes, size_t* scales_bytes);

@@ -7,6 +7,7 @@ fails loudly otherwise and there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -567,6 +568,11 @@ def _launch_stream(where: str, dev: int, stream):
     return _current_stream() if stream is None else stream.cuda_stream
 
 
+def _allocating(stream):
+    """Where a call makes its own result, it belongs to the stream that the call runs on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def make_gated_desc(T, D, F, act=SF_ACT_SILU) -> sf_gated_ffn_desc:
     return sf_gated_ffn_desc(T, D, F, act, 0)
 
@@ -652,7 +658,8 @@ def sf_fp4_quantize(X, fmt: int, scale: float, out=None, stream=None):
     rows, cols = X.shape
     n = _scale_bytes(rows, cols, fmt)
     if out is None:
-        out = torch.empty((rows, cols // 2), dtype=u8, device=X.device), torch.empty((n,), dtype=u8, device=X.device)
+        with _allocating(stream):
+            out = torch.empty((rows, cols // 2), dtype=u8, device=X.device), torch.empty((n,), dtype=u8, device=X.device)
     codes, scales = out
     _check(lib().sf_fp4_quantize(X.data_ptr(), rows, cols, ld, fmt, scale, _tensor(w, "codes", codes, u8, (rows, cols // 2), dev),
                                  _tensor(w, "scales", scales, u8, (n,), dev), _launch_stream(w, dev, stream)), w)
@@ -665,7 +672,8 @@ def sf_fp4_dequantize(codes, scales, fmt: int, alpha: float, out=None, stream=No
     rows, half = _matrix_shape(w, codes)
     cols = 2 * half
     if out is None:
-        out = torch.empty((rows, cols), dtype=torch.bfloat16, device=codes.device)
+        with _allocating(stream):
+            out = torch.empty((rows, cols), dtype=torch.bfloat16, device=codes.device)
     ld = _row_stride(w, "out", out)
     if out.shape != (rows, cols) or out.get_device() != dev:
         raise _refused(w, "out", out, torch.bfloat16, (rows, cols))
@@ -688,10 +696,10 @@ def sf_gemm_fp4(A, a_scales, B, b_scales, fmt: int, alpha: float, C_out=None, wo
     Nc, K = _matrix_shape(w, B)[0], 2 * half
     a, a_s = _tensor(w, "A", A, u8, (Mr, half), dev), _tensor(w, "a_scales", a_scales, u8, (_scale_bytes(Mr, K, fmt),), dev)
     b, b_s = _tensor(w, "B", B, u8, (Nc, half), dev), _tensor(w, "b_scales", b_scales, u8, (_scale_bytes(Nc, K, fmt),), dev)
-    if C_out is None:
-        C_out = torch.empty((Mr, Nc), dtype=torch.bfloat16, device=A.device)
-    if workspace is None:
-        workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device)
+    if C_out is None or workspace is None:
+        with _allocating(stream):
+            C_out = torch.empty((Mr, Nc), dtype=_BF16, device=A.device) if C_out is None else C_out
+            workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device) if workspace is None else workspace
     _check(lib().sf_gemm_fp4(a, a_s, b, b_s, fmt, _tensor(w, "C_out", C_out, _BF16, (Mr, Nc), dev), Mr, Nc, K, alpha,
                              *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
     return C_out
@@ -707,10 +715,10 @@ def sf_gemm_fp4_gated(A, a_scales, Bg, bg_scales, Bu, bu_scales, fmt: int, act: 
     a, a_s = _tensor(w, "A", A, u8, (Mr, half), dev), _tensor(w, "a_scales", a_scales, u8, (_scale_bytes(Mr, K, fmt),), dev)
     g, g_s = _tensor(w, "Bg", Bg, u8, shape, dev), _tensor(w, "bg_scales", bg_scales, u8, tiles, dev)
     u, u_s = _tensor(w, "Bu", Bu, u8, shape, dev), _tensor(w, "bu_scales", bu_scales, u8, tiles, dev)
-    if H_out is None:
-        H_out = torch.empty((Mr, Nc), dtype=torch.bfloat16, device=A.device)
-    if workspace is None:
-        workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device)
+    if H_out is None or workspace is None:
+        with _allocating(stream):
+            H_out = torch.empty((Mr, Nc), dtype=_BF16, device=A.device) if H_out is None else H_out
+            workspace = _workspace(sf_gemm_fp4_workspace_size(Mr, Nc, K), A.device) if workspace is None else workspace
     _check(lib().sf_gemm_fp4_gated(a, a_s, g, g_s, u, u_s, fmt, act, _tensor(w, "H_out", H_out, _BF16, (Mr, Nc), dev), Mr, Nc, K,
                                    alpha_g, alpha_u, *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
     return H_out

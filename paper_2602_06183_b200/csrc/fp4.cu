@@ -215,6 +215,13 @@ bool plain_power(float f, int* e) {
 
 int fmt_of(int format) { return format == SF_FP4_NV ? FMT_NV : format == SF_FP4_MX ? FMT_MX : -1; }
 
+Span codes_span(const void* p, int64_t rows, int64_t cols) { return {p, (size_t)rows * (size_t)cols / 2}; }
+Span scales_span(const void* p, int64_t rows, int64_t cols, int format) {
+  return {p, (size_t)ceil_div(rows, 128) * (size_t)scale_tiles(fmt_of(format), cols) * 512};
+}
+// bf16 rows, from the first element to the last
+Span rows_span(const void* p, int64_t rows, int64_t cols, int64_t ld) { return {p, 2 * ((size_t)(rows - 1) * (size_t)ld + (size_t)cols)}; }
+
 int fp4_shape(int64_t rows, int64_t cols, int format) {
   if (fmt_of(format) < 0) return SF_ERR_UNSUPPORTED;
   return rows < 0 || cols < 0 || cols % 32 || rows > kMaxSize || cols > kMaxSize ? SF_ERR_SHAPE : SF_OK;
@@ -230,8 +237,8 @@ extern "C" {
 int sf_fp4_sizes(int64_t rows, int64_t cols, int format, size_t* codes_bytes, size_t* scales_bytes) {
   SF_TRY(fp4_shape(rows, cols, format));
   if (!codes_bytes || !scales_bytes) return SF_ERR_NULL;
-  *codes_bytes = (size_t)rows * (size_t)cols / 2;
-  *scales_bytes = (size_t)ceil_div(rows, 128) * (size_t)scale_tiles(fmt_of(format), cols) * 512;
+  *codes_bytes = codes_span(nullptr, rows, cols).n;
+  *scales_bytes = scales_span(nullptr, rows, cols, format).n;
   return SF_OK;
 }
 
@@ -240,6 +247,7 @@ int sf_fp4_quantize(const void* X, int64_t rows, int64_t cols, int64_t ld, int f
   if (rows == 0 || cols == 0) return SF_OK;
   if (!X || !codes || !scales) return SF_ERR_NULL;
   if (ld < cols || ld % 8 || !aligned16(X) || !aligned16(codes) || !aligned16(scales)) return SF_ERR_ALIGN;
+  if (!apart({codes_span(codes, rows, cols), scales_span(scales, rows, cols, format)}, {rows_span(X, rows, cols, ld)})) return SF_ERR_UNSUPPORTED;
   const int fmt = fmt_of(format);
   const int64_t k_tiles = scale_tiles(fmt, cols);
   const QuantGrid g = quant_grid(rows, k_tiles * (fmt == FMT_NV ? 4 : 8));
@@ -261,6 +269,7 @@ int sf_fp4_dequantize(const void* codes, const void* scales, int64_t rows, int64
   if (rows == 0 || cols == 0) return SF_OK;
   if (!Y || !codes || !scales) return SF_ERR_NULL;
   if (ld < cols || ld % 8 || !aligned16(Y) || !aligned16(codes) || !aligned16(scales)) return SF_ERR_ALIGN;
+  if (!apart({rows_span(Y, rows, cols, ld)}, {codes_span(codes, rows, cols), scales_span(scales, rows, cols, format)})) return SF_ERR_UNSUPPORTED;
   const int fmt = fmt_of(format);
   const QuantGrid g = quant_grid(rows, cols / 8);
   if (g.blocks > 0x0FFFFFFF) return SF_ERR_SHAPE;
@@ -291,6 +300,9 @@ int sf_gemm_fp4(const void* A, const void* a_scales, const void* B, const void* 
   if (!A || !a_scales || !B || !b_scales || !C || !workspace) return SF_ERR_NULL;
   if (!aligned16(A) || !aligned16(a_scales) || !aligned16(B) || !aligned16(b_scales) || !aligned16(C) || !aligned16(workspace)) return SF_ERR_ALIGN;
   if (workspace_bytes < need) return SF_ERR_WORKSPACE;
+  if (!apart({rows_span(C, Mr, Nc, Nc), {workspace, need}}, {codes_span(A, Mr, K), scales_span(a_scales, Mr, K, format), codes_span(B, Nc, K),
+                                                            scales_span(b_scales, Nc, K, format)}))
+    return SF_ERR_UNSUPPORTED;
   SF_TRY(check_arch());
   const Operand a{A, a_scales}, b{B, b_scales};
   return format == SF_FP4_NV ? run_nt<FMT_NV>(a, b, Mr, Nc, K, alpha, C, (int*)workspace, (cudaStream_t)stream)
@@ -309,6 +321,10 @@ int sf_gemm_fp4_gated(const void* A, const void* a_scales, const void* Bg, const
       !aligned16(H) || !aligned16(workspace))
     return SF_ERR_ALIGN;
   if (workspace_bytes < need) return SF_ERR_WORKSPACE;
+  if (!apart({rows_span(H, Mr, Nc, Nc), {workspace, need}},
+             {codes_span(A, Mr, K), scales_span(a_scales, Mr, K, format), codes_span(Bg, Nc, K), scales_span(bg_scales, Nc, K, format),
+              codes_span(Bu, Nc, K), scales_span(bu_scales, Nc, K, format)}))
+    return SF_ERR_UNSUPPORTED;
   SF_TRY(check_arch());
   const Operand a{A, a_scales}, g{Bg, bg_scales}, u{Bu, bu_scales};
   return format == SF_FP4_NV

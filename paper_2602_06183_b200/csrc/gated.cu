@@ -8,8 +8,6 @@
 // tokens they are sums of two bf16 numbers, see kTwoTerms); P and
 // Q are kept in float32 (8 bytes a hidden value where bf16 would take 4), because dG and dU would otherwise be rounded two or three times: the
 // error of dWu against 64 bits is then 1.8 times that of a result that is rounded once at its end, with them it is 1.4 times.
-#include <initializer_list>
-
 #include "products.cuh"
 
 namespace sf {
@@ -158,6 +156,9 @@ int sf_gated_ffn_fwd(const sf_gated_ffn_desc* desc, const void* X, const void* W
       (fwd_ctx && !aligned16(fwd_ctx)))
     return SF_ERR_ALIGN;
   if ((fwd_ctx && fwd_ctx_bytes < z.h + 2 * z.f) || workspace_bytes < kStatus + (fwd_ctx ? 0 : z.h)) return SF_ERR_WORKSPACE;
+  const size_t td = 2 * (size_t)desc->T * (size_t)desc->D, df = 2 * (size_t)desc->D * (size_t)desc->F;
+  if (!apart({{Y, td}, {fwd_ctx, z.h + 2 * z.f}, {workspace, kStatus + (fwd_ctx ? 0 : z.h)}}, {{X, td}, {Wg, df}, {Wu, df}, {Wd, df}}))
+    return SF_ERR_UNSUPPORTED;
   SF_TRY(check_arch());
   cudaStream_t s = (cudaStream_t)stream;
   uint8_t* h = fwd_ctx ? (uint8_t*)fwd_ctx : (uint8_t*)workspace + kStatus;
@@ -193,6 +194,10 @@ int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const void* 
   if (!aligned16(dY) || !aligned16(X) || !aligned16(Wg) || !aligned16(Wu) || !aligned16(Wd) || !aligned16(fwd_ctx) || !aligned16(workspace))
     return SF_ERR_ALIGN;
   if (fwd_ctx_bytes < z.h + 2 * z.f || workspace_bytes < kStatus + 2 * z.h) return SF_ERR_WORKSPACE;
+  const size_t td = 2 * (size_t)T * (size_t)D, df = 2 * (size_t)D * (size_t)F;
+  if (!apart({{dX, td}, {dWg, df}, {dWu, df}, {dWd, df}, {workspace, kStatus + 2 * z.h}},
+             {{dY, td}, {X, td}, {Wg, df}, {Wu, df}, {Wd, df}, {fwd_ctx, z.h + 2 * z.f}}))
+    return SF_ERR_UNSUPPORTED;
   SF_TRY(check_arch());
   const uint8_t* h = (const uint8_t*)fwd_ctx;
   uint8_t* dg = (uint8_t*)workspace + kStatus;

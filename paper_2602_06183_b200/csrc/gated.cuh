@@ -4,6 +4,9 @@
 
 #include <cuda.h>
 
+#include <cstdint>
+#include <initializer_list>
+
 #include "gemm_tc.cuh"
 #include "sf_common.cuh"
 #include "tc_ptx.cuh"
@@ -57,9 +60,10 @@ __device__ __forceinline__ void gate_act(float g, float& a, float& da) {
     a = g * c;
     da = fmaf(g, 0.3989422804014327f * e, c);
   } else if constexpr (kAct == SF_ACT_GELU_TANH) {
-    // 0.5 (1 + tanh(z)) = sigmoid(2 z), z = sqrt(2 / pi) (g + 0.044715 g^3)
+    // 0.5 (1 + tanh(z)) = sigmoid(2 z), z = sqrt(2 / pi) (g + 0.044715 g^3); the sigmoid is 0 or 1 long before the square is cut off, which
+    // without that would be infinite from 2^64 on and meet a factor of 0 in the derivative
     constexpr float k = 1.5957691216057308f, c3 = 0.044715f;
-    const float g2 = g * g, s = sigmoid32(k * g * fmaf(c3, g2, 1.f));
+    const float g2 = fminf(g * g, 1e30f), s = sigmoid32(k * g * fmaf(c3, g2, 1.f));
     a = g * s;
     da = fmaf(a * (1.f - s), k * fmaf(3.f * c3, g2, 1.f), s);
   } else {
@@ -130,5 +134,25 @@ struct Operand {
   const void* data;
   const void* scales;
 };
+
+// Whether nothing that a call writes lies in what it reads or in something else that it writes. (The launches of a call read their inputs
+// while others store results, so a shared byte would give results that depend on the order.) Absent ones are NULL.
+struct Span {
+  const void* p;
+  size_t n;
+};
+inline bool meet(const Span& a, const Span& b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return x && y && x < y + b.n && y < x + a.n;
+}
+inline bool apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span* w = written.begin(); w != written.end(); ++w) {
+    for (const Span& r : read)
+      if (meet(*w, r)) return false;
+    for (const Span* v = written.begin(); v != w; ++v)
+      if (meet(*w, *v)) return false;
+  }
+  return true;
+}
 
 }  // namespace sf

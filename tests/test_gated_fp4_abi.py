@@ -46,6 +46,41 @@ def test_gated_calls_refuse_before_launching(lib):
     assert lib.sf_gated_ffn_fwd(C.byref(binding.make_gated_desc(0, 64, 128)), None, None, None, None, None, None, 0, None, 0, None) == SF_OK
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a call that were not refused would run on pointers to nothing")
+def test_shared_bytes_are_refused(lib):
+    """Every buffer far from the others but for the last byte of one and the first of another. (None of these calls gets past the check.)"""
+    at = {k: (i + 1) << 30 for i, k in enumerate("X Wg Wu Wd Y c w dY dX dWg dWu dWd".split())}
+    T, D, F = 24, 64, 128
+    d = binding.make_gated_desc(T, D, F)
+    ctx, ws = binding.sf_gated_ffn_workspace_size(d)
+    size = dict(X=2 * T * D, Y=2 * T * D, dY=2 * T * D, dX=2 * T * D, c=ctx, w=ws, **{k: 2 * D * F for k in "Wg Wu Wd dWg dWu dWd".split()})
+
+    def run(call, names, n_in):
+        for i, a in enumerate(names):
+            for b in names[:i]:
+                if i < n_in and names.index(b) < n_in:
+                    continue                                     # inputs may be one another
+                for x, y in ((a, b), (b, a)):                    # x ends on y's first 16 bytes
+                    p = dict(at)
+                    p[x] = at[y] + 16 - size[x]
+                    assert call(*(C.c_void_p(p[k]) for k in names)) == SF_ERR_UNSUPPORTED, (x, y)
+    size["w"] = 256                                                  # H lies in the context
+    run(lambda X, g, u, dn, Y, c, w: lib.sf_gated_ffn_fwd(C.byref(d), X, g, u, dn, Y, c, ctx, w, ws, None), "X Wg Wu Wd Y c w".split(), 4)
+    size["w"] = ws
+    run(lambda dY, X, g, u, dn, c, dX, dg, du, dd, w: lib.sf_gated_ffn_bwd(C.byref(d), dY, X, g, u, dn, c, ctx, dX, dg, du, dd, w, ws, None),
+        "dY X Wg Wu Wd c dX dWg dWu dWd w".split(), 6)
+
+    at = {k: (i + 1) << 30 for i, k in enumerate("A sa B sb U su C w X c s".split())}
+    M, N, K, ld = 130, 72, 96, 104
+    size = dict(A=M * K // 2, sa=2 * 2 * 512, B=N * K // 2, sb=2 * 512, U=N * K // 2, su=2 * 512, C=2 * M * N, w=256, c=M * K // 2, s=2 * 2 * 512,
+                X=2 * ((M - 1) * ld + K))
+    run(lambda A, sa, B, sb, Cc, w: lib.sf_gemm_fp4(A, sa, B, sb, 0, Cc, M, N, K, 1.0, w, 256, None), "A sa B sb C w".split(), 4)
+    run(lambda A, sa, B, sb, U, su, Cc, w: lib.sf_gemm_fp4_gated(A, sa, B, sb, U, su, 0, 0, Cc, M, N, K, 1.0, 1.0, w, 256, None),
+        "A sa B sb U su C w".split(), 6)
+    run(lambda X, c, s: lib.sf_fp4_quantize(X, M, K, ld, 0, 1.0, c, s, None), "X c s".split(), 1)
+    run(lambda c, s, X: lib.sf_fp4_dequantize(c, s, M, K, 0, 1.0, X, ld, None), "c s X".split(), 2)
+
+
 def test_fp4_calls_refuse_before_launching(lib):
     assert binding.sf_fp4_sizes(3, 96, binding.SF_FP4_NV) == (3 * 48, 2 * 512)
     assert binding.sf_fp4_sizes(129, 96, binding.SF_FP4_MX) == (129 * 48, 2 * 512)

@@ -191,6 +191,30 @@ def test_captured_and_replayed(M):
         assert np.array_equal(bits(C), want[i])
 
 
+def test_results_belong_to_the_stream_that_is_handed_over():
+    """Memory that the current stream may still be using is not given to a call on another one."""
+    M, N, K = 2048, 4096, 256
+    A, B = (binding.sf_fp4_quantize(to_dev(synth.normal_bf16((n, K), 0, 1, seed=n)), binding.SF_FP4_NV, 1.0) for n in (M, N))
+    want = bits(binding.sf_gemm_fp4(*A, *B, binding.SF_FP4_NV, 1.0))
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+
+    def freed(*shape, dtype=torch.bfloat16):
+        return torch.empty(shape, dtype=dtype, device="cuda").data_ptr()
+    at = freed(M, N)
+    C = binding.sf_gemm_fp4(*A, *B, binding.SF_FP4_NV, 1.0, stream=s)
+    s.synchronize()
+    assert C.data_ptr() != at and np.array_equal(bits(C), want)
+    at = freed(M, N)
+    assert binding.sf_gemm_fp4_gated(*A, *B, *B, binding.SF_FP4_NV, 0, 1.0, 1.0, stream=s).data_ptr() != at
+    at = freed(M, N // 2, dtype=torch.uint8)
+    q = binding.sf_fp4_quantize(C, binding.SF_FP4_NV, 1.0, stream=s)
+    assert q[0].data_ptr() != at
+    at = freed(M, N)
+    assert binding.sf_fp4_dequantize(*q, binding.SF_FP4_NV, 1.0, stream=s).data_ptr() != at
+    s.synchronize()
+
+
 @pytest.mark.parametrize("T", [1, 40, 300])
 def test_trained_block_served_on_four_bits(T):
     """The two halves together, as they are used: a training step of the block in bf16, an update of its weights, the weights quantised

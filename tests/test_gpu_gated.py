@@ -136,6 +136,53 @@ def test_activation_in_its_tails(act):
         assert not f32(b.Y.t)[:, 1:].any()
 
 
+@pytest.mark.parametrize("T", [3, 200])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh", "relu"])
+def test_gates_whose_square_is_infinite(act, T):
+    """Gates of +- 2^66 with U = 1: H, act'(G) and so every gradient are exact: zero, or a power of two times at most T."""
+    D, F, big, tiny = 8, 16, 2.0 ** 66, 2.0 ** -20
+    X, Wg, Wu, Wd, dY = np.zeros((T, D)), np.zeros((F, D)), np.zeros((F, D)), np.zeros((D, F)), np.zeros((T, D))
+    X[:, 0], X[:, 1], Wu[:, 1], dY[:, 2] = big, 1.0, 1.0, tiny
+    Wg[:8, 0], Wg[8:, 0], Wd[2, 0], Wd[2, 8] = 1.0, -1.0, 1.0, 1.0
+    b = Block(T, D, F, act, X, Wg, Wu, Wd, dY)
+    b.fwd()
+    b.bwd()
+    b.check()
+    on = np.zeros(F); on[0] = tiny                         # dH is that for features 0 and 8, whose gates are on and off   # noqa: E702
+    Y = np.zeros((T, D)); Y[:, 2] = big   # noqa: E702
+    dX = np.zeros((T, D)); dX[:, 0], dX[:, 1] = tiny, tiny * big   # noqa: E702
+    _same(b.Y.t, Y, "Y")
+    _same(b.out["dX"].t, dX, "dX")
+    _same(b.out["dWg"].t, np.outer(on, X.sum(0)), "dWg")
+    _same(b.out["dWu"].t, np.outer(on * big, X.sum(0)), "dWu")
+    _same(b.out["dWd"].t, np.outer(dY.sum(0), np.repeat([big, 0.0], 8)), "dWd")
+
+
+def test_buffers_side_by_side():
+    """Outputs that touch an input without sharing a byte are taken."""
+    T, D, F = 20, 64, 128
+    X, Wg, Wu, Wd, dY = _normals(T, D, F, 11)
+    apart = Block(T, D, F, "silu", X, Wg, Wu, Wd, dY)
+    apart.fwd()
+    apart.bwd()
+    shapes = [(T, D), (T, D), (F, D), (F, D), (F, D), (F, D), (D, F), (D, F), (T, D), (T, D)]     # X Y Wg dWg Wu dWu Wd dWd dY dX
+    room, views = torch.empty(sum(a * c for a, c in shapes), dtype=torch.bfloat16, device="cuda"), []
+    for s in shapes:
+        views.append(room[:s[0] * s[1]].view(s))
+        room = room[s[0] * s[1]:]
+    x, y, wg, dwg, wu, dwu, wd, dwd, dy, dx = views
+    for v, a in zip((x, wg, wu, wd, dy), (X, Wg, Wu, Wd, dY)):
+        v.copy_(_dev(a))
+    ctx, ws = binding.alloc_gated_ffn_buffers(apart.desc)
+    binding.sf_gated_ffn_fwd(apart.desc, x, wg, wu, wd, y, ctx, ws)
+    binding.sf_gated_ffn_bwd(apart.desc, dy, x, wg, wu, wd, ctx, dx, dwg, dwu, dwd, ws)
+    assert np.array_equal(bits(y), bits(apart.Y.t))
+    for k, v in zip(GRADS, (dx, dwg, dwu, dwd)):
+        assert np.array_equal(bits(v), bits(apart.out[k].t)), k
+    with pytest.raises(binding.SparseFFNError):
+        binding.sf_gated_ffn_bwd(apart.desc, dy, x, wg, wu, wd, ctx, dy, dwg, dwu, dwd, ws)       # the gradient in place
+
+
 def test_left_out_outputs():
     T, D, F = 70, 72, 136
     b = Block(T, D, F, "silu", *_normals(T, D, F, 5))
