@@ -66,7 +66,7 @@ struct PairCfg {
   static constexpr int kMaps = kKind == PK_DW ? 9 : kKind == PK_DX ? 5 : kKind == PK_NT ? (kFp4 ? 5 : 3)
                              : kKind == PK_FWD ? (kFp4 ? 7 : 4) : 6;
   static_assert(kBN == 256 || (kFp4 && kBN == 128), "tile width");
-  static_assert(kMode == PM_FULL || !kFp4, "4-bit operands: widths of whole row blocks of scales");
+  static_assert(kMode == PM_FULL || !kFp4 || (kMode == PM_SPLIT && kBN == 128), "4-bit operands: widths of whole row blocks of scales");
   static_assert(!kFp4 || kKind == PK_NT || (kKind == PK_FWD && kBN == 256), "4-bit operands: K-major, whole row blocks of scales");
   static_assert(kStages >= 3 && kSmem <= kPairSmemMax && kSmem > 228 * 1024 / 2, "one CTA per SM");
   static_assert(kScaleCol + 2 * kScaleCols <= 512, "TMEM columns");
@@ -220,7 +220,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
   const int b_chunks = (half + 63) >> 6;                   // MN-major B: chunks of 64 columns
   const bool sums = kKind == PK_DW && kMode != PM_SPLIT && args.term_rows > 0;
   const uint32_t stage_tx = sums   ? 2u * (uint32_t)(8192 + b_chunks * 4096)
-                            : kVar ? 2u * (uint32_t)(Cfg::kABytes + (Cfg::kBMN ? b_chunks * 8192 : half * 128)) : 2u * Cfg::kStageBytes;
+                            : kVar ? 2u * (uint32_t)(Cfg::kABytes + (Cfg::kBMN ? b_chunks * 8192 : half * 128) + Cfg::kScaleBytes)
+                                   : 2u * Cfg::kStageBytes;
   int num_tiles = args.num_m[0] * args.num_n[0];
   if (kKind == PK_DW)
     for (int j = 1; j < args.jobs; ++j) num_tiles += args.num_m[j] * args.num_n[j];

@@ -203,7 +203,27 @@ int launch_best(const PairArgs& a, cudaStream_t s, F&& make, PairPlan* taken = n
   return launch_plan<kKind>(plan, b, s, make);
 }
 
-template <int kFmt, int kBN>
+// A 4-bit product, by the same estimate: rounds of tiles of 256 or of 128 columns, a stage of either (bounded by what the L2 delivers), what a
+// tile costs beside; or tiles of 128 columns with the reduction split over two to four pairs of a cluster (300 x 1024 x 8192 12.0 us
+// unsplit, 8.9 over three; 513 x 1032 x 4096 8.3 and 7.8 over two; gated ones, whose sums are twice as many, gained nothing: 11.0 and 11.1
+// at 513 x 1032 x 4096).
+inline int plan_fp4(int64_t M, int64_t N, int64_t nkb, PairPlan* plan) {
+  const FewRoom* room;
+  SF_TRY((few_room<FMT_BF16, FK_NT, 16>(&room)));
+  const int64_t pairs = sm_count_now() / 2, tiles = tiles_of(M, N, 128);
+  const double wide = (double)ceil_div(tiles_of(M, N, 256), pairs) * (nkb * 600 + 900) + 4900;
+  const double narrow = (double)ceil_div(tiles, pairs) * (nkb * 450 + 200) + 2900;
+  *plan = wide <= narrow ? PairPlan{PM_FULL, 256, 1, 0, wide, 0} : PairPlan{PM_FULL, 128, 1, 0, narrow, 0};
+  for (int S = 2; S <= 4 && S <= nkb; ++S) {
+    const int64_t at_once = room->clusters[2 * S - 1];
+    if (at_once <= 0) continue;
+    const double c = (double)ceil_div(tiles, at_once) * ((double)ceil_div(nkb, S) * 450 + 4600 + (double)ceil_div(128, 64 * S) * (1000 + 250 * S));
+    if (c < 0.97 * plan->clocks) *plan = PairPlan{PM_SPLIT, 128, S, 0, c, 0};
+  }
+  return SF_OK;
+}
+
+template <int kFmt, int kBN, int kMode>
 int run_nt_fp4(const Operand& A, const Operand& B, int64_t K, void* C, const PairArgs& a, cudaStream_t s) {
   PairMaps<5> m;
   SF_TRY(kmajor_map(&m.m[0], kFmt, A.data, a.M[0], K, 128));
@@ -211,7 +231,7 @@ int run_nt_fp4(const Operand& A, const Operand& B, int64_t K, void* C, const Pai
   SF_TRY(make_tmap_store(&m.m[2], C, a.M[0], a.N[0]));
   SF_TRY(scale_map(&m.m[3], kFmt, A.scales, a.M[0], K));
   SF_TRY(scale_map(&m.m[4], kFmt, B.scales, a.N[0], K));
-  return launch_pair<PK_NT, kBN, kFmt, PM_FULL>(m, a, s);
+  return launch_pair<PK_NT, kBN, kFmt, kMode>(m, a, s);
 }
 
 // C[M, N] = alpha A B^T; M, N, K > 0. early_weights: the launch before this one is another product of the same call, which does not
@@ -235,10 +255,12 @@ int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, 
       return make_tmap_store(&m[2], C, M, N);
     });
   } else {
-    // rounds of tiles, a stage of 256 or of 128 columns (bounded by shared memory), and what a tile costs beside
-    const int64_t pairs = sm_count_now() / 2;
-    const int64_t wide = ceil_div(tiles_of(M, N, 256), pairs) * (nkb * 600 + 900), narrow = ceil_div(tiles_of(M, N, 128), pairs) * (nkb * 450 + 200);
-    return wide <= narrow ? run_nt_fp4<kFmt, 256>(A, B, K, C, a, s) : run_nt_fp4<kFmt, 128>(A, B, K, C, a, s);
+    PairPlan plan;
+    SF_TRY(plan_fp4(M, N, nkb, &plan));
+    a.bn = plan.bn; a.parts = plan.parts;
+    return plan.mode == PM_SPLIT ? run_nt_fp4<kFmt, 128, PM_SPLIT>(A, B, K, C, a, s)
+         : plan.bn == 256        ? run_nt_fp4<kFmt, 256, PM_FULL>(A, B, K, C, a, s)
+                                 : run_nt_fp4<kFmt, 128, PM_FULL>(A, B, K, C, a, s);
   }
 }
 

@@ -80,10 +80,11 @@ def _operand(rows, K, fmt, r, scales):
     return fp4.values(codes, by, fmt), _dev8(fp4.pack(codes)), _dev8(fp4.tile(by, fill=0xFF if fmt == "mx" else 0x7F))
 
 
-# powers of two from 1/2 to 2 (nv: E4M3 0x30, 0x38, 0x40): products are multiples of 1/16 below 144, sums of up to 2000 of them exact
+# powers of two from 1/2 to 2 (nv: E4M3 0x30, 0x38, 0x40): products are multiples of 1/16 below 144, sums of up to 7000 of them exact (below 2^20)
 SIMPLE = {"nv": [0x30, 0x38, 0x40], "mx": [126, 127, 128]}
 SHAPES = [(1, 8, 32), (1, 200, 96), (2, 128, 256), (5, 520, 1056), (16, 136, 288), (17, 264, 64), (33, 1032, 512), (64, 72, 800),
-          (65, 392, 160), (128, 128, 1024), (129, 8, 32), (129, 264, 320), (200, 136, 544), (256, 256, 256), (257, 520, 1312), (520, 776, 96)]
+          (65, 392, 160), (128, 128, 1024), (129, 8, 32), (129, 264, 320), (200, 136, 544), (256, 256, 256), (257, 520, 1312), (520, 776, 96),
+          (200, 136, 4096), (300, 1032, 4096), (513, 1032, 4096)]         # reductions split over four, three and two pairs
 
 
 def _same(got, ref, what):
