@@ -129,16 +129,19 @@ int sf_gated_ffn_step_plan(const sf_gated_ffn_desc* desc, sf_gated_ffn_plan* pla
     plan->form[i] = p.mode == PM_SPLIT ? SF_GATED_SPLIT : SF_GATED_TILES; plan->cols[i] = p.bn; plan->parts[i] = p.parts;
     return (int)SF_OK;
   };
-  if (T <= kFewTokens) {
+  if (gated_by_few(FMT_BF16, T, kd)) {
     SF_TRY(few(ActTag<FK_GATED>{}, SF_GATED_H, F, kd, 1));
-    SF_TRY(few(ActTag<FK_NT>{}, SF_GATED_Y, D, kf, terms_of(T)));
-    SF_TRY(few(ActTag<FK_BWD>{}, SF_GATED_DH, F, kd, 1));
-    SF_TRY(few(ActTag<FK_DX>{}, SF_GATED_DX, D, 2 * kf, terms_of(T)));
     plan->form[SF_GATED_H_KEPT] = plan->form[SF_GATED_H]; plan->cols[SF_GATED_H_KEPT] = plan->cols[SF_GATED_H];
     plan->parts[SF_GATED_H_KEPT] = plan->parts[SF_GATED_H];
   } else {
     SF_TRY(pairs(PK_FWD, SF_GATED_H, {{T, F}}, kd));
     SF_TRY(pairs(PK_FWD_SAVE, SF_GATED_H_KEPT, {{T, F}}, kd));
+  }
+  if (T <= kFewTokens) {
+    SF_TRY(few(ActTag<FK_NT>{}, SF_GATED_Y, D, kf, terms_of(T)));
+    SF_TRY(few(ActTag<FK_BWD>{}, SF_GATED_DH, F, kd, 1));
+    SF_TRY(few(ActTag<FK_DX>{}, SF_GATED_DX, D, 2 * kf, terms_of(T)));
+  } else {
     SF_TRY(pairs(PK_NT, SF_GATED_Y, {{T, D}}, kf));
     SF_TRY(pairs(PK_BWD, SF_GATED_DH, {{T, F}}, kd));
     SF_TRY(pairs(PK_DX, SF_GATED_DX, {{T, D}}, 2 * kf));

@@ -18,12 +18,14 @@ namespace {
 
 // Up to this many tokens the weights are streamed past them (few_tokens.cuh), which is the better side where the weights are large.
 // Few tokens against pairs, us: forward of 77 x 1408 x 5504 20 / 28, of 128 x 2048 x 2048 17.8 / 21.3, 100 x 8192 x 1024 of 4 bits
-// 7.3 / 11.7; the other way for small weights (forward of 100 x 512 x 512 10.0 / 8.8, 100 x 1024 x 1024 gated of 4 bits 8.7 / 6.8) and
-// at the upper end (step of 128 x 2048 x 8192 128 / 116).
-#ifndef SF_FEW_TOKENS
-#define SF_FEW_TOKENS 128
-#endif
-constexpr int64_t kFewTokens = SF_FEW_TOKENS;
+// 7.3 / 11.7; the other way at the upper end (step of 128 x 2048 x 8192 128 / 116).
+constexpr int64_t kFewTokens = 128;
+
+// Two projections are an exception beyond 64 tokens where the reduction is short: there is little of it to split, and the sums of twice the
+// columns through shared memory are most of the time. Forward of the block, both projections by few tokens / on pairs, us back to back:
+// 123 x 360 x 264 19.1 / 11.9, 100 x 512 x 512 14.4 / 11.2, 128 x 1024 x 1024 16.0 / 13.2; but 128 x 2048 x 2048 18.1 / 20.0. The projections of
+// 4 bits alone, 128 x 512 x 512 7.9 / 6.1, 128 x 4096 x 2048 10.5 / 9.1; but 70 x 2048 x 4096 8.3 / 10.8, 96 x 1024 x 8192 11.5 / 15.5.
+inline bool gated_by_few(int fmt, int64_t T, int nkb) { return T <= 64 || (T <= kFewTokens && nkb > (fmt == FMT_BF16 ? 16 : 8)); }
 
 // Up to this many tokens the operands in between (H, dG, dU) are held as sums of two bf16 numbers, which the few-token products take as
 // twice the tokens: there is room for them in the instruction's columns, and the products wait for the weights. With so few tokens
@@ -270,7 +272,7 @@ template <int kFmt>
 int run_gated(const Operand& A, const Operand& Bg, const Operand& Bu, int64_t M, int64_t N, int64_t K, int act, float alpha_g,
               float alpha_u, void* H, float* P, float* Q, int* status, cudaStream_t s, int terms = 1) {
   const int nkb = k_blocks(kFmt, K);
-  if (M <= kFewTokens) {
+  if (gated_by_few(kFmt, M, nkb)) {
     FewArgs a{};
     a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.act = act; a.alpha = alpha_g; a.alpha2 = alpha_u; a.C = H; a.P = P; a.Q = Q;
     a.status = status; a.in_terms = 1; a.out_terms = terms;

@@ -72,7 +72,7 @@ SHAPES = [(1, 8, 8), (1, 264, 520), (2, 72, 136), (7, 1000, 328), (16, 64, 128),
 # of narrower width, and reductions split over two to four pairs
 FORM_SHAPES = [(130, 1408, 8), (130, 8, 1032), (257, 392, 1160), (513, 256, 2048), (513, 520, 2048), (513, 776, 1160), (513, 2048, 520),
                (513, 1024, 1032), (513, 1408, 1032), (1000, 8, 8), (1500, 1032, 8), (1000, 4096, 520), (3000, 256, 2048),
-               (3000, 1024, 1160), (4096, 776, 264), (1295, 1120, 2360)]
+               (3000, 1024, 1160), (4096, 776, 264), (1295, 1120, 2360), (65, 1096, 136), (128, 1032, 200)]
 
 
 @pytest.mark.parametrize("T,D,F", SHAPES + FORM_SHAPES)
