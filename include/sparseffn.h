@@ -315,7 +315,8 @@ SF_API int sf_ffn_step_host(const sf_ffn_desc* desc, int dense, const void* host
  *
  * T >= 0 of any size (a single token and a training batch take the same call); D and F positive multiples of 8; each size at most
  * 2^28. Tensors are contiguous. One rounding each: H (an operand of the second product; with T <= 16 a sum of two bf16 numbers) and Y; G
- * and U stay in float32. A non-finite value makes the results that it enters non-finite.
+ * and U stay in float32. A NaN makes the results that it enters NaN, whatever the activation; an infinity makes them infinite or NaN, but for a
+ * gate of -infinity under the two ReLUs, whose value and derivative are 0.
  *
  * sf_gated_ffn_fwd:  fwd_ctx NULL: inference, H lies in the workspace. Otherwise fwd_ctx receives what the backward pass needs: H in
  *     bf16, act(G) and U act'(G) in float32 (10 bytes per token and feature, 12 with T <= 16). Y is the same either way.

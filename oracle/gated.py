@@ -31,7 +31,7 @@ def act(name, g):
             s, t = 1 / (1 + np.exp(-2 * z)), 1 / (1 + np.exp(2 * z))      # (1 + tanh z) / 2, which cancels below, and (1 - tanh z) / 2
         return g * s, s + 2 * g * s * t * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * g * g)
     r = np.maximum(g, 0.0)
-    return (r, (g > 0).astype(np.float64)) if name == "relu" else (r * r, 2 * r)
+    return (r, np.where(np.isnan(g), g, g > 0)) if name == "relu" else (r * r, 2 * r)
 
 
 def rne_bf16(x):

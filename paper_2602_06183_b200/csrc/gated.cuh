@@ -25,6 +25,12 @@ __device__ __forceinline__ float rcp32(float x) {
   asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// max(x, 0) that keeps a NaN, as the products and the other activations do (fmaxf answers 0).
+__device__ __forceinline__ float relu32(float x) {
+  float r;
+  asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ float sigmoid32(float x) { return rcp32(1.f + __expf(-x)); }
 
 // The normal distribution from its tail, Phi(-x) = e^(-x^2 / 2) p(1 / (1 + 0.3 x)) for x >= 0: the tail over its exponential is smooth in that
@@ -67,9 +73,9 @@ __device__ __forceinline__ void gate_act(float g, float& a, float& da) {
     a = g * s;
     da = fmaf(a * (1.f - s), k * fmaf(3.f * c3, g2, 1.f), s);
   } else {
-    const float r = fmaxf(g, 0.f);
+    const float r = relu32(g);
     a = kAct == SF_ACT_RELU ? r : r * r;
-    da = kAct == SF_ACT_RELU ? (g > 0.f ? 1.f : 0.f) : 2.f * r;
+    da = kAct == SF_ACT_RELU ? (r > 0.f ? 1.f : r) : 2.f * r;
   }
 }
 

@@ -36,6 +36,12 @@ def test_backward_is_the_difference_of_forward(name):
             assert abs((hi - lo) / (2 * h) - grads[k][0][i]) < 1e-6 * max(1.0, abs(grads[k][0][i]))
 
 
+@pytest.mark.parametrize("name", gated.ACTS)
+def test_a_gate_that_is_not_a_number_stays_one(name):
+    P, dP = gated.act(name, np.array([np.nan, -1.0, 2.0]))
+    assert np.isnan(P).tolist() == [True, False, False] and np.isnan(dP).tolist() == [True, False, False]
+
+
 def test_e2m1_ties_and_clamping():
     y = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 5.0001, 7.0, np.inf, -0.25, -0.75, -9.0], np.float32)
     want = [0.0, 1.0, 1.0, 2.0, 2.0, 4.0, 4.0, 6.0, 6.0, 6.0, -0.0, -1.0, -6.0]
