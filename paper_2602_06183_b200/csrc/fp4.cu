@@ -185,11 +185,13 @@ dequantize_fp4_kernel(const uint32_t* __restrict__ codes, const uint8_t* __restr
         o[i] = *reinterpret_cast<const uint32_t*>(&r);
       }
     } else {
-      const float sf = scale_value(by[j], kFmt);
+      // (up to 6 2^127 leaves float32 before the product with a small alpha brings it back: two powers of two change sides, exactly)
+      const bool far = kFmt == FMT_MX && by[j] >= 250u && by[j] < 255u && fabsf(alpha) < 1.f;
+      const float sf = scale_value(far ? by[j] - 2u : by[j], kFmt), al = far ? 4.f * alpha : alpha;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const __half2 h = __half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(q[j] >> (8 * i) & 0xFFu), __NV_E2M1));
-        o[i] = bf16x2(__fmul_rn(__fmul_rn(__low2float(h), sf), alpha), __fmul_rn(__fmul_rn(__high2float(h), sf), alpha));
+        o[i] = bf16x2(__fmul_rn(__fmul_rn(__low2float(h), sf), al), __fmul_rn(__fmul_rn(__high2float(h), sf), al));
       }
     }
     if (row_of(j) < rows && unit_of(j) < units)
