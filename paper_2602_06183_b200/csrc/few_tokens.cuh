@@ -176,6 +176,9 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
   tc_fence_after();
   const uint32_t tmem_base = ctl->tmem_base;
 
+  // The launch before this one writes the tokens, and may read what this one writes. Waiting here also keeps that launch's time out of the
+  // budgets of the roles' own waits, which the first tokens end.
+  if (warp != 0) pdl_wait();
   if (warp == 0) {
     const bool issues = elect_one();
     // what fits the ring of weights that are known to be there is fetched while the launch before this one ends
@@ -272,7 +275,6 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
     tc_fence_after();
     tmem_dealloc(tmem_base, Cfg::kTmem);
   }
-  pdl_wait();                                              // (the producer has waited; the output may be read by the launch before)
   // the cluster's threads share the sums, four neighbouring output columns to a thread; all partial sums of a value are fetched at once
   const uint32_t part = smem_u32(smem);
   for (int i = rank * kFewThreads + threadIdx.x; i < args.T * 32; i += S * kFewThreads) {

@@ -46,3 +46,25 @@ def test_kernels_that_take_all_of_tmem_have_an_sm_to_themselves():
     allocating = [b for b in re.split(r"\n__global__ ", text)[1:] if "tmem_alloc" in b[:b.index("\n}\n")]]
     assert len(allocating) == 3
     assert len(re.findall(r"static_assert\(.*kExclusiveSmem", text)) == 3          # one-CTA, CTA-pair and 512-row kernels
+
+
+def test_bounded_waits_begin_behind_the_launch_before():
+    """A wait's budget counts from its first poll. A role that polls for operands which are only loaded once the launch before this one
+    has ended would spend the budget on that launch: so every role waits for that launch first, by an instruction that has no budget. (A launch that
+    runs beside the one before it, and does not read its results, is the exception.)"""
+    checked = []
+    for p in sorted(glob.glob(os.path.join(CSRC, "*.cu*"))):
+        text = open(p).read()
+        for body in re.split(r"\n__global__ ", text)[1:]:
+            body = body[:body.index("\n}\n")]
+            if "mbar_wait" not in body or "pdl_wait" not in body:
+                continue
+            name = re.search(r"\b(\w+_kernel)\(", body).group(1)
+            checked.append(name)
+            before = body[:body.index("mbar_wait")]                          # (of the first role; what all of them run is indented by two)
+            if re.search(r"\n  (if \(!args\.beside\) )?pdl_wait\(\);", before):
+                continue
+            # the role that loads may fetch what it knows to be there first
+            assert re.search(r"\n  if \(warp != 0\) pdl_wait\(\);\n  if \(warp == 0\) {\n", before), name
+            assert re.search(r"\n    pdl_wait\(\);", before), name
+    assert {"pair_product_kernel", "few_tokens_kernel"} <= set(checked) and len(checked) >= 5, checked
