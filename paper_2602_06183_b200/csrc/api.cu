@@ -3,18 +3,18 @@
 
 namespace sf {
 
-int g_last_cuda_error = 0;
+std::atomic<int> g_last_cuda_error{0};
 
 int check_arch() {
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
-  static int cached_major[64] = {0};
+  static std::atomic<int> cached_major[64]{};
   if (dev >= 0 && dev < 64 && cached_major[dev] == 0) {
     int major = 0;
     SF_CUDA_TRY(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
     cached_major[dev] = major;
   }
-  const int major = (dev >= 0 && dev < 64) ? cached_major[dev] : 0;
+  const int major = (dev >= 0 && dev < 64) ? cached_major[dev].load() : 0;
   return major == 10 ? SF_OK : SF_ERR_ARCH;
 }
 

@@ -15,8 +15,6 @@
 // cluster barriers are reached by every warp because their own waits are.
 #pragma once
 
-#include <atomic>
-
 #include "gated.cuh"
 
 namespace sf {

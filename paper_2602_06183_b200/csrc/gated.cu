@@ -13,7 +13,7 @@
 namespace sf {
 
 int sm_count_now() {
-  static int n[64] = {0};
+  static std::atomic<int> n[64]{};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return 148; }
   if (n[dev] == 0) {
@@ -30,7 +30,7 @@ int encode(void* map, CUtensorMapDataType type, int rank, const void* base, cons
            const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
   typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  static Encode fn = nullptr;
+  static std::atomic<Encode> fn{nullptr};
   if (!fn) {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -39,7 +39,7 @@ int encode(void* map, CUtensorMapDataType type, int rank, const void* base, cons
     fn = reinterpret_cast<Encode>(p);
   }
   const cuuint32_t one[3] = {1, 1, 1};
-  const CUresult r = fn(reinterpret_cast<CUtensorMap*>(map), type, rank, const_cast<void*>(base), dims, strides, box, one,
+  const CUresult r = fn.load()(reinterpret_cast<CUtensorMap*>(map), type, rank, const_cast<void*>(base), dims, strides, box, one,
                         CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r == CUDA_SUCCESS) return SF_OK;
   g_last_cuda_error = (int)r;

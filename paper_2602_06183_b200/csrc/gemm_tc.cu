@@ -1851,7 +1851,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 EncodeTiledFn get_encode_fn() {
-  static EncodeTiledFn fn = nullptr;
+  static std::atomic<EncodeTiledFn> fn{nullptr};
   if (!fn) {
     void* p = nullptr;
     cudaDriverEntryPointQueryResult qres;
@@ -1891,7 +1891,7 @@ int make_store_map(CUtensorMap* m, void* C, int64_t rows, int64_t cols, int64_t 
 }
 
 int sm_count() {
-  static int n[64] = {0};
+  static std::atomic<int> n[64]{};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
   if (n[dev] == 0) {
@@ -1905,7 +1905,7 @@ int sm_count() {
 template <int kMode, bool kAMN, bool kBMN, int kEpi>
 int launch_one(const CUtensorMap& ta, const CUtensorMap& tb, const GemmArgs& a, cudaStream_t s) {
   auto kern = gemm_tc_kernel<kMode, kAMN, kBMN, kEpi>;
-  static bool attr_done[64] = {false};
+  static std::atomic<bool> attr_done[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_done[dev]) {
@@ -1935,7 +1935,7 @@ int launch_two(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& 
   constexpr bool tma_store = tma_store2(kEpi, kExpand != 0, kVar);
   constexpr int smem = smem_bytes2(kMode != MODE_DENSE, kBN, kEpi, kExpand != 0, kFp8, tma_store ? (threads / 32 - 2) * store_bufs2(kMode != MODE_DENSE, kEpi) : 0);
   static_assert(smem <= 232448 && smem >= kExclusiveSmem, "shared memory per CTA: fits, and one CTA per SM");
-  static bool attr_done[64] = {false};
+  static std::atomic<bool> attr_done[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_done[dev]) {
@@ -1960,7 +1960,7 @@ int launch_two(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& 
 }
 
 int64_t l2_bytes() {
-  static int n[64] = {0};
+  static std::atomic<int> n[64]{};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 126 << 20;
   if (n[dev] == 0) {
@@ -1985,7 +1985,7 @@ int launch_tall(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap&
   auto kern = gemm_tall_kernel<kBMN, kEpi, kFp8>;
   constexpr int smem = tall_smem(kEpi, kBMN, kFp8);
   static_assert(smem <= 232448 && smem >= kExclusiveSmem, "shared memory per CTA: fits, and one CTA per SM");
-  static bool attr_done[64] = {false};
+  static std::atomic<bool> attr_done[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_done[dev]) {

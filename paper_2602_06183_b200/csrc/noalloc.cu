@@ -21,7 +21,7 @@ static __device__ __align__(256) unsigned char g_noalloc_scratch[kNoAllocStatusB
 // only a handle for the runtime; the address a kernel can use comes from cudaGetSymbolAddress with
 // the owning device current.
 int noalloc_scratch(unsigned char** out) {
-  static unsigned char* cached[64] = {nullptr};
+  static std::atomic<unsigned char*> cached[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return SF_ERR_UNSUPPORTED;

@@ -597,7 +597,7 @@ template <int kKind, int kBN, int kFmt, int kMode>
 int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps>& maps, PairArgs a, cudaStream_t s) {
   using Cfg = PairCfg<kKind, kBN, kFmt, kMode>;
   auto kern = pair_product_kernel<kKind, kBN, kFmt, kMode>;
-  static bool attr_done[64] = {false};
+  static std::atomic<bool> attr_done[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_done[dev]) {

@@ -388,15 +388,17 @@ int launch_prune24(const void* W, int64_t rows, int64_t cols, int64_t ld, int gr
     const int64_t px = (cols + kPanelC - 1) / kPanelC, py = (rows + kPanelK - 1) / kPanelK;
     if (px * py > (int64_t)1 << 30) return SF_ERR_SHAPE;
     const int num_panels = (int)(px * py);
-    static bool attr_done[64] = {false};
-    static int sms[64] = {0};
+    static std::atomic<bool> attr_done[64]{};
+    static std::atomic<int> sms[64]{};
     int dev = 0;
     SF_CUDA_TRY(cudaGetDevice(&dev));
     if (dev < 0 || dev >= 64) return SF_ERR_UNSUPPORTED;
     if (!attr_done[dev]) {
       SF_CUDA_TRY(cudaFuncSetAttribute(prune24_cols_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kColsSmemBytes));
       SF_CUDA_TRY(cudaFuncSetAttribute(prune24_cols_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kColsSmemBytes));
-      SF_CUDA_TRY(cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev));
+      int count = 0;
+      SF_CUDA_TRY(cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, dev));
+      sms[dev] = count;
       attr_done[dev] = true;
     }
     alignas(64) CUtensorMap tm, tv;
@@ -417,15 +419,17 @@ int launch_prune24_cols_fp8(const void* W, int64_t rows, int64_t cols, int64_t l
   const int64_t px = (cols + kPanelC - 1) / kPanelC, py = (rows + kPanelK - 1) / kPanelK;
   if (px * py > (int64_t)1 << 30) return SF_ERR_SHAPE;
   const int num_panels = (int)(px * py);
-  static bool attr_done[64] = {false};
-  static int sms[64] = {0};
+  static std::atomic<bool> attr_done[64]{};
+  static std::atomic<int> sms[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return SF_ERR_UNSUPPORTED;
   if (!attr_done[dev]) {
     SF_CUDA_TRY(cudaFuncSetAttribute(prune24_cols_kernel<false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kColsSmemBytes));
     SF_CUDA_TRY(cudaFuncSetAttribute(prune24_cols_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kColsSmemBytes));
-    SF_CUDA_TRY(cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev));
+    int count = 0;
+    SF_CUDA_TRY(cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, dev));
+    sms[dev] = count;
     attr_done[dev] = true;
   }
   alignas(64) CUtensorMap tm;

@@ -427,7 +427,7 @@ int sf_routed_ffn_fwd(const sf_router_desc* desc, const void* X, const void* W1,
   }
   trace_mark(s);
   // step 2: token order, tile tables, gathered X
-  static bool attr_done[64] = {false};
+  static std::atomic<bool> attr_done[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   const int gsm = (d.E * 1024 + kMaxExperts + 1) * 4;

@@ -5,14 +5,18 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <utility>
 
 #include "../../include/sparseffn.h"
 
 namespace sf {
 
+// What the entry points remember (attributes that are set, properties of a device, addresses) is found once a process, by whichever threads come
+// first: each finds and stores the same value, in a std::atomic, which also orders what it stands for.
+
 // Most recent failing cudaError_t (process-wide, informational).
-extern int g_last_cuda_error;
+extern std::atomic<int> g_last_cuda_error;
 
 // Reports a failed call as a status. The runtime keeps a failed call's error until it is asked for it: it is taken out here, or
 // the next launch check of this host thread would report it as its own.

@@ -467,7 +467,7 @@ int launch_vnm(const void* P, int64_t T, int64_t F, int64_t ld, int V, int M, in
                void* vals24, void* meta24, void* meta24_hw, void* relu24, cudaStream_t s) {
   if (T == 0 || F == 0) return SF_OK;
   const size_t smem = (size_t)V * (kCW + kPad) * 2 + kCW * 4 + kCW + kCW;
-  static bool attr_set[64] = {false};                         // per device
+  static std::atomic<bool> attr_set[64]{};                         // per device
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_set[dev]) {
@@ -485,7 +485,7 @@ int launch_vnm(const void* P, int64_t T, int64_t F, int64_t ld, int V, int M, in
     // 256-column strips measured as fast as 128-column ones at V = 128 and 15 % faster at V = 64
     // (the kernel is bound by instruction issue, not by resident CTAs)
     constexpr int kW8 = 256;
-    static bool attr8[64] = {false};
+    static std::atomic<bool> attr8[64]{};
     if (dev < 0 || dev >= 64 || !attr8[dev]) {
       SF_CUDA_TRY(cudaFuncSetAttribute(vnm8_kernel<kW8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        128 * (kW8 + kPad) * 2 + kW8 * 6 + (kW8 / 8) * 7 * 17));

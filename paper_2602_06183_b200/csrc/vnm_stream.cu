@@ -445,8 +445,8 @@ static int launch_stream_t(const void* P, int64_t T, int64_t F, int64_t ld, int 
   int st = make_tmap_2d(&tm, P, T, F, ld, kSW, (uint32_t)V, false);
   if (st != SF_OK) return st;
   const size_t smem = 128 + (size_t)kSlots * V * kSW * 2 + kSlots * sizeof(StripAux<kSW>) + sizeof(StreamCtl);
-  static bool attr_done[64] = {false};
-  static int sms[64] = {0};
+  static std::atomic<bool> attr_done[64]{};
+  static std::atomic<int> sms[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return SF_ERR_UNSUPPORTED;
@@ -454,7 +454,9 @@ static int launch_stream_t(const void* P, int64_t T, int64_t F, int64_t ld, int 
     SF_CUDA_TRY(cudaFuncSetAttribute(vnm_stream_kernel<kSW, kM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      128 + kSlots * 128 * kSW * 2 + kSlots * (int)sizeof(StripAux<kSW>) +
                                          (int)sizeof(StreamCtl)));
-    SF_CUDA_TRY(cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev));
+    int count = 0;
+    SF_CUDA_TRY(cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, dev));
+    sms[dev] = count;
     attr_done[dev] = true;
   }
   const int64_t nstrips = (T / V) * ((F + kSW - 1) / kSW);
@@ -474,14 +476,16 @@ static int launch_stream8(const void* P, int64_t T, int64_t F, int64_t ld, int V
   constexpr int kSlotAux = (kSW / 8) * (int)sizeof(Stream8Sel), kMost = 96 * 1024 + 8 * 1024;
   const int strip = V * kSW * 2, fit = 96 * 1024 / strip, nslots = fit < 3 ? 3 : fit > kMaxSlots8 ? kMaxSlots8 : fit;
   const size_t smem = 1024 + (size_t)nslots * (strip + kSlotAux) + sizeof(Stream8Ctl);
-  static bool attr_done[64] = {false};
-  static int sms[64] = {0};
+  static std::atomic<bool> attr_done[64]{};
+  static std::atomic<int> sms[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return SF_ERR_UNSUPPORTED;
   if (!attr_done[dev]) {
     SF_CUDA_TRY(cudaFuncSetAttribute(vnm8_stream_kernel<kSW>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
-    SF_CUDA_TRY(cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev));
+    int count = 0;
+    SF_CUDA_TRY(cudaDeviceGetAttribute(&count, cudaDevAttrMultiProcessorCount, dev));
+    sms[dev] = count;
     attr_done[dev] = true;
   }
   const int64_t nstrips = (T / V) * ((F + kSW - 1) / kSW), resident = (int64_t)sms[dev] * 2;     // two CTAs of 101 KB at most
