@@ -26,30 +26,10 @@ int sm_count_now() {
 
 namespace {
 
-int encode(void* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
-           const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
-  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  static std::atomic<Encode> fn{nullptr};
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
-      return cuda_fail(cudaErrorUnknown);
-    fn = reinterpret_cast<Encode>(p);
-  }
-  const cuuint32_t one[3] = {1, 1, 1};
-  const CUresult r = fn.load()(reinterpret_cast<CUtensorMap*>(map), type, rank, const_cast<void*>(base), dims, strides, box, one,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r == CUDA_SUCCESS) return SF_OK;
-  g_last_cuda_error = (int)r;
-  return SF_ERR_CUDA;
-}
-
 int encode_2d(void* map, CUtensorMapDataType type, int bytes, const void* base, int64_t rows, int64_t cols, CUtensorMapSwizzle swizzle) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)cols * bytes};
   const cuuint32_t box[2] = {32, 32};
-  return encode(map, type, 2, base, dims, strides, box, swizzle);
+  return encode_map(map, type, 2, base, dims, strides, box, swizzle);
 }
 
 }  // namespace
@@ -63,7 +43,7 @@ int make_tmap_store(void* map, void* base, int64_t rows, int64_t cols) {
 int make_tmap_scales(void* map, const void* base, int64_t row_blocks, int64_t k_tiles, uint32_t box_tiles) {
   const cuuint64_t dims[3] = {128, (cuuint64_t)k_tiles, (cuuint64_t)row_blocks}, strides[2] = {512, 512 * (cuuint64_t)k_tiles};
   const cuuint32_t box[3] = {128, box_tiles, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+  return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 namespace {

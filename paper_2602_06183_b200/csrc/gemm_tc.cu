@@ -1846,43 +1846,16 @@ gemm_tall_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constan
 
 // ---- host side -----------------------------------------------------------------------------------
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encode_fn() {
-  static std::atomic<EncodeTiledFn> fn{nullptr};
-  if (!fn) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) != cudaSuccess ||
-        qres != cudaDriverEntryPointSuccess)
-      return nullptr;
-    fn = reinterpret_cast<EncodeTiledFn>(p);
-  }
-  return fn;
-}
-
 // 2D tensor map over a row-major [rows, cols] matrix of 2-byte (bf16, uint16) or 4-byte (uint32) elements;
 // box = {box_cols, box_rows}.
 int make_tmap(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols,
               uint32_t box_rows, CUtensorMapSwizzle swz, int kind = 0 /* 0 bf16, 1 uint32, 2 uint16 */) {
-  EncodeTiledFn fn = get_encode_fn();
-  if (!fn) return cuda_fail(cudaErrorUnknown);
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const bool u32 = kind == 1;
   cuuint64_t strides[1] = {(cuuint64_t)ld * (u32 ? 4 : 2)};
   cuuint32_t box[2] = {box_cols, box_rows};
-  cuuint32_t estr[2] = {1, 1};
-  CUresult r = fn(m, u32 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : (kind == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16), 2,
-                  const_cast<void*>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) {
-    g_last_cuda_error = (int)r;
-    return SF_ERR_CUDA;
-  }
-  return SF_OK;
+  return encode_map(m, u32 ? CU_TENSOR_MAP_DATA_TYPE_UINT32 : (kind == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16), 2,
+                    base, dims, strides, box, swz);
 }
 
 // Map of a plain store: C [rows, cols] bf16, chunks of 32 x 32 (see store_chunk).
@@ -2092,6 +2065,37 @@ bool use_two_cta(int64_t M) { return M >= 256; }
 
 int gemm_cta_pairs() { return sm_count() / 2; }
 
+int encode_map(void* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+               const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
+  typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static std::atomic<Encode> found{nullptr};
+  Encode fn = found;
+  if (!fn) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+      return cuda_fail(cudaErrorUnknown);
+    found = fn = reinterpret_cast<Encode>(p);
+  }
+  const cuuint32_t one[3] = {1, 1, 1};
+  auto encode = [&] {
+    return fn(reinterpret_cast<CUtensorMap*>(map), type, rank, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  };
+  CUresult r = encode();
+  // The driver wants a context, which a host thread has from its first runtime call that needs one; this may be the thread's first call.
+  if (r == CUDA_ERROR_INVALID_CONTEXT) {
+    int dev = 0;
+    SF_CUDA_TRY(cudaGetDevice(&dev));
+    SF_CUDA_TRY(cudaSetDevice(dev));
+    r = encode();
+  }
+  if (r == CUDA_SUCCESS) return SF_OK;
+  g_last_cuda_error = (int)r;
+  return SF_ERR_CUDA;
+}
+
 int make_tmap_2d(void* map, const void* base, int64_t rows, int64_t cols, int64_t ld, uint32_t box_cols,
                  uint32_t box_rows, bool swizzle128) {
   return make_tmap(reinterpret_cast<CUtensorMap*>(map), base, rows, cols, ld, box_cols, box_rows,
@@ -2099,17 +2103,10 @@ int make_tmap_2d(void* map, const void* base, int64_t rows, int64_t cols, int64_
 }
 
 int make_tmap_pairs(void* map, const void* base, int64_t rows, int64_t cols, uint32_t box_cols, uint32_t box_pairs) {
-  EncodeTiledFn fn = get_encode_fn();
-  if (!fn) return cuda_fail(cudaErrorUnknown);
   cuuint64_t dims[3] = {(cuuint64_t)cols, 2, (cuuint64_t)rows / 2};
   cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * 4};
-  cuuint32_t box[3] = {box_cols, 1, box_pairs}, estr[3] = {1, 1, 1};
-  const CUresult r = fn(reinterpret_cast<CUtensorMap*>(map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
-                        box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r == CUDA_SUCCESS) return SF_OK;
-  g_last_cuda_error = (int)r;
-  return SF_ERR_CUDA;
+  cuuint32_t box[3] = {box_cols, 1, box_pairs};
+  return encode_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 int gemm_dense(const void* A, bool a_kmajor, const void* B, bool b_kmajor, int64_t M, int64_t N, int64_t K, int epi,

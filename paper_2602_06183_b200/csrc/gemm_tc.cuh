@@ -1,6 +1,7 @@
 // Internal interface of the tensor-core products (gemm_tc.cu).
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -181,6 +182,10 @@ int gemm_fp8(bool sparse, const void* A, const void* meta, const void* B, int64_
 // C[T,N] = A_vnm[T,F] Bt[F,N]; A_vnm packed (vals [T, 2F/Mv], hardware-ordered metadata, colidx).
 int gemm_venom(const void* a_vals, const uint8_t* meta_hw, const uint8_t* colidx, const void* Bt, int64_t T,
                int64_t F, int64_t N, int V, int Mv, void* C, int64_t ldc, int* status, cudaStream_t s);
+
+// Tensor map (a CUtensorMap, 64-byte aligned) of rank 2 or 3, innermost dimension first; no interleaving, zeros beyond the edges.
+int encode_map(void* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+               const cuuint32_t* box, CUtensorMapSwizzle swizzle);
 
 // 2D TMA descriptor (a CUtensorMap, 128 bytes, 64-byte aligned) over a row-major [rows, cols] matrix of 2-byte
 // elements with leading dimension ld; box = {box_cols, box_rows}.
