@@ -148,10 +148,11 @@ def lib() -> C.CDLL:
             raise FileNotFoundError(
                 f"{LIB_PATH} is missing: build it with `python -m paper_2602_06183_b200.build` "
                 "(there is no fallback implementation)")
-        _lib = C.CDLL(LIB_PATH)
+        loaded = C.CDLL(LIB_PATH)
         for name, (res, args) in _SIGNATURES.items():
-            fn = getattr(_lib, name)
+            fn = getattr(loaded, name)
             fn.restype, fn.argtypes = res, args
+        _lib = loaded                    # complete: another thread may take it from here on
     return _lib
 
 
