@@ -380,7 +380,8 @@ SF_API int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const
  * row are written as 0 and must be; the rows beyond the last are neither written nor used.
  *
  * sf_fp4_sizes:       bytes of codes and scales of a [rows, cols] matrix.
- * sf_fp4_quantize:    X bf16 [rows, cols] (ld >= cols, ld % 8 == 0) -> codes uint8 [rows, cols/2], scales.
+ * sf_fp4_quantize:    X bf16 [rows, cols] (ld >= cols, ld % 8 == 0) -> codes uint8 [rows, cols/2], scales. An infinite `scale` is
+ *                     refused (SF_ERR_UNSUPPORTED).
  * sf_fp4_dequantize:  Y[r, c] = bf16(code * sf * alpha), alpha normally 1 / scale (ld as above).
  * sf_gemm_fp4:        C[Mr,Nc] = bf16(alpha * A B^T), A [Mr,K] and B [Nc,K] of one format, alpha normally 1 / (scale_A scale_B);
  *                     float32 accumulation. With few rows of A (tokens) the other operand is streamed once.

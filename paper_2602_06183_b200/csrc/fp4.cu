@@ -249,6 +249,7 @@ int sf_fp4_quantize(const void* X, int64_t rows, int64_t cols, int64_t ld, int f
   if (rows == 0 || cols == 0) return SF_OK;
   if (!X || !codes || !scales) return SF_ERR_NULL;
   if (ld < cols || ld % 8 || !aligned16(X) || !aligned16(codes) || !aligned16(scales)) return SF_ERR_ALIGN;
+  if (std::isinf(scale)) return SF_ERR_UNSUPPORTED;         // (0 times it is NaN, which a block's largest magnitude does not show)
   if (!apart({codes_span(codes, rows, cols), scales_span(scales, rows, cols, format)}, {rows_span(X, rows, cols, ld)})) return SF_ERR_UNSUPPORTED;
   const int fmt = fmt_of(format);
   const int64_t k_tiles = scale_tiles(fmt, cols);

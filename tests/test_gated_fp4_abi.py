@@ -135,3 +135,10 @@ def test_binding_refuses_tensors_that_would_be_read_as_something_else(lib):
         return
     assert _status(fwd) == SF_ERR_UNSUPPORTED and _status(gemm) == SF_ERR_UNSUPPORTED
     assert _status(lambda: binding.sf_fp4_quantize(torch.zeros(4, 64, dtype=bf), 0, 1.0)) == SF_ERR_UNSUPPORTED
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a call that were not refused would run on pointers to nothing")
+def test_an_infinite_scale_is_refused(lib):
+    """x scale would be NaN for every zero of x, which the largest magnitude of a block, taken before the product, does not show."""
+    q = lambda scale, rows=4: lib.sf_fp4_quantize(C.c_void_p(1 << 30), rows, 64, 64, 0, scale, C.c_void_p(2 << 30), C.c_void_p(3 << 30), None)   # noqa: E731
+    assert q(float("inf")) == SF_ERR_UNSUPPORTED and q(float("-inf")) == SF_ERR_UNSUPPORTED and q(float("inf"), rows=0) == SF_OK
