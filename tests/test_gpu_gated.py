@@ -396,3 +396,24 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(Y[-tail:], small[0]) and torch.equal(dX[-tail:], small[1])
     assert not bool(Y[:-tail].any()) and not bool(dX[:-tail].any())
     assert all(torch.equal(a, b) for a, b in zip(g, small[2]))          # every other token is zero
+
+
+@pytest.mark.parametrize("T", [9, 70, 300])
+def test_left_out_outputs_in_every_form(T):
+    """Sums of two terms, few tokens, CTA pairs: which outputs are asked for changes neither the others' bits nor memory that was not asked for."""
+    D, F = 72, 136
+    b = Block(T, D, F, "silu", *_normals(T, D, F, 5))
+    b.fwd()
+    b.bwd()
+    whole = {k: bits(b.out[k].t) for k in GRADS}
+    for mask in range(15):
+        only = tuple(k for i, k in enumerate(GRADS) if mask >> i & 1)
+        for k in GRADS:
+            b.out[k].t.fill_(7.0)
+        b.bwd(only)
+        for k in GRADS:
+            if k in only:
+                assert np.array_equal(bits(b.out[k].t), whole[k]), (only, k)
+            else:
+                assert bool((b.out[k].t == 7.0).all()), (only, k)
+    b.check()
