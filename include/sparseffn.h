@@ -396,6 +396,12 @@ SF_API int sf_fp4_quantize(const void* X, int64_t rows, int64_t cols, int64_t ld
 SF_API int sf_fp4_dequantize(const void* codes, const void* scales, int64_t rows, int64_t cols, int format, float alpha,
                              void* Y, int64_t ld, void* stream);
 SF_API int sf_gemm_fp4_workspace_size(int64_t Mr, int64_t Nc, int64_t K, size_t* bytes);
+/* How a product of these sizes runs on the current device (gated: sf_gemm_fp4_gated), as sf_gated_ffn_step_plan says it: sf_gated_form,
+ * columns of its tiles or the tokens that the kernel is made for, and the parts of the reduction. */
+typedef struct sf_fp4_plan {
+  int32_t form, cols, parts;
+} sf_fp4_plan;
+SF_API int sf_gemm_fp4_plan(int64_t Mr, int64_t Nc, int64_t K, int format, int gated, sf_fp4_plan* plan);
 SF_API int sf_gemm_fp4(const void* A, const void* a_scales, const void* B, const void* b_scales, int format, void* C,
                        int64_t Mr, int64_t Nc, int64_t K, float alpha, void* workspace, size_t workspace_bytes,
                        void* stream);

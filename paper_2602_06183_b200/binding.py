@@ -54,6 +54,10 @@ class sf_gated_ffn_plan(C.Structure):
     _fields_ = [("form", C.c_int32 * 6), ("cols", C.c_int32 * 6), ("parts", C.c_int32 * 6)]
 
 
+class sf_fp4_plan(C.Structure):
+    _fields_ = [("form", C.c_int32), ("cols", C.c_int32), ("parts", C.c_int32)]
+
+
 SF_GATED_H, SF_GATED_H_KEPT, SF_GATED_Y, SF_GATED_DH, SF_GATED_DX, SF_GATED_DW = range(6)
 SF_GATED_NONE, SF_GATED_FEW, SF_GATED_TILES, SF_GATED_SPLIT = range(4)
 SF_ACT_SILU, SF_ACT_GELU, SF_ACT_GELU_TANH, SF_ACT_RELU, SF_ACT_SQRELU = range(5)
@@ -114,6 +118,7 @@ _SIGNATURES = {
     "sf_fp4_quantize": (_i32, [_vp, _i64, _i64, _i64, _i32, C.c_float, _vp, _vp, _vp]),
     "sf_fp4_dequantize": (_i32, [_vp, _vp, _i64, _i64, _i32, C.c_float, _vp, _i64, _vp]),
     "sf_gemm_fp4_workspace_size": (_i32, [_i64, _i64, _i64, C.POINTER(_sz)]),
+    "sf_gemm_fp4_plan": (_i32, [_i64, _i64, _i64, _i32, _i32, C.POINTER(sf_fp4_plan)]),
     "sf_gemm_fp4": (_i32, [_vp, _vp, _vp, _vp, _i32, _vp, _i64, _i64, _i64, C.c_float, _vp, _sz, _vp]),
     "sf_gemm_fp4_gated": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i64, C.c_float, C.c_float, _vp,
                                  _sz, _vp]),
@@ -688,6 +693,12 @@ def sf_gemm_fp4_workspace_size(Mr: int, Nc: int, K: int) -> int:
     a = _sz()
     _check(lib().sf_gemm_fp4_workspace_size(Mr, Nc, K, C.byref(a)), "sf_gemm_fp4_workspace_size")
     return a.value
+
+
+def sf_gemm_fp4_plan(Mr: int, Nc: int, K: int, fmt: int, gated: bool = False) -> sf_fp4_plan:
+    plan = sf_fp4_plan()
+    _check(lib().sf_gemm_fp4_plan(Mr, Nc, K, fmt, gated, C.byref(plan)), "sf_gemm_fp4_plan")
+    return plan
 
 
 def sf_gemm_fp4(A, a_scales, B, b_scales, fmt: int, alpha: float, C_out=None, workspace=None, stream=None):

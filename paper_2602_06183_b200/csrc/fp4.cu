@@ -224,6 +224,25 @@ Span scales_span(const void* p, int64_t rows, int64_t cols, int format) {
 // bf16 rows, from the first element to the last
 Span rows_span(const void* p, int64_t rows, int64_t cols, int64_t ld) { return {p, 2 * ((size_t)(rows - 1) * (size_t)ld + (size_t)cols)}; }
 
+template <int kFmt>
+int fp4_plan(int64_t M, int64_t N, int64_t K, bool gated, sf_fp4_plan* plan) {
+  const int nkb = k_blocks(kFmt, K);
+  PairPlan p;
+  if (gated ? gated_by_few(kFmt, M, nkb) : M <= kFewTokens) {
+    FewArgs a{};
+    a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.in_terms = 1;
+    NoMaps none;
+    SF_TRY(gated ? (run_few<kFmt, FK_GATED>(a, nullptr, none, &p)) : (run_few<kFmt, FK_NT>(a, nullptr, none, &p)));
+    *plan = sf_fp4_plan{SF_GATED_FEW, p.bn, p.parts};
+  } else if (gated) {
+    *plan = sf_fp4_plan{SF_GATED_TILES, 256, 1};
+  } else {
+    SF_TRY(plan_fp4(M, N, nkb, &p));
+    *plan = sf_fp4_plan{p.mode == PM_SPLIT ? SF_GATED_SPLIT : SF_GATED_TILES, p.bn, p.parts};
+  }
+  return SF_OK;
+}
+
 int fp4_shape(int64_t rows, int64_t cols, int format) {
   if (fmt_of(format) < 0) return SF_ERR_UNSUPPORTED;
   return rows < 0 || cols < 0 || cols % 32 || rows > kMaxSize || cols > kMaxSize ? SF_ERR_SHAPE : SF_OK;
@@ -292,6 +311,16 @@ int sf_gemm_fp4_workspace_size(int64_t Mr, int64_t Nc, int64_t K, size_t* bytes)
   if (Mr < 0 || Nc < 0 || K <= 0 || Nc % 8 || K % 32 || Mr > kMaxSize || Nc > kMaxSize || K > kMaxSize) return SF_ERR_SHAPE;
   *bytes = kStatus;
   return SF_OK;
+}
+
+int sf_gemm_fp4_plan(int64_t Mr, int64_t Nc, int64_t K, int format, int gated, sf_fp4_plan* plan) {
+  size_t need;
+  if (fmt_of(format) < 0) return SF_ERR_UNSUPPORTED;
+  SF_TRY(sf_gemm_fp4_workspace_size(Mr, Nc, K, &need));
+  if (!plan) return SF_ERR_NULL;
+  *plan = sf_fp4_plan{SF_GATED_NONE, 0, 0};
+  if (Mr == 0 || Nc == 0) return SF_OK;
+  return format == SF_FP4_NV ? fp4_plan<FMT_NV>(Mr, Nc, K, gated != 0, plan) : fp4_plan<FMT_MX>(Mr, Nc, K, gated != 0, plan);
 }
 
 int sf_gemm_fp4(const void* A, const void* a_scales, const void* B, const void* b_scales, int format, void* C, int64_t Mr, int64_t Nc,
