@@ -100,8 +100,6 @@ struct PairCtl {
 
 struct PairTile { int job, m0, n0; };     // first row of the pair's tile, first column (PK_FWD: first feature)
 
-// The raster of the other products: bands of eight tile rows, rows fastest inside a band, so that the tiles which run at
-// the same time share few operand panels.
 // The n-th tile of a pair: every num_pairs-th one; the first late_rounds rounds are shared by the pairs that are not late.
 __device__ __forceinline__ int nth_tile(const PairArgs& a, int n, int pair, int num_pairs) {
   const int r = a.late_rounds, e = a.first_late;
@@ -109,6 +107,8 @@ __device__ __forceinline__ int nth_tile(const PairArgs& a, int n, int pair, int 
   return pair >= e ? r * e + n * num_pairs + pair : n < r ? n * e + pair : r * e + (n - r) * num_pairs + pair;
 }
 
+// The raster of the other products: bands of eight tile rows, rows fastest inside a band, so that the tiles which run at
+// the same time share few operand panels.
 template <int kKind>
 __device__ __forceinline__ PairTile pair_tile(const PairArgs& a, int tile, int cols) {
   int j = 0;
