@@ -314,8 +314,9 @@ SF_API int sf_ffn_step_host(const sf_ffn_desc* desc, int dense, const void* host
  *     G = X Wg^T,  U = X Wu^T,  H = act(G) * U,  Y = H Wd^T           X, Y [T,D];  Wg, Wu [F,D];  Wd [D,F]; all bf16
  *
  * T >= 0 of any size (a single token and a training batch take the same call); D and F positive multiples of 8; each size at most
- * 2^28. Tensors are contiguous. One rounding each: H (an operand of the second product; with T <= 16 a sum of two bf16 numbers) and Y; G
- * and U stay in float32. A NaN makes the results that it enters NaN, whatever the activation; an infinity makes them infinite or NaN, but for a
+ * 2^28. Tensors are contiguous. One rounding each: H (an operand of the second product) and Y; G
+ * and U stay in float32. With T <= 16 H is a sum of two bf16 numbers, and so are dG and dU: there a row's error is that of one rounding,
+ * from 17 tokens on 1.4 times that, and the same row has other last bits in a call of 16 tokens and in one of 17. A NaN makes the results that it enters NaN, whatever the activation; an infinity makes them infinite or NaN, but for a
  * gate of -infinity under the two ReLUs, whose value and derivative are 0.
  *
  * sf_gated_ffn_fwd:  fwd_ctx NULL: inference, H lies in the workspace. Otherwise fwd_ctx receives what the backward pass needs: H in
@@ -375,7 +376,7 @@ SF_API int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const
  *     code = e2m1(x scale / sf)   to nearest, ties to the even code, clamped at 6                  (float32 quotient)
  *
  * A block whose sf is 0 has codes of 0 (with the signs of x). Infinities clamp to 6 sf; a NaN makes its block's scale, and so the whole block, NaN.
- * Scale bytes (E4M3 bits, or the exponent + 127) lie in tiles of 128 rows x 4 blocks, 512 bytes each: block c of row r is byte
+ * Scale bytes (E4M3 bits without a sign, or the exponent + 127) lie in tiles of 128 rows x 4 blocks, 512 bytes each: block c of row r is byte
  * 16 (r % 32) + 4 (r % 128 / 32) + c % 4 of tile (r / 128) * ceil(blocks / 4) + c / 4. Of a ragged last tile the blocks beyond the
  * row are written as 0 and must be; the rows beyond the last are neither written nor used.
  *
@@ -386,7 +387,7 @@ SF_API int sf_gated_ffn_bwd(const sf_gated_ffn_desc* desc, const void* dY, const
  * sf_gemm_fp4:        C[Mr,Nc] = bf16(alpha * A B^T), A [Mr,K] and B [Nc,K] of one format, alpha normally 1 / (scale_A scale_B);
  *                     float32 accumulation. With few rows of A (tokens) the other operand is streamed once.
  * sf_gemm_fp4_gated:  H[Mr,Nc] = bf16(act(alpha_g A Bg^T) * (alpha_u A Bu^T)): the first half of the gated block on 4-bit operands.
- * Any Mr and rows; cols and K multiples of 32; Nc a multiple of 8; sizes at most 2^28.
+ * Any Mr and rows, cols and Nc may be 0; cols and K multiples of 32, K positive (an empty sum is refused); Nc a multiple of 8; sizes at most 2^28.
  * Outputs that share a byte with an input are refused (SF_ERR_UNSUPPORTED; rows with a stride count from the first to the last element).
  * `workspace`: sf_gemm_fp4_workspace_size() bytes, the first 256 the status word as everywhere. */
 typedef enum sf_fp4_format { SF_FP4_NV = 0, SF_FP4_MX = 1 } sf_fp4_format;
