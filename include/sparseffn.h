@@ -411,6 +411,81 @@ SF_API int sf_gemm_fp4_gated(const void* A, const void* a_scales, const void* Bg
                              float alpha_g, float alpha_u, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * What stands around the layer in a step (the paper has none of it; a step needs it next to what is above).
+ *
+ * Root-mean-square norm with the residual's addition, in front of the layer. T >= 0 tokens, D a positive multiple of 8, at most 32768.
+ *
+ *     S = bf16(X + residual),   r = 1 / sqrt(mean of the row's S^2 + eps),   y = S r gamma
+ *
+ * sf_rmsnorm_fwd:  X bf16 [T, D] (leading dimension ldx >= D, ldx % 8 == 0); residual bf16 [T, D] or NULL (then S = X); gamma bf16 [D]. Any of
+ *     the outputs may be NULL, but not both Y and codes:
+ *       sum    bf16 [T, D]   S. May be `residual` itself, or X (with ldx == D)
+ *       Y      bf16 [T, D]   y
+ *       codes  uint8 [T, D]  y as E4M3 codes. With scales (float32 [T]): scales[t] = top / 448, top = max(the row's largest |y|, 2^-96), code =
+ *                            e4m3(y * (448 / top)), for sf_gemm_fp8_rows. With scales NULL: code = e4m3(y * scale), as sf_fp8_quantize
+ *       rstd   float32 [T]   r, for the backward pass
+ *     The squares are summed in float32. An infinity makes its own element NaN and the others of its row 0, a NaN its whole row.
+ * sf_rmsnorm_bwd:  dY bf16 [T, D], S and r of the forward call, dS the gradient that comes to S from elsewhere (bf16 [T, D] or NULL):
+ *       n = S r,  q = dY gamma,  dX = dS + r (q - n mean(q n)) [T, D] (of X and of the residual alike),  dgamma = sum over t of dY n [D], bf16.
+ *     Either output may be NULL. dX may be dY or dS itself. With T == 0 dgamma is zero. The same call gives the same bits.
+ * Outputs that otherwise share a byte with one another or with an input are refused (SF_ERR_UNSUPPORTED), and so is a negative or NaN eps.
+ * workspace (needed with dgamma): sf_rmsnorm_bwd_workspace_size bytes; no status word, nothing to be zeroed. */
+SF_API int sf_rmsnorm_fwd(const void* X, int64_t ldx, const void* residual, const void* gamma, int64_t T, int64_t D, float eps, void* sum,
+                          void* Y, void* codes, void* scales, float scale, void* rstd, void* stream);
+SF_API int sf_rmsnorm_bwd_workspace_size(int64_t T, int64_t D, size_t* bytes);
+SF_API int sf_rmsnorm_bwd(const void* dY, const void* sum, const void* gamma, const void* rstd, const void* dS, int64_t T, int64_t D, void* dX,
+                          void* dgamma, void* workspace, size_t workspace_bytes, void* stream);
+
+/* E4M3 product of rows with scales: C[Mr,Nc] = bf16(alpha a_scales[m] A B^T), A uint8 [Mr,K] and B uint8 [Nc,K] E4M3 codes, a_scales float32 [Mr];
+ * float32 accumulation. alpha is normally 1 / the scale of B. Any Mr >= 0 (with few rows B is streamed once); Nc a multiple of 8, may be 0; K
+ * a positive multiple of 16; sizes at most 2^28. Outputs that share a byte with an input are refused (SF_ERR_UNSUPPORTED).
+ * `workspace`: sf_gemm_fp8_rows_workspace_size() bytes, the first 256 the status word as everywhere. */
+SF_API int sf_gemm_fp8_rows_workspace_size(int64_t Mr, int64_t Nc, int64_t K, size_t* bytes);
+SF_API int sf_gemm_fp8_rows(const void* A, const void* a_scales, const void* B, void* C, int64_t Mr, int64_t Nc, int64_t K, float alpha,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* The router's balance loss and its gradients. logits float32 [T, E] and expert int32 [T] as sf_router_route writes them (or SF_RCTX_LOGITS,
+ * SF_RCTX_EXPERT of a routed step). A token whose expert lies outside [0, E), as padding may be marked, is left out everywhere. With n_e
+ * tokens at expert e, n in all, p = softmax of a token's logits and lse their log-sum-exp:
+ *
+ *     balance = E sum_e (n_e / n) (sum_t p_te / n),   z = sum_t lse_t^2 / n,   loss = balance_coef balance + z_coef z
+ *
+ * 1 <= E <= 16, 0 <= T <= 2^28. With n == 0 all of it is 0.
+ * sf_router_balance_fwd:  loss float32 [3] (loss, balance, z); counts int32 [E] (the n_e).
+ * sf_router_balance_bwd:  X bf16 [T, D], means bf16 [E, D] (logits = X means^T), D a positive multiple of 8, at most 2^20; counts as the forward
+ *     call wrote them (they are not differentiated); dloss float32 [1] on the device, the gradient of loss, or NULL for 1:
+ *       dl[t,e] = dloss p_te (balance_coef E / n^2 (n_e - sum_j n_j p_tj) + 2 z_coef lse_t / n)
+ *       dX [T, D] = dX_in + dl means (dX_in bf16 [T, D] or NULL for 0; dX may be dX_in itself),   dmeans [E, D] = dl^T X,  bf16.
+ *     Either output may be NULL. With T == 0 dmeans is zero. dl stays in float32, or as a sum of two bf16 numbers.
+ * The same call gives the same bits. `workspace`: sf_router_balance_workspace_size() bytes for either call, the first 256 zeroed once before
+ * first use; calls that may overlap on the GPU need workspaces of their own. Outputs that otherwise share a byte with one another or with
+ * an input are refused (SF_ERR_UNSUPPORTED). */
+SF_API int sf_router_balance_workspace_size(int64_t T, int64_t D, int E, size_t* bytes);
+SF_API int sf_router_balance_fwd(const void* logits, const void* expert, int64_t T, int E, float balance_coef, float z_coef, void* loss,
+                                 void* counts, void* workspace, size_t workspace_bytes, void* stream);
+SF_API int sf_router_balance_bwd(const void* logits, const void* expert, const void* counts, const void* dloss, const void* X, const void* means,
+                                 int64_t T, int64_t D, int E, float balance_coef, float z_coef, const void* dX_in, void* dX, void* dmeans,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Orthogonalising an update (a weight's gradient or its momentum) by Newton-Schulz products:
+ *
+ *     X_0 = G / |G|  (Frobenius norm; a G of zeros stays zero),   X <- a X + (b A + c A^2) X with A = X X^T,  `steps` times,   O = bf16(scale X)
+ *
+ * for G with at most as many rows as columns; of a higher one the transpose is taken, and that of the result. G is SF_BF16 or SF_F32 [rows, cols],
+ * leading dimension ldg >= cols; O bf16 [rows, cols], ldo >= cols. Any rows, cols >= 0; the larger at most 2^24, the smaller at most 2^16. G and O are
+ * aligned to their element; rows of O whose starts are multiples of 16 bytes save a copy. 1 <= steps <= 64. (a, b, c): the quintic a s + b s^3 + c s^5
+ * has to keep [0, 1.25] within [-1.25, 1.25] and |b l + c l^2| <= 7.5 up to l = 1.5625, with |a|, |b|, |c| <= 8 (SF_ERR_UNSUPPORTED otherwise); (3.4445,
+ * -4.7750, 2.0315) is usual. A NaN or an infinity in G makes all of O NaN.
+ * The products' operands are fp16; X is held as a sum of two of them and the diagonals of A and A^2 in float32, so that the error of the result
+ * is about that of its rounding to bf16. The same call gives the same bits.
+ * `workspace`: sf_orthogonalize_workspace_size() bytes, the first 256 the status word as everywhere. Outputs that share a byte with the
+ * input are refused (SF_ERR_UNSUPPORTED). */
+typedef enum sf_type { SF_BF16 = 0, SF_F32 = 1 } sf_type;
+SF_API int sf_orthogonalize_workspace_size(int64_t rows, int64_t cols, size_t* bytes);
+SF_API int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_t ldg, int steps, float a, float b, float c, float scale,
+                            void* O, int64_t ldo, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Sparse/dense step schedule (Section 5.3.2) and speed-up arithmetic (Sections 3.1 and 5.1).
  * Host-side logic; nothing here touches the GPU except the two dispatchers.
  *

@@ -62,6 +62,7 @@ SF_GATED_H, SF_GATED_H_KEPT, SF_GATED_Y, SF_GATED_DH, SF_GATED_DX, SF_GATED_DW =
 SF_GATED_NONE, SF_GATED_FEW, SF_GATED_TILES, SF_GATED_SPLIT = range(4)
 SF_ACT_SILU, SF_ACT_GELU, SF_ACT_GELU_TANH, SF_ACT_RELU, SF_ACT_SQRELU = range(5)
 SF_FP4_NV, SF_FP4_MX = range(2)
+SF_BF16, SF_F32 = range(2)
 
 
 class sf_schedule(C.Structure):
@@ -122,6 +123,16 @@ _SIGNATURES = {
     "sf_gemm_fp4": (_i32, [_vp, _vp, _vp, _vp, _i32, _vp, _i64, _i64, _i64, C.c_float, _vp, _sz, _vp]),
     "sf_gemm_fp4_gated": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, _i64, _i64, _i64, C.c_float, C.c_float, _vp,
                                  _sz, _vp]),
+    "sf_rmsnorm_fwd": (_i32, [_vp, _i64, _vp, _vp, _i64, _i64, C.c_float, _vp, _vp, _vp, _vp, C.c_float, _vp, _vp]),
+    "sf_rmsnorm_bwd_workspace_size": (_i32, [_i64, _i64, C.POINTER(_sz)]),
+    "sf_rmsnorm_bwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "sf_gemm_fp8_rows_workspace_size": (_i32, [_i64, _i64, _i64, C.POINTER(_sz)]),
+    "sf_gemm_fp8_rows": (_i32, [_vp, _vp, _vp, _vp, _i64, _i64, _i64, C.c_float, _vp, _sz, _vp]),
+    "sf_router_balance_workspace_size": (_i32, [_i64, _i64, _i32, C.POINTER(_sz)]),
+    "sf_router_balance_fwd": (_i32, [_vp, _vp, _i64, _i32, C.c_float, C.c_float, _vp, _vp, _vp, _sz, _vp]),
+    "sf_router_balance_bwd": (_i32, [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i32, C.c_float, C.c_float, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "sf_orthogonalize_workspace_size": (_i32, [_i64, _i64, C.POINTER(_sz)]),
+    "sf_orthogonalize": (_i32, [_vp, _i32, _i64, _i64, _i64, _i32, C.c_float, C.c_float, C.c_float, C.c_float, _vp, _i64, _vp, _sz, _vp]),
     "sf_schedule_step_kind": (_i32, [C.POINTER(sf_schedule), _i64, C.POINTER(_i32)]),
     "sf_schedule_speedup": (_i32, [C.POINTER(sf_schedule), C.c_double, C.POINTER(C.c_double)]),
     "sf_ffn_flop_fraction": (_i32, [_i64, _i64, _i64, _i64, _i64, C.POINTER(C.c_double)]),
@@ -734,6 +745,164 @@ def sf_gemm_fp4_gated(A, a_scales, Bg, bg_scales, Bu, bu_scales, fmt: int, act: 
     _check(lib().sf_gemm_fp4_gated(a, a_s, g, g_s, u, u_s, fmt, act, _tensor(w, "H_out", H_out, _BF16, (Mr, Nc), dev), Mr, Nc, K,
                                    alpha_g, alpha_u, *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
     return H_out
+
+
+# ---- around the layer: norm, E4M3 rows, balance loss, orthogonalised update --------------------------------
+# Checked like the calls above. What a call makes for itself (outputs, workspace) belongs to the stream that it runs on.
+
+_F32, _I32 = torch.float32, torch.int32
+
+
+def _optional(where: str, name: str, t, dtype, shape, dev: int):
+    return None if t is None else _tensor(where, name, t, dtype, shape, dev)
+
+
+def _sized(call: str, *args) -> int:
+    n = _sz()
+    _check(getattr(lib(), call)(*args, C.byref(n)), call)
+    return n.value
+
+
+def sf_rmsnorm_fwd(X, gamma, eps: float, residual=None, sum=None, Y=None, codes=None, scales=None, scale: float = 1.0, rstd=None, stream=None):
+    """S = bf16(X + residual), y = S gamma / rms(S) of every row: S to ``sum``, y as bf16 to ``Y`` or as E4M3 to ``codes`` (with a
+    scale to every row in ``scales``, or the given ``scale``), 1 / rms to ``rstd``. What is None is not written; without Y and codes a Y is made.
+    X may be a strided row view. Returns Y (or the codes)."""
+    w, dev = "sf_rmsnorm_fwd", X.get_device()
+    ld = _row_stride(w, "X", X)
+    T, D = X.shape
+    if Y is None and codes is None:
+        with _allocating(stream):
+            Y = torch.empty((T, D), dtype=_BF16, device=X.device)
+    _check(lib().sf_rmsnorm_fwd(X.data_ptr(), ld, _optional(w, "residual", residual, _BF16, (T, D), dev), _tensor(w, "gamma", gamma, _BF16, (D,), dev),
+                                T, D, eps, _optional(w, "sum", sum, _BF16, (T, D), dev), _optional(w, "Y", Y, _BF16, (T, D), dev),
+                                _optional(w, "codes", codes, _U8, (T, D), dev), _optional(w, "scales", scales, _F32, (T,), dev), scale,
+                                _optional(w, "rstd", rstd, _F32, (T,), dev), _launch_stream(w, dev, stream)), w)
+    return codes if Y is None else Y
+
+
+def sf_rmsnorm_bwd_workspace_size(T: int, D: int) -> int:
+    return _sized("sf_rmsnorm_bwd_workspace_size", T, D)
+
+
+def sf_rmsnorm_bwd(dY, S, gamma, rstd, dS=None, dX=None, dgamma=None, workspace=None, stream=None):
+    """Gradients of sf_rmsnorm_fwd from dY, its sum S and its rstd, dS added: into ``dX`` and ``dgamma``, of which a None is left out (both
+    None: both are made). Returns (dX, dgamma)."""
+    w, dev = "sf_rmsnorm_bwd", dY.get_device()
+    T, D = _matrix_shape(w, dY)
+    both = dX is None and dgamma is None
+    if both or (dgamma is not None and workspace is None):
+        with _allocating(stream):
+            if both:
+                dX, dgamma = torch.empty((T, D), dtype=_BF16, device=dY.device), torch.empty((D,), dtype=_BF16, device=dY.device)
+            if workspace is None:
+                workspace = torch.empty((sf_rmsnorm_bwd_workspace_size(T, D),), dtype=_U8, device=dY.device)
+    _check(lib().sf_rmsnorm_bwd(_tensor(w, "dY", dY, _BF16, (T, D), dev), _tensor(w, "S", S, _BF16, (T, D), dev), _tensor(w, "gamma", gamma, _BF16, (D,), dev),
+                                _tensor(w, "rstd", rstd, _F32, (T,), dev), _optional(w, "dS", dS, _BF16, (T, D), dev), T, D,
+                                _optional(w, "dX", dX, _BF16, (T, D), dev), _optional(w, "dgamma", dgamma, _BF16, (D,), dev),
+                                *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
+    return dX, dgamma
+
+
+def sf_gemm_fp8_rows_workspace_size(Mr: int, Nc: int, K: int) -> int:
+    return _sized("sf_gemm_fp8_rows_workspace_size", Mr, Nc, K)
+
+
+def sf_gemm_fp8_rows(A, a_scales, B, alpha: float, C_out=None, workspace=None, stream=None):
+    """C[Mr,Nc] = bf16(alpha * a_scales[m] * A B^T) of E4M3 codes A [Mr,K] and B [Nc,K], a float32 scale to every row of A."""
+    w, u8, dev = "sf_gemm_fp8_rows", _U8, A.get_device()
+    Mr, K = _matrix_shape(w, A)
+    Nc = _matrix_shape(w, B)[0]
+    if C_out is None or workspace is None:
+        with _allocating(stream):
+            C_out = torch.empty((Mr, Nc), dtype=_BF16, device=A.device) if C_out is None else C_out
+            workspace = _workspace(sf_gemm_fp8_rows_workspace_size(Mr, Nc, K), A.device) if workspace is None else workspace
+    _check(lib().sf_gemm_fp8_rows(_tensor(w, "A", A, u8, (Mr, K), dev), _tensor(w, "a_scales", a_scales, _F32, (Mr,), dev),
+                                  _tensor(w, "B", B, u8, (Nc, K), dev), _tensor(w, "C_out", C_out, _BF16, (Mr, Nc), dev), Mr, Nc, K, alpha,
+                                  *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
+    return C_out
+
+
+def sf_router_balance_workspace_size(T: int, D: int, E: int) -> int:
+    return _sized("sf_router_balance_workspace_size", T, D, E)
+
+
+def _logits_shape(where: str, t):
+    if t.dim() != 2:
+        raise SparseFFNError(SF_ERR_SHAPE, f"{where}: logits must be a matrix")
+    return t.shape
+
+
+def sf_router_balance_fwd(logits, expert, balance_coef: float, z_coef: float = 0.0, loss=None, counts=None, workspace=None, stream=None):
+    """(loss float32 [3], counts int32 [E]) of logits float32 [T,E] and expert int32 [T] (tokens outside [0,E) are left out): the loss with its
+    coefficients, the balance and the z term, and the tokens of every expert."""
+    w, dev = "sf_router_balance_fwd", logits.get_device()
+    T, E = _logits_shape(w, logits)
+    if loss is None or counts is None or workspace is None:
+        with _allocating(stream):
+            loss = torch.empty((3,), dtype=_F32, device=logits.device) if loss is None else loss
+            counts = torch.empty((E,), dtype=_I32, device=logits.device) if counts is None else counts
+            workspace = _workspace(sf_router_balance_workspace_size(T, 8, E), logits.device) if workspace is None else workspace
+    _check(lib().sf_router_balance_fwd(_tensor(w, "logits", logits, _F32, (T, E), dev), _tensor(w, "expert", expert, _I32, (T,), dev), T, E, balance_coef,
+                                       z_coef, _tensor(w, "loss", loss, _F32, (3,), dev), _tensor(w, "counts", counts, _I32, (E,), dev),
+                                       *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
+    return loss, counts
+
+
+def sf_router_balance_bwd(logits, expert, counts, balance_coef: float, z_coef: float, X, means, dloss=None, dX_in=None, dX=None, dmeans=None,
+                          workspace=None, stream=None):
+    """Gradients of sf_router_balance_fwd's loss (times ``dloss`` float32 [1], or 1): dX = dX_in + dl means and dmeans = dl^T X, of which a None is
+    left out (both None: both are made). Returns (dX, dmeans)."""
+    w, dev = "sf_router_balance_bwd", logits.get_device()
+    T, E = _logits_shape(w, logits)
+    D = _matrix_shape(w, X)[1]
+    both = dX is None and dmeans is None
+    if both or (dmeans is not None and workspace is None):
+        with _allocating(stream):
+            if both:
+                dX, dmeans = torch.empty((T, D), dtype=_BF16, device=X.device), torch.empty((E, D), dtype=_BF16, device=X.device)
+            if workspace is None:
+                workspace = _workspace(sf_router_balance_workspace_size(T, D, E), X.device)
+    _check(lib().sf_router_balance_bwd(_tensor(w, "logits", logits, _F32, (T, E), dev), _tensor(w, "expert", expert, _I32, (T,), dev),
+                                       _tensor(w, "counts", counts, _I32, (E,), dev), _optional(w, "dloss", dloss, _F32, (1,), dev),
+                                       _tensor(w, "X", X, _BF16, (T, D), dev), _tensor(w, "means", means, _BF16, (E, D), dev), T, D, E, balance_coef, z_coef,
+                                       _optional(w, "dX_in", dX_in, _BF16, (T, D), dev), _optional(w, "dX", dX, _BF16, (T, D), dev),
+                                       _optional(w, "dmeans", dmeans, _BF16, (E, D), dev), *_buffer(w, "workspace", workspace, dev),
+                                       _launch_stream(w, dev, stream)), w)
+    return dX, dmeans
+
+
+def sf_orthogonalize_workspace_size(rows: int, cols: int) -> int:
+    return _sized("sf_orthogonalize_workspace_size", rows, cols)
+
+
+def _rows_of(where: str, name: str, t, dtypes, shape, dev: int) -> int:
+    """Leading dimension of a matrix of contiguous rows, of one of these types, that shape and device."""
+    if t.dtype not in dtypes or tuple(t.shape) != shape:
+        raise SparseFFNError(SF_ERR_SHAPE, f"{where}: {name} is {t.dtype} {tuple(t.shape)}, wanted {' or '.join(map(str, dtypes))} {shape}")
+    if (t.size(1) > 1 and t.stride(1) != 1) or (t.size(0) > 1 and t.stride(0) < t.size(1)):
+        raise SparseFFNError(SF_ERR_ALIGN, f"{where}: {name}'s rows are not contiguous, or share elements")
+    if t.get_device() != dev:
+        raise SparseFFNError(SF_ERR_UNSUPPORTED, f"{where}: {name} is on {t.device}, another device than the first tensor")
+    return t.stride(0) if t.size(0) > 1 else t.size(1)
+
+
+def sf_orthogonalize(G, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), scale: float = 1.0, out=None, workspace=None, stream=None):
+    """O = bf16(scale * X) after ``steps`` of X <- a X + (b A + c A^2) X, A = X X^T, from X = G / |G|; G bf16 or float32. G and ``out`` may be
+    strided row views."""
+    w, dev = "sf_orthogonalize", G.get_device()
+    if G.dim() != 2:
+        raise SparseFFNError(SF_ERR_SHAPE, f"{w}: G must be a matrix")
+    rows, cols = G.shape
+    ldg = _rows_of(w, "G", G, (_BF16, _F32), (rows, cols), dev)
+    if out is None or workspace is None:
+        with _allocating(stream):
+            out = torch.empty((rows, cols), dtype=_BF16, device=G.device) if out is None else out
+            workspace = _workspace(sf_orthogonalize_workspace_size(rows, cols), G.device) if workspace is None else workspace
+    a, b, c = coefficients
+    _check(lib().sf_orthogonalize(G.data_ptr(), SF_F32 if G.dtype is _F32 else SF_BF16, rows, cols, ldg, steps, a, b, c, scale, out.data_ptr(),
+                                  _rows_of(w, "out", out, (_BF16,), (rows, cols), dev), *_buffer(w, "workspace", workspace, dev),
+                                  _launch_stream(w, dev, stream)), w)
+    return out
 
 
 def make_schedule(warmup_steps: int, sparse_steps: int, total_steps: int) -> sf_schedule:

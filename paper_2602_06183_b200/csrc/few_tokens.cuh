@@ -31,7 +31,7 @@ enum FewKind { FK_NT, FK_GATED, FK_DX, FK_BWD };
 
 template <int kFmt, int kKind, int kN>
 struct FewCfg {
-  static constexpr bool kFp4 = kFmt != FMT_BF16, kGated = kKind == FK_GATED, kWMN = kKind == FK_DX || kKind == FK_BWD;
+  static constexpr bool kFp4 = is_fp4(kFmt), kGated = kKind == FK_GATED, kWMN = kKind == FK_DX || kKind == FK_BWD;
   static constexpr int kMats = kGated ? 2 : 1;
   static constexpr int kTiles = kFmt == FMT_NV ? 4 : kFmt == FMT_MX ? 2 : 0;
   static constexpr int kWBytes = 16384, kXBytes = kN * 128;
@@ -51,7 +51,7 @@ struct FewCfg {
 };
 
 struct FewArgs {
-  int T, N, nkb;                     // tokens, output columns, k-blocks (64 K of bf16, 256 K of 4 bits)
+  int T, N, nkb;                     // tokens, output columns, k-blocks (64 K of bf16, 128 K of E4M3, 256 K of 4 bits)
   int in_terms, out_terms;           // 2: the tokens' operand, or the results, are sums of two bf16: rows t and T + t (see kTwoTerms)
   int nkb0;                          // FK_DX: those of the first pair
   int act;
@@ -62,6 +62,7 @@ struct FewArgs {
   void* C;                           // [T, N] bf16 (FK_BWD: dU)
   void* C2;                          // FK_BWD: dG
   float *P, *Q;                      // FK_GATED: written, optional; FK_BWD: read
+  const float* row_scales;           // E4M3: of the tokens
   int* status;
 };
 struct FewMaps { CUtensorMap x, w0, w1, sx, s0, s1; };      // (FK_DX: the second pair is w1 and sx)
@@ -198,7 +199,7 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
     }
     pdl_trigger();
   } else if (warp == 1) {
-    constexpr uint32_t idesc = kFp4 ? idesc_fp4(128, kN, kFmt) : idesc_bf16(128, kN, Cfg::kWMN, false, false);
+    constexpr uint32_t idesc = kFp4 ? idesc_fp4(128, kN, kFmt) : idesc_plain(kFmt, 128, kN, Cfg::kWMN, false);
     constexpr uint64_t proto = desc_proto(16, 1024, kSwizzle128B), w_proto = desc_proto(Cfg::kWMN ? 8192 : 16, 1024, kSwizzle128B);
     constexpr uint32_t w_step = (Cfg::kWMN ? 2048 : 32) >> 4;
     constexpr uint64_t s_proto = desc_proto(128, 128, kSwizzleNone);
@@ -234,6 +235,8 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
               const uint32_t id = kFmt == FMT_NV ? 0u : (uint32_t)(k & 1) * 2u;
               mma_fp4_1cta<kFmt>(tmem + m * kN, wd, xd, idesc | id << 4 | id << 29, scol + 4 * (m * kTiles + i),
                                  scol + 4 * (kMats * kTiles + i), k > 0 ? 1u : more);
+            } else if constexpr (kFmt == FMT_E4M3) {
+              mma_f8(tmem + m * kN, wd, xd, idesc, k > 0 ? 1u : more);
             } else {
               mma_f16(tmem + m * kN, wd, xd, idesc, k > 0 ? 1u : more);
             }
@@ -302,6 +305,11 @@ few_tokens_kernel(const __grid_constant__ FewMaps maps, const FewArgs args) {
     if (kFp4)
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[e] *= args.alpha;
+    if constexpr (kFmt == FMT_E4M3) {
+      const float f = args.alpha * __ldg(args.row_scales + t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] *= f;
+    }
     const int64_t at = (int64_t)t * args.N + f;
     if constexpr (kGated) {
       const float4 y = sum[kMats - 1];

@@ -26,8 +26,8 @@ int sm_count_now() {
 
 namespace {
 
-int encode_2d(void* map, CUtensorMapDataType type, int bytes, const void* base, int64_t rows, int64_t cols, CUtensorMapSwizzle swizzle) {
-  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)cols * bytes};
+int encode_2d(void* map, CUtensorMapDataType type, int bytes, const void* base, int64_t rows, int64_t cols, int64_t ld, CUtensorMapSwizzle swizzle) {
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * bytes};
   const cuuint32_t box[2] = {32, 32};
   return encode_map(map, type, 2, base, dims, strides, box, swizzle);
 }
@@ -35,10 +35,10 @@ int encode_2d(void* map, CUtensorMapDataType type, int bytes, const void* base, 
 }  // namespace
 
 int make_tmap_f32(void* map, const void* base, int64_t rows, int64_t cols) {
-  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, rows, cols, CU_TENSOR_MAP_SWIZZLE_128B);
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, base, rows, cols, cols, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-int make_tmap_store(void* map, void* base, int64_t rows, int64_t cols) {
-  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols, CU_TENSOR_MAP_SWIZZLE_64B);
+int make_tmap_store(void* map, const void* base, int64_t rows, int64_t cols, int64_t ld) {
+  return encode_2d(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, rows, cols, ld ? ld : cols, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 int make_tmap_scales(void* map, const void* base, int64_t row_blocks, int64_t k_tiles, uint32_t box_tiles) {
   const cuuint64_t dims[3] = {128, (cuuint64_t)k_tiles, (cuuint64_t)row_blocks}, strides[2] = {512, 512 * (cuuint64_t)k_tiles};

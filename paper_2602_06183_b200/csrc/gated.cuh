@@ -14,7 +14,8 @@
 namespace sf {
 
 // Operand formats of a product.
-enum OperandFmt { FMT_BF16 = 0, FMT_NV = 1, FMT_MX = 2 };
+enum OperandFmt { FMT_BF16 = 0, FMT_NV = 1, FMT_MX = 2, FMT_E4M3 = 3, FMT_F16 = 4 };
+constexpr bool is_fp4(int fmt) { return fmt == FMT_NV || fmt == FMT_MX; }
 
 // ---- activations ----------------------------------------------------------------------------------------
 // Value and derivative of the gate's activation in float32. The sigmoid is written with the exponential of -x, so that neither
@@ -126,12 +127,17 @@ __host__ __device__ constexpr uint32_t idesc_fp4(uint32_t M, uint32_t N, int fmt
   return (1u << 7) | (1u << 10) | ((N >> 3) << 17) | (fmt == FMT_MX ? 1u << 23 : 0u) | ((M >> 7) << 27);
 }
 
+// Instruction descriptor of a product without block scales (idesc_bf16, or that of E4M3 or fp16 operands, whose type fields are 0).
+__host__ __device__ constexpr uint32_t idesc_plain(int fmt, uint32_t M, uint32_t N, bool a_mn, bool b_mn) {
+  return ptx::idesc_bf16(M, N, a_mn, b_mn, false) & ~(fmt == FMT_BF16 ? 0u : (7u << 7) | (7u << 10));
+}
+
 // ---- tensor maps ------------------------------------------------------------------------------------------
 int sm_count_now();
 // [rows, cols] of 4-byte floats, box 32 x 32, 128-byte swizzle.
 int make_tmap_f32(void* map, const void* base, int64_t rows, int64_t cols);
-// Stores of bf16 [rows, cols], box 32 x 32, 64-byte swizzle.
-int make_tmap_store(void* map, void* base, int64_t rows, int64_t cols);
+// bf16 or fp16 [rows, cols], box 32 x 32, 64-byte swizzle (leading dimension ld: 0 for cols).
+int make_tmap_store(void* map, const void* base, int64_t rows, int64_t cols, int64_t ld = 0);
 // Scale tiles of a 4-bit operand: [row blocks][tiles along K][128 words], box {128, tiles, 1}.
 int make_tmap_scales(void* map, const void* base, int64_t row_blocks, int64_t k_tiles, uint32_t box_tiles);
 

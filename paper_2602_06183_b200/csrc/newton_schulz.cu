@@ -1,0 +1,350 @@
+// Orthogonalising an update by Newton-Schulz products: X_0 = G / |G| (Frobenius), and a number of times
+//     A = X X^T,   X <- (a I + b A + c A^2) X            with X as wide as it is high at least (G, or its transpose)
+// which takes every singular value of X through the quintic a s + b s^3 + c s^5 and leaves the singular vectors.
+//
+// A quintic that brings small singular values up quickly (a = 3.4) also brings up what rounding puts in their place, 3.4 times with every
+// step, and the values near 1 it moves about rather than to 1. So the operands' roundings decide what comes out. With X in bf16 the error
+// against 64 bits is 1 to 2 percent for a random matrix and 10 to 30 for one of low rank. Here:
+//   - operands are fp16 (11 bits to bf16's 8, the same rate), kept in range by powers of two: |X| <= 1.25 in every norm that matters, so X
+//     is held as 2^14 X, A as 2^14 A, B as 2^12 B;
+//   - X is kept as a sum of two fp16 numbers. The products see the first; a X, the larger part for small singular values, is added in
+//     float32 from both. This alone takes the error at rank 8 from 2.6 % to 0.03 %, and costs no product;
+//   - the diagonals of A and B, which are far larger than the rest, are held apart in float32 and multiplied in the epilogues:
+//     A = D + A', A^2 = D^2 + D A' + A' D + A'^2, B X = diag(B) X + B' X. A matrix of 512 x 2048: 0.3 % to 0.05 %.
+// Then the final rounding to bf16 (0.17 %) is the largest error.
+//
+// Launches: norm (partial sums in double), conversion (with the transposition of a high G), then three a step (PK_GRAM, PK_POLY, PK_APPLY of
+// pair_product.cuh). X X^T and A^2 are symmetric: half of their tiles are computed. Flops a step, m <= n: m^2 n + m^3 + 2 m^2 n.
+#include "products.cuh"
+
+namespace sf {
+namespace {
+
+constexpr size_t kStatus = 256, kScalars = 256;       // status word; the first step's factor
+constexpr int kNormCtas = 512;
+constexpr int64_t kMostSide = 1 << 24, kMostSmall = 1 << 16;
+
+struct NsShape {
+  int64_t m, n, ldm, ldn, mp;          // small and large side, leading dimensions, m in whole tiles
+  bool high;                           // G has more rows than columns
+  size_t sums, diag_a, diag_b, a, b, x[4], total;
+};
+
+int ns_shape(int64_t rows, int64_t cols, NsShape* z) {
+  if (rows < 0 || cols < 0 || rows > kMostSide || cols > kMostSide) return SF_ERR_SHAPE;
+  z->high = rows > cols;
+  z->m = z->high ? cols : rows;
+  z->n = z->high ? rows : cols;
+  if (z->m > kMostSmall) return SF_ERR_SHAPE;
+  auto up8 = [](int64_t v) { return (v + 7) / 8 * 8; };
+  z->ldm = up8(z->m);
+  z->ldn = up8(z->n);
+  z->mp = ceil_div(z->m, 256) * 256;
+  size_t o = kStatus + kScalars;
+  auto take = [&](size_t bytes) { const size_t r = o; o += (bytes + 255) & ~(size_t)255; return r; };
+  z->sums = take(8 * kNormCtas);
+  z->diag_a = take(4 * (size_t)z->mp);
+  z->diag_b = take(4 * (size_t)z->mp);
+  z->a = take(2 * (size_t)z->m * (size_t)z->ldm);
+  z->b = take(2 * (size_t)z->m * (size_t)z->ldm);
+  // (either of the last step's unused targets may hold the result on its way to rows that TMA cannot write)
+  const size_t x = 2 * (size_t)z->m * (size_t)z->ldn, y = 2 * (size_t)z->n * (size_t)z->ldm;
+  for (int i = 0; i < 4; ++i) z->x[i] = take(x > y ? x : y);
+  z->total = o;
+  return SF_OK;
+}
+
+// ---- the norm ---------------------------------------------------------------------------------------------
+template <bool kF32>
+__device__ __forceinline__ float element(const void* G, int64_t i) {
+  if constexpr (kF32) return __ldg(reinterpret_cast<const float*>(G) + i);
+  else return bf16_bits_to_float(__ldg(reinterpret_cast<const uint16_t*>(G) + i));
+}
+
+// Squares are summed in double: neither the largest nor the smallest float32 has one that leaves its range. wide: rows of 16-byte pieces.
+template <bool kF32>
+__global__ void __launch_bounds__(256)
+ns_norm_kernel(const void* __restrict__ G, int64_t rows, int64_t cols, int64_t ld, int wide, double* __restrict__ sums) {
+  __shared__ double part[8];
+  pdl_wait();
+  pdl_trigger();
+  constexpr int kPiece = kF32 ? 4 : 8;
+  double s = 0;
+  const int64_t per_row = wide ? cols / kPiece : cols, first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  const int64_t dr = step / per_row, dc = step - dr * per_row;
+  int64_t r = first / per_row, c = first - r * per_row;
+  for (; r < rows;) {
+    if (wide) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(G) + (r * ld + c * kPiece) * (kF32 ? 4 : 2)));
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kF32) {
+          const double x = __uint_as_float(w[i]);
+          s = fma(x, x, s);
+        } else {
+          const double x = bf16_bits_to_float(w[i] & 0xFFFFu), y = bf16_bits_to_float(w[i] >> 16);
+          s = fma(x, x, s);
+          s = fma(y, y, s);
+        }
+      }
+    } else {
+      const double x = element<kF32>(G, r * ld + c);
+      s = fma(x, x, s);
+    }
+    r += dr;
+    c += dc;
+    if (c >= per_row) { c -= per_row; ++r; }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 8; ++w) s += part[w];
+    sums[blockIdx.x] = s;
+  }
+}
+
+// ---- the first X -------------------------------------------------------------------------------------------
+// G 2^k in fp16 (two terms of a float32 G; a bf16 G fits one), k such that its norm lies in [2^13, 2^14); what is left of the norm, a factor of
+// 1 to 2 that is no power of two, goes into the first step's float32 arithmetic (*first), so that a bf16 G is not rounded at all. A G
+// of zeros stays zero; where G's norm is not finite the factor is NaN, and so is every result.
+struct NsScale { float lo, hi; };      // two powers of two whose product is 2^k
+__device__ __forceinline__ NsScale ns_scale(const double* __restrict__ sums, int count, float* first, double* shared) {
+  double s = 0;
+  for (int i = threadIdx.x; i < count; i += 256) s += __ldcg(sums + i);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = s;
+  __syncthreads();
+  s = shared[0];
+#pragma unroll
+  for (int w = 1; w < 8; ++w) s += shared[w];
+  const double norm = sqrt(s);
+  int k = 0;
+  float f = 0.f;
+  if (!(norm < INFINITY)) {
+    f = __uint_as_float(0x7FC00000u);
+  } else if (norm > 0) {
+    k = 13 - ilogb(norm);
+    f = (float)(16384.0 / scalbn(norm, k));
+  }
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *first = f;
+  const int h = k / 2;
+  return NsScale{scalbnf(1.f, h), scalbnf(1.f, k - h)};
+}
+__device__ __forceinline__ void ns_terms(float x, const NsScale& z, uint16_t& hi, uint16_t& lo) {
+  const float y = x * z.lo * z.hi;
+  const __half h = __float2half_rn(y), l = __float2half_rn(y - __half2float(h));
+  hi = __half_as_ushort(h);
+  lo = __half_as_ushort(l);
+}
+
+// As it lies: pieces of eight elements of a row (the last one of a row may be short; the padding behind it is written as 0).
+template <bool kF32>
+__global__ void __launch_bounds__(256)
+ns_convert_kernel(const void* __restrict__ G, int64_t rows, int64_t cols, int64_t ld, int wide, const double* __restrict__ sums, int count,
+                  float* __restrict__ first, uint4* __restrict__ hi, uint4* __restrict__ lo) {
+  __shared__ double shared[8];
+  pdl_wait();
+  pdl_trigger();
+  const NsScale z = ns_scale(sums, count, first, shared);
+  const int64_t per_row = (cols + 7) / 8, total = rows * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / per_row, c = (i - r * per_row) * 8;
+    float x[8];
+    if (wide) {                                            // whole pieces on 16-byte boundaries
+      if constexpr (kF32) {
+        const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(G) + r * ld + c);
+        const float4 u = __ldg(p), v = __ldg(p + 1);
+        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w; x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
+      } else {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(G) + r * ld + c));
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[2 * j] = bf16_bits_to_float(w[j] & 0xFFFFu); x[2 * j + 1] = bf16_bits_to_float(w[j] >> 16); }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = c + j < cols ? element<kF32>(G, r * ld + c + j) : 0.f;
+    }
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint16_t h0, l0, h1, l1;
+      ns_terms(x[2 * j], z, h0, l0);
+      ns_terms(x[2 * j + 1], z, h1, l1);
+      h[j] = h0 | (uint32_t)h1 << 16;
+      l[j] = l0 | (uint32_t)l1 << 16;
+    }
+    hi[i] = make_uint4(h[0], h[1], h[2], h[3]);
+    if (kF32) lo[i] = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+
+// Transposed: X [cols, ldn] from G [rows, cols], 64 x 64 elements to a CTA at a time.
+template <bool kF32>
+__global__ void __launch_bounds__(256)
+ns_convert_transposed_kernel(const void* __restrict__ G, int64_t rows, int64_t cols, int64_t ld, const double* __restrict__ sums, int count,
+                             float* __restrict__ first, int64_t ldn, uint16_t* __restrict__ hi, uint16_t* __restrict__ lo) {
+  __shared__ double shared[8];
+  __shared__ float tile[64][65];
+  pdl_wait();
+  pdl_trigger();
+  const NsScale z = ns_scale(sums, count, first, shared);
+  const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+  const int64_t tiles_c = (cols + 63) / 64, tiles = (rows + 63) / 64 * tiles_c;
+  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const int64_t r0 = t / tiles_c * 64, c0 = (t - t / tiles_c * tiles_c) * 64;
+    __syncthreads();
+#pragma unroll
+    for (int j = y; j < 64; j += 4)
+      if (r0 + j < rows && c0 + x < cols) tile[j][x] = element<kF32>(G, (r0 + j) * ld + c0 + x);
+    __syncthreads();
+#pragma unroll
+    for (int j = y; j < 64; j += 4)
+      if (c0 + j < cols && r0 + x < rows) {
+        uint16_t h, l;
+        ns_terms(tile[x][j], z, h, l);
+        hi[(c0 + j) * ldn + r0 + x] = h;
+        if (kF32) lo[(c0 + j) * ldn + r0 + x] = l;
+      }
+  }
+}
+
+// Rows that TMA cannot write (their stride is no multiple of 16 bytes): from a copy that it can.
+__global__ void __launch_bounds__(256)
+ns_copy_kernel(const uint16_t* __restrict__ from, int64_t ldf, int64_t rows, int64_t cols, int64_t ld, uint16_t* __restrict__ out) {
+  pdl_wait();
+  pdl_trigger();
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / cols, c = i - r * cols;
+    out[r * ld + c] = __ldcg(from + r * ldf + c);
+  }
+}
+
+// Whether the quintic keeps the singular values in the range that the fp16 operands are scaled for: from [0, 1.25] into itself, and its
+// factors within theirs.
+bool ns_bounded(double a, double b, double c) {
+  if (!(std::fabs(a) <= 8 && std::fabs(b) <= 8 && std::fabs(c) <= 8)) return false;
+  auto f = [&](double s) { return std::fabs(s * (a + s * s * (b + s * s * c))); };
+  auto g = [&](double l) { return std::fabs(l * (b + l * c)); };           // of B, for the eigenvalue l of A
+  double most = f(1.25), most_b = g(1.5625);
+  const double disc = 9 * b * b - 20 * a * c;                              // a + 3 b l + 5 c l^2 = 0, l = s^2
+  for (int i = 0; i < 2; ++i) {
+    const double l = c != 0 ? (disc < 0 ? -1 : (-3 * b + (i ? 1 : -1) * std::sqrt(disc)) / (10 * c)) : b != 0 ? -a / (3 * b) : -1;
+    if (l > 0 && l < 1.5625) most = std::fmax(most, f(std::sqrt(l)));
+  }
+  const double l = c != 0 ? -b / (2 * c) : -1;
+  if (l > 0 && l < 1.5625) most_b = std::fmax(most_b, g(l));
+  return most <= 1.25 && most_b <= 7.5;
+}
+
+size_t matrix_bytes(int64_t rows, int64_t cols, int64_t ld, int size) {
+  return rows > 0 && cols > 0 ? (size_t)size * ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) : 0;
+}
+
+}  // namespace
+}  // namespace sf
+
+using namespace sf;
+
+extern "C" {
+
+int sf_orthogonalize_workspace_size(int64_t rows, int64_t cols, size_t* bytes) {
+  NsShape z;
+  SF_TRY(ns_shape(rows, cols, &z));
+  if (!bytes) return SF_ERR_NULL;
+  *bytes = z.total;
+  return SF_OK;
+}
+
+int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_t ldg, int steps, float a, float b, float c, float scale, void* O,
+                     int64_t ldo, void* workspace, size_t workspace_bytes, void* stream) {
+  NsShape z;
+  if (type != SF_BF16 && type != SF_F32) return SF_ERR_UNSUPPORTED;
+  SF_TRY(ns_shape(rows, cols, &z));
+  if (steps < 1 || steps > 64 || !ns_bounded(a, b, c)) return SF_ERR_UNSUPPORTED;
+  if (rows == 0 || cols == 0) return SF_OK;
+  if (!G || !O || !workspace) return SF_ERR_NULL;
+  const int size = type == SF_F32 ? 4 : 2;
+  if (ldg < cols || ldo < cols || (uintptr_t)G % size || (uintptr_t)O % 2 || !aligned16(workspace)) return SF_ERR_ALIGN;
+  if (workspace_bytes < z.total) return SF_ERR_WORKSPACE;
+  if (!apart({{O, matrix_bytes(rows, cols, ldo, 2)}, {workspace, z.total}}, {{G, matrix_bytes(rows, cols, ldg, size)}})) return SF_ERR_UNSUPPORTED;
+  SF_TRY(check_arch());
+  cudaStream_t s = (cudaStream_t)stream;
+  uint8_t* w = (uint8_t*)workspace;
+  float *first = (float*)(w + kStatus), *diag_a = (float*)(w + z.diag_a), *diag_b = (float*)(w + z.diag_b);
+  double* sums = (double*)(w + z.sums);
+  const bool f32 = type == SF_F32;
+  const int piece = 16 / size;
+  const bool wide = aligned16(G) && ldg % piece == 0 && cols % 8 == 0;
+  const int64_t pieces = rows * (wide ? cols / piece : cols);
+  const int norm_ctas = (int)(ceil_div(pieces, 512) < kNormCtas ? ceil_div(pieces, 512) : kNormCtas);
+  SF_TRY(launch_pdl(f32 ? ns_norm_kernel<true> : ns_norm_kernel<false>, dim3(norm_ctas), 256, 0, s, G, rows, cols, ldg, (int)wide, sums));
+  if (z.high) {
+    const int64_t tiles = ceil_div(rows, 64) * ceil_div(cols, 64), most = 8 * sm_count_now();
+    SF_TRY(launch_pdl(f32 ? ns_convert_transposed_kernel<true> : ns_convert_transposed_kernel<false>, dim3((unsigned)(tiles < most ? tiles : most)), 256, 0,
+                      s, G, rows, cols, ldg, (const double*)sums, norm_ctas, first, z.ldn, (uint16_t*)(w + z.x[0]), (uint16_t*)(w + z.x[1])));
+  } else {
+    const int64_t ctas = ceil_div(rows * ceil_div(cols, 8), 256), most = 8 * sm_count_now();
+    SF_TRY(launch_pdl(f32 ? ns_convert_kernel<true> : ns_convert_kernel<false>, dim3((unsigned)(ctas < most ? ctas : most)), 256, 0, s, G, rows, cols, ldg,
+                      (int)wide, (const double*)sums, norm_ctas, first, (uint4*)(w + z.x[0]), (uint4*)(w + z.x[1])));
+  }
+  PairArgs p{};
+  p.jobs = 1;
+  p.status = (int*)workspace;
+  p.M[0] = p.N[0] = (int)z.m;
+  p.ns.a = a; p.ns.b = b; p.ns.c = c;
+  p.ns.scale = scale / 16384.f;
+  p.ns.transposed = z.high;
+  const bool direct = aligned16(O) && ldo % 8 == 0;
+  for (int k = 0; k < steps; ++k) {
+    const uint8_t *xh = w + z.x[2 * (k & 1)], *xl = w + z.x[2 * (k & 1) + 1];
+    uint8_t *yh = w + z.x[2 * (~k & 1)], *yl = w + z.x[2 * (~k & 1) + 1];
+    p.ns.first = k == 0 ? first : nullptr;
+    p.ns.last = k == steps - 1;
+    p.ns.two_terms = k > 0 || f32;
+    PairArgs q = p;
+    q.ns.diag_out = diag_a;
+    q.nkb = q.nkb0 = k_blocks(FMT_F16, z.n);
+    SF_TRY((launch_best<PK_GRAM, FMT_F16>(q, s, [&](CUtensorMap* m, int bn) {
+      SF_TRY(make_tmap_2d(&m[0], xh, z.m, z.n, z.ldn, 64, 128, true));
+      SF_TRY(make_tmap_2d(&m[1], xh, z.m, z.n, z.ldn, 64, bn / 2, true));
+      return make_tmap_store(&m[2], w + z.a, z.m, z.m, z.ldm);
+    })));
+    q = p;
+    q.ns.first = nullptr;
+    q.ns.diag_in = diag_a;
+    q.ns.diag_out = diag_b;
+    q.nkb = q.nkb0 = k_blocks(FMT_F16, z.m);
+    SF_TRY((launch_best<PK_POLY, FMT_F16>(q, s, [&](CUtensorMap* m, int bn) {
+      SF_TRY(make_tmap_2d(&m[0], w + z.a, z.m, z.m, z.ldm, 64, 128, true));
+      SF_TRY(make_tmap_2d(&m[1], w + z.a, z.m, z.m, z.ldm, 64, bn / 2, true));
+      SF_TRY(make_tmap_store(&m[2], w + z.b, z.m, z.m, z.ldm));
+      return make_tmap_store(&m[3], w + z.a, z.m, z.m, z.ldm);
+    })));
+    q = p;
+    q.ns.diag_in = diag_b;
+    q.N[0] = (int)z.n;
+    q.nkb = q.nkb0 = k_blocks(FMT_F16, z.m);
+    SF_TRY((launch_best<PK_APPLY, FMT_F16>(q, s, [&](CUtensorMap* m, int) {
+      SF_TRY(make_tmap_2d(&m[0], w + z.b, z.m, z.m, z.ldm, 64, 128, true));
+      SF_TRY(make_tmap_2d(&m[1], xh, z.m, z.n, z.ldn, 64, 64, true));
+      SF_TRY(make_tmap_store(&m[2], xh, z.m, z.n, z.ldn));
+      SF_TRY(make_tmap_store(&m[3], xl, z.m, z.n, z.ldn));
+      SF_TRY(make_tmap_store(&m[5], yl, z.m, z.n, z.ldn));
+      if (!q.ns.last) return make_tmap_store(&m[4], yh, z.m, z.n, z.ldn);
+      if (direct) return make_tmap_store(&m[4], O, rows, cols, ldo);
+      return make_tmap_store(&m[4], yh, rows, cols, z.high ? z.ldm : z.ldn);
+    })));
+  }
+  if (direct) return SF_OK;
+  const uint16_t* from = (const uint16_t*)(w + z.x[2 * (steps & 1)]);
+  const int64_t ctas = ceil_div(rows * cols, 256), most = 8 * sm_count_now();
+  return launch_pdl(ns_copy_kernel, dim3((unsigned)(ctas < most ? ctas : most)), 256, 0, s, from, z.high ? z.ldm : z.ldn, rows, cols, ldo, (uint16_t*)O);
+}
+
+}  // extern "C"

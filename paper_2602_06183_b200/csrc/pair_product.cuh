@@ -10,6 +10,11 @@
 //            product of the two is taken in registers and neither projection is written.
 //   PK_FWD_SAVE  the same, and P = act(g), Q = u act'(g) in float32 for the backward pass
 //   PK_BWD   dU = (A B) P, dG = (A B) Q                     A = dY, B = Wd [K, N]; dH is never written
+// and the three of an orthogonalised update (see newton_schulz.cu), of which the first two are symmetric: tiles on and below the
+// diagonal are computed, what lies below it is stored twice.
+//   PK_GRAM  A = X X^T                                      off the diagonal in fp16, the diagonal in float32
+//   PK_POLY  B = b A + c A^2                                the same; a on the diagonal too
+//   PK_APPLY X' = B X                                       B X in fp16 products, the diagonal's part in float32
 //
 // CTA = 10 warps: TMA producer, MMA issuer, two sets of four epilogue warps that share a tile's columns. Every wait is bounded
 // (see gemm_tc.cu): on expiry the CTA raises the status word and leaves.
@@ -22,6 +27,8 @@
 // Products of 4 bits, 4096 x 4096 x 8192, blocks of 16: 56 us (4.9 PFLOP/s, 78 %).
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "gated.cuh"
 
 namespace sf {
@@ -29,7 +36,7 @@ namespace {
 
 using namespace ptx;
 
-enum PairKind { PK_NT, PK_DX, PK_DW, PK_FWD, PK_FWD_SAVE, PK_BWD };
+enum PairKind { PK_NT, PK_DX, PK_DW, PK_FWD, PK_FWD_SAVE, PK_BWD, PK_GRAM, PK_POLY, PK_APPLY };
 
 constexpr int kPairThreads = 320;
 constexpr int kPairSmemMax = 232448;
@@ -41,11 +48,12 @@ enum PairMode { PM_FULL, PM_WIDTH, PM_SPLIT };
 
 template <int kKind, int kBN, int kFmt, int kMode>
 struct PairCfg {
-  static constexpr bool kFp4 = kFmt != FMT_BF16;
+  static constexpr bool kFp4 = is_fp4(kFmt);
   static constexpr bool kAMN = kKind == PK_DW;
-  static constexpr bool kBMN = kKind == PK_DX || kKind == PK_DW || kKind == PK_BWD;
+  static constexpr bool kBMN = kKind == PK_DX || kKind == PK_DW || kKind == PK_BWD || kKind == PK_APPLY;
+  static constexpr bool kSym = kKind == PK_GRAM || kKind == PK_POLY, kNs = kSym || kKind == PK_APPLY;
   static constexpr bool kGated = kKind == PK_FWD || kKind == PK_FWD_SAVE;
-  static constexpr bool kWide = kKind == PK_FWD_SAVE || kKind == PK_BWD;         // float32 chunks in the epilogue
+  static constexpr bool kWide = kKind == PK_FWD_SAVE || kKind == PK_BWD || kNs;   // float32 chunks in the epilogue, or pairs of 16-bit ones
   static constexpr int kHalf = kBN / 2;                                          // columns of B that a CTA holds
   static constexpr int kBChunks = (kHalf + 63) / 64;                             // MN-major B: chunks of 64 columns
   static constexpr int kABytes = 16384;
@@ -64,7 +72,7 @@ struct PairCfg {
   static constexpr uint32_t kScaleCol = kAccs * kBN;
   static constexpr uint32_t kScaleACols = kTiles * 4, kScaleCols = kScaleACols * (1 + kBBlocks);    // of one stage
   static constexpr int kMaps = kKind == PK_DW ? 9 : kKind == PK_DX ? 5 : kKind == PK_NT ? (kFp4 ? 5 : 3)
-                             : kKind == PK_FWD ? (kFp4 ? 7 : 4) : 6;
+                             : kKind == PK_FWD ? (kFp4 ? 7 : 4) : kKind == PK_GRAM ? 3 : kKind == PK_POLY ? 4 : 6;
   static_assert(kBN == 256 || (kFp4 && kBN == 128), "tile width");
   static_assert(kMode == PM_FULL || !kFp4 || (kMode == PM_SPLIT && kBN == 128), "4-bit operands: widths of whole row blocks of scales");
   static_assert(!kFp4 || kKind == PK_NT || (kKind == PK_FWD && kBN == 256), "4-bit operands: K-major, whole row blocks of scales");
@@ -72,6 +80,16 @@ struct PairCfg {
   static_assert(kScaleCol + 2 * kScaleCols <= 512, "TMEM columns");
 };
 
+// The products of an orthogonalised update. X is held as 2^14 times itself, A as 2^14, B as 2^12 times (see newton_schulz.cu).
+struct NsArgs {
+  const float* first;                // the first step's X is to be multiplied by *first (NULL: 1)
+  const float* diag_in;              // PK_POLY: the diagonal of A; PK_APPLY: that of B
+  float* diag_out;                   // PK_GRAM, PK_POLY
+  float a, b, c;                     // PK_POLY
+  int two_terms;                     // PK_APPLY: X has a second term
+  int last, transposed;              // PK_APPLY: the result is written as bf16 times `scale`, and as its transpose
+  float scale;
+};
 struct PairArgs {
   int jobs;
   int num_m[3], num_n[3];            // tiles of each job
@@ -89,16 +107,29 @@ struct PairArgs {
   // `late_rounds` tiles of this one, which those pairs leave to the others.
   int beside, first_late, late_rounds;
   int* status;
+  const float* row_scales;           // E4M3 operands: a factor to every row of A
+  NsArgs ns;
 };
 template <int N> struct PairMaps { CUtensorMap m[N]; };
 
 struct PairCtl {
-  uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], epi_full[8];
+  uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], epi_full[16];
   uint32_t tmem_base;
   int abort_flag;
 };
 
 struct PairTile { int job, m0, n0; };     // first row of the pair's tile, first column (PK_FWD: first feature)
+
+// Tiles of 256 x cols of a symmetric M x M that have a part on or below the diagonal: in a row of tiles, and in all.
+__host__ __device__ inline int lower_tiles_of_row(int m, int M, int cols) {
+  const int end = (m + 1) * 256 < M ? (m + 1) * 256 : M;
+  return (end + cols - 1) / cols;
+}
+__host__ __device__ inline int64_t lower_tiles(int M, int cols) {
+  int64_t n = 0;
+  for (int m = 0; m * 256 < M; ++m) n += lower_tiles_of_row(m, M, cols);
+  return n;
+}
 
 // The n-th tile of a pair: every num_pairs-th one; the first late_rounds rounds are shared by the pairs that are not late.
 __device__ __forceinline__ int nth_tile(const PairArgs& a, int n, int pair, int num_pairs) {
@@ -111,6 +142,11 @@ __device__ __forceinline__ int nth_tile(const PairArgs& a, int n, int pair, int 
 // the same time share few operand panels.
 template <int kKind>
 __device__ __forceinline__ PairTile pair_tile(const PairArgs& a, int tile, int cols) {
+  if constexpr (kKind == PK_GRAM || kKind == PK_POLY) {
+    int m = 0;
+    for (int n; tile >= (n = lower_tiles_of_row(m, a.M[0], cols)); ++m) tile -= n;
+    return PairTile{0, m * 256, tile * cols};
+  }
   int j = 0;
   if (kKind == PK_DW) {
     while (j < a.jobs - 1 && tile >= a.num_m[j] * a.num_n[j]) { tile -= a.num_m[j] * a.num_n[j]; ++j; }
@@ -198,6 +234,129 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar, int pair) {
       : "memory");
 }
 
+// ---- epilogue of an orthogonalised update's products ---------------------------------------------------------
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 from_f16x2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+// This lane's row of a chunk that is in a buffer, and its row of results as a column of one.
+__device__ __forceinline__ void row_get(const uint8_t* b, int lane, uint32_t (&w)[16]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint4 x = *reinterpret_cast<const uint4*>(b + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4));
+    w[4 * j] = x.x; w[4 * j + 1] = x.y; w[4 * j + 2] = x.z; w[4 * j + 3] = x.w;
+  }
+}
+__device__ __forceinline__ void column_put(uint8_t* b, int lane, const uint32_t (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    *reinterpret_cast<uint16_t*>(b + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2) = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+}
+struct NsRow { float scale, diag; };
+// What a row of a tile needs (arrays are padded to whole tiles).
+template <int kKind>
+__device__ __forceinline__ NsRow ns_begin(const PairArgs& args, int row) {
+  NsRow r;
+  r.scale = args.ns.first ? __ldcg(args.ns.first) : 1.f;
+  r.diag = kKind == PK_GRAM ? 0.f : __ldcg(args.ns.diag_in + row);
+  return r;
+}
+// A chunk of 32 x 32 sums, this lane's row of it, to its results. b: half of the warp's buffer, with what ns_fetch brought.
+template <int kKind>
+__device__ __forceinline__ bool ns_chunk(const PairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* b, uint64_t* loaded,
+                                         uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
+  constexpr float k14 = 1.f / 16384.f;
+  uint32_t w[16];
+  if constexpr (kKind == PK_GRAM) {
+    const float f = r.scale * r.scale * k14;
+    float d = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      float x = __uint_as_float(v[i]) * f;
+      if (row == col && i == lane) { d = x * k14; x = 0.f; }
+      v[i] = __float_as_uint(x);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = f16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+    if (row == col && row + lane < args.M[0]) args.ns.diag_out[row + lane] = d;
+    if (lane == 0) bulk_wait_read<1>();                    // the store before the last, from this half
+    __syncwarp();
+  } else {
+    if (!mbar_wait_warp(loaded, phase, abort_flag)) return false;
+    row_get(b, lane, w);
+    if constexpr (kKind == PK_POLY) {
+      const float pb = args.ns.b, pc = args.ns.c;
+      float d = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float4 dc = __ldcg(reinterpret_cast<const float4*>(args.ns.diag_in + col) + j);
+        const float2 a0 = from_f16x2(w[2 * j]), a1 = from_f16x2(w[2 * j + 1]);
+        const float a[4] = {a0.x * k14, a0.y * k14, a1.x * k14, a1.y * k14}, e[4] = {dc.x, dc.y, dc.z, dc.w};
+        float o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int i = 4 * j + k;
+          const float sq = __uint_as_float(v[i]) * (k14 * k14);
+          o[k] = 4096.f * fmaf(pc, fmaf(r.diag + e[k], a[k], sq), pb * a[k]);
+          if (row == col && i == lane) { d = fmaf(pc, fmaf(r.diag, r.diag, sq), fmaf(pb, r.diag, args.ns.a)); o[k] = 0.f; }
+        }
+        w[2 * j] = f16x2(o[0], o[1]);
+        w[2 * j + 1] = f16x2(o[2], o[3]);
+      }
+      if (row == col && row + lane < args.M[0]) args.ns.diag_out[row + lane] = d;
+    } else {
+      uint32_t lo[16];
+      if (args.ns.two_terms) row_get(b + 2048, lane, lo);
+      else
+#pragma unroll
+        for (int i = 0; i < 16; ++i) lo[i] = 0u;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float2 h = from_f16x2(w[i]), l = from_f16x2(lo[i]);
+        const float y0 = r.scale * fmaf(r.diag, h.x + l.x, __uint_as_float(v[2 * i]) * (1.f / 4096.f));
+        const float y1 = r.scale * fmaf(r.diag, h.y + l.y, __uint_as_float(v[2 * i + 1]) * (1.f / 4096.f));
+        if (args.ns.last) {
+          w[i] = bf16x2(y0 * args.ns.scale, y1 * args.ns.scale);
+        } else {
+          w[i] = f16x2(y0, y1);
+          const float2 g = from_f16x2(w[i]);
+          lo[i] = f16x2(y0 - g.x, y1 - g.y);
+        }
+      }
+      __syncwarp();                                        // every row has been read
+      if (args.ns.last) {
+        if (args.ns.transposed) column_put(b, lane, w);
+        else row_bf16(b, lane, w);
+      } else {
+        row_bf16(b, lane, w);
+        row_bf16(b + 2048, lane, lo);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        const bool t = args.ns.last && args.ns.transposed;
+        tma_store_2d(&maps[4], b, t ? row : col, t ? col : row);
+        if (!args.ns.last) tma_store_2d(&maps[5], b + 2048, col, row);
+        bulk_commit();
+      }
+      return true;
+    }
+    __syncwarp();
+  }
+  // as it lies, and mirrored
+  row_bf16(b, lane, w);
+  if (row != col) column_put(b + 2048, lane, w);
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_2d(&maps[2], b, col, row);
+    if (row != col) tma_store_2d(&maps[2], b + 2048, row, col);
+    bulk_commit();
+  }
+  return true;
+}
+
 template <int kKind, int kBN, int kFmt, int kMode>
 __global__ void __launch_bounds__(kPairThreads, 1)
 pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps> maps, const PairArgs args) {
@@ -222,7 +381,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
   const uint32_t stage_tx = sums   ? 2u * (uint32_t)(8192 + b_chunks * 4096)
                             : kVar ? 2u * (uint32_t)(Cfg::kABytes + (Cfg::kBMN ? b_chunks * 8192 : half * 128) + Cfg::kScaleBytes)
                                    : 2u * Cfg::kStageBytes;
-  int num_tiles = args.num_m[0] * args.num_n[0];
+  int num_tiles = Cfg::kSym ? args.num_n[0] : args.num_m[0] * args.num_n[0];
   if (kKind == PK_DW)
     for (int j = 1; j < args.jobs; ++j) num_tiles += args.num_m[j] * args.num_n[j];
 
@@ -236,7 +395,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       mbar_init(&ctl->tmem_full[b], 1);
       mbar_init(&ctl->tmem_empty[b], 16);                  // eight epilogue warps of either CTA
     }
-    for (int w = 0; w < 8; ++w) mbar_init(&ctl->epi_full[w], 1);
+    for (int w = 0; w < 16; ++w) mbar_init(&ctl->epi_full[w], 1);
     ctl->abort_flag = 0;
     fence_mbar_init();
   }
@@ -316,7 +475,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
   } else if (warp == 1) {
     // =========================== MMA issuer (leader CTA only) ===========================
     if (rank == 0) {
-      constexpr uint32_t idesc_full = kFp4 ? idesc_fp4(256, kBN, kFmt) : idesc_bf16(256, kBN, Cfg::kAMN, Cfg::kBMN, false);
+      constexpr uint32_t idesc_full = kFp4 ? idesc_fp4(256, kBN, kFmt) : idesc_plain(kFmt, 256, kBN, Cfg::kAMN, Cfg::kBMN);
       const uint32_t idesc = kVar ? idesc_full - ((uint32_t)(kBN - bn) >> 3 << 17) : idesc_full;
       constexpr uint64_t a_proto = desc_proto(Cfg::kAMN ? 8192 : 16, 1024, kSwizzle128B);
       constexpr uint64_t b_proto = desc_proto(Cfg::kBMN ? 8192 : 16, 1024, kSwizzle128B);
@@ -365,7 +524,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
           } else if (issues) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              if (kKind != PK_DW || k < 2 || !sums) mma_f16_2cta(d, a + k * a_step, b + k * b_step, idesc, k > 0 ? 1u : more);
+              if constexpr (kFmt == FMT_E4M3) mma_f8_2cta(d, a + k * a_step, b + k * b_step, idesc, k > 0 ? 1u : more);
+              else if (kKind != PK_DW || k < 2 || !sums) mma_f16_2cta(d, a + k * a_step, b + k * b_step, idesc, k > 0 ? 1u : more);
             commit_pair(&ctl->empty[stage], part);
           }
           __syncwarp();
@@ -397,12 +557,27 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       put_chunk_end(m, bufs + buf * kBufBytes, col, row, lane);
       buf ^= 1u;
     };
+    // PK_POLY: a chunk of A; PK_APPLY: one of X, both terms; into one of the two halves of the warp's buffer
+    auto ns_fetch = [&](int ch, int n0, int row, uint32_t h) {
+      if constexpr (Cfg::kNs && kKind != PK_GRAM) {
+        if (lane == 0) {
+          bulk_wait_read<0>();
+          const bool two = kKind == PK_APPLY && args.ns.two_terms;
+          uint8_t* b = bufs + h * kBufBytes;
+          mbar_arrive_expect_tx(loaded + 8 * h, two ? 4096u : 2048u);
+          tma_load_2d(b, &maps.m[kKind == PK_POLY ? 3 : 2], loaded + 8 * h, n0 + ch * 32, row);
+          if (two) tma_load_2d(b + 2048, &maps.m[3], loaded + 8 * h, n0 + ch * 32, row);
+        }
+        __syncwarp();
+      }
+    };
     for (int n = 0, tile; (tile = nth_tile(args, n, pair, num_pairs)) < num_tiles; ++n) {
       const PairTile t = pair_tile<kKind>(args, tile, tile_cols);
       const int row = t.m0 + rank * 128 + q * 32;
       const int M = kKind == PK_DW ? args.M[t.job] : args.M[0], N = kKind == PK_DW ? args.N[t.job] : args.N[0];
       // chunks of 32 output columns that are there; the two sets take them in turn
-      const int chunks = row < M ? min(tile_cols >> 5, (N - t.n0 + 31) >> 5) : 0;
+      int chunks = row < M ? min(tile_cols >> 5, (N - t.n0 + 31) >> 5) : 0;
+      if (Cfg::kSym) chunks = min(chunks, ((row - t.n0) >> 5) + 1);        // the rest is another chunk's mirror image
       auto fetch = [&](int ch) {                           // PK_BWD: P and Q of a chunk
         if (lane == 0) {
           bulk_wait_read<0>();
@@ -412,6 +587,12 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
         }
       };
       if (kKind == PK_BWD && part * 2 + set < chunks) fetch(part * 2 + set);
+      const float row_scale = kFmt == FMT_E4M3 ? args.alpha * (row + lane < M ? __ldg(args.row_scales + row + lane) : 0.f) : 1.f;
+      NsRow ns_row;
+      if constexpr (Cfg::kNs) {
+        ns_row = ns_begin<kKind>(args, row + lane);
+        if (kKind != PK_GRAM && part * 2 + set < chunks) ns_fetch(part * 2 + set, t.n0, row, buf);
+      }
       if (!mbar_wait_warp(&ctl->tmem_full[acc], acc_phase, abort_flag)) {
         if constexpr (!kSplit) break;
       }
@@ -454,6 +635,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
         for (int i = 0; i < 16; ++i) {
           float lo = __uint_as_float(v[2 * i]), hi = __uint_as_float(v[2 * i + 1]);
           if (kFp4) { lo *= args.alpha; hi *= args.alpha; }
+          if (kFmt == FMT_E4M3) { lo *= row_scale; hi *= row_scale; }
           w[i] = bf16x2(lo, hi);
         }
       };
@@ -462,6 +644,12 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
         const int col = t.n0 + ch * 32;
         if constexpr (kGated) {
           gated_chunk(v, u, col);
+        } else if constexpr (Cfg::kNs) {
+          const bool ok = ns_chunk<kKind>(args, maps.m, ns_row, v, bufs + buf * kBufBytes, loaded + 8 * buf, load_phase >> buf & 1u, abort_flag, col,
+                                          row, lane);
+          load_phase ^= 1u << buf;
+          buf ^= 1u;
+          return ok;
         } else if constexpr (kKind == PK_BWD) {
           uint32_t du[16], dg[16];
           if (!mbar_wait_warp(loaded, load_phase, abort_flag)) return false;
@@ -545,6 +733,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
           uint32_t v[32], u[32];
           tmem_ld_32x32b_x32(taddr + ch * 32, v);
           if constexpr (kGated) tmem_ld_32x32b_x32(taddr + half + ch * 32, u);
+          if constexpr (Cfg::kNs && kKind != PK_GRAM)
+            if (ch + 2 < chunks) ns_fetch(ch + 2, t.n0, row, buf ^ 1u);       // beside this chunk's work
           tmem_ld_wait_on(v);
           if constexpr (kGated) tmem_ld_wait_on(u);
           if (!(ok = chunk(v, u, ch))) break;
@@ -564,6 +754,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
         for (int ch = part * 2 + set; ch < chunks; ch += 2 * parts) {
           uint32_t v[32], u[32];
           if (kKind == PK_BWD && ch != part * 2 + set) fetch(ch);
+          if constexpr (Cfg::kNs && kKind != PK_GRAM)
+            if (ch != part * 2 + set) ns_fetch(ch, t.n0, row, buf);
           sum_parts(v, from + (uint32_t)ch * 16384u, rank, parts);
           if constexpr (kGated) sum_parts(u, from + (uint32_t)(ch + (half >> 5)) * 16384u, rank, parts);
           if (!chunk(v, u, ch)) break;
@@ -610,6 +802,10 @@ int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps>& maps, P
     a.num_m[j] = (a.M[j] + 255) / 256;
     a.num_n[j] = (a.N[j] + cols - 1) / cols;
     tiles += (int64_t)a.num_m[j] * a.num_n[j];
+  }
+  if (Cfg::kSym) {                                         // (the kernel reads num_n as the number of tiles)
+    tiles = lower_tiles(a.M[0], cols);
+    a.num_n[0] = (int)(tiles < 0x3FFFFFFF ? tiles : 0x3FFFFFFF);
   }
   if (tiles > 0x3FFFFFFF / (2 * parts)) return SF_ERR_SHAPE;
   const int64_t most = sm_count_now() / 2, pairs = kMode == PM_SPLIT ? tiles * parts : tiles < most ? tiles : most;

@@ -38,7 +38,7 @@ constexpr int64_t kMaxSize = (int64_t)1 << 28;      // of a dimension: coordinat
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // K in 2-byte units of a row, and k-blocks (64 units each)
-inline int64_t row_units(int fmt, int64_t K) { return fmt == FMT_BF16 ? K : K / 4; }
+inline int64_t row_units(int fmt, int64_t K) { return is_fp4(fmt) ? K / 4 : fmt == FMT_E4M3 ? K / 2 : K; }
 inline int k_blocks(int fmt, int64_t K) { return (int)ceil_div(row_units(fmt, K), 64); }
 // scale tiles along K of a 4-bit operand
 inline int64_t scale_tiles(int fmt, int64_t K) { return ceil_div(K, fmt == FMT_NV ? 64 : 128); }
@@ -54,6 +54,9 @@ inline int scale_map(void* m, int fmt, const void* p, int64_t rows, int64_t K) {
 }
 
 inline int64_t tiles_of(int64_t M, int64_t N, int64_t cols) { return ceil_div(M, 256) * ceil_div(N, cols); }
+inline int64_t tiles_of(int kind, int64_t M, int64_t N, int64_t cols) {
+  return kind == PK_GRAM || kind == PK_POLY ? lower_tiles((int)M, (int)cols) : tiles_of(M, N, cols);
+}
 
 // How a product on CTA pairs is cut, by its estimated clocks. Persistent tiles: rounds of nkb stages. Split: rounds of clusters, each with
 // its part of the stages, and with the sums through distributed shared memory and an epilogue that nothing runs beside.
@@ -65,15 +68,15 @@ inline int64_t tiles_of(int64_t M, int64_t N, int64_t cols) { return ceil_div(M,
 struct PairPlan { int mode, bn, parts; int64_t pairs; double clocks, per_tile; };      // pairs that it holds; estimates
 struct PairJob { int64_t M, N; };
 inline PairPlan pair_plan(int kind, const PairJob* jobs, int njobs, int64_t nkb, const FewRoom& room) {
-  const bool gated = kind == PK_FWD || kind == PK_FWD_SAVE, bmn = kind == PK_DX || kind == PK_DW || kind == PK_BWD;
-  const double chunk = kind == PK_FWD ? 1200 : kind == PK_FWD_SAVE ? 2400 : kind == PK_BWD ? 2200 : 1000;   // 32 output columns of a warp
+  const bool gated = kind == PK_FWD || kind == PK_FWD_SAVE, bmn = kind == PK_DX || kind == PK_DW || kind == PK_BWD || kind == PK_APPLY;
+  const double chunk = kind == PK_FWD ? 1200 : kind == PK_FWD_SAVE ? 2400 : kind == PK_BWD ? 2200 : kind == PK_POLY || kind == PK_APPLY ? 1800 : 1000;   // 32 output columns of a warp
   PairPlan best{PM_FULL, 256, 1, 0, 0, 0};
   double least = 0;
   const int64_t pairs = sm_count_now() / 2;
   for (int bn = 256; bn >= 64; bn -= gated ? 64 : 32) {
     const int cols = gated ? bn / 2 : bn;
     int64_t tiles = 0;
-    for (int j = 0; j < njobs; ++j) tiles += tiles_of(jobs[j].M, jobs[j].N, cols);
+    for (int j = 0; j < njobs; ++j) tiles += tiles_of(kind, jobs[j].M, jobs[j].N, cols);
     const double smem = bmn ? 256 + 64 * ceil_div(bn, 128) + bn / 2 : 256 + bn, stage = smem > 2 * bn ? smem : 2 * bn;
     const double epilogue = 900 + chunk * (double)ceil_div(cols, 64);
     for (int S = 1; S <= 4 && S <= nkb; ++S) {
@@ -156,7 +159,7 @@ int run_few_rows(const Operand& X, const Operand& W0, const Operand& W1, int64_t
     m.w1 = m.w0;
     if (kKind == FK_GATED) SF_TRY(kmajor_map(&m.w1, kFmt, W1.data, N, K, 128));
     m.sx = m.s0 = m.s1 = m.x;
-    if (kFmt != FMT_BF16) {
+    if (is_fp4(kFmt)) {
       SF_TRY(scale_map(&m.sx, kFmt, X.scales, a.T, K));
       SF_TRY(scale_map(&m.s0, kFmt, W0.scales, N, K));
       if (kKind == FK_GATED) SF_TRY(scale_map(&m.s1, kFmt, W1.scales, N, K));
@@ -166,15 +169,15 @@ int run_few_rows(const Operand& X, const Operand& W0, const Operand& W1, int64_t
 }
 
 // Launches the kernel of a plan: make(maps, bn) fills the tensor maps for tiles of that width.
-template <int kKind, typename F>
+template <int kKind, int kFmt = FMT_BF16, typename F>
 int launch_plan(const PairPlan& plan, PairArgs a, cudaStream_t s, F&& make) {
-  PairMaps<PairCfg<kKind, 256, FMT_BF16, PM_FULL>::kMaps> maps;
+  PairMaps<PairCfg<kKind, 256, kFmt, PM_FULL>::kMaps> maps;
   SF_TRY(make(maps.m, plan.bn));
   a.bn = plan.bn;
   a.parts = plan.parts;
-  return plan.mode == PM_FULL    ? launch_pair<kKind, 256, FMT_BF16, PM_FULL>(maps, a, s)
-         : plan.mode == PM_WIDTH ? launch_pair<kKind, 256, FMT_BF16, PM_WIDTH>(maps, a, s)
-                                 : launch_pair<kKind, 256, FMT_BF16, PM_SPLIT>(maps, a, s);
+  return plan.mode == PM_FULL    ? launch_pair<kKind, 256, kFmt, PM_FULL>(maps, a, s)
+         : plan.mode == PM_WIDTH ? launch_pair<kKind, 256, kFmt, PM_WIDTH>(maps, a, s)
+                                 : launch_pair<kKind, 256, kFmt, PM_SPLIT>(maps, a, s);
 }
 // The same from the sizes.
 inline int plan_pairs(int kind, const PairArgs& a, PairPlan* plan) {
@@ -185,12 +188,12 @@ inline int plan_pairs(int kind, const PairArgs& a, PairPlan* plan) {
   *plan = pair_plan(kind, jobs, a.jobs, a.nkb, *room);
   return SF_OK;
 }
-template <int kKind, typename F>
+template <int kKind, int kFmt = FMT_BF16, typename F>
 int launch_best(const PairArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr, const PairPlan* beside = nullptr) {
   PairPlan plan;
   SF_TRY(plan_pairs(kKind, a, &plan));
   if (taken) *taken = plan;
-  if (!beside) return launch_plan<kKind>(plan, a, s, make);
+  if (!beside) return launch_plan<kKind, kFmt>(plan, a, s, make);
   PairArgs b = a;
   b.beside = 1;
   const int64_t pairs = sm_count_now() / 2;
@@ -202,7 +205,7 @@ int launch_best(const PairArgs& a, cudaStream_t s, F&& make, PairPlan* taken = n
     for (int j = 0; j < a.jobs; ++j) tiles += tiles_of(a.M[j], a.N[j], plan.bn);
     if (tiles <= b.first_late) b.late_rounds = 0;
   }
-  return launch_plan<kKind>(plan, b, s, make);
+  return launch_plan<kKind, kFmt>(plan, b, s, make);
 }
 
 // A 4-bit product, by the same estimate: rounds of tiles of 256 or of 128 columns, a stage of either (bounded by what the L2 delivers), what a
@@ -246,12 +249,14 @@ int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, 
     FewArgs a{};
     a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.alpha = a.alpha2 = alpha; a.C = C; a.status = status;
     a.early_weights = early_weights; a.in_terms = terms; a.out_terms = 1;
+    if (kFmt == FMT_E4M3) a.row_scales = (const float*)A.scales;
     return run_few_rows<kFmt, FK_NT>(A, B, B, N, K, a, s);
   }
   PairArgs a{};
   a.jobs = 1; a.M[0] = (int)M; a.N[0] = (int)N; a.nkb = a.nkb0 = nkb; a.alpha = alpha; a.status = status;
-  if constexpr (kFmt == FMT_BF16) {
-    return launch_best<PK_NT>(a, s, [&](CUtensorMap* m, int bn) {
+  if constexpr (!is_fp4(kFmt)) {
+    if (kFmt == FMT_E4M3) a.row_scales = (const float*)A.scales;
+    return launch_best<PK_NT, kFmt>(a, s, [&](CUtensorMap* m, int bn) {
       SF_TRY(kmajor_map(&m[0], kFmt, A.data, M, K, 128));
       SF_TRY(kmajor_map(&m[1], kFmt, B.data, N, K, bn / 2));
       return make_tmap_store(&m[2], C, M, N);

@@ -1,0 +1,399 @@
+// Root-mean-square norm of a residual stream, in front of the layer:
+//   forward   S = bf16(X + R),  r = 1 / sqrt(mean_row(S^2) + eps),  y = S r gamma  ->  bf16, or E4M3 codes with a scale to every row
+//   backward  n = S r,  q = dY gamma,  dX = dS + r (q - n mean_row(q n)),  dgamma = sum over rows of dY n
+// The norm is that of the sum as it is stored, so that the backward pass, which has only the stored one, differentiates what was computed.
+// Sums are in float32; S, y, dX and dgamma are rounded once each.
+//
+// Memory bounds them: 8 bytes an element forward (7 with codes) and 8 backward. A row stays in the registers of one group of threads from
+// its load to its store; the only thing that crosses warps is a row's sum.
+#include "fp8_fmt.cuh"
+#include "gated.cuh"
+#include "sums.cuh"
+
+#define SF_TRY(expr)              \
+  do {                            \
+    int _st = (expr);             \
+    if (_st != SF_OK) return _st; \
+  } while (0)
+
+namespace sf {
+namespace {
+
+constexpr int64_t kMaxRows = (int64_t)1 << 28;
+constexpr int64_t kMaxWidth = 32768;
+constexpr int kBwdCtas = 296;          // of the backward pass, at most: each leaves one row of partial sums of dgamma
+
+// Past the L1: every element is read once. (Not the read-only path: the sum may be written where an input lies.)
+__device__ __forceinline__ uint4 load_once(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// A row's group of threads: one warp, or several that meet at a barrier of their own (the group's number + 1).
+struct Group {
+  int index, lane, size;
+  float* slots;                        // 2 x 32 of shared memory, taken in turn: one barrier to a reduction
+  int turn;
+  template <bool kMax>
+  __device__ __forceinline__ float reduce(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float w = __shfl_xor_sync(0xFFFFFFFFu, v, o);
+      v = kMax ? max_nan(v, w) : v + w;
+    }
+    if (size > 32) {
+      float* at = slots + turn * 32;
+      turn ^= 1;
+      const int warps = size >> 5;
+      if ((lane & 31) == 0) at[lane >> 5] = v;
+      asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(size) : "memory");
+      const float w = (lane & 31) < warps ? at[lane & 31] : 0.f;      // (0 is neutral for both: magnitudes)
+      v = w;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const float u = __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        v = kMax ? max_nan(v, u) : v + u;
+      }
+    }
+    return v;
+  }
+};
+
+struct NormArgs {
+  const uint16_t *X, *R, *gamma;
+  int64_t ldx, T;
+  uint16_t *sum, *Y;
+  uint8_t* codes;
+  float *scales, *rstd;
+  float scale, eps;
+  int D, tpr;                          // tpr: threads to a row
+};
+
+// Smallest magnitude that a row's scale is made for: a row of zeros has codes of 0 and a scale that is not 0.
+constexpr float kLeastAmax = 1.2621774483536189e-29f;      // 2^-96
+
+template <int V>
+__global__ void __launch_bounds__(1024)
+rmsnorm_kernel(const NormArgs a) {
+  __shared__ float slots[4][64];
+  Group g;
+  g.index = (int)threadIdx.x / a.tpr;
+  g.lane = (int)threadIdx.x - g.index * a.tpr;
+  g.size = a.tpr;
+  g.slots = slots[g.index];
+  g.turn = 0;
+  const int64_t row = (int64_t)blockIdx.x * (blockDim.x / a.tpr) + g.index;
+  const int vecs = a.D >> 3;
+  const uint4* gamma = reinterpret_cast<const uint4*>(a.gamma);
+  pdl_wait();
+  pdl_trigger();
+  if (row >= a.T) return;              // whole groups
+  uint4 s[V];
+  {
+    const uint4* x = reinterpret_cast<const uint4*>(a.X + row * a.ldx);
+    const uint4* r = reinterpret_cast<const uint4*>(a.R + row * a.D);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = g.lane + j * a.tpr;
+      s[j] = c < vecs ? load_once(x + c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (a.R) {
+      uint4 t[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int c = g.lane + j * a.tpr;
+        t[j] = c < vecs ? load_once(r + c) : make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        s[j].x = pack2(lo32(s[j].x) + lo32(t[j].x), hi32(s[j].x) + hi32(t[j].x));
+        s[j].y = pack2(lo32(s[j].y) + lo32(t[j].y), hi32(s[j].y) + hi32(t[j].y));
+        s[j].z = pack2(lo32(s[j].z) + lo32(t[j].z), hi32(s[j].z) + hi32(t[j].z));
+        s[j].w = pack2(lo32(s[j].w) + lo32(t[j].w), hi32(s[j].w) + hi32(t[j].w));
+      }
+    }
+  }
+  if (a.sum) {
+    uint4* out = reinterpret_cast<uint4*>(a.sum + row * a.D);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (g.lane + j * a.tpr < vecs) out[g.lane + j * a.tpr] = s[j];
+  }
+  float ss = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float l = lo32(word(s[j], i)), h = hi32(word(s[j], i));
+      ss = fmaf(l, l, ss);
+      ss = fmaf(h, h, ss);
+    }
+  ss = g.reduce<false>(ss);
+  const float rstd = __frsqrt_rn(ss / (float)a.D + a.eps);
+  if (a.rstd && g.lane == 0) a.rstd[row] = rstd;
+  auto normed = [&](const uint4& v, const uint4& w, int i, float& l, float& h) {
+    l = lo32(word(v, i)) * rstd * lo32(word(w, i));
+    h = hi32(word(v, i)) * rstd * hi32(word(w, i));
+  };
+  float inv = a.scale;
+  if (a.codes && a.scales) {           // a row's own scale: its largest magnitude becomes 448
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = g.lane + j * a.tpr;
+      if (c >= vecs) continue;
+      const uint4 w = __ldg(gamma + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float l, h;
+        normed(s[j], w, i, l, h);
+        top = max_nan(top, max_nan(fabsf(l), fabsf(h)));
+      }
+    }
+    top = max_nan(g.reduce<true>(top), kLeastAmax);
+    inv = __fdiv_rn(448.f, top);
+    if (g.lane == 0) a.scales[row] = __fdiv_rn(top, 448.f);
+  }
+  uint4* y = reinterpret_cast<uint4*>(a.Y + row * a.D);
+  uint2* q = reinterpret_cast<uint2*>(a.codes + row * a.D);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int c = g.lane + j * a.tpr;
+    if (c >= vecs) continue;
+    const uint4 w = __ldg(gamma + c);
+    uint32_t o[4], b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float l, h;
+      normed(s[j], w, i, l, h);
+      o[i] = pack2(l, h);
+      b[i] = e4m3x2(__fmul_rn(l, inv), __fmul_rn(h, inv));
+    }
+    if (a.Y) y[c] = make_uint4(o[0], o[1], o[2], o[3]);
+    if (a.codes) q[c] = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
+  }
+}
+
+struct NormBwdArgs {
+  const uint16_t *dY, *S, *gamma, *dS;
+  const float* rstd;
+  int64_t T;
+  uint16_t *dX, *dgamma;
+  float* parts;                        // [gridDim.x, D]
+  int D, tpr;
+};
+
+template <int V>
+__global__ void __launch_bounds__(V >= 4 ? 1024 : 512)
+rmsnorm_bwd_kernel(const NormBwdArgs a) {
+  __shared__ float slots[16][64];
+  extern __shared__ float sums[];      // [groups - 1][D] at the end
+  const int groups = (int)blockDim.x / a.tpr;
+  Group g;
+  g.index = (int)threadIdx.x / a.tpr;
+  g.lane = (int)threadIdx.x - g.index * a.tpr;
+  g.size = a.tpr;
+  g.slots = slots[g.index];
+  g.turn = 0;
+  const int vecs = a.D >> 3;
+  pdl_wait();
+  pdl_trigger();
+  float dg[V][8];
+  uint4 w[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int c = g.lane + j * a.tpr;
+    w[j] = c < vecs ? __ldg(reinterpret_cast<const uint4*>(a.gamma) + c) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[j][i] = 0.f;
+  }
+  const float inv_d = 1.f / (float)a.D;
+  for (int64_t row = (int64_t)blockIdx.x * groups + g.index; row < a.T; row += (int64_t)gridDim.x * groups) {
+    const uint4 *dy = reinterpret_cast<const uint4*>(a.dY + row * a.D), *s = reinterpret_cast<const uint4*>(a.S + row * a.D),
+                *ds = reinterpret_cast<const uint4*>(a.dS + row * a.D);
+    uint4 d[V], x[V], e[V];
+    const float r = __ldg(a.rstd + row);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = g.lane + j * a.tpr;
+      const bool in = c < vecs;
+      d[j] = in ? load_once(dy + c) : make_uint4(0u, 0u, 0u, 0u);
+      x[j] = in ? load_once(s + c) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (a.dS && a.dX) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int c = g.lane + j * a.tpr;
+        e[j] = c < vecs ? load_once(ds + c) : make_uint4(0u, 0u, 0u, 0u);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) e[j] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    float c1 = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t dw = word(d[j], i), xw = word(x[j], i), ww = word(w[j], i);
+        const float tl = lo32(dw) * (lo32(xw) * r), th = hi32(dw) * (hi32(xw) * r);
+        dg[j][2 * i] += tl;
+        dg[j][2 * i + 1] += th;
+        c1 = fmaf(tl, lo32(ww), c1);
+        c1 = fmaf(th, hi32(ww), c1);
+      }
+    if (!a.dX) continue;
+    const float m = g.reduce<false>(c1) * inv_d;
+    uint4* out = reinterpret_cast<uint4*>(a.dX + row * a.D);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = g.lane + j * a.tpr;
+      uint32_t o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t dw = word(d[j], i), xw = word(x[j], i), ww = word(w[j], i), ew = word(e[j], i);
+        o[i] = pack2(fmaf(r, fmaf(-lo32(xw) * r, m, lo32(dw) * lo32(ww)), lo32(ew)), fmaf(r, fmaf(-hi32(xw) * r, m, hi32(dw) * hi32(ww)), hi32(ew)));
+      }
+      if (c < vecs) out[c] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+  }
+  if (!a.dgamma) return;
+  // the groups' sums, in their order
+  if (g.index > 0)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = g.lane + j * a.tpr;
+      float4* at = reinterpret_cast<float4*>(sums + (int64_t)(g.index - 1) * a.D + c * 8);
+      if (c < vecs) {
+        at[0] = make_float4(dg[j][0], dg[j][1], dg[j][2], dg[j][3]);
+        at[1] = make_float4(dg[j][4], dg[j][5], dg[j][6], dg[j][7]);
+      }
+    }
+  if (groups > 1) __syncthreads();
+  if (g.index > 0) return;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int c = g.lane + j * a.tpr;
+    if (c >= vecs) continue;
+    for (int k = 0; k < groups - 1; ++k) {
+      const float4* at = reinterpret_cast<const float4*>(sums + (int64_t)k * a.D + c * 8);
+      const float4 p = at[0], q = at[1];
+      dg[j][0] += p.x; dg[j][1] += p.y; dg[j][2] += p.z; dg[j][3] += p.w;
+      dg[j][4] += q.x; dg[j][5] += q.y; dg[j][6] += q.z; dg[j][7] += q.w;
+    }
+    if (gridDim.x == 1) {              // one CTA had every row: its sums are the result
+      reinterpret_cast<uint4*>(a.dgamma)[c] =
+          make_uint4(pack2(dg[j][0], dg[j][1]), pack2(dg[j][2], dg[j][3]), pack2(dg[j][4], dg[j][5]), pack2(dg[j][6], dg[j][7]));
+    } else {
+      float4* at = reinterpret_cast<float4*>(a.parts + (int64_t)blockIdx.x * a.D + c * 8);
+      at[0] = make_float4(dg[j][0], dg[j][1], dg[j][2], dg[j][3]);
+      at[1] = make_float4(dg[j][4], dg[j][5], dg[j][6], dg[j][7]);
+    }
+  }
+}
+
+// Vectors of a row to a thread, and threads to a row. Few rows: as many threads as there are vectors, for latency. Many: four vectors,
+// whose loads are under way at once, and as many rows to an SM.
+// (threads: that a row may have with fewer than four vectors each; with four, 1024)
+struct RowPlan { int v, tpr; };
+RowPlan row_plan(int64_t T, int64_t D, int most, int threads) {
+  const int vecs = (int)(D / 8);
+  int v = T <= sm_count_now() ? 1 : vecs <= 32 ? 1 : vecs <= 64 ? 2 : most;
+  while (v < 4 && (vecs + v - 1) / v > threads) v *= 2;
+  return RowPlan{v, ((vecs + v - 1) / v + 31) / 32 * 32};
+}
+
+int bwd_ctas(int64_t T) { return (int)(T < kBwdCtas ? T : kBwdCtas); }
+
+int norm_shape(int64_t T, int64_t D) { return T < 0 || T > kMaxRows || D <= 0 || D % 8 || D > kMaxWidth ? SF_ERR_SHAPE : SF_OK; }
+
+}  // namespace
+}  // namespace sf
+
+using namespace sf;
+
+extern "C" {
+
+int sf_rmsnorm_fwd(const void* X, int64_t ldx, const void* residual, const void* gamma, int64_t T, int64_t D, float eps, void* sum, void* Y,
+                   void* codes, void* scales, float scale, void* rstd, void* stream) {
+  SF_TRY(norm_shape(T, D));
+  if (!(eps >= 0.f)) return SF_ERR_UNSUPPORTED;
+  if (T == 0) return SF_OK;
+  if (!X || !gamma || (!Y && !codes) || (scales && !codes)) return SF_ERR_NULL;
+  if (ldx < D || ldx % 8 || !aligned16(X) || !aligned16(residual) || !aligned16(gamma) || !aligned16(sum) || !aligned16(Y) || !aligned16(codes) ||
+      !aligned16(scales) || !aligned16(rstd))
+    return SF_ERR_ALIGN;
+  const size_t td = 2 * (size_t)T * (size_t)D, t4 = 4 * (size_t)T;
+  const Span x{X, 2 * ((size_t)(T - 1) * (size_t)ldx + (size_t)D)}, r{residual, td};
+  // the sum may take the place of one of the two that it is made of, and of nothing else
+  const bool in_x = sum && sum == X && ldx == D, in_r = sum && sum == residual;
+  if (!apart({{sum, td}, {Y, td}, {codes, td / 2}, {scales, t4}, {rstd, t4}},
+             {in_x ? Span{nullptr, 0} : x, in_r ? Span{nullptr, 0} : r, {gamma, 2 * (size_t)D}}) ||
+      ((in_x || in_r) && !apart({{Y, td}, {codes, td / 2}, {scales, t4}, {rstd, t4}}, {x, r})))
+    return SF_ERR_UNSUPPORTED;
+  SF_TRY(check_arch());
+  const RowPlan p = row_plan(T, D, 4, 1024);
+  const int groups = p.tpr >= 128 ? 1 : 128 / p.tpr;
+  NormArgs a{};
+  a.X = (const uint16_t*)X; a.R = (const uint16_t*)residual; a.gamma = (const uint16_t*)gamma; a.ldx = ldx; a.T = T;
+  a.sum = (uint16_t*)sum; a.Y = (uint16_t*)Y; a.codes = (uint8_t*)codes; a.scales = (float*)scales; a.rstd = (float*)rstd;
+  a.scale = scale; a.eps = eps; a.D = (int)D; a.tpr = p.tpr;
+  auto kern = p.v == 1 ? rmsnorm_kernel<1> : p.v == 2 ? rmsnorm_kernel<2> : rmsnorm_kernel<4>;
+  return launch_pdl(kern, dim3((unsigned)((T + groups - 1) / groups)), (unsigned)(groups * p.tpr), 0, (cudaStream_t)stream, a);
+}
+
+int sf_rmsnorm_bwd_workspace_size(int64_t T, int64_t D, size_t* bytes) {
+  SF_TRY(norm_shape(T, D));
+  if (!bytes) return SF_ERR_NULL;
+  *bytes = 4 * (size_t)bwd_ctas(T) * (size_t)D;
+  return SF_OK;
+}
+
+int sf_rmsnorm_bwd(const void* dY, const void* sum, const void* gamma, const void* rstd, const void* dS, int64_t T, int64_t D, void* dX,
+                   void* dgamma, void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need;
+  SF_TRY(sf_rmsnorm_bwd_workspace_size(T, D, &need));
+  if (!aligned16(dX) || !aligned16(dgamma)) return SF_ERR_ALIGN;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (T == 0) {                                            // no row: an empty sum
+    SF_TRY(check_arch());
+    if (dgamma) SF_CUDA_TRY(cudaMemsetAsync(dgamma, 0, 2 * (size_t)D, s));
+    return SF_OK;
+  }
+  if (!dX && !dgamma) return SF_OK;
+  if (!dY || !sum || !gamma || !rstd || (dgamma && !workspace)) return SF_ERR_NULL;
+  if (!aligned16(dY) || !aligned16(sum) || !aligned16(gamma) || !aligned16(rstd) || !aligned16(dS) || !aligned16(workspace)) return SF_ERR_ALIGN;
+  if (dgamma && workspace_bytes < need) return SF_ERR_WORKSPACE;
+  const size_t td = 2 * (size_t)T * (size_t)D, d2 = 2 * (size_t)D;
+  const Span parts{dgamma ? workspace : nullptr, need};
+  // dX may take the place of dY or of dS
+  if (!apart({{dX, td}, {dgamma, d2}, parts}, {{dX && dX == dY ? nullptr : dY, td}, {sum, td}, {gamma, d2}, {rstd, 4 * (size_t)T}, {dX && dX == dS ? nullptr : dS, td}}) ||
+      !apart({{dgamma, d2}, parts}, {{dY, td}, {dS, td}}))
+    return SF_ERR_UNSUPPORTED;
+  SF_TRY(check_arch());
+  const RowPlan p = row_plan(T, D, 2, 512);
+  const int ctas = bwd_ctas(T);
+  int groups = 512 / p.tpr;
+  const int64_t rows = (T + ctas - 1) / ctas;              // of a CTA
+  if (groups > rows) groups = (int)rows;
+  if (groups > 16) groups = 16;
+  while (groups > 1 && (int64_t)(groups - 1) * D * 4 > 40960) --groups;
+  if (groups < 1) groups = 1;
+  NormBwdArgs a{};
+  a.dY = (const uint16_t*)dY; a.S = (const uint16_t*)sum; a.gamma = (const uint16_t*)gamma; a.dS = (const uint16_t*)dS; a.rstd = (const float*)rstd;
+  a.T = T; a.dX = (uint16_t*)dX; a.dgamma = (uint16_t*)dgamma; a.parts = (float*)workspace; a.D = (int)D; a.tpr = p.tpr;
+  const size_t smem = (size_t)(groups - 1) * (size_t)D * 4;
+  auto kern = p.v == 1 ? rmsnorm_bwd_kernel<1> : p.v == 2 ? rmsnorm_bwd_kernel<2> : rmsnorm_bwd_kernel<4>;
+  SF_TRY(launch_pdl(kern, dim3((unsigned)ctas), (unsigned)(groups * p.tpr), smem, s, a));
+  if (!dgamma || ctas == 1) return SF_OK;
+  return launch_sum_parts((const float*)workspace, ctas, D, dgamma, s);
+}
+
+}  // extern "C"
