@@ -457,8 +457,8 @@ SF_API int sf_gemm_fp8_rows(const void* A, const void* a_scales, const void* B, 
  *       dl[t,e] = dloss p_te (balance_coef E / n^2 (n_e - sum_j n_j p_tj) + 2 z_coef lse_t / n)
  *       dX [T, D] = dX_in + dl means (dX_in bf16 [T, D] or NULL for 0; dX may be dX_in itself),   dmeans [E, D] = dl^T X,  bf16.
  *     Either output may be NULL. With T == 0 dmeans is zero. dl stays in float32, or as a sum of two bf16 numbers.
- * The same call gives the same bits. `workspace`: sf_router_balance_workspace_size() bytes for either call, the first 256 zeroed once before
- * first use; calls that may overlap on the GPU need workspaces of their own. Outputs that otherwise share a byte with one another or with
+ * The same call gives the same bits. `workspace`: sf_router_balance_workspace_size() bytes for either call, the first 256 the status word as
+ * everywhere (zeroed once before first use); calls that may overlap on the GPU need workspaces of their own. Outputs that otherwise share a byte with one another or with
  * an input are refused (SF_ERR_UNSUPPORTED). */
 SF_API int sf_router_balance_workspace_size(int64_t T, int64_t D, int E, size_t* bytes);
 SF_API int sf_router_balance_fwd(const void* logits, const void* expert, int64_t T, int E, float balance_coef, float z_coef, void* loss,

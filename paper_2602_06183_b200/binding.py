@@ -856,7 +856,7 @@ def sf_router_balance_bwd(logits, expert, counts, balance_coef: float, z_coef: f
     T, E = _logits_shape(w, logits)
     D = _matrix_shape(w, X)[1]
     both = dX is None and dmeans is None
-    if both or (dmeans is not None and workspace is None):
+    if both or workspace is None:
         with _allocating(stream):
             if both:
                 dX, dmeans = torch.empty((T, D), dtype=_BF16, device=X.device), torch.empty((E, D), dtype=_BF16, device=X.device)
