@@ -32,7 +32,8 @@ constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostCols = (int64_t)1 << 20;
 constexpr int kLossCtas = 148, kLossThreads = 256;
 constexpr size_t kHead = 256, kDone = 128;                 // status word; the word that counts the CTAs that have finished
 
-struct LossPart { float p[kMostExperts]; float z; int n[kMostExperts]; };
+// (z in double: a masked row's log-sum-exp may be the lowest float32, whose square is none)
+struct LossPart { float p[kMostExperts]; double z; int n[kMostExperts]; };
 
 struct Softmax { float p[kMostExperts], lse; };
 // Of E logits; entries from E on are 0.
@@ -70,7 +71,7 @@ balance_loss_kernel(const float* __restrict__ logits, const int* __restrict__ ex
     const int ex = __ldg(expert + t);
     if ((unsigned)ex >= (unsigned)E) continue;
     const Softmax s = softmax_of(logits + t * E, E);
-    a.z = fmaf(s.lse, s.lse, a.z);
+    a.z = fma((double)s.lse, (double)s.lse, a.z);
 #pragma unroll
     for (int e = 0; e < kMostExperts; ++e) {
       a.p[e] += s.p[e];
@@ -107,7 +108,7 @@ balance_loss_kernel(const float* __restrict__ logits, const int* __restrict__ ex
   long long n = 0;
   if (lane < 17)
     for (int i = 0; i < (int)gridDim.x; ++i) {
-      p += lane < 16 ? __ldcg(&parts[i].p[lane]) : __ldcg(&parts[i].z);
+      p += lane < 16 ? (double)__ldcg(&parts[i].p[lane]) : __ldcg(&parts[i].z);
       if (lane < 16) n += __ldcg(&parts[i].n[lane]);
     }
   long long all = n;
