@@ -13,8 +13,14 @@
 //     A = D + A', A^2 = D^2 + D A' + A' D + A'^2, B X = diag(B) X + B' X. A matrix of 512 x 2048: 0.3 % to 0.05 %.
 // Then the final rounding to bf16 (0.17 %) is the largest error.
 //
-// Launches: norm (partial sums in double), conversion (with the transposition of a high G), then three a step (PK_GRAM, PK_POLY, PK_APPLY of
-// pair_product.cuh). X X^T and A^2 are symmetric: half of their tiles are computed. Flops a step, m <= n: m^2 n + m^3 + 2 m^2 n.
+// Several steps at once, where X is wide: a step multiplies X by a polynomial of A, so what X becomes after g steps is Q X with Q a product of
+// polynomials of the first A, and the A of the next step is A B^2 (B = a I + b A + c A^2): all of them symmetric, of the small side, and
+// commuting. Then X is read and written once for g steps, 3 m^2 n + (4 g - 3) m^3 flops in place of 3 g m^2 n + g m^3 (m <= n; halves of the
+// symmetric products). What rounding leaves in A where it has no eigenvalue grows 11.9 times with a step, so A is made anew from X after three
+// steps, then after every two, and A is held in two terms for what is added elementwise. (Five steps at once: errors of 0.4 to 6 %.)
+//
+// Launches: norm (partial sums in double), conversion (with the transposition of a high G), then PK_GRAM, PK_SYMM and PK_APPLY of
+// pair_product.cuh: three for a single step, 4 g - 1 for g at once. Half of the tiles of the symmetric ones are computed.
 #include "products.cuh"
 
 namespace sf {
@@ -26,9 +32,13 @@ constexpr int64_t kMostSide = 1 << 24, kMostSmall = 1 << 16;
 
 struct NsShape {
   int64_t m, n, ldm, ldn, mp;          // small and large side, leading dimensions, m in whole tiles
-  bool high;                           // G has more rows than columns
-  size_t sums, diag_a, diag_b, a, b, x[4], total;
+  bool high, grouped;                  // G has more rows than columns; several steps at once
+  int matrices;                        // symmetric ones
+  size_t sums, sym[5], second, diag[5], x[4], total;      // (second: that term of the first matrix)
 };
+
+// Several steps at once pay where X is wider than high and the products are longer than what a launch costs.
+bool ns_grouped(int64_t m, int64_t n) { return m >= 1024 && 2 * n >= 3 * m; }
 
 int ns_shape(int64_t rows, int64_t cols, NsShape* z) {
   if (rows < 0 || cols < 0 || rows > kMostSide || cols > kMostSide) return SF_ERR_SHAPE;
@@ -40,14 +50,17 @@ int ns_shape(int64_t rows, int64_t cols, NsShape* z) {
   z->ldm = up8(z->m);
   z->ldn = up8(z->n);
   z->mp = ceil_div(z->m, 256) * 256;
+  z->grouped = ns_grouped(z->m, z->n);
+  z->matrices = z->grouped ? 5 : 2;
   size_t o = kStatus + kScalars;
   auto take = [&](size_t bytes) { const size_t r = o; o += (bytes + 255) & ~(size_t)255; return r; };
   z->sums = take(8 * kNormCtas);
-  z->diag_a = take(4 * (size_t)z->mp);
-  z->diag_b = take(4 * (size_t)z->mp);
-  z->a = take(2 * (size_t)z->m * (size_t)z->ldm);
-  z->b = take(2 * (size_t)z->m * (size_t)z->ldm);
-  // (either of the last step's unused targets may hold the result on its way to rows that TMA cannot write)
+  for (int i = 0; i < z->matrices; ++i) {
+    z->sym[i] = take(2 * (size_t)z->m * (size_t)z->ldm);
+    z->diag[i] = take(4 * (size_t)z->mp);
+  }
+  z->second = z->grouped ? take(2 * (size_t)z->m * (size_t)z->ldm) : z->sym[0];
+  // (either of the last product's unused targets may hold the result on its way to rows that TMA cannot write)
   const size_t x = 2 * (size_t)z->m * (size_t)z->ldn, y = 2 * (size_t)z->n * (size_t)z->ldm;
   for (int i = 0; i < 4; ++i) z->x[i] = take(x > y ? x : y);
   z->total = o;
@@ -226,19 +239,24 @@ ns_copy_kernel(const uint16_t* __restrict__ from, int64_t ldf, int64_t rows, int
 }
 
 // Whether the quintic keeps the singular values in the range that the fp16 operands are scaled for: from [0, 1.25] into itself, and its
-// factors within theirs.
-bool ns_bounded(double a, double b, double c) {
+// factors within theirs. p: the largest |a + b l + c l^2| of an eigenvalue l of A, which is at most 1.25^2.
+bool ns_bounded(double a, double b, double c, double* p) {
   if (!(std::fabs(a) <= 8 && std::fabs(b) <= 8 && std::fabs(c) <= 8)) return false;
+  constexpr double top = 1.5625;
   auto f = [&](double s) { return std::fabs(s * (a + s * s * (b + s * s * c))); };
-  auto g = [&](double l) { return std::fabs(l * (b + l * c)); };           // of B, for the eigenvalue l of A
-  double most = f(1.25), most_b = g(1.5625);
+  auto q = [&](double l) { return l * (b + l * c); };
+  double most = f(1.25), most_b = std::fabs(q(top));
+  *p = std::fmax(std::fabs(a), std::fabs(a + q(top)));
   const double disc = 9 * b * b - 20 * a * c;                              // a + 3 b l + 5 c l^2 = 0, l = s^2
   for (int i = 0; i < 2; ++i) {
     const double l = c != 0 ? (disc < 0 ? -1 : (-3 * b + (i ? 1 : -1) * std::sqrt(disc)) / (10 * c)) : b != 0 ? -a / (3 * b) : -1;
-    if (l > 0 && l < 1.5625) most = std::fmax(most, f(std::sqrt(l)));
+    if (l > 0 && l < top) most = std::fmax(most, f(std::sqrt(l)));
   }
   const double l = c != 0 ? -b / (2 * c) : -1;
-  if (l > 0 && l < 1.5625) most_b = std::fmax(most_b, g(l));
+  if (l > 0 && l < top) {
+    most_b = std::fmax(most_b, std::fabs(q(l)));
+    *p = std::fmax(*p, std::fabs(a + q(l)));
+  }
   return most <= 1.25 && most_b <= 7.5;
 }
 
@@ -266,7 +284,8 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
   NsShape z;
   if (type != SF_BF16 && type != SF_F32) return SF_ERR_UNSUPPORTED;
   SF_TRY(ns_shape(rows, cols, &z));
-  if (steps < 1 || steps > 64 || !ns_bounded(a, b, c)) return SF_ERR_UNSUPPORTED;
+  double p_most;
+  if (steps < 1 || steps > 64 || !ns_bounded(a, b, c, &p_most)) return SF_ERR_UNSUPPORTED;
   if (rows == 0 || cols == 0) return SF_OK;
   if (!G || !O || !workspace) return SF_ERR_NULL;
   const int size = type == SF_F32 ? 4 : 2;
@@ -276,7 +295,7 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
   SF_TRY(check_arch());
   cudaStream_t s = (cudaStream_t)stream;
   uint8_t* w = (uint8_t*)workspace;
-  float *first = (float*)(w + kStatus), *diag_a = (float*)(w + z.diag_a), *diag_b = (float*)(w + z.diag_b);
+  float* first = (float*)(w + kStatus);
   double* sums = (double*)(w + z.sums);
   const bool f32 = type == SF_F32;
   const int piece = 16 / size;
@@ -297,41 +316,82 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
   p.jobs = 1;
   p.status = (int*)workspace;
   p.M[0] = p.N[0] = (int)z.m;
-  p.ns.a = a; p.ns.b = b; p.ns.c = c;
   p.ns.scale = scale / 16384.f;
   p.ns.transposed = z.high;
   const bool direct = aligned16(O) && ldo % 8 == 0;
-  for (int k = 0; k < steps; ++k) {
-    const uint8_t *xh = w + z.x[2 * (k & 1)], *xl = w + z.x[2 * (k & 1) + 1];
-    uint8_t *yh = w + z.x[2 * (~k & 1)], *yl = w + z.x[2 * (~k & 1) + 1];
-    p.ns.first = k == 0 ? first : nullptr;
-    p.ns.last = k == steps - 1;
-    p.ns.two_terms = k > 0 || f32;
+  // exponents: of A 14, of a product that is `most` at most, so that it stays below 2^15
+  auto exponent = [](double most) { return 14 - (int)std::ceil(std::log2(std::fmax(most, 1.0))); };
+  struct Sym { int at, e, two; };      // number of the matrix, exponent, whether it has two terms (the first may)
+  auto matrix = [&](const Sym& x) { return SymMatrix{(const float*)(w + z.diag[x.at]), std::ldexp(1.f, -x.e), x.two}; };
+  auto map = [&](CUtensorMap* m, const Sym& x, int term) { return make_tmap_store(m, w + (term && x.two ? z.second : z.sym[x.at]), z.m, z.m, z.ldm); };
+  auto target = [&](PairArgs& q, const Sym& x) {
+    q.ns.diag_out = (float*)(w + z.diag[x.at]);
+    q.ns.up = std::ldexp(1.f, x.e);
+    q.ns.two_out = x.two;
+  };
+  // out = c0 I + c1 x + c2 x y
+  auto product = [&](const Sym& x, const Sym& y, float c0, float c1, float c2, const Sym& out) {
     PairArgs q = p;
-    q.ns.diag_out = diag_a;
+    q.ns.m1 = matrix(x);
+    q.ns.m2 = matrix(y);
+    q.ns.same = x.at == y.at;
+    q.ns.c0 = c0; q.ns.c1 = c1; q.ns.c2 = c2;
+    target(q, out);
+    q.ns.down = std::ldexp(1.f, -x.e - y.e);
+    q.nkb = q.nkb0 = k_blocks(FMT_F16, z.m);
+    return launch_best<PK_SYMM, FMT_F16>(q, s, [&](CUtensorMap* m, int bn) {
+      SF_TRY(make_tmap_2d(&m[0], w + z.sym[x.at], z.m, z.m, z.ldm, 64, 128, true));
+      SF_TRY(make_tmap_2d(&m[1], w + z.sym[y.at], z.m, z.m, z.ldm, 64, bn / 2, true));
+      SF_TRY(map(&m[2], out, 0));
+      SF_TRY(map(&m[3], out, 1));
+      SF_TRY(map(&m[4], x, 0));
+      SF_TRY(map(&m[5], x, 1));
+      return map(&m[6], y, 0);
+    });
+  };
+  int groups = 0;
+  for (int done = 0; done < steps; ++groups) {
+    const int most = !z.grouped ? 1 : done == 0 ? 3 : 2, g = steps - done < most ? steps - done : most;
+    const uint8_t *xh = w + z.x[2 * (groups & 1)], *xl = w + z.x[2 * (groups & 1) + 1];
+    uint8_t *yh = w + z.x[2 * (~groups & 1)], *yl = w + z.x[2 * (~groups & 1) + 1];
+    const Sym A{0, 14, g > 1};
+    PairArgs q = p;
+    q.ns.first = done == 0 ? first : nullptr;
+    target(q, A);
+    q.ns.down = std::ldexp(1.f, -28);
     q.nkb = q.nkb0 = k_blocks(FMT_F16, z.n);
     SF_TRY((launch_best<PK_GRAM, FMT_F16>(q, s, [&](CUtensorMap* m, int bn) {
       SF_TRY(make_tmap_2d(&m[0], xh, z.m, z.n, z.ldn, 64, 128, true));
       SF_TRY(make_tmap_2d(&m[1], xh, z.m, z.n, z.ldn, 64, bn / 2, true));
-      return make_tmap_store(&m[2], w + z.a, z.m, z.m, z.ldm);
+      SF_TRY(map(&m[2], A, 0));
+      return map(&m[3], A, 1);
     })));
+    Sym Q{-1, 0, 0};
+    double q_most = 1;
+    for (int k = 0; k < g; ++k) {
+      // matrices 1 to 3 hold B and Q in turn (with k == 2 the first B is no longer needed), 4 holds A B
+      const Sym B{k == 1 ? 2 : 1, exponent(p_most), 0}, AB{4, exponent(1.5625 * p_most), 0};
+      SF_TRY(product(A, A, a, b, c, B));
+      if (k < g - 1) {
+        SF_TRY(product(A, B, 0.f, 0.f, 1.f, AB));
+        SF_TRY(product(AB, B, 0.f, 0.f, 1.f, A));
+      }
+      q_most *= p_most;
+      const Sym next{k == 1 ? 3 : 2, exponent(q_most), 0};
+      if (k > 0) SF_TRY(product(Q, B, 0.f, 0.f, 1.f, next));
+      Q = k == 0 ? B : next;
+    }
+    done += g;
     q = p;
-    q.ns.first = nullptr;
-    q.ns.diag_in = diag_a;
-    q.ns.diag_out = diag_b;
-    q.nkb = q.nkb0 = k_blocks(FMT_F16, z.m);
-    SF_TRY((launch_best<PK_POLY, FMT_F16>(q, s, [&](CUtensorMap* m, int bn) {
-      SF_TRY(make_tmap_2d(&m[0], w + z.a, z.m, z.m, z.ldm, 64, 128, true));
-      SF_TRY(make_tmap_2d(&m[1], w + z.a, z.m, z.m, z.ldm, 64, bn / 2, true));
-      SF_TRY(make_tmap_store(&m[2], w + z.b, z.m, z.m, z.ldm));
-      return make_tmap_store(&m[3], w + z.a, z.m, z.m, z.ldm);
-    })));
-    q = p;
-    q.ns.diag_in = diag_b;
+    q.ns.first = groups == 0 ? first : nullptr;
+    q.ns.last = done == steps;
+    q.ns.two_terms = groups > 0 || f32;
+    q.ns.diag_in = (const float*)(w + z.diag[Q.at]);
+    q.ns.down = std::ldexp(1.f, -Q.e);
     q.N[0] = (int)z.n;
     q.nkb = q.nkb0 = k_blocks(FMT_F16, z.m);
     SF_TRY((launch_best<PK_APPLY, FMT_F16>(q, s, [&](CUtensorMap* m, int) {
-      SF_TRY(make_tmap_2d(&m[0], w + z.b, z.m, z.m, z.ldm, 64, 128, true));
+      SF_TRY(make_tmap_2d(&m[0], w + z.sym[Q.at], z.m, z.m, z.ldm, 64, 128, true));
       SF_TRY(make_tmap_2d(&m[1], xh, z.m, z.n, z.ldn, 64, 64, true));
       SF_TRY(make_tmap_store(&m[2], xh, z.m, z.n, z.ldn));
       SF_TRY(make_tmap_store(&m[3], xl, z.m, z.n, z.ldn));
@@ -342,7 +402,7 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
     })));
   }
   if (direct) return SF_OK;
-  const uint16_t* from = (const uint16_t*)(w + z.x[2 * (steps & 1)]);
+  const uint16_t* from = (const uint16_t*)(w + z.x[2 * (groups & 1)]);
   const int64_t ctas = ceil_div(rows * cols, 256), most = 8 * sm_count_now();
   return launch_pdl(ns_copy_kernel, dim3((unsigned)(ctas < most ? ctas : most)), 256, 0, s, from, z.high ? z.ldm : z.ldn, rows, cols, ldo, (uint16_t*)O);
 }

@@ -13,8 +13,8 @@
 // and the three of an orthogonalised update (see newton_schulz.cu), of which the first two are symmetric: tiles on and below the
 // diagonal are computed, what lies below it is stored twice.
 //   PK_GRAM  A = X X^T                                      off the diagonal in fp16, the diagonal in float32
-//   PK_POLY  B = b A + c A^2                                the same; a on the diagonal too
-//   PK_APPLY X' = B X                                       B X in fp16 products, the diagonal's part in float32
+//   PK_SYMM  c0 I + c1 M1 + c2 M1 M2                        of symmetric matrices that commute, the diagonals' parts in float32
+//   PK_APPLY X' = Q X                                       the diagonal's part in float32
 //
 // CTA = 10 warps: TMA producer, MMA issuer, two sets of four epilogue warps that share a tile's columns. Every wait is bounded
 // (see gemm_tc.cu): on expiry the CTA raises the status word and leaves.
@@ -36,7 +36,7 @@ namespace {
 
 using namespace ptx;
 
-enum PairKind { PK_NT, PK_DX, PK_DW, PK_FWD, PK_FWD_SAVE, PK_BWD, PK_GRAM, PK_POLY, PK_APPLY };
+enum PairKind { PK_NT, PK_DX, PK_DW, PK_FWD, PK_FWD_SAVE, PK_BWD, PK_GRAM, PK_SYMM, PK_APPLY };
 
 constexpr int kPairThreads = 320;
 constexpr int kPairSmemMax = 232448;
@@ -51,7 +51,7 @@ struct PairCfg {
   static constexpr bool kFp4 = is_fp4(kFmt);
   static constexpr bool kAMN = kKind == PK_DW;
   static constexpr bool kBMN = kKind == PK_DX || kKind == PK_DW || kKind == PK_BWD || kKind == PK_APPLY;
-  static constexpr bool kSym = kKind == PK_GRAM || kKind == PK_POLY, kNs = kSym || kKind == PK_APPLY;
+  static constexpr bool kSym = kKind == PK_GRAM || kKind == PK_SYMM, kNs = kSym || kKind == PK_APPLY;
   static constexpr bool kGated = kKind == PK_FWD || kKind == PK_FWD_SAVE;
   static constexpr bool kWide = kKind == PK_FWD_SAVE || kKind == PK_BWD || kNs;   // float32 chunks in the epilogue, or pairs of 16-bit ones
   static constexpr int kHalf = kBN / 2;                                          // columns of B that a CTA holds
@@ -72,7 +72,7 @@ struct PairCfg {
   static constexpr uint32_t kScaleCol = kAccs * kBN;
   static constexpr uint32_t kScaleACols = kTiles * 4, kScaleCols = kScaleACols * (1 + kBBlocks);    // of one stage
   static constexpr int kMaps = kKind == PK_DW ? 9 : kKind == PK_DX ? 5 : kKind == PK_NT ? (kFp4 ? 5 : 3)
-                             : kKind == PK_FWD ? (kFp4 ? 7 : 4) : kKind == PK_GRAM ? 3 : kKind == PK_POLY ? 4 : 6;
+                             : kKind == PK_FWD ? (kFp4 ? 7 : 4) : kKind == PK_GRAM ? 4 : kKind == PK_SYMM ? 7 : 6;
   static_assert(kBN == 256 || (kFp4 && kBN == 128), "tile width");
   static_assert(kMode == PM_FULL || !kFp4 || (kMode == PM_SPLIT && kBN == 128), "4-bit operands: widths of whole row blocks of scales");
   static_assert(!kFp4 || kKind == PK_NT || (kKind == PK_FWD && kBN == 256), "4-bit operands: K-major, whole row blocks of scales");
@@ -80,13 +80,23 @@ struct PairCfg {
   static_assert(kScaleCol + 2 * kScaleCols <= 512, "TMEM columns");
 };
 
-// The products of an orthogonalised update. X is held as 2^14 times itself, A as 2^14, B as 2^12 times (see newton_schulz.cu).
+// The products of an orthogonalised update. A matrix is held as a power of two times itself, in fp16, in one term or two; a symmetric one
+// without its diagonal, which is apart in float32 (see newton_schulz.cu). up: 2^e of the result; down: 2^-e of the operands together.
+struct SymMatrix {
+  const float* diag;
+  float down;                          // 2^-e
+  int two;                             // terms: the second factor has one
+};
 struct NsArgs {
   const float* first;                // the first step's X is to be multiplied by *first (NULL: 1)
-  const float* diag_in;              // PK_POLY: the diagonal of A; PK_APPLY: that of B
-  float* diag_out;                   // PK_GRAM, PK_POLY
-  float a, b, c;                     // PK_POLY
-  int two_terms;                     // PK_APPLY: X has a second term
+  SymMatrix m1, m2;                  // PK_SYMM: the factors
+  int same;                          // ... which are one and the same
+  float c0, c1, c2;                  // ... c0 I + c1 M1 + c2 M1 M2
+  const float* diag_in;              // PK_APPLY: the diagonal of the matrix that is applied
+  float* diag_out;                   // PK_GRAM, PK_SYMM
+  float up, down;
+  int two_out;                       // PK_GRAM, PK_SYMM: the result has two terms
+  int two_terms;                     // PK_APPLY: X has
   int last, transposed;              // PK_APPLY: the result is written as bf16 times `scale`, and as its transpose
   float scale;
 };
@@ -142,7 +152,7 @@ __device__ __forceinline__ int nth_tile(const PairArgs& a, int n, int pair, int 
 // the same time share few operand panels.
 template <int kKind>
 __device__ __forceinline__ PairTile pair_tile(const PairArgs& a, int tile, int cols) {
-  if constexpr (kKind == PK_GRAM || kKind == PK_POLY) {
+  if constexpr (kKind == PK_GRAM || kKind == PK_SYMM) {
     int m = 0;
     for (int n; tile >= (n = lower_tiles_of_row(m, a.M[0], cols)); ++m) tile -= n;
     return PairTile{0, m * 256, tile * cols};
@@ -253,105 +263,137 @@ __device__ __forceinline__ void column_put(uint8_t* b, int lane, const uint32_t 
   for (int i = 0; i < 32; ++i)
     *reinterpret_cast<uint16_t*>(b + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2) = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
 }
-struct NsRow { float scale, diag; };
+struct NsRow { float scale, d1, d2; };
 // What a row of a tile needs (arrays are padded to whole tiles).
 template <int kKind>
 __device__ __forceinline__ NsRow ns_begin(const PairArgs& args, int row) {
-  NsRow r;
-  r.scale = args.ns.first ? __ldcg(args.ns.first) : 1.f;
-  r.diag = kKind == PK_GRAM ? 0.f : __ldcg(args.ns.diag_in + row);
+  NsRow r{1.f, 0.f, 0.f};
+  if (kKind != PK_SYMM && args.ns.first) r.scale = __ldcg(args.ns.first);
+  if (kKind == PK_SYMM) { r.d1 = __ldcg(args.ns.m1.diag + row); r.d2 = __ldcg(args.ns.m2.diag + row); }
+  if (kKind == PK_APPLY) r.d1 = __ldcg(args.ns.diag_in + row);
   return r;
 }
-// A chunk of 32 x 32 sums, this lane's row of it, to its results. b: half of the warp's buffer, with what ns_fetch brought.
+// A chunk of 32 x 32 sums of a symmetric result, this lane's row of it: as it lies and mirrored, one term or two. bufs: the warp's buffer of
+// four times 2 KB. PK_GRAM: half, that half of it which a result of one term takes. PK_SYMM: the buffer holds the factors' chunks (ns_fetch), and
+// the result takes their place; dcol: the second factor's diagonal at this lane's column.
 template <int kKind>
-__device__ __forceinline__ bool ns_chunk(const PairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* b, uint64_t* loaded,
-                                         uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
-  constexpr float k14 = 1.f / 16384.f;
-  uint32_t w[16];
+__device__ __forceinline__ bool ns_symmetric(const PairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* bufs, uint32_t half,
+                                             float dcol, uint64_t* loaded, uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
+  const bool on_diag = row == col;
+  const float up = args.ns.up;
+  float d = 0.f;
   if constexpr (kKind == PK_GRAM) {
-    const float f = r.scale * r.scale * k14;
-    float d = 0.f;
+    const float f = r.scale * r.scale * args.ns.down;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       float x = __uint_as_float(v[i]) * f;
-      if (row == col && i == lane) { d = x * k14; x = 0.f; }
-      v[i] = __float_as_uint(x);
+      if (on_diag && i == lane) { d = x; x = 0.f; }
+      v[i] = __float_as_uint(x * up);
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = f16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-    if (row == col && row + lane < args.M[0]) args.ns.diag_out[row + lane] = d;
-    if (lane == 0) bulk_wait_read<1>();                    // the store before the last, from this half
-    __syncwarp();
   } else {
+    const float c1 = args.ns.c1, c2 = args.ns.c2, down = args.ns.down, down1 = args.ns.m1.down, down2 = args.ns.m2.down;
+    const bool same = args.ns.same, two1 = args.ns.m1.two;
     if (!mbar_wait_warp(loaded, phase, abort_flag)) return false;
-    row_get(b, lane, w);
-    if constexpr (kKind == PK_POLY) {
-      const float pb = args.ns.b, pc = args.ns.c;
-      float d = 0.f;
+    uint32_t h1[16], l1[16], h2[16];
+    row_get(bufs, lane, h1);
+    if (two1) row_get(bufs + 2048, lane, l1);
+    if (!same) row_get(bufs + 4096, lane, h2);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float4 dc = __ldcg(reinterpret_cast<const float4*>(args.ns.diag_in + col) + j);
-        const float2 a0 = from_f16x2(w[2 * j]), a1 = from_f16x2(w[2 * j + 1]);
-        const float a[4] = {a0.x * k14, a0.y * k14, a1.x * k14, a1.y * k14}, e[4] = {dc.x, dc.y, dc.z, dc.w};
-        float o[4];
+    for (int q = 0; q < 16; ++q) {
+      float2 x = from_f16x2(h1[q]);
+      if (two1) { const float2 y = from_f16x2(l1[q]); x.x += y.x; x.y += y.y; }
+      x.x *= down1; x.y *= down1;
+      float2 z = x;
+      if (!same) {
+        z = from_f16x2(h2[q]);
+        z.x *= down2; z.y *= down2;
+      }
+      const float a[2] = {x.x, x.y}, b[2] = {z.x, z.y};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int i = 4 * j + k;
-          const float sq = __uint_as_float(v[i]) * (k14 * k14);
-          o[k] = 4096.f * fmaf(pc, fmaf(r.diag + e[k], a[k], sq), pb * a[k]);
-          if (row == col && i == lane) { d = fmaf(pc, fmaf(r.diag, r.diag, sq), fmaf(pb, r.diag, args.ns.a)); o[k] = 0.f; }
-        }
-        w[2 * j] = f16x2(o[0], o[1]);
-        w[2 * j + 1] = f16x2(o[2], o[3]);
+      for (int u = 0; u < 2; ++u) {
+        const int i = 2 * q + u;
+        const float p = __uint_as_float(v[i]) * down;
+        float o = fmaf(c2, fmaf(r.d1, b[u], fmaf(a[u], __shfl_sync(0xFFFFFFFFu, dcol, i), p)), c1 * a[u]);
+        if (on_diag && i == lane) { d = fmaf(c2, fmaf(r.d1, r.d2, p), fmaf(c1, r.d1, args.ns.c0)); o = 0.f; }
+        v[i] = __float_as_uint(o * up);
       }
-      if (row == col && row + lane < args.M[0]) args.ns.diag_out[row + lane] = d;
-    } else {
-      uint32_t lo[16];
-      if (args.ns.two_terms) row_get(b + 2048, lane, lo);
-      else
-#pragma unroll
-        for (int i = 0; i < 16; ++i) lo[i] = 0u;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float2 h = from_f16x2(w[i]), l = from_f16x2(lo[i]);
-        const float y0 = r.scale * fmaf(r.diag, h.x + l.x, __uint_as_float(v[2 * i]) * (1.f / 4096.f));
-        const float y1 = r.scale * fmaf(r.diag, h.y + l.y, __uint_as_float(v[2 * i + 1]) * (1.f / 4096.f));
-        if (args.ns.last) {
-          w[i] = bf16x2(y0 * args.ns.scale, y1 * args.ns.scale);
-        } else {
-          w[i] = f16x2(y0, y1);
-          const float2 g = from_f16x2(w[i]);
-          lo[i] = f16x2(y0 - g.x, y1 - g.y);
-        }
-      }
-      __syncwarp();                                        // every row has been read
-      if (args.ns.last) {
-        if (args.ns.transposed) column_put(b, lane, w);
-        else row_bf16(b, lane, w);
-      } else {
-        row_bf16(b, lane, w);
-        row_bf16(b + 2048, lane, lo);
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        const bool t = args.ns.last && args.ns.transposed;
-        tma_store_2d(&maps[4], b, t ? row : col, t ? col : row);
-        if (!args.ns.last) tma_store_2d(&maps[5], b + 2048, col, row);
-        bulk_commit();
-      }
-      return true;
     }
-    __syncwarp();
   }
-  // as it lies, and mirrored
+  if (on_diag && row + lane < args.M[0]) args.ns.diag_out[row + lane] = d;
+  const bool two = args.ns.two_out;
+  uint8_t* b = bufs;
+  if constexpr (kKind == PK_GRAM) {
+    if (!two) b += half * 4096u;
+    if (lane == 0) {
+      if (two) bulk_wait_read<0>();
+      else bulk_wait_read<1>();                            // the store before the last, from this half
+    }
+  }
+  __syncwarp();                                            // (PK_SYMM: every row has been read)
+  uint32_t w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = f16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
   row_bf16(b, lane, w);
-  if (row != col) column_put(b + 2048, lane, w);
+  if (!on_diag) column_put(b + 2048, lane, w);
+  if (two) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float2 h = from_f16x2(w[i]);
+      w[i] = f16x2(__uint_as_float(v[2 * i]) - h.x, __uint_as_float(v[2 * i + 1]) - h.y);
+    }
+    row_bf16(b + 4096, lane, w);
+    if (!on_diag) column_put(b + 6144, lane, w);
+  }
   fence_proxy_async_smem();
   __syncwarp();
   if (lane == 0) {
     tma_store_2d(&maps[2], b, col, row);
-    if (row != col) tma_store_2d(&maps[2], b + 2048, row, col);
+    if (!on_diag) tma_store_2d(&maps[2], b + 2048, row, col);
+    if (two) {
+      tma_store_2d(&maps[3], b + 4096, col, row);
+      if (!on_diag) tma_store_2d(&maps[3], b + 6144, row, col);
+    }
+    bulk_commit();
+  }
+  return true;
+}
+// A chunk of Q X, with what ns_fetch brought to b, a half of the warp's buffer.
+__device__ __forceinline__ bool ns_apply(const PairArgs& args, const CUtensorMap* maps, const NsRow& r, const uint32_t (&v)[32], uint8_t* b, uint64_t* loaded,
+                                         uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
+  if (!mbar_wait_warp(loaded, phase, abort_flag)) return false;
+  uint32_t w[16], lo[16];
+  row_get(b, lane, w);
+  if (args.ns.two_terms) row_get(b + 2048, lane, lo);
+  else
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lo[i] = 0u;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float2 h = from_f16x2(w[i]), l = from_f16x2(lo[i]);
+    const float y0 = r.scale * fmaf(r.d1, h.x + l.x, __uint_as_float(v[2 * i]) * args.ns.down);
+    const float y1 = r.scale * fmaf(r.d1, h.y + l.y, __uint_as_float(v[2 * i + 1]) * args.ns.down);
+    if (args.ns.last) {
+      w[i] = bf16x2(y0 * args.ns.scale, y1 * args.ns.scale);
+    } else {
+      w[i] = f16x2(y0, y1);
+      const float2 g = from_f16x2(w[i]);
+      lo[i] = f16x2(y0 - g.x, y1 - g.y);
+    }
+  }
+  __syncwarp();                                            // every row has been read
+  if (args.ns.last) {
+    if (args.ns.transposed) column_put(b, lane, w);
+    else row_bf16(b, lane, w);
+  } else {
+    row_bf16(b, lane, w);
+    row_bf16(b + 2048, lane, lo);
+  }
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    const bool t = args.ns.last && args.ns.transposed;
+    tma_store_2d(&maps[4], b, t ? row : col, t ? col : row);
+    if (!args.ns.last) tma_store_2d(&maps[5], b + 2048, col, row);
     bulk_commit();
   }
   return true;
@@ -557,16 +599,25 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       put_chunk_end(m, bufs + buf * kBufBytes, col, row, lane);
       buf ^= 1u;
     };
-    // PK_POLY: a chunk of A; PK_APPLY: one of X, both terms; into one of the two halves of the warp's buffer
+    // PK_APPLY: a chunk of X, both terms, into one of the two halves of the warp's buffer; PK_SYMM: the factors' chunks into all of it
+    float ns_dcol = 0.f;
     auto ns_fetch = [&](int ch, int n0, int row, uint32_t h) {
-      if constexpr (Cfg::kNs && kKind != PK_GRAM) {
+      const int col = n0 + ch * 32;
+      if constexpr (kKind == PK_SYMM) ns_dcol = __ldcg(args.ns.m2.diag + col + lane);
+      if constexpr (kKind == PK_APPLY || kKind == PK_SYMM) {
         if (lane == 0) {
           bulk_wait_read<0>();
-          const bool two = kKind == PK_APPLY && args.ns.two_terms;
-          uint8_t* b = bufs + h * kBufBytes;
-          mbar_arrive_expect_tx(loaded + 8 * h, two ? 4096u : 2048u);
-          tma_load_2d(b, &maps.m[kKind == PK_POLY ? 3 : 2], loaded + 8 * h, n0 + ch * 32, row);
-          if (two) tma_load_2d(b + 2048, &maps.m[3], loaded + 8 * h, n0 + ch * 32, row);
+          if constexpr (kKind == PK_APPLY) {
+            uint8_t* b = bufs + h * kBufBytes;
+            mbar_arrive_expect_tx(loaded + 8 * h, args.ns.two_terms ? 4096u : 2048u);
+            tma_load_2d(b, &maps.m[2], loaded + 8 * h, col, row);
+            if (args.ns.two_terms) tma_load_2d(b + 2048, &maps.m[3], loaded + 8 * h, col, row);
+          } else {
+            mbar_arrive_expect_tx(loaded, 2048u * (1u + (args.ns.m1.two ? 1u : 0u) + (args.ns.same ? 0u : 1u)));
+            tma_load_2d(bufs, &maps.m[4], loaded, col, row);
+            if (args.ns.m1.two) tma_load_2d(bufs + 2048, &maps.m[5], loaded, col, row);
+            if (!args.ns.same) tma_load_2d(bufs + 4096, &maps.m[6], loaded, col, row);
+          }
         }
         __syncwarp();
       }
@@ -644,9 +695,13 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
         const int col = t.n0 + ch * 32;
         if constexpr (kGated) {
           gated_chunk(v, u, col);
-        } else if constexpr (Cfg::kNs) {
-          const bool ok = ns_chunk<kKind>(args, maps.m, ns_row, v, bufs + buf * kBufBytes, loaded + 8 * buf, load_phase >> buf & 1u, abort_flag, col,
-                                          row, lane);
+        } else if constexpr (Cfg::kSym) {
+          const bool ok = ns_symmetric<kKind>(args, maps.m, ns_row, v, bufs, buf, ns_dcol, loaded, load_phase & 1u, abort_flag, col, row, lane);
+          load_phase ^= 1u;
+          buf ^= 1u;
+          return ok;
+        } else if constexpr (kKind == PK_APPLY) {
+          const bool ok = ns_apply(args, maps.m, ns_row, v, bufs + buf * kBufBytes, loaded + 8 * buf, load_phase >> buf & 1u, abort_flag, col, row, lane);
           load_phase ^= 1u << buf;
           buf ^= 1u;
           return ok;
@@ -733,12 +788,14 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
           uint32_t v[32], u[32];
           tmem_ld_32x32b_x32(taddr + ch * 32, v);
           if constexpr (kGated) tmem_ld_32x32b_x32(taddr + half + ch * 32, u);
-          if constexpr (Cfg::kNs && kKind != PK_GRAM)
+          if constexpr (kKind == PK_APPLY)
             if (ch + 2 < chunks) ns_fetch(ch + 2, t.n0, row, buf ^ 1u);       // beside this chunk's work
           tmem_ld_wait_on(v);
           if constexpr (kGated) tmem_ld_wait_on(u);
           if (!(ok = chunk(v, u, ch))) break;
           if (kKind == PK_BWD && ch + 2 < chunks) fetch(ch + 2);
+          if constexpr (kKind == PK_SYMM)
+            if (ch + 2 < chunks) ns_fetch(ch + 2, t.n0, row, 0);
         }
         if (!ok) break;
         release();
@@ -754,7 +811,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
         for (int ch = part * 2 + set; ch < chunks; ch += 2 * parts) {
           uint32_t v[32], u[32];
           if (kKind == PK_BWD && ch != part * 2 + set) fetch(ch);
-          if constexpr (Cfg::kNs && kKind != PK_GRAM)
+          if constexpr (kKind == PK_APPLY || kKind == PK_SYMM)
             if (ch != part * 2 + set) ns_fetch(ch, t.n0, row, buf);
           sum_parts(v, from + (uint32_t)ch * 16384u, rank, parts);
           if constexpr (kGated) sum_parts(u, from + (uint32_t)(ch + (half >> 5)) * 16384u, rank, parts);

@@ -55,7 +55,7 @@ inline int scale_map(void* m, int fmt, const void* p, int64_t rows, int64_t K) {
 
 inline int64_t tiles_of(int64_t M, int64_t N, int64_t cols) { return ceil_div(M, 256) * ceil_div(N, cols); }
 inline int64_t tiles_of(int kind, int64_t M, int64_t N, int64_t cols) {
-  return kind == PK_GRAM || kind == PK_POLY ? lower_tiles((int)M, (int)cols) : tiles_of(M, N, cols);
+  return kind == PK_GRAM || kind == PK_SYMM ? lower_tiles((int)M, (int)cols) : tiles_of(M, N, cols);
 }
 
 // How a product on CTA pairs is cut, by its estimated clocks. Persistent tiles: rounds of nkb stages. Split: rounds of clusters, each with
@@ -69,7 +69,7 @@ struct PairPlan { int mode, bn, parts; int64_t pairs; double clocks, per_tile; }
 struct PairJob { int64_t M, N; };
 inline PairPlan pair_plan(int kind, const PairJob* jobs, int njobs, int64_t nkb, const FewRoom& room) {
   const bool gated = kind == PK_FWD || kind == PK_FWD_SAVE, bmn = kind == PK_DX || kind == PK_DW || kind == PK_BWD || kind == PK_APPLY;
-  const double chunk = kind == PK_FWD ? 1200 : kind == PK_FWD_SAVE ? 2400 : kind == PK_BWD ? 2200 : kind == PK_POLY || kind == PK_APPLY ? 1800 : 1000;   // 32 output columns of a warp
+  const double chunk = kind == PK_FWD ? 1200 : kind == PK_FWD_SAVE ? 2400 : kind == PK_BWD ? 2200 : kind == PK_SYMM || kind == PK_APPLY ? 1800 : 1000;   // 32 output columns of a warp
   PairPlan best{PM_FULL, 256, 1, 0, 0, 0};
   double least = 0;
   const int64_t pairs = sm_count_now() / 2;
