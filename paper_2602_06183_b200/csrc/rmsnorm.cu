@@ -21,7 +21,7 @@ namespace {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 28;
 constexpr int64_t kMaxWidth = 32768;
-constexpr int kBwdCtas = 296;          // of the backward pass, at most: each leaves one row of partial sums of dgamma
+constexpr int kBwdCtas = 148;          // of the backward pass, at most: each leaves one row of partial sums of dgamma
 
 // Past the L1: every element is read once. (Not the read-only path: the sum may be written where an input lies.)
 __device__ __forceinline__ uint4 load_once(const uint4* p) {
@@ -36,33 +36,36 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// A row's group of threads: one warp, or several that meet at a barrier of their own (the group's number + 1).
+// A row's group of threads: 8, 16 or 32 lanes of a warp, or several warps that meet at a barrier of their own (the group's number + 1). Every
+// lane of a warp comes to a reduction, whether its row is there or not.
 struct Group {
   int index, lane, size;
-  float* slots;                        // 2 x 32 of shared memory, taken in turn: one barrier to a reduction
+  float* slots;                        // 2 x 64 of shared memory, taken in turn: one barrier to a reduction
   int turn;
+  // The group's sum of v and, with kMax, its largest m (a magnitude).
   template <bool kMax>
-  __device__ __forceinline__ float reduce(float v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float w = __shfl_xor_sync(0xFFFFFFFFu, v, o);
-      v = kMax ? max_nan(v, w) : v + w;
+  __device__ __forceinline__ void reduce(float& v, float& m) {
+    for (int o = size < 32 ? size >> 1 : 16; o > 0; o >>= 1) {
+      v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+      if (kMax) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
     }
     if (size > 32) {
-      float* at = slots + turn * 32;
+      float* at = slots + turn * 64;
       turn ^= 1;
-      const int warps = size >> 5;
-      if ((lane & 31) == 0) at[lane >> 5] = v;
+      const int warps = size >> 5, l = lane & 31;
+      if (l == 0) {
+        at[lane >> 5] = v;
+        if (kMax) at[32 + (lane >> 5)] = m;
+      }
       asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(size) : "memory");
-      const float w = (lane & 31) < warps ? at[lane & 31] : 0.f;      // (0 is neutral for both: magnitudes)
-      v = w;
+      v = l < warps ? at[l] : 0.f;
+      if (kMax) m = l < warps ? at[32 + l] : 0.f;
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) {
-        const float u = __shfl_xor_sync(0xFFFFFFFFu, v, o);
-        v = kMax ? max_nan(v, u) : v + u;
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        if (kMax) m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
       }
     }
-    return v;
   }
 };
 
@@ -79,22 +82,23 @@ struct NormArgs {
 // Smallest magnitude that a row's scale is made for: a row of zeros has codes of 0 and a scale that is not 0.
 constexpr float kLeastAmax = 1.2621774483536189e-29f;      // 2^-96
 
-template <int V>
+// kRows: codes with a scale to every row.
+template <int V, bool kRows>
 __global__ void __launch_bounds__(1024)
 rmsnorm_kernel(const NormArgs a) {
-  __shared__ float slots[4][64];
+  __shared__ float slots[2][128];       // (of groups of more than a warp)
   Group g;
   g.index = (int)threadIdx.x / a.tpr;
   g.lane = (int)threadIdx.x - g.index * a.tpr;
   g.size = a.tpr;
-  g.slots = slots[g.index];
+  g.slots = slots[a.tpr > 32 ? g.index : 0];
   g.turn = 0;
   const int64_t row = (int64_t)blockIdx.x * (blockDim.x / a.tpr) + g.index;
-  const int vecs = a.D >> 3;
+  const bool here = row < a.T;
+  const int vecs = here ? a.D >> 3 : 0;                    // of this row
   const uint4* gamma = reinterpret_cast<const uint4*>(a.gamma);
   pdl_wait();
   pdl_trigger();
-  if (row >= a.T) return;              // whole groups
   uint4 s[V];
   {
     const uint4* x = reinterpret_cast<const uint4*>(a.X + row * a.ldx);
@@ -126,40 +130,32 @@ rmsnorm_kernel(const NormArgs a) {
     for (int j = 0; j < V; ++j)
       if (g.lane + j * a.tpr < vecs) out[g.lane + j * a.tpr] = s[j];
   }
-  float ss = 0.f;
+  // the largest |y| of a row is r times the largest |S gamma|: found beside the sum of squares, it costs no pass and no barrier of its own
+  float ss = 0.f, top = 0.f;
 #pragma unroll
-  for (int j = 0; j < V; ++j)
+  for (int j = 0; j < V; ++j) {
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (kRows && g.lane + j * a.tpr < vecs) w = __ldg(gamma + g.lane + j * a.tpr);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float l = lo32(word(s[j], i)), h = hi32(word(s[j], i));
       ss = fmaf(l, l, ss);
       ss = fmaf(h, h, ss);
+      if (kRows) top = max_nan(top, max_nan(fabsf(l * lo32(word(w, i))), fabsf(h * hi32(word(w, i)))));
     }
-  ss = g.reduce<false>(ss);
+  }
+  g.reduce<kRows>(ss, top);
   const float rstd = __frsqrt_rn(ss / (float)a.D + a.eps);
-  if (a.rstd && g.lane == 0) a.rstd[row] = rstd;
+  if (a.rstd && here && g.lane == 0) a.rstd[row] = rstd;
   auto normed = [&](const uint4& v, const uint4& w, int i, float& l, float& h) {
     l = lo32(word(v, i)) * rstd * lo32(word(w, i));
     h = hi32(word(v, i)) * rstd * hi32(word(w, i));
   };
   float inv = a.scale;
-  if (a.codes && a.scales) {           // a row's own scale: its largest magnitude becomes 448
-    float top = 0.f;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = g.lane + j * a.tpr;
-      if (c >= vecs) continue;
-      const uint4 w = __ldg(gamma + c);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float l, h;
-        normed(s[j], w, i, l, h);
-        top = max_nan(top, max_nan(fabsf(l), fabsf(h)));
-      }
-    }
-    top = max_nan(g.reduce<true>(top), kLeastAmax);
+  if (kRows) {                         // a row's own scale: its largest magnitude becomes 448
+    top = max_nan(top * rstd, kLeastAmax);
     inv = __fdiv_rn(448.f, top);
-    if (g.lane == 0) a.scales[row] = __fdiv_rn(top, 448.f);
+    if (here && g.lane == 0) a.scales[row] = __fdiv_rn(top, 448.f);
   }
   uint4* y = reinterpret_cast<uint4*>(a.Y + row * a.D);
   uint2* q = reinterpret_cast<uint2*>(a.codes + row * a.D);
@@ -181,6 +177,8 @@ rmsnorm_kernel(const NormArgs a) {
   }
 }
 
+constexpr int kBwdSmem = 196608;       // of the ring, at most
+
 struct NormBwdArgs {
   const uint16_t *dY, *S, *gamma, *dS;
   const float* rstd;
@@ -190,21 +188,52 @@ struct NormBwdArgs {
   int D, tpr;
 };
 
-template <int V>
-__global__ void __launch_bounds__(V >= 4 ? 1024 : 512)
+__device__ __forceinline__ void copy_async(uint32_t saddr, const uint4* p) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(saddr), "l"(p) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A group takes every so many rows; the vectors of the next kStages - 1 rows are on their way to shared memory while one is worked on. Each
+// thread fetches what it will read itself, so nothing but a row's mean crosses threads. With the rows loaded into registers when their turn
+// came (two groups of 256 threads to an SM) 16384 x 4096 took 112 us, DRAM waiting for the reductions.
+template <int V, int kStages>
+__global__ void __launch_bounds__(kStages == 1 ? 1024 : 512)
 rmsnorm_bwd_kernel(const NormBwdArgs a) {
-  __shared__ float slots[16][64];
-  extern __shared__ float sums[];      // [groups - 1][D] at the end
+  __shared__ float slots[8][128];       // (of groups of more than a warp)
+  extern __shared__ uint4 ring[];      // [stage][dY, S, dS][V][threads]; at the end the groups' sums
   const int groups = (int)blockDim.x / a.tpr;
   Group g;
   g.index = (int)threadIdx.x / a.tpr;
   g.lane = (int)threadIdx.x - g.index * a.tpr;
   g.size = a.tpr;
-  g.slots = slots[g.index];
+  g.slots = slots[a.tpr > 32 ? g.index : 0];
   g.turn = 0;
   const int vecs = a.D >> 3;
+  const int64_t step = (int64_t)gridDim.x * groups, first = (int64_t)blockIdx.x * groups;
+  const bool adds = a.dS && a.dX;
   pdl_wait();
   pdl_trigger();
+  const uint32_t at = ptx::smem_u32(ring + threadIdx.x), piece = blockDim.x * 16u;
+  auto fetch = [&](int64_t base, int stage) {
+    const int64_t row = base + g.index;
+    if (row < a.T) {
+      const uint4 *dy = reinterpret_cast<const uint4*>(a.dY + row * a.D), *s = reinterpret_cast<const uint4*>(a.S + row * a.D),
+                  *ds = reinterpret_cast<const uint4*>(a.dS + row * a.D);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int c = g.lane + j * a.tpr;
+        if (c >= vecs) continue;
+        const uint32_t to = at + (uint32_t)(stage * 3 * V + j) * piece;
+        copy_async(to, dy + c);
+        copy_async(to + V * piece, s + c);
+        if (adds) copy_async(to + 2 * V * piece, ds + c);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) fetch(first + i * step, i);
   float dg[V][8];
   uint4 w[V];
 #pragma unroll
@@ -215,55 +244,56 @@ rmsnorm_bwd_kernel(const NormBwdArgs a) {
     for (int i = 0; i < 8; ++i) dg[j][i] = 0.f;
   }
   const float inv_d = 1.f / (float)a.D;
-  for (int64_t row = (int64_t)blockIdx.x * groups + g.index; row < a.T; row += (int64_t)gridDim.x * groups) {
-    const uint4 *dy = reinterpret_cast<const uint4*>(a.dY + row * a.D), *s = reinterpret_cast<const uint4*>(a.S + row * a.D),
-                *ds = reinterpret_cast<const uint4*>(a.dS + row * a.D);
-    uint4 d[V], x[V], e[V];
-    const float r = __ldg(a.rstd + row);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = g.lane + j * a.tpr;
-      const bool in = c < vecs;
-      d[j] = in ? load_once(dy + c) : make_uint4(0u, 0u, 0u, 0u);
-      x[j] = in ? load_once(s + c) : make_uint4(0u, 0u, 0u, 0u);
-    }
-    if (a.dS && a.dX) {
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int c = g.lane + j * a.tpr;
-        e[j] = c < vecs ? load_once(ds + c) : make_uint4(0u, 0u, 0u, 0u);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) e[j] = make_uint4(0u, 0u, 0u, 0u);
-    }
+  int stage = 0;
+  float r = first + g.index < a.T ? __ldg(a.rstd + first + g.index) : 0.f;
+  for (int64_t base = first; base < a.T; base += step) {
+    const int64_t row = base + g.index;
+    const bool here = row < a.T;
+    fetch(base + (kStages - 1) * step, stage == 0 ? kStages - 1 : stage - 1);
+    const float r_next = row + step < a.T ? __ldg(a.rstd + row + step) : 0.f;
+    copy_wait<kStages - 1>();
+    const uint4* mine = ring + threadIdx.x + (size_t)stage * 3 * V * blockDim.x;
     float c1 = 0.f;
 #pragma unroll
-    for (int j = 0; j < V; ++j)
+    for (int j = 0; j < V; ++j) {
+      if (!here || g.lane + j * a.tpr >= vecs) continue;
+      const uint4 d = mine[j * blockDim.x], x = mine[(V + j) * blockDim.x];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t dw = word(d[j], i), xw = word(x[j], i), ww = word(w[j], i);
+        const uint32_t dw = word(d, i), xw = word(x, i), ww = word(w[j], i);
         const float tl = lo32(dw) * (lo32(xw) * r), th = hi32(dw) * (hi32(xw) * r);
         dg[j][2 * i] += tl;
         dg[j][2 * i + 1] += th;
         c1 = fmaf(tl, lo32(ww), c1);
         c1 = fmaf(th, hi32(ww), c1);
       }
-    if (!a.dX) continue;
-    const float m = g.reduce<false>(c1) * inv_d;
-    uint4* out = reinterpret_cast<uint4*>(a.dX + row * a.D);
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int c = g.lane + j * a.tpr;
-      uint32_t o[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t dw = word(d[j], i), xw = word(x[j], i), ww = word(w[j], i), ew = word(e[j], i);
-        o[i] = pack2(fmaf(r, fmaf(-lo32(xw) * r, m, lo32(dw) * lo32(ww)), lo32(ew)), fmaf(r, fmaf(-hi32(xw) * r, m, hi32(dw) * hi32(ww)), hi32(ew)));
-      }
-      if (c < vecs) out[c] = make_uint4(o[0], o[1], o[2], o[3]);
     }
+    if (a.dX) {
+      float none = 0.f;
+      g.reduce<false>(c1, none);
+      const float m = c1 * inv_d;
+      uint4* out = reinterpret_cast<uint4*>(a.dX + row * a.D);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int c = g.lane + j * a.tpr;
+        if (!here || c >= vecs) continue;
+        const uint4 d = mine[j * blockDim.x], x = mine[(V + j) * blockDim.x],
+                    e = adds ? mine[(2 * V + j) * blockDim.x] : make_uint4(0u, 0u, 0u, 0u);
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t dw = word(d, i), xw = word(x, i), ww = word(w[j], i), ew = word(e, i);
+          o[i] = pack2(fmaf(r, fmaf(-lo32(xw) * r, m, lo32(dw) * lo32(ww)), lo32(ew)), fmaf(r, fmaf(-hi32(xw) * r, m, hi32(dw) * hi32(ww)), hi32(ew)));
+        }
+        out[c] = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+    }
+    r = r_next;
+    if (++stage == kStages) stage = 0;
   }
+  copy_wait<0>();                      // (what was fetched for rows that are not there: nothing, but the groups are counted)
+  float* sums = reinterpret_cast<float*>(ring);            // [groups - 1][D]
+  __syncthreads();                     // every thread has read what it fetched
   if (!a.dgamma) return;
   // the groups' sums, in their order
   if (g.index > 0)
@@ -299,15 +329,22 @@ rmsnorm_bwd_kernel(const NormBwdArgs a) {
   }
 }
 
-// Vectors of a row to a thread, and threads to a row. Few rows: as many threads as there are vectors, for latency. Many: four vectors,
-// whose loads are under way at once, and as many rows to an SM.
-// (threads: that a row may have with fewer than four vectors each; with four, 1024)
+// Vectors of a row to a thread, and threads to a row. Few rows: as many threads as there are vectors, for latency. Many: several vectors,
+// whose loads are under way at once, and as many rows to an SM. Rows of less than a warp's 32 vectors share it.
 struct RowPlan { int v, tpr; };
-RowPlan row_plan(int64_t T, int64_t D, int most, int threads) {
+int whole_warps(int threads) { return (threads + 31) / 32 * 32; }
+RowPlan fwd_plan(int64_t T, int64_t D) {
   const int vecs = (int)(D / 8);
-  int v = T <= sm_count_now() ? 1 : vecs <= 32 ? 1 : vecs <= 64 ? 2 : most;
-  while (v < 4 && (vecs + v - 1) / v > threads) v *= 2;
-  return RowPlan{v, ((vecs + v - 1) / v + 31) / 32 * 32};
+  if (vecs <= 32) return RowPlan{1, vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32};
+  const int v = T <= sm_count_now() && vecs <= 1024 ? 1 : T <= sm_count_now() && vecs <= 2048 ? 2 : vecs <= 64 ? 2 : 4;
+  return RowPlan{v, whole_warps((vecs + v - 1) / v)};
+}
+// Backward: 512 threads hold a row of 4096 vectors' eighth in one to four vectors each; a row of more than 16384 takes 1024.
+RowPlan bwd_plan(int64_t T, int64_t D) {
+  const int vecs = (int)(D / 8);
+  if (vecs <= 32) return RowPlan{1, vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32};
+  const int v = T <= kBwdCtas && vecs <= 512 ? 1 : vecs <= 1024 ? 2 : 4;
+  return RowPlan{v, whole_warps((vecs + v - 1) / v)};
 }
 
 int bwd_ctas(int64_t T) { return (int)(T < kBwdCtas ? T : kBwdCtas); }
@@ -339,13 +376,14 @@ int sf_rmsnorm_fwd(const void* X, int64_t ldx, const void* residual, const void*
       ((in_x || in_r) && !apart({{Y, td}, {codes, td / 2}, {scales, t4}, {rstd, t4}}, {x, r})))
     return SF_ERR_UNSUPPORTED;
   SF_TRY(check_arch());
-  const RowPlan p = row_plan(T, D, 4, 1024);
+  const RowPlan p = fwd_plan(T, D);
   const int groups = p.tpr >= 128 ? 1 : 128 / p.tpr;
   NormArgs a{};
   a.X = (const uint16_t*)X; a.R = (const uint16_t*)residual; a.gamma = (const uint16_t*)gamma; a.ldx = ldx; a.T = T;
   a.sum = (uint16_t*)sum; a.Y = (uint16_t*)Y; a.codes = (uint8_t*)codes; a.scales = (float*)scales; a.rstd = (float*)rstd;
   a.scale = scale; a.eps = eps; a.D = (int)D; a.tpr = p.tpr;
-  auto kern = p.v == 1 ? rmsnorm_kernel<1> : p.v == 2 ? rmsnorm_kernel<2> : rmsnorm_kernel<4>;
+  auto kern = scales ? (p.v == 1 ? rmsnorm_kernel<1, true> : p.v == 2 ? rmsnorm_kernel<2, true> : rmsnorm_kernel<4, true>)
+                     : (p.v == 1 ? rmsnorm_kernel<1, false> : p.v == 2 ? rmsnorm_kernel<2, false> : rmsnorm_kernel<4, false>);
   return launch_pdl(kern, dim3((unsigned)((T + groups - 1) / groups)), (unsigned)(groups * p.tpr), 0, (cudaStream_t)stream, a);
 }
 
@@ -378,20 +416,27 @@ int sf_rmsnorm_bwd(const void* dY, const void* sum, const void* gamma, const voi
       !apart({{dgamma, d2}, parts}, {{dY, td}, {dS, td}}))
     return SF_ERR_UNSUPPORTED;
   SF_TRY(check_arch());
-  const RowPlan p = row_plan(T, D, 2, 512);
+  const RowPlan p = bwd_plan(T, D);
   const int ctas = bwd_ctas(T);
-  int groups = 512 / p.tpr;
   const int64_t rows = (T + ctas - 1) / ctas;              // of a CTA
+  int groups = p.tpr > 512 ? 1 : 512 / p.tpr;
   if (groups > rows) groups = (int)rows;
-  if (groups > 16) groups = 16;
-  while (groups > 1 && (int64_t)(groups - 1) * D * 4 > 40960) --groups;
-  if (groups < 1) groups = 1;
+  while (groups * p.tpr % 32) ++groups;                    // whole warps
   NormBwdArgs a{};
   a.dY = (const uint16_t*)dY; a.S = (const uint16_t*)sum; a.gamma = (const uint16_t*)gamma; a.dS = (const uint16_t*)dS; a.rstd = (const float*)rstd;
   a.T = T; a.dX = (uint16_t*)dX; a.dgamma = (uint16_t*)dgamma; a.parts = (float*)workspace; a.D = (int)D; a.tpr = p.tpr;
-  const size_t smem = (size_t)(groups - 1) * (size_t)D * 4;
-  auto kern = p.v == 1 ? rmsnorm_bwd_kernel<1> : p.v == 2 ? rmsnorm_bwd_kernel<2> : rmsnorm_bwd_kernel<4>;
-  SF_TRY(launch_pdl(kern, dim3((unsigned)ctas), (unsigned)(groups * p.tpr), smem, s, a));
+  const int threads = groups * p.tpr, stages = p.v < 4 ? 4 : threads > 512 ? 1 : 2;
+  const size_t smem = (size_t)stages * 3 * p.v * threads * 16;
+  auto kern = p.v == 1 ? rmsnorm_bwd_kernel<1, 4> : p.v == 2 ? rmsnorm_bwd_kernel<2, 4> : stages == 2 ? rmsnorm_bwd_kernel<4, 2> : rmsnorm_bwd_kernel<4, 1>;
+  static std::atomic<bool> attr_done[64]{};
+  int dev = 0;
+  SF_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64 || !attr_done[dev]) {
+    for (auto k : {rmsnorm_bwd_kernel<1, 4>, rmsnorm_bwd_kernel<2, 4>, rmsnorm_bwd_kernel<4, 2>, rmsnorm_bwd_kernel<4, 1>})
+      SF_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kBwdSmem));
+    if (dev >= 0 && dev < 64) attr_done[dev] = true;
+  }
+  SF_TRY(launch_pdl(kern, dim3((unsigned)ctas), (unsigned)threads, smem, s, a));
   if (!dgamma || ctas == 1) return SF_OK;
   return launch_sum_parts((const float*)workspace, ctas, D, dgamma, s);
 }
