@@ -473,7 +473,7 @@ SF_API int sf_router_balance_bwd(const void* logits, const void* expert, const v
  *
  * for G with at most as many rows as columns; of a higher one the transpose is taken, and that of the result. G is SF_BF16 or SF_F32 [rows, cols],
  * leading dimension ldg >= cols; O bf16 [rows, cols], ldo >= cols. Any rows, cols >= 0; the larger at most 2^24, the smaller at most 2^16. G and O are
- * aligned to their element; rows of O whose starts are multiples of 16 bytes save a copy. 1 <= steps <= 64. (a, b, c): the quintic a s + b s^3 + c s^5
+ * aligned to their element; rows of O that start on multiples of 16 bytes are written fastest. 1 <= steps <= 64. (a, b, c): the quintic a s + b s^3 + c s^5
  * has to keep [0, 1.25] within [-1.25, 1.25] and |b l + c l^2| <= 7.5 up to l = 1.5625, with |a|, |b|, |c| <= 8 (SF_ERR_UNSUPPORTED otherwise); (3.4445,
  * -4.7750, 2.0315) is usual. A NaN or an infinity in G makes all of O NaN.
  * The products' operands are fp16; X is held as a sum of two of them and the diagonals of A and A^2 in float32, so that the error of the result

@@ -753,10 +753,6 @@ def sf_gemm_fp4_gated(A, a_scales, Bg, bg_scales, Bu, bu_scales, fmt: int, act: 
 _F32, _I32 = torch.float32, torch.int32
 
 
-def _optional(where: str, name: str, t, dtype, shape, dev: int):
-    return None if t is None else _tensor(where, name, t, dtype, shape, dev)
-
-
 def _sized(call: str, *args) -> int:
     n = _sz()
     _check(getattr(lib(), call)(*args, C.byref(n)), call)
@@ -768,15 +764,15 @@ def sf_rmsnorm_fwd(X, gamma, eps: float, residual=None, sum=None, Y=None, codes=
     scale to every row in ``scales``, or the given ``scale``), 1 / rms to ``rstd``. What is None is not written; without Y and codes a Y is made.
     X may be a strided row view. Returns Y (or the codes)."""
     w, dev = "sf_rmsnorm_fwd", X.get_device()
-    ld = _row_stride(w, "X", X)
-    T, D = X.shape
+    T, D = shape = _matrix_shape(w, X)
+    ld = D if X.dtype is _BF16 and X.is_contiguous() else _row_stride(w, "X", X)
     if Y is None and codes is None:
         with _allocating(stream):
             Y = torch.empty((T, D), dtype=_BF16, device=X.device)
-    _check(lib().sf_rmsnorm_fwd(X.data_ptr(), ld, _optional(w, "residual", residual, _BF16, (T, D), dev), _tensor(w, "gamma", gamma, _BF16, (D,), dev),
-                                T, D, eps, _optional(w, "sum", sum, _BF16, (T, D), dev), _optional(w, "Y", Y, _BF16, (T, D), dev),
-                                _optional(w, "codes", codes, _U8, (T, D), dev), _optional(w, "scales", scales, _F32, (T,), dev), scale,
-                                _optional(w, "rstd", rstd, _F32, (T,), dev), _launch_stream(w, dev, stream)), w)
+    _check(lib().sf_rmsnorm_fwd(X.data_ptr(), ld, None if residual is None else _tensor(w, "residual", residual, _BF16, shape, dev), _tensor(w, "gamma", gamma, _BF16, (D,), dev),
+                                T, D, eps, None if sum is None else _tensor(w, "sum", sum, _BF16, shape, dev), None if Y is None else _tensor(w, "Y", Y, _BF16, shape, dev),
+                                None if codes is None else _tensor(w, "codes", codes, _U8, shape, dev), None if scales is None else _tensor(w, "scales", scales, _F32, (T,), dev), scale,
+                                None if rstd is None else _tensor(w, "rstd", rstd, _F32, (T,), dev), _launch_stream(w, dev, stream)), w)
     return codes if Y is None else Y
 
 
@@ -788,7 +784,7 @@ def sf_rmsnorm_bwd(dY, S, gamma, rstd, dS=None, dX=None, dgamma=None, workspace=
     """Gradients of sf_rmsnorm_fwd from dY, its sum S and its rstd, dS added: into ``dX`` and ``dgamma``, of which a None is left out (both
     None: both are made). Returns (dX, dgamma)."""
     w, dev = "sf_rmsnorm_bwd", dY.get_device()
-    T, D = _matrix_shape(w, dY)
+    T, D = shape = _matrix_shape(w, dY)
     both = dX is None and dgamma is None
     if both or (dgamma is not None and workspace is None):
         with _allocating(stream):
@@ -796,9 +792,9 @@ def sf_rmsnorm_bwd(dY, S, gamma, rstd, dS=None, dX=None, dgamma=None, workspace=
                 dX, dgamma = torch.empty((T, D), dtype=_BF16, device=dY.device), torch.empty((D,), dtype=_BF16, device=dY.device)
             if workspace is None:
                 workspace = torch.empty((sf_rmsnorm_bwd_workspace_size(T, D),), dtype=_U8, device=dY.device)
-    _check(lib().sf_rmsnorm_bwd(_tensor(w, "dY", dY, _BF16, (T, D), dev), _tensor(w, "S", S, _BF16, (T, D), dev), _tensor(w, "gamma", gamma, _BF16, (D,), dev),
-                                _tensor(w, "rstd", rstd, _F32, (T,), dev), _optional(w, "dS", dS, _BF16, (T, D), dev), T, D,
-                                _optional(w, "dX", dX, _BF16, (T, D), dev), _optional(w, "dgamma", dgamma, _BF16, (D,), dev),
+    _check(lib().sf_rmsnorm_bwd(_tensor(w, "dY", dY, _BF16, shape, dev), _tensor(w, "S", S, _BF16, shape, dev), _tensor(w, "gamma", gamma, _BF16, (D,), dev),
+                                _tensor(w, "rstd", rstd, _F32, (T,), dev), None if dS is None else _tensor(w, "dS", dS, _BF16, shape, dev), T, D,
+                                None if dX is None else _tensor(w, "dX", dX, _BF16, shape, dev), None if dgamma is None else _tensor(w, "dgamma", dgamma, _BF16, (D,), dev),
                                 *_buffer(w, "workspace", workspace, dev), _launch_stream(w, dev, stream)), w)
     return dX, dgamma
 
@@ -863,10 +859,10 @@ def sf_router_balance_bwd(logits, expert, counts, balance_coef: float, z_coef: f
             if workspace is None:
                 workspace = _workspace(sf_router_balance_workspace_size(T, D, E), X.device)
     _check(lib().sf_router_balance_bwd(_tensor(w, "logits", logits, _F32, (T, E), dev), _tensor(w, "expert", expert, _I32, (T,), dev),
-                                       _tensor(w, "counts", counts, _I32, (E,), dev), _optional(w, "dloss", dloss, _F32, (1,), dev),
+                                       _tensor(w, "counts", counts, _I32, (E,), dev), None if dloss is None else _tensor(w, "dloss", dloss, _F32, (1,), dev),
                                        _tensor(w, "X", X, _BF16, (T, D), dev), _tensor(w, "means", means, _BF16, (E, D), dev), T, D, E, balance_coef, z_coef,
-                                       _optional(w, "dX_in", dX_in, _BF16, (T, D), dev), _optional(w, "dX", dX, _BF16, (T, D), dev),
-                                       _optional(w, "dmeans", dmeans, _BF16, (E, D), dev), *_buffer(w, "workspace", workspace, dev),
+                                       None if dX_in is None else _tensor(w, "dX_in", dX_in, _BF16, (T, D), dev), None if dX is None else _tensor(w, "dX", dX, _BF16, (T, D), dev),
+                                       None if dmeans is None else _tensor(w, "dmeans", dmeans, _BF16, (E, D), dev), *_buffer(w, "workspace", workspace, dev),
                                        _launch_stream(w, dev, stream)), w)
     return dX, dmeans
 

@@ -60,9 +60,7 @@ int ns_shape(int64_t rows, int64_t cols, NsShape* z) {
     z->diag[i] = take(4 * (size_t)z->mp);
   }
   z->second = z->grouped ? take(2 * (size_t)z->m * (size_t)z->ldm) : z->sym[0];
-  // (either of the last product's unused targets may hold the result on its way to rows that TMA cannot write)
-  const size_t x = 2 * (size_t)z->m * (size_t)z->ldn, y = 2 * (size_t)z->n * (size_t)z->ldm;
-  for (int i = 0; i < 4; ++i) z->x[i] = take(x > y ? x : y);
+  for (int i = 0; i < 4; ++i) z->x[i] = take(2 * (size_t)z->m * (size_t)z->ldn);
   z->total = o;
   return SF_OK;
 }
@@ -227,17 +225,6 @@ ns_convert_transposed_kernel(const void* __restrict__ G, int64_t rows, int64_t c
   }
 }
 
-// Rows that TMA cannot write (their stride is no multiple of 16 bytes): from a copy that it can.
-__global__ void __launch_bounds__(256)
-ns_copy_kernel(const uint16_t* __restrict__ from, int64_t ldf, int64_t rows, int64_t cols, int64_t ld, uint16_t* __restrict__ out) {
-  pdl_wait();
-  pdl_trigger();
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / cols, c = i - r * cols;
-    out[r * ld + c] = __ldcg(from + r * ldf + c);
-  }
-}
-
 // Whether the quintic keeps the singular values in the range that the fp16 operands are scaled for: from [0, 1.25] into itself, and its
 // factors within theirs. p: the largest |a + b l + c l^2| of an eigenvalue l of A, which is at most 1.25^2.
 bool ns_bounded(double a, double b, double c, double* p) {
@@ -385,6 +372,8 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
     q = p;
     q.ns.first = groups == 0 ? first : nullptr;
     q.ns.last = done == steps;
+    q.ns.out = direct ? nullptr : (uint16_t*)O;
+    q.ns.ldo = ldo;
     q.ns.two_terms = groups > 0 || f32;
     q.ns.diag_in = (const float*)(w + z.diag[Q.at]);
     q.ns.down = std::ldexp(1.f, -Q.e);
@@ -397,14 +386,10 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
       SF_TRY(make_tmap_store(&m[3], xl, z.m, z.n, z.ldn));
       SF_TRY(make_tmap_store(&m[5], yl, z.m, z.n, z.ldn));
       if (!q.ns.last) return make_tmap_store(&m[4], yh, z.m, z.n, z.ldn);
-      if (direct) return make_tmap_store(&m[4], O, rows, cols, ldo);
-      return make_tmap_store(&m[4], yh, rows, cols, z.high ? z.ldm : z.ldn);
+      return direct ? make_tmap_store(&m[4], O, rows, cols, ldo) : make_tmap_store(&m[4], yh, z.m, z.n, z.ldn);
     })));
   }
-  if (direct) return SF_OK;
-  const uint16_t* from = (const uint16_t*)(w + z.x[2 * (groups & 1)]);
-  const int64_t ctas = ceil_div(rows * cols, 256), most = 8 * sm_count_now();
-  return launch_pdl(ns_copy_kernel, dim3((unsigned)(ctas < most ? ctas : most)), 256, 0, s, from, z.high ? z.ldm : z.ldn, rows, cols, ldo, (uint16_t*)O);
+  return SF_OK;
 }
 
 }  // extern "C"

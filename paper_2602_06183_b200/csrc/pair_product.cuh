@@ -63,7 +63,7 @@ struct PairCfg {
   static constexpr int kBBlocks = kBN / 128;                                     // row blocks of B's scales
   static constexpr int kScaleBytes = kTiles * 512 * (1 + kBBlocks);
   static constexpr int kStageBytes = kABytes + kBBytes + kScaleBytes;
-  static constexpr int kEpiWarpBytes = kWide ? 8192 : 4096;
+  static constexpr int kEpiWarpBytes = kKind == PK_SYMM ? 12288 : kWide ? 8192 : 4096;
   static constexpr int kRoom = (kPairSmemMax - 2048 - 8 * kEpiWarpBytes) / kStageBytes;
   static constexpr int kStages = kRoom < 8 ? kRoom : 8;
   static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kEpiWarpBytes + 1024;
@@ -99,6 +99,8 @@ struct NsArgs {
   int two_terms;                     // PK_APPLY: X has
   int last, transposed;              // PK_APPLY: the result is written as bf16 times `scale`, and as its transpose
   float scale;
+  uint16_t* out;                     // ... where its rows do not start on multiples of 16 bytes: here, leading dimension ldo
+  int64_t ldo;
 };
 struct PairArgs {
   int jobs;
@@ -273,12 +275,11 @@ __device__ __forceinline__ NsRow ns_begin(const PairArgs& args, int row) {
   if (kKind == PK_APPLY) r.d1 = __ldcg(args.ns.diag_in + row);
   return r;
 }
-// A chunk of 32 x 32 sums of a symmetric result, this lane's row of it: as it lies and mirrored, one term or two. bufs: the warp's buffer of
-// four times 2 KB. PK_GRAM: half, that half of it which a result of one term takes. PK_SYMM: the buffer holds the factors' chunks (ns_fetch), and
-// the result takes their place; dcol: the second factor's diagonal at this lane's column.
+// A chunk of 32 x 32 sums of a symmetric result, this lane's row of it: as it lies and mirrored, one term or two, to b, a half of the warp's
+// buffer, and from there to the matrix. PK_SYMM: b holds the factors' chunks (ns_fetch), and the result takes their place; dcol: the second
+// factor's diagonal at this lane's column.
 template <int kKind>
-__device__ __forceinline__ bool ns_symmetric(const PairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* bufs, uint32_t half,
-                                             float dcol, uint64_t* loaded, uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
+__device__ __forceinline__ bool ns_symmetric(const PairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* b, float dcol, uint64_t* loaded, uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
   const bool on_diag = row == col;
   const float up = args.ns.up;
   float d = 0.f;
@@ -295,9 +296,9 @@ __device__ __forceinline__ bool ns_symmetric(const PairArgs& args, const CUtenso
     const bool same = args.ns.same, two1 = args.ns.m1.two;
     if (!mbar_wait_warp(loaded, phase, abort_flag)) return false;
     uint32_t h1[16], l1[16], h2[16];
-    row_get(bufs, lane, h1);
-    if (two1) row_get(bufs + 2048, lane, l1);
-    if (!same) row_get(bufs + 4096, lane, h2);
+    row_get(b, lane, h1);
+    if (two1) row_get(b + 2048, lane, l1);
+    if (!same) row_get(b + 4096, lane, h2);
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
       float2 x = from_f16x2(h1[q]);
@@ -308,52 +309,44 @@ __device__ __forceinline__ bool ns_symmetric(const PairArgs& args, const CUtenso
         z = from_f16x2(h2[q]);
         z.x *= down2; z.y *= down2;
       }
-      const float a[2] = {x.x, x.y}, b[2] = {z.x, z.y};
+      const float a[2] = {x.x, x.y}, c[2] = {z.x, z.y};
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int i = 2 * q + u;
         const float p = __uint_as_float(v[i]) * down;
-        float o = fmaf(c2, fmaf(r.d1, b[u], fmaf(a[u], __shfl_sync(0xFFFFFFFFu, dcol, i), p)), c1 * a[u]);
+        float o = fmaf(c2, fmaf(r.d1, c[u], fmaf(a[u], __shfl_sync(0xFFFFFFFFu, dcol, i), p)), c1 * a[u]);
         if (on_diag && i == lane) { d = fmaf(c2, fmaf(r.d1, r.d2, p), fmaf(c1, r.d1, args.ns.c0)); o = 0.f; }
         v[i] = __float_as_uint(o * up);
       }
     }
   }
   if (on_diag && row + lane < args.M[0]) args.ns.diag_out[row + lane] = d;
-  const bool two = args.ns.two_out;
-  uint8_t* b = bufs;
-  if constexpr (kKind == PK_GRAM) {
-    if (!two) b += half * 4096u;
-    if (lane == 0) {
-      if (two) bulk_wait_read<0>();
-      else bulk_wait_read<1>();                            // the store before the last, from this half
-    }
-  }
+  if (kKind == PK_GRAM && lane == 0) bulk_wait_read<1>();  // the store before the last, from this half
   __syncwarp();                                            // (PK_SYMM: every row has been read)
   uint32_t w[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) w[i] = f16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-  row_bf16(b, lane, w);
-  if (!on_diag) column_put(b + 2048, lane, w);
-  if (two) {
+  auto store = [&](const CUtensorMap* m) {
+    row_bf16(b, lane, w);
+    if (!on_diag) column_put(b + 2048, lane, w);
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_2d(m, b, col, row);
+      if (!on_diag) tma_store_2d(m, b + 2048, row, col);
+      bulk_commit();
+    }
+  };
+  store(&maps[2]);
+  if (args.ns.two_out) {
+    if (lane == 0) bulk_wait_read<0>();
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const float2 h = from_f16x2(w[i]);
       w[i] = f16x2(__uint_as_float(v[2 * i]) - h.x, __uint_as_float(v[2 * i + 1]) - h.y);
     }
-    row_bf16(b + 4096, lane, w);
-    if (!on_diag) column_put(b + 6144, lane, w);
-  }
-  fence_proxy_async_smem();
-  __syncwarp();
-  if (lane == 0) {
-    tma_store_2d(&maps[2], b, col, row);
-    if (!on_diag) tma_store_2d(&maps[2], b + 2048, row, col);
-    if (two) {
-      tma_store_2d(&maps[3], b + 4096, col, row);
-      if (!on_diag) tma_store_2d(&maps[3], b + 6144, row, col);
-    }
-    bulk_commit();
+    store(&maps[3]);
   }
   return true;
 }
@@ -390,9 +383,18 @@ __device__ __forceinline__ bool ns_apply(const PairArgs& args, const CUtensorMap
   }
   fence_proxy_async_smem();
   __syncwarp();
-  if (lane == 0) {
-    const bool t = args.ns.last && args.ns.transposed;
-    tma_store_2d(&maps[4], b, t ? row : col, t ? col : row);
+  const bool t = args.ns.last && args.ns.transposed;
+  const int x0 = t ? row : col, y0 = t ? col : row;        // of the chunk in the result
+  if (args.ns.last && args.ns.out) {
+    // a row of the chunk at a time, a lane to an element
+    const int cols = t ? args.M[0] : args.N[0], rows = t ? args.N[0] : args.M[0];
+    if (x0 + lane < cols)
+      for (int i = 0; i < 32 && y0 + i < rows; ++i)
+        args.ns.out[(int64_t)(y0 + i) * args.ns.ldo + x0 + lane] =
+            *reinterpret_cast<const uint16_t*>(b + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2);
+    __syncwarp();
+  } else if (lane == 0) {
+    tma_store_2d(&maps[4], b, x0, y0);
     if (!args.ns.last) tma_store_2d(&maps[5], b + 2048, col, row);
     bulk_commit();
   }
@@ -599,24 +601,29 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       put_chunk_end(m, bufs + buf * kBufBytes, col, row, lane);
       buf ^= 1u;
     };
-    // PK_APPLY: a chunk of X, both terms, into one of the two halves of the warp's buffer; PK_SYMM: the factors' chunks into all of it
-    float ns_dcol = 0.f;
+    // PK_APPLY: a chunk of X, both terms, into one of the two halves of the warp's buffer; PK_SYMM: the factors' chunks
+    float ns_dcol[2] = {0.f, 0.f};
     auto ns_fetch = [&](int ch, int n0, int row, uint32_t h) {
       const int col = n0 + ch * 32;
-      if constexpr (kKind == PK_SYMM) ns_dcol = __ldcg(args.ns.m2.diag + col + lane);
+      if constexpr (kKind == PK_SYMM) {
+        const float d = __ldcg(args.ns.m2.diag + col + lane);
+        if (h) ns_dcol[1] = d;
+        else ns_dcol[0] = d;
+      }
       if constexpr (kKind == PK_APPLY || kKind == PK_SYMM) {
         if (lane == 0) {
           bulk_wait_read<0>();
+          uint8_t* b = bufs + h * kBufBytes;
+          uint64_t* bar = loaded + 8 * h;
           if constexpr (kKind == PK_APPLY) {
-            uint8_t* b = bufs + h * kBufBytes;
-            mbar_arrive_expect_tx(loaded + 8 * h, args.ns.two_terms ? 4096u : 2048u);
-            tma_load_2d(b, &maps.m[2], loaded + 8 * h, col, row);
-            if (args.ns.two_terms) tma_load_2d(b + 2048, &maps.m[3], loaded + 8 * h, col, row);
+            mbar_arrive_expect_tx(bar, args.ns.two_terms ? 4096u : 2048u);
+            tma_load_2d(b, &maps.m[2], bar, col, row);
+            if (args.ns.two_terms) tma_load_2d(b + 2048, &maps.m[3], bar, col, row);
           } else {
-            mbar_arrive_expect_tx(loaded, 2048u * (1u + (args.ns.m1.two ? 1u : 0u) + (args.ns.same ? 0u : 1u)));
-            tma_load_2d(bufs, &maps.m[4], loaded, col, row);
-            if (args.ns.m1.two) tma_load_2d(bufs + 2048, &maps.m[5], loaded, col, row);
-            if (!args.ns.same) tma_load_2d(bufs + 4096, &maps.m[6], loaded, col, row);
+            mbar_arrive_expect_tx(bar, 2048u * (1u + (args.ns.m1.two ? 1u : 0u) + (args.ns.same ? 0u : 1u)));
+            tma_load_2d(b, &maps.m[4], bar, col, row);
+            if (args.ns.m1.two) tma_load_2d(b + 2048, &maps.m[5], bar, col, row);
+            if (!args.ns.same) tma_load_2d(b + 4096, &maps.m[6], bar, col, row);
           }
         }
         __syncwarp();
@@ -696,8 +703,9 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
         if constexpr (kGated) {
           gated_chunk(v, u, col);
         } else if constexpr (Cfg::kSym) {
-          const bool ok = ns_symmetric<kKind>(args, maps.m, ns_row, v, bufs, buf, ns_dcol, loaded, load_phase & 1u, abort_flag, col, row, lane);
-          load_phase ^= 1u;
+          const bool ok = ns_symmetric<kKind>(args, maps.m, ns_row, v, bufs + buf * kBufBytes, buf ? ns_dcol[1] : ns_dcol[0], loaded + 8 * buf, load_phase >> buf & 1u, abort_flag,
+                                              col, row, lane);
+          load_phase ^= 1u << buf;
           buf ^= 1u;
           return ok;
         } else if constexpr (kKind == PK_APPLY) {
@@ -788,14 +796,12 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
           uint32_t v[32], u[32];
           tmem_ld_32x32b_x32(taddr + ch * 32, v);
           if constexpr (kGated) tmem_ld_32x32b_x32(taddr + half + ch * 32, u);
-          if constexpr (kKind == PK_APPLY)
+          if constexpr (kKind == PK_APPLY || kKind == PK_SYMM)
             if (ch + 2 < chunks) ns_fetch(ch + 2, t.n0, row, buf ^ 1u);       // beside this chunk's work
           tmem_ld_wait_on(v);
           if constexpr (kGated) tmem_ld_wait_on(u);
           if (!(ok = chunk(v, u, ch))) break;
           if (kKind == PK_BWD && ch + 2 < chunks) fetch(ch + 2);
-          if constexpr (kKind == PK_SYMM)
-            if (ch + 2 < chunks) ns_fetch(ch + 2, t.n0, row, 0);
         }
         if (!ok) break;
         release();

@@ -101,15 +101,28 @@ balance_loss_kernel(const float* __restrict__ logits, const int* __restrict__ ex
     last = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;      // (and back to 0 with the last one)
   }
   __syncthreads();
-  if (!last || warp != 0) return;
+  if (!last) return;                   // (the whole CTA)
   __threadfence();
-  // one expert to a lane, the parts in their order; z in lane 16
+  // one expert to a lane, z in lane 16; every eighth part to a warp, then the warps' sums in their order
+  __shared__ double sums[kLossThreads / 32][17];
+  __shared__ int nums[kLossThreads / 32][16];
   double p = 0;
-  long long n = 0;
-  if (lane < 17)
-    for (int i = 0; i < (int)gridDim.x; ++i) {
+  int n = 0;
+  if (lane < 17) {
+#pragma unroll 4
+    for (int i = warp; i < (int)gridDim.x; i += kLossThreads / 32) {
       p += lane < 16 ? (double)__ldcg(&parts[i].p[lane]) : __ldcg(&parts[i].z);
       if (lane < 16) n += __ldcg(&parts[i].n[lane]);
+    }
+    sums[warp][lane] = p;
+    if (lane < 16) nums[warp][lane] = n;
+  }
+  __syncthreads();
+  if (warp != 0) return;
+  if (lane < 17)
+    for (int w = 1; w < kLossThreads / 32; ++w) {
+      p += sums[w][lane];
+      if (lane < 16) n += nums[w][lane];
     }
   long long all = n;
 #pragma unroll
@@ -120,7 +133,7 @@ balance_loss_kernel(const float* __restrict__ logits, const int* __restrict__ ex
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) b += __shfl_xor_sync(0xFFFFFFFFu, b, o, 16);
   const double z = __shfl_sync(0xFFFFFFFFu, p, 16) * inv;
-  if (lane < E) counts[lane] = (int)n;
+  if (lane < E) counts[lane] = n;
   if (lane == 0) {
     loss[0] = (float)((double)cb * b + (double)cz * z);
     loss[1] = (float)b;
@@ -164,8 +177,9 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t saddr, uint32_t (&v)[
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(saddr) : "memory");
 }
+// (not volatile: the compiler may move it among the others)
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 // Where the half `h` (8 experts) of a token's dl lies: neighbouring rows of 32 bytes, halves exchanged in every other four rows, so that eight
@@ -289,31 +303,39 @@ balance_grad_kernel(const __grid_constant__ BalanceMaps maps, const BalanceArgs 
       ldmatrix_x4(base + kDlBytes + n_at, al);
       ldmatrix_x4_trans(base + t_at, th);
       ldmatrix_x4_trans(base + kDlBytes + t_at, tl);
+      // eight products at a time, none of which waits for the one before it
+      uint32_t b[8][2];                                    // X, 16 tokens x 8 columns, as the second operand
+      float d[8][4];
+      const int r = half * 16 + (lane >> 2);
+      uint8_t* const p = sd + r * 128 + (lane & 3) * 4;     // of chunk j: 16 (j ^ (r & 7)) on; eight rows on, the same
 #pragma unroll
       for (int j = 0; j < 8; j += 2) {
-        uint32_t b[4];                                     // X, 16 tokens x 16 columns, as the second operand
+        uint32_t x[4];
         const int row = half * 16 + (lane & 15);
-        ldmatrix_x4_trans(smem_u32(sx) + (uint32_t)(row * 128 + (((j + (lane >> 4)) ^ (row & 7)) << 4)), b);
+        ldmatrix_x4_trans(smem_u32(sx) + (uint32_t)(row * 128 + (((j + (lane >> 4)) ^ (row & 7)) << 4)), x);
+        b[j][0] = x[0]; b[j][1] = x[1]; b[j + 1][0] = x[2]; b[j + 1][1] = x[3];
+      }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          mma_16816(dm[j + i], th, b[2 * i], b[2 * i + 1]);
-          mma_16816(dm[j + i], tl, b[2 * i], b[2 * i + 1]);
+      for (int j = 0; j < 8; ++j) {
+        d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.f;
+        if (a.adds) {
+          const uint32_t u = *reinterpret_cast<const uint32_t*>(p + ((j ^ (r & 7)) << 4)), v = *reinterpret_cast<const uint32_t*>(p + 1024 + ((j ^ (r & 7)) << 4));
+          d[j][0] = lo32(u); d[j][1] = hi32(u); d[j][2] = lo32(v); d[j][3] = hi32(v);
         }
-        if (a.writes) {
+      }
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float d[4] = {0.f, 0.f, 0.f, 0.f};
-            const int r = half * 16 + (lane >> 2);
-            uint32_t* p = reinterpret_cast<uint32_t*>(sd + r * 128 + (((j + i) ^ (r & 7)) << 4) + (lane & 3) * 4);
-            uint32_t* q = p + 8 * 32;                      // eight rows on (the same swizzle)
-            if (a.adds) {
-              d[0] = lo32(*p); d[1] = hi32(*p); d[2] = lo32(*q); d[3] = hi32(*q);
-            }
-            mma_16816(d, ah, mean[j + i][0], mean[j + i][1]);
-            mma_16816(d, al, mean[j + i][0], mean[j + i][1]);
-            *p = pack2(d[0], d[1]);
-            *q = pack2(d[2], d[3]);
-          }
+      for (int j = 0; j < 8; ++j) mma_16816(dm[j], th, b[j][0], b[j][1]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mma_16816(d[j], ah, mean[j][0], mean[j][1]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mma_16816(dm[j], tl, b[j][0], b[j][1]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mma_16816(d[j], al, mean[j][0], mean[j][1]);
+      if (a.writes) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          *reinterpret_cast<uint32_t*>(p + ((j ^ (r & 7)) << 4)) = pack2(d[j][0], d[j][1]);
+          *reinterpret_cast<uint32_t*>(p + 1024 + ((j ^ (r & 7)) << 4)) = pack2(d[j][2], d[j][3]);
         }
       }
     }
