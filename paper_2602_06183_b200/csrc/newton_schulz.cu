@@ -72,7 +72,25 @@ __device__ __forceinline__ float element(const void* G, int64_t i) {
   else return bf16_bits_to_float(__ldg(reinterpret_cast<const uint16_t*>(G) + i));
 }
 
-// Squares are summed in double: neither the largest nor the smallest float32 has one that leaves its range. wide: rows of 16-byte pieces.
+// Squares are summed in double: neither the largest nor the smallest float32 has one that leaves its range, and the sum does not depend on
+// how the rows lie. wide: rows of whole pieces of 16 bytes on their boundaries, four of which are under way at once.
+template <bool kF32>
+__device__ __forceinline__ double sum_squares(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  double s = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (kF32) {
+      const double x = __uint_as_float(w[i]);
+      s = fma(x, x, s);
+    } else {
+      const double x = bf16_bits_to_float(w[i] & 0xFFFFu), y = bf16_bits_to_float(w[i] >> 16);
+      s = fma(x, x, s);
+      s = fma(y, y, s);
+    }
+  }
+  return s;
+}
 template <bool kF32>
 __global__ void __launch_bounds__(256)
 ns_norm_kernel(const void* __restrict__ G, int64_t rows, int64_t cols, int64_t ld, int wide, double* __restrict__ sums) {
@@ -80,32 +98,31 @@ ns_norm_kernel(const void* __restrict__ G, int64_t rows, int64_t cols, int64_t l
   pdl_wait();
   pdl_trigger();
   constexpr int kPiece = kF32 ? 4 : 8;
-  double s = 0;
   const int64_t per_row = wide ? cols / kPiece : cols, first = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   const int64_t dr = step / per_row, dc = step - dr * per_row;
   int64_t r = first / per_row, c = first - r * per_row;
-  for (; r < rows;) {
-    if (wide) {
-      const uint4 v = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(G) + (r * ld + c * kPiece) * (kF32 ? 4 : 2)));
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (kF32) {
-          const double x = __uint_as_float(w[i]);
-          s = fma(x, x, s);
-        } else {
-          const double x = bf16_bits_to_float(w[i] & 0xFFFFu), y = bf16_bits_to_float(w[i] >> 16);
-          s = fma(x, x, s);
-          s = fma(y, y, s);
-        }
-      }
-    } else {
-      const double x = element<kF32>(G, r * ld + c);
-      s = fma(x, x, s);
-    }
+  auto next = [&] {
     r += dr;
     c += dc;
     if (c >= per_row) { c -= per_row; ++r; }
+  };
+  double s = 0;
+  if (wide) {
+    while (r < rows) {
+      uint4 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < rows) v[i] = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(G) + (r * ld + c * kPiece) * (kF32 ? 4 : 2)));
+        next();
+      }
+      s += (sum_squares<kF32>(v[0]) + sum_squares<kF32>(v[1])) + (sum_squares<kF32>(v[2]) + sum_squares<kF32>(v[3]));
+    }
+  } else {
+    for (; r < rows; next()) {
+      const double x = element<kF32>(G, r * ld + c);
+      s = fma(x, x, s);
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);

@@ -90,15 +90,22 @@ balance_loss_kernel(const float* __restrict__ logits, const int* __restrict__ ex
   }
   if (lane == 0) warps[warp] = a;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < kLossThreads / 32; ++w) {
-      a.z += warps[w].z;
+  // the warps' sums, in their order: a value to a lane
+  if (warp == 0) {
+    LossPart& out = parts[blockIdx.x];
+    double z = 0;
+    float p = 0.f;
+    int n = 0;
 #pragma unroll
-      for (int e = 0; e < kMostExperts; ++e) { a.p[e] += warps[w].p[e]; a.n[e] += warps[w].n[e]; }
+    for (int w = 0; w < kLossThreads / 32; ++w) {
+      if (lane == 16) z += warps[w].z;
+      if (lane < 16) { p += warps[w].p[lane]; n += warps[w].n[lane]; }
     }
-    parts[blockIdx.x] = a;
+    if (lane == 16) out.z = z;
+    if (lane < 16) { out.p[lane] = p; out.n[lane] = n; }
     __threadfence();
-    last = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;      // (and back to 0 with the last one)
+    __syncwarp();
+    if (lane == 0) last = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;      // (and back to 0 with the last one)
   }
   __syncthreads();
   if (!last) return;                   // (the whole CTA)
