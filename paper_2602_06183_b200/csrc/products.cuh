@@ -27,6 +27,11 @@ constexpr int64_t kFewTokens = 128;
 // 4 bits alone, 128 x 512 x 512 7.9 / 6.1, 128 x 4096 x 2048 10.5 / 9.1; but 70 x 2048 x 4096 8.3 / 10.8, 96 x 1024 x 8192 11.5 / 15.5.
 inline bool gated_by_few(int fmt, int64_t T, int nkb) { return T <= 64 || (T <= kFewTokens && nkb > (fmt == FMT_BF16 ? 16 : 8)); }
 
+// E4M3 rows: the same, but the pairs' half-empty tiles win where a short reduction leaves little to split and few columns fill the chip either
+// way. Few tokens / pairs, us, in graph replay: 65 to 128 tokens of 8192 x 1024 6.2 to 7.6 / 5.9, of 512 x 512 4.9 to 6.8 / 3.9; but of 16384 x 512
+// 5.5 to 7.4 / 7.2, of 2048 x 2048 4.9 to 5.9 / 7.4, of 8192 x 8192 13.9 to 15.9 / 17.1.
+inline bool rows_by_few(int64_t T, int64_t N, int nkb) { return T <= 64 || (T <= kFewTokens && (nkb > 8 || N > 8192)); }
+
 // Up to this many tokens the operands in between (H, dG, dU) are held as sums of two bf16 numbers, which the few-token products take as
 // twice the tokens: there is room for them in the instruction's columns, and the products wait for the weights. With so few tokens
 // a result rests on a handful of large hidden values, and rounding those once showed: the error of Y against 64 bits was 1.3 to 1.6 times
@@ -245,7 +250,7 @@ template <int kFmt>
 int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, float alpha, void* C, int* status, cudaStream_t s,
            bool early_weights = false, int terms = 1) {
   const int nkb = k_blocks(kFmt, K);
-  if (M <= kFewTokens) {
+  if (kFmt == FMT_E4M3 ? rows_by_few(M, N, nkb) : M <= kFewTokens) {
     FewArgs a{};
     a.T = (int)M; a.N = (int)N; a.nkb = nkb; a.alpha = a.alpha2 = alpha; a.C = C; a.status = status;
     a.early_weights = early_weights; a.in_terms = terms; a.out_terms = 1;
