@@ -21,7 +21,7 @@
 //
 // Launches: norm (partial sums in double), conversion (with the transposition of a high G), then PK_GRAM, PK_SYMM and PK_APPLY of
 // pair_product.cuh: three for a single step, 4 g - 1 for g at once. Half of the tiles of the symmetric ones are computed.
-#include "products.cuh"
+#include "newton_small.cuh"
 
 namespace sf {
 namespace {
@@ -66,12 +66,6 @@ int ns_shape(int64_t rows, int64_t cols, NsShape* z) {
 }
 
 // ---- the norm ---------------------------------------------------------------------------------------------
-template <bool kF32>
-__device__ __forceinline__ float element(const void* G, int64_t i) {
-  if constexpr (kF32) return __ldg(reinterpret_cast<const float*>(G) + i);
-  else return bf16_bits_to_float(__ldg(reinterpret_cast<const uint16_t*>(G) + i));
-}
-
 // Squares are summed in double: neither the largest nor the smallest float32 has one that leaves its range, and the sum does not depend on
 // how the rows lie. wide: rows of whole pieces of 16 bytes on their boundaries, four of which are under way at once.
 template <bool kF32>
@@ -136,10 +130,6 @@ ns_norm_kernel(const void* __restrict__ G, int64_t rows, int64_t cols, int64_t l
 }
 
 // ---- the first X -------------------------------------------------------------------------------------------
-// G 2^k in fp16 (two terms of a float32 G; a bf16 G fits one), k such that its norm lies in [2^13, 2^14); what is left of the norm, a factor of
-// 1 to 2 that is no power of two, goes into the first step's float32 arithmetic (*first), so that a bf16 G is not rounded at all. A G
-// of zeros stays zero; where G's norm is not finite the factor is NaN, and so is every result.
-struct NsScale { float lo, hi; };      // two powers of two whose product is 2^k
 __device__ __forceinline__ NsScale ns_scale(const double* __restrict__ sums, int count, float* first, double* shared) {
   double s = 0;
   for (int i = threadIdx.x; i < count; i += 256) s += __ldcg(sums + i);
@@ -150,26 +140,11 @@ __device__ __forceinline__ NsScale ns_scale(const double* __restrict__ sums, int
   s = shared[0];
 #pragma unroll
   for (int w = 1; w < 8; ++w) s += shared[w];
-  const double norm = sqrt(s);
-  int k = 0;
-  float f = 0.f;
-  if (!(norm < INFINITY)) {
-    f = __uint_as_float(0x7FC00000u);
-  } else if (norm > 0) {
-    k = 13 - ilogb(norm);
-    f = (float)(16384.0 / scalbn(norm, k));
-  }
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *first = f;
-  const int h = k / 2;
-  return NsScale{scalbnf(1.f, h), scalbnf(1.f, k - h)};
+  float f;
+  const NsScale z = ns_scale_of(s, &f);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *first = f;
+  return z;
 }
-__device__ __forceinline__ void ns_terms(float x, const NsScale& z, uint16_t& hi, uint16_t& lo) {
-  const float y = x * z.lo * z.hi;
-  const __half h = __float2half_rn(y), l = __float2half_rn(y - __half2float(h));
-  hi = __half_as_ushort(h);
-  lo = __half_as_ushort(l);
-}
-
 // As it lies: pieces of eight elements of a row (the last one of a row may be short; the padding behind it is written as 0).
 template <bool kF32>
 __global__ void __launch_bounds__(256)
@@ -264,6 +239,52 @@ bool ns_bounded(double a, double b, double c, double* p) {
   return most <= 1.25 && most_b <= 7.5;
 }
 
+// The whole update in one launch, where it fits: *taken says whether it was made. (A cluster of 16 CTAs is more than every device has to offer.)
+template <bool kF32, int kTiles>
+int launch_small(const SmallShape& z, const SmallArgs& a, cudaStream_t s, bool* taken) {
+  auto kern = ns_small_kernel<kF32, kTiles>;
+  static std::atomic<int> most[64]{};  // CTAs of a cluster that the device takes, found once: 1 to 16, or -1
+  int dev = 0;
+  SF_CUDA_TRY(cudaGetDevice(&dev));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)z.ctas);
+  cfg.blockDim = dim3(kSmallThreads);
+  cfg.dynamicSmemBytes = z.smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)z.ctas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  int have = dev >= 0 && dev < 64 ? most[dev].load() : 0;
+  if (have == 0) {
+    SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem));
+    SF_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    have = -1;
+    for (int n = kSmallCtas; n >= 1 && have < 0; n /= 2) {
+      cudaLaunchConfig_t q = cfg;
+      cudaLaunchAttribute at = attr[0];
+      at.val.clusterDim.x = (unsigned)n;
+      q.gridDim = dim3((unsigned)n);
+      q.dynamicSmemBytes = kSmallSmem;
+      q.stream = nullptr;
+      q.attrs = &at;
+      q.numAttrs = 1;
+      int fit = 0;
+      SF_CUDA_TRY(cudaOccupancyMaxActiveClusters(&fit, kern, &q));
+      if (fit > 0) have = n;
+    }
+    if (dev >= 0 && dev < 64) most[dev] = have;
+  }
+  *taken = z.ctas <= have;
+  if (!*taken) return SF_OK;
+  SF_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, a));
+  return SF_OK;
+}
+
 size_t matrix_bytes(int64_t rows, int64_t cols, int64_t ld, int size) {
   return rows > 0 && cols > 0 ? (size_t)size * ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) : 0;
 }
@@ -302,6 +323,18 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
   float* first = (float*)(w + kStatus);
   double* sums = (double*)(w + z.sums);
   const bool f32 = type == SF_F32;
+  SmallShape small;
+  if (small_shape(z.m, z.n, &small)) {
+    SmallArgs q{};
+    q.G = G; q.O = (uint16_t*)O; q.ldg = ldg; q.ldo = ldo;
+    q.m = (int)z.m; q.n = (int)z.n; q.high = z.high; q.steps = steps;
+    q.a = a; q.b = b; q.c = c; q.scale = scale / 16384.f;
+    q.mp = small.mp; q.w = small.w; q.ldx = small.ldx; q.ldm = small.ldm;
+    bool taken = false;
+    SF_TRY(small.tiles == 1 ? (f32 ? launch_small<true, 1>(small, q, s, &taken) : launch_small<false, 1>(small, q, s, &taken))
+                            : (f32 ? launch_small<true, 2>(small, q, s, &taken) : launch_small<false, 2>(small, q, s, &taken)));
+    if (taken) return SF_OK;
+  }
   const int piece = 16 / size;
   const bool wide = aligned16(G) && ldg % piece == 0 && cols % 8 == 0;
   const int64_t pieces = rows * (wide ? cols / piece : cols);

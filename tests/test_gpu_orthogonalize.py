@@ -56,6 +56,22 @@ def test_sizes(m, n, dtype):
     _check(_run(_dev(G, dtype)), G)
 
 
+@pytest.mark.parametrize("m,n", [(16, 33), (5, 16000), (16, 17000), (33, 4096), (33, 8192), (8200, 33), (64, 100), (90, 96), (96, 2561), (2000, 70), (127, 1030), (128, 1024),
+                                 (128, 1025), (4096, 128), (100, 4097), (129, 1024)])
+def test_around_the_edges_of_one_launch(m, n):
+    """Updates of at most 128 rows (or columns) are made in one launch, in clusters of 1 to 16 CTAs, as long as a warp's columns fit."""
+    G = _gradient(m, n, 6)
+    _check(_run(_dev(G)), G)
+
+
+@pytest.mark.parametrize("m,n", [(40, 90), (90, 40), (128, 700), (130, 300)])
+def test_steps_one_after_the_other(m, n):
+    """k steps and then none differ from k steps by nothing but the result's rounding: every number of them is right."""
+    G = _gradient(m, n, 7)
+    for steps in range(1, 8):
+        _check(_run(_dev(G), steps), G, steps)
+
+
 @pytest.mark.parametrize("m,n,rank", [(200, 320, 1), (320, 200, 3), (256, 256, 8), (300, 1000, 40)])
 def test_low_rank(m, n, rank):
     """Where roundings would grow most: directions of no size are brought up 3.4 times with every step."""
@@ -129,6 +145,33 @@ def test_larger_ones_against_64_bits_on_the_device():
             x = a * x + (bb * A + c * A @ A) @ x
         x = x if m <= n else x.T
         assert float((_run(G).double() - x).norm() / x.norm()) < U16 + 5e-3
+
+
+def _on_device(G, steps):
+    x = G.double() if G.shape[0] <= G.shape[1] else G.double().T
+    x = x / x.norm()
+    a, bb, c = around.ABC
+    for _ in range(steps):
+        A = x @ x.T
+        x = a * x + (bb * A + c * A @ A) @ x
+    return x if G.shape[0] <= G.shape[1] else x.T
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 6])
+def test_several_steps_at_once(steps):
+    """1024 rows and more of a wide matrix: three steps at once, then two at a time. The bound is that of the larger ones above."""
+    for m, n in ((1030, 1600), (1700, 1030)):
+        g = torch.Generator("cuda").manual_seed(m + steps)
+        f = torch.arange(1, 257, device="cuda") ** -0.5
+        G = (torch.randn(m, 256, generator=g, device="cuda") * f @ torch.randn(256, n, generator=g, device="cuda") + 0.3 * torch.randn(m, n, generator=g, device="cuda")).to(BF)
+        x = _on_device(G, steps)
+        for dtype in (BF, torch.float32):
+            got = _run(G.to(dtype), steps)
+            assert float((got.double() - x).norm() / x.norm()) < U16 + 5e-3
+    G = torch.zeros((1024, 1536), dtype=BF, device="cuda")
+    assert not _run(G, steps).any()
+    G[5, 7] = float("nan")
+    assert bool(torch.isnan(_run(G, steps)).all())
 
 
 def test_captured_replayed_on_another_stream_and_side_by_side():
