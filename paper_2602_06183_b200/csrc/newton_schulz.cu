@@ -349,7 +349,7 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
     SF_TRY(launch_pdl(f32 ? ns_convert_kernel<true> : ns_convert_kernel<false>, dim3((unsigned)(ctas < most ? ctas : most)), 256, 0, s, G, rows, cols, ldg,
                       (int)wide, (const double*)sums, norm_ctas, first, (uint4*)(w + z.x[0]), (uint4*)(w + z.x[1])));
   }
-  PairArgs p{};
+  NsPairArgs p{};
   p.jobs = 1;
   p.status = (int*)workspace;
   p.M[0] = p.N[0] = (int)z.m;
@@ -361,14 +361,14 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
   struct Sym { int at, e, two; };      // number of the matrix, exponent, whether it has two terms (the first may)
   auto matrix = [&](const Sym& x) { return SymMatrix{(const float*)(w + z.diag[x.at]), std::ldexp(1.f, -x.e), x.two}; };
   auto map = [&](CUtensorMap* m, const Sym& x, int term) { return make_tmap_store(m, w + (term && x.two ? z.second : z.sym[x.at]), z.m, z.m, z.ldm); };
-  auto target = [&](PairArgs& q, const Sym& x) {
+  auto target = [&](NsPairArgs& q, const Sym& x) {
     q.ns.diag_out = (float*)(w + z.diag[x.at]);
     q.ns.up = std::ldexp(1.f, x.e);
     q.ns.two_out = x.two;
   };
   // out = c0 I + c1 x + c2 x y
   auto product = [&](const Sym& x, const Sym& y, float c0, float c1, float c2, const Sym& out) {
-    PairArgs q = p;
+    NsPairArgs q = p;
     q.ns.m1 = matrix(x);
     q.ns.m2 = matrix(y);
     q.ns.same = x.at == y.at;
@@ -392,7 +392,7 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
     const uint8_t *xh = w + z.x[2 * (groups & 1)], *xl = w + z.x[2 * (groups & 1) + 1];
     uint8_t *yh = w + z.x[2 * (~groups & 1)], *yl = w + z.x[2 * (~groups & 1) + 1];
     const Sym A{0, 14, g > 1};
-    PairArgs q = p;
+    NsPairArgs q = p;
     q.ns.first = done == 0 ? first : nullptr;
     target(q, A);
     q.ns.down = std::ldexp(1.f, -28);

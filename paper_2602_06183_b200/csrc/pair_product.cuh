@@ -29,6 +29,8 @@
 
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "gated.cuh"
 
 namespace sf {
@@ -71,6 +73,7 @@ struct PairCfg {
   static constexpr int kAccs = kFp4 && kBN == 256 ? 1 : 2;
   static constexpr uint32_t kScaleCol = kAccs * kBN;
   static constexpr uint32_t kScaleACols = kTiles * 4, kScaleCols = kScaleACols * (1 + kBBlocks);    // of one stage
+  static constexpr int kEpiBars = kKind == PK_APPLY || kKind == PK_SYMM ? 16 : 8;
   static constexpr int kMaps = kKind == PK_DW ? 9 : kKind == PK_DX ? 5 : kKind == PK_NT ? (kFp4 ? 5 : 3)
                              : kKind == PK_FWD ? (kFp4 ? 7 : 4) : kKind == PK_GRAM ? 4 : kKind == PK_SYMM ? 7 : 6;
   static_assert(kBN == 256 || (kFp4 && kBN == 128), "tile width");
@@ -80,6 +83,24 @@ struct PairCfg {
   static_assert(kScaleCol + 2 * kScaleCols <= 512, "TMEM columns");
 };
 
+struct PairArgs {
+  int jobs;
+  int num_m[3], num_n[3];            // tiles of each job
+  int M[3], N[3];                    // its output (PK_FWD: N features)
+  int nkb, nkb0;                     // k-blocks in all, and of the first pair of operands (PK_DX)
+  int act;
+  int bn;                            // tile width (PM_WIDTH, PM_SPLIT)
+  int parts;                         // pairs of a cluster (PM_SPLIT)
+  // PK_DW of up to 16 tokens, whose sums of two (A's in the jobs of the mask, else B's) have their second terms from this row on: 0 otherwise
+  int term_rows, sums_in_a;
+  float alpha, alpha2;
+  int early_next;                    // the next launch is let in at the start: several rounds of tiles (see long_dense in gemm_tc.cu), or it runs beside
+  // Beside the launch before it, which let it in behind its own wait and whose results it does not read (its end is waited for at the end, so that the
+  // order of the stream is kept; that launch does not wait for this one): that one holds the pairs from `first_late` on for about
+  // `late_rounds` tiles of this one, which those pairs leave to the others.
+  int beside, first_late, late_rounds;
+  int* status;
+};
 // The products of an orthogonalised update. A matrix is held as a power of two times itself, in fp16, in one term or two; a symmetric one
 // without its diagonal, which is apart in float32 (see newton_schulz.cu). up: 2^e of the result; down: 2^-e of the operands together.
 struct SymMatrix {
@@ -102,30 +123,16 @@ struct NsArgs {
   uint16_t* out;                     // ... where its rows do not start on multiples of 16 bytes: here, leading dimension ldo
   int64_t ldo;
 };
-struct PairArgs {
-  int jobs;
-  int num_m[3], num_n[3];            // tiles of each job
-  int M[3], N[3];                    // its output (PK_FWD: N features)
-  int nkb, nkb0;                     // k-blocks in all, and of the first pair of operands (PK_DX)
-  int act;
-  int bn;                            // tile width (PM_WIDTH, PM_SPLIT)
-  int parts;                         // pairs of a cluster (PM_SPLIT)
-  // PK_DW of up to 16 tokens, whose sums of two (A's in the jobs of the mask, else B's) have their second terms from this row on: 0 otherwise
-  int term_rows, sums_in_a;
-  float alpha, alpha2;
-  int early_next;                    // the next launch is let in at the start: several rounds of tiles (see long_dense in gemm_tc.cu), or it runs beside
-  // Beside the launch before it, which let it in behind its own wait and whose results it does not read (its end is waited for at the end, so that the
-  // order of the stream is kept; that launch does not wait for this one): that one holds the pairs from `first_late` on for about
-  // `late_rounds` tiles of this one, which those pairs leave to the others.
-  int beside, first_late, late_rounds;
-  int* status;
-  const float* row_scales;           // E4M3 operands: a factor to every row of A
-  NsArgs ns;
-};
+// What a kind needs beside (the others' kernels do not carry it: with 180 bytes more of arguments the step of 8192 x 4096 x 16384 took 3 % longer).
+struct RowPairArgs : PairArgs { const float* row_scales; };      // E4M3 operands: a factor to every row of A
+struct NsPairArgs : PairArgs { NsArgs ns; };
+template <int kKind, int kFmt>
+using PairArgsOf = std::conditional_t<kKind == PK_GRAM || kKind == PK_SYMM || kKind == PK_APPLY, NsPairArgs, std::conditional_t<kFmt == FMT_E4M3, RowPairArgs, PairArgs>>;
 template <int N> struct PairMaps { CUtensorMap m[N]; };
 
+template <int kEpi>                  // barriers of the epilogue warps' loads
 struct PairCtl {
-  uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], epi_full[16];
+  uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], epi_full[kEpi];
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -268,7 +275,7 @@ __device__ __forceinline__ void column_put(uint8_t* b, int lane, const uint32_t 
 struct NsRow { float scale, d1, d2; };
 // What a row of a tile needs (arrays are padded to whole tiles).
 template <int kKind>
-__device__ __forceinline__ NsRow ns_begin(const PairArgs& args, int row) {
+__device__ __forceinline__ NsRow ns_begin(const NsPairArgs& args, int row) {
   NsRow r{1.f, 0.f, 0.f};
   if (kKind != PK_SYMM && args.ns.first) r.scale = __ldcg(args.ns.first);
   if (kKind == PK_SYMM) { r.d1 = __ldcg(args.ns.m1.diag + row); r.d2 = __ldcg(args.ns.m2.diag + row); }
@@ -279,7 +286,7 @@ __device__ __forceinline__ NsRow ns_begin(const PairArgs& args, int row) {
 // buffer, and from there to the matrix. PK_SYMM: b holds the factors' chunks (ns_fetch), and the result takes their place; dcol: the second
 // factor's diagonal at this lane's column.
 template <int kKind>
-__device__ __forceinline__ bool ns_symmetric(const PairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* b, float dcol, uint64_t* loaded, uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
+__device__ __forceinline__ bool ns_symmetric(const NsPairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* b, float dcol, uint64_t* loaded, uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
   const bool on_diag = row == col;
   const float up = args.ns.up;
   float d = 0.f;
@@ -351,7 +358,7 @@ __device__ __forceinline__ bool ns_symmetric(const PairArgs& args, const CUtenso
   return true;
 }
 // A chunk of Q X, with what ns_fetch brought to b, a half of the warp's buffer.
-__device__ __forceinline__ bool ns_apply(const PairArgs& args, const CUtensorMap* maps, const NsRow& r, const uint32_t (&v)[32], uint8_t* b, uint64_t* loaded,
+__device__ __forceinline__ bool ns_apply(const NsPairArgs& args, const CUtensorMap* maps, const NsRow& r, const uint32_t (&v)[32], uint8_t* b, uint64_t* loaded,
                                          uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
   if (!mbar_wait_warp(loaded, phase, abort_flag)) return false;
   uint32_t w[16], lo[16];
@@ -403,7 +410,7 @@ __device__ __forceinline__ bool ns_apply(const PairArgs& args, const CUtensorMap
 
 template <int kKind, int kBN, int kFmt, int kMode>
 __global__ void __launch_bounds__(kPairThreads, 1)
-pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps> maps, const PairArgs args) {
+pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps> maps, const PairArgsOf<kKind, kFmt> args) {
   using Cfg = PairCfg<kKind, kBN, kFmt, kMode>;
   constexpr bool kFp4 = Cfg::kFp4, kGated = Cfg::kGated, kVar = kMode != PM_FULL, kSplit = kMode == PM_SPLIT;
   constexpr int kStages = Cfg::kStages, kAccs = Cfg::kAccs;
@@ -412,7 +419,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
   extern __shared__ uint8_t smem_dyn[];
   uint8_t* smem = smem_dyn + align_pad(smem_dyn, 1024);
   uint8_t* epi = smem + kStages * Cfg::kStageBytes;
-  PairCtl* ctl = reinterpret_cast<PairCtl*>(epi + 8 * Cfg::kEpiWarpBytes);
+  using Ctl = PairCtl<Cfg::kEpiBars>;
+  Ctl* ctl = reinterpret_cast<Ctl*>(epi + 8 * Cfg::kEpiWarpBytes);
   volatile int* abort_flag = &ctl->abort_flag;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = (int)cluster_ctarank(), rank = cta & 1, part = kSplit ? cta >> 1 : 0;
@@ -439,7 +447,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       mbar_init(&ctl->tmem_full[b], 1);
       mbar_init(&ctl->tmem_empty[b], 16);                  // eight epilogue warps of either CTA
     }
-    for (int w = 0; w < 16; ++w) mbar_init(&ctl->epi_full[w], 1);
+    for (int w = 0; w < Cfg::kEpiBars; ++w) mbar_init(&ctl->epi_full[w], 1);
     ctl->abort_flag = 0;
     fence_mbar_init();
   }
@@ -645,7 +653,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
         }
       };
       if (kKind == PK_BWD && part * 2 + set < chunks) fetch(part * 2 + set);
-      const float row_scale = kFmt == FMT_E4M3 ? args.alpha * (row + lane < M ? __ldg(args.row_scales + row + lane) : 0.f) : 1.f;
+      float row_scale = 1.f;
+      if constexpr (kFmt == FMT_E4M3) row_scale = args.alpha * (row + lane < M ? __ldg(args.row_scales + row + lane) : 0.f);
       NsRow ns_row;
       if constexpr (Cfg::kNs) {
         ns_row = ns_begin<kKind>(args, row + lane);
@@ -849,7 +858,7 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
 }
 
 template <int kKind, int kBN, int kFmt, int kMode>
-int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps>& maps, PairArgs a, cudaStream_t s) {
+int launch_pair(const PairMaps<PairCfg<kKind, kBN, kFmt, kMode>::kMaps>& maps, PairArgsOf<kKind, kFmt> a, cudaStream_t s) {
   using Cfg = PairCfg<kKind, kBN, kFmt, kMode>;
   auto kern = pair_product_kernel<kKind, kBN, kFmt, kMode>;
   static std::atomic<bool> attr_done[64]{};

@@ -175,7 +175,7 @@ int run_few_rows(const Operand& X, const Operand& W0, const Operand& W1, int64_t
 
 // Launches the kernel of a plan: make(maps, bn) fills the tensor maps for tiles of that width.
 template <int kKind, int kFmt = FMT_BF16, typename F>
-int launch_plan(const PairPlan& plan, PairArgs a, cudaStream_t s, F&& make) {
+int launch_plan(const PairPlan& plan, PairArgsOf<kKind, kFmt> a, cudaStream_t s, F&& make) {
   PairMaps<PairCfg<kKind, 256, kFmt, PM_FULL>::kMaps> maps;
   SF_TRY(make(maps.m, plan.bn));
   a.bn = plan.bn;
@@ -194,12 +194,12 @@ inline int plan_pairs(int kind, const PairArgs& a, PairPlan* plan) {
   return SF_OK;
 }
 template <int kKind, int kFmt = FMT_BF16, typename F>
-int launch_best(const PairArgs& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr, const PairPlan* beside = nullptr) {
+int launch_best(const PairArgsOf<kKind, kFmt>& a, cudaStream_t s, F&& make, PairPlan* taken = nullptr, const PairPlan* beside = nullptr) {
   PairPlan plan;
   SF_TRY(plan_pairs(kKind, a, &plan));
   if (taken) *taken = plan;
   if (!beside) return launch_plan<kKind, kFmt>(plan, a, s, make);
-  PairArgs b = a;
+  PairArgsOf<kKind, kFmt> b = a;
   b.beside = 1;
   const int64_t pairs = sm_count_now() / 2;
   if (beside->pairs < pairs && plan.mode != PM_SPLIT) {
@@ -257,10 +257,10 @@ int run_nt(const Operand& A, const Operand& B, int64_t M, int64_t N, int64_t K, 
     if (kFmt == FMT_E4M3) a.row_scales = (const float*)A.scales;
     return run_few_rows<kFmt, FK_NT>(A, B, B, N, K, a, s);
   }
-  PairArgs a{};
+  PairArgsOf<PK_NT, kFmt> a{};
   a.jobs = 1; a.M[0] = (int)M; a.N[0] = (int)N; a.nkb = a.nkb0 = nkb; a.alpha = alpha; a.status = status;
   if constexpr (!is_fp4(kFmt)) {
-    if (kFmt == FMT_E4M3) a.row_scales = (const float*)A.scales;
+    if constexpr (kFmt == FMT_E4M3) a.row_scales = (const float*)A.scales;
     return launch_best<PK_NT, kFmt>(a, s, [&](CUtensorMap* m, int bn) {
       SF_TRY(kmajor_map(&m[0], kFmt, A.data, M, K, 128));
       SF_TRY(kmajor_map(&m[1], kFmt, B.data, N, K, bn / 2));
