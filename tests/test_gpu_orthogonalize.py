@@ -159,8 +159,9 @@ def _on_device(G, steps):
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6])
 def test_several_steps_at_once(steps):
-    """1024 rows and more of a wide matrix: three steps at once, then two at a time. The bound is that of the larger ones above."""
-    for m, n in ((1030, 1600), (1700, 1030)):
+    """Matrices much wider than high (m (n - m) of 6 x 2^20 and more): three steps at once, then two at a time. The bound is that of the larger
+    ones above."""
+    for m, n in ((1030, 1600), (1700, 1030), (1030, 7300), (13000, 520), (40, 160000), (2100, 5200)):
         g = torch.Generator("cuda").manual_seed(m + steps)
         f = torch.arange(1, 257, device="cuda") ** -0.5
         G = (torch.randn(m, 256, generator=g, device="cuda") * f @ torch.randn(256, n, generator=g, device="cuda") + 0.3 * torch.randn(m, n, generator=g, device="cuda")).to(BF)
@@ -168,7 +169,7 @@ def test_several_steps_at_once(steps):
         for dtype in (BF, torch.float32):
             got = _run(G.to(dtype), steps)
             assert float((got.double() - x).norm() / x.norm()) < U16 + 5e-3
-    G = torch.zeros((1024, 1536), dtype=BF, device="cuda")
+    G = torch.zeros((1024, 7300), dtype=BF, device="cuda")
     assert not _run(G, steps).any()
     G[5, 7] = float("nan")
     assert bool(torch.isnan(_run(G, steps)).all())
