@@ -424,7 +424,8 @@ SF_API int sf_gemm_fp4_gated(const void* A, const void* a_scales, const void* Bg
  *       codes  uint8 [T, D]  y as E4M3 codes. With scales (float32 [T]): scales[t] = top / 448, top = max(the row's largest |y|, 2^-96), code =
  *                            e4m3(y * (448 / top)), for sf_gemm_fp8_rows. With scales NULL: code = e4m3(y * scale), as sf_fp8_quantize
  *       rstd   float32 [T]   r, for the backward pass
- *     The squares are summed in float32. An infinity makes its own element NaN and the others of its row 0, a NaN its whole row.
+ *     The squares are summed in float32. An infinity makes its own element NaN and the others of its row 0, a NaN its whole row; the scale
+ *     of a row with either is NaN, and so are its codes.
  * sf_rmsnorm_bwd:  dY bf16 [T, D], S and r of the forward call, dS the gradient that comes to S from elsewhere (bf16 [T, D] or NULL):
  *       n = S r,  q = dY gamma,  dX = dS + r (q - n mean(q n)) [T, D] (of X and of the residual alike),  dgamma = sum over t of dY n [D], bf16.
  *     Either output may be NULL. dX may be dY or dS itself. With T == 0 dgamma is zero. The same call gives the same bits.

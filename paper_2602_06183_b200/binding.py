@@ -652,9 +652,9 @@ def _scale_bytes(rows: int, cols: int, fmt: int) -> int:
     return ((rows + 127 >> 7) * (cols + (1 << lg) - 1 >> lg)) << 9
 
 
-def _matrix_shape(where: str, t):
+def _matrix_shape(where: str, t, name: str = "codes"):
     if t.dim() != 2:
-        raise SparseFFNError(SF_ERR_SHAPE, f"{where}: codes must be a matrix")
+        raise SparseFFNError(SF_ERR_SHAPE, f"{where}: {name} must be a matrix")
     return t.shape
 
 
@@ -764,14 +764,17 @@ def sf_rmsnorm_fwd(X, gamma, eps: float, residual=None, sum=None, Y=None, codes=
     scale to every row in ``scales``, or the given ``scale``), 1 / rms to ``rstd``. What is None is not written; without Y and codes a Y is made.
     X may be a strided row view. Returns Y (or the codes)."""
     w, dev = "sf_rmsnorm_fwd", X.get_device()
-    T, D = shape = _matrix_shape(w, X)
+    T, D = shape = _matrix_shape(w, X, "X")
     ld = D if X.dtype is _BF16 and X.is_contiguous() else _row_stride(w, "X", X)
     if Y is None and codes is None:
         with _allocating(stream):
             Y = torch.empty((T, D), dtype=_BF16, device=X.device)
-    _check(lib().sf_rmsnorm_fwd(X.data_ptr(), ld, None if residual is None else _tensor(w, "residual", residual, _BF16, shape, dev), _tensor(w, "gamma", gamma, _BF16, (D,), dev),
-                                T, D, eps, None if sum is None else _tensor(w, "sum", sum, _BF16, shape, dev), None if Y is None else _tensor(w, "Y", Y, _BF16, shape, dev),
-                                None if codes is None else _tensor(w, "codes", codes, _U8, shape, dev), None if scales is None else _tensor(w, "scales", scales, _F32, (T,), dev), scale,
+    _check(lib().sf_rmsnorm_fwd(X.data_ptr(), ld, None if residual is None else _tensor(w, "residual", residual, _BF16, shape, dev),
+                                _tensor(w, "gamma", gamma, _BF16, (D,), dev), T, D, eps,
+                                None if sum is None else _tensor(w, "sum", sum, _BF16, shape, dev),
+                                None if Y is None else _tensor(w, "Y", Y, _BF16, shape, dev),
+                                None if codes is None else _tensor(w, "codes", codes, _U8, shape, dev),
+                                None if scales is None else _tensor(w, "scales", scales, _F32, (T,), dev), scale,
                                 None if rstd is None else _tensor(w, "rstd", rstd, _F32, (T,), dev), _launch_stream(w, dev, stream)), w)
     return codes if Y is None else Y
 
@@ -784,7 +787,7 @@ def sf_rmsnorm_bwd(dY, S, gamma, rstd, dS=None, dX=None, dgamma=None, workspace=
     """Gradients of sf_rmsnorm_fwd from dY, its sum S and its rstd, dS added: into ``dX`` and ``dgamma``, of which a None is left out (both
     None: both are made). Returns (dX, dgamma)."""
     w, dev = "sf_rmsnorm_bwd", dY.get_device()
-    T, D = shape = _matrix_shape(w, dY)
+    T, D = shape = _matrix_shape(w, dY, "dY")
     both = dX is None and dgamma is None
     if both or (dgamma is not None and workspace is None):
         with _allocating(stream):
@@ -822,17 +825,11 @@ def sf_router_balance_workspace_size(T: int, D: int, E: int) -> int:
     return _sized("sf_router_balance_workspace_size", T, D, E)
 
 
-def _logits_shape(where: str, t):
-    if t.dim() != 2:
-        raise SparseFFNError(SF_ERR_SHAPE, f"{where}: logits must be a matrix")
-    return t.shape
-
-
 def sf_router_balance_fwd(logits, expert, balance_coef: float, z_coef: float = 0.0, loss=None, counts=None, workspace=None, stream=None):
     """(loss float32 [3], counts int32 [E]) of logits float32 [T,E] and expert int32 [T] (tokens outside [0,E) are left out): the loss with its
     coefficients, the balance and the z term, and the tokens of every expert."""
     w, dev = "sf_router_balance_fwd", logits.get_device()
-    T, E = _logits_shape(w, logits)
+    T, E = _matrix_shape(w, logits, "logits")
     if loss is None or counts is None or workspace is None:
         with _allocating(stream):
             loss = torch.empty((3,), dtype=_F32, device=logits.device) if loss is None else loss
@@ -849,8 +846,8 @@ def sf_router_balance_bwd(logits, expert, counts, balance_coef: float, z_coef: f
     """Gradients of sf_router_balance_fwd's loss (times ``dloss`` float32 [1], or 1): dX = dX_in + dl means and dmeans = dl^T X, of which a None is
     left out (both None: both are made). Returns (dX, dmeans)."""
     w, dev = "sf_router_balance_bwd", logits.get_device()
-    T, E = _logits_shape(w, logits)
-    D = _matrix_shape(w, X)[1]
+    T, E = _matrix_shape(w, logits, "logits")
+    D = _matrix_shape(w, X, "X")[1]
     both = dX is None and dmeans is None
     if both or workspace is None:
         with _allocating(stream):

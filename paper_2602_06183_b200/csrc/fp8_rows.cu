@@ -1,6 +1,7 @@
 // C = bf16(alpha a_scales[row] A B^T) of E4M3 operands, for any number of rows of A: what the norm's 8-bit output, a scale to every token, is
 // made for. The kernels are those of the gated block and of the 4-bit products (few tokens: the weights are streamed past them; more: tiles
-// on CTA pairs) with tcgen05.mma.kind::f8f6f4; the scales are factors of the epilogue.
+// on CTA pairs) with tcgen05.mma.kind::f8f6f4; the scales are factors of the epilogue. 1 x 16384 x 4096: 13.0 us (67 MB, 5.2 TB/s, weights from
+// HBM); 8192 x 16384 x 4096: 378 (2.9 PFLOP/s) in short runs, 435 (2.5) under the power cap, the tensor pipe active in 92 % of the cycles.
 #include "products.cuh"
 
 namespace sf {

@@ -121,3 +121,13 @@ def test_wrong_types_and_shapes_are_refused(lib):
     with pytest.raises(binding.SparseFFNError) as e:
         binding.sf_orthogonalize(X.T, out=z((64, 4), dtype=bf), workspace=z(9))
     assert e.value.status == SF_ERR_ALIGN
+
+
+def test_gradients_of_the_balance_loss_drain_their_copies_after_an_expired_wait():
+    """As for the products' kernels: a CTA that gave up a wait lets the copies into its shared memory land before it leaves, and says so."""
+    import os
+    text = open(os.path.join(build.CSRC, "balance_grad.cuh")).read()
+    body = text[text.index("\nbalance_grad_kernel("):]
+    body = body[:body.index("\n}\n")]
+    assert "tma_load_2d(" in body and "drain_after_expiry()" in body and "atomicExch(a.status, 1)" in body
+    assert body.index("pdl_wait()") < body.index("mbar_wait_warp(")          # a wait's budget begins behind the launch before

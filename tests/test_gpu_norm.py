@@ -133,6 +133,7 @@ def test_what_is_not_finite_or_zero():
     assert np.abs(y[4]).max() < 1e-20 and np.isfinite(v[4]).all() and np.allclose(np.mean(y[5].astype(np.float64) ** 2), 1, rtol=1e-2)
     assert not f32(b.sf_rmsnorm_fwd(X[3:4], G, 1e-6)).any()
     assert np.isnan(f32(b.sf_rmsnorm_fwd(X[3:4], G, 0.0))).all()       # 0 / 0
+    assert bool(torch.isnan(scales[1:3]).all()) and np.isnan(v[1:3]).all() and bool(torch.isfinite(scales[3:]).all())
 
 
 def test_no_tokens():
