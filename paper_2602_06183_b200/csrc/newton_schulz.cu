@@ -40,11 +40,13 @@ struct NsShape {
 };
 
 // Several steps at once save 6 m^2 (n - m) flops and the passes over X, and cost six more products of the small side, which halves of tiles and
-// single rounds leave half used; with few rows they are launches, and the passes count. Single steps / three and two at once, us: 64 x 9000 109 / 92,
+// single rounds leave half used; with fewer rows they are launches, and the passes count. Single steps / three and two at once, us:
 // 512 x 4096 119 / 125, 512 x 9000 173 / 149; 1024 x 4096 194 / 215, 1024 x 8192 252 / 242; 1400 x 5600 320 / 335, 1400 x 11200
 // 467 / 399; 2048 x 3072 277 / 288, 2048 x 6144 423 / 345; 3000 x 4500 965 / 970, 3000 x 9000 1611 / 1243; 4096 x 4096 1189 / 1336, 4096 x 6144 1615 / 1526,
 // 4096 x 16384 3844 / 2219.
-bool ns_grouped(int64_t m, int64_t n) { return (m > 1024 ? m : 1024) * (n - m) >= (int64_t)6 << 20; }
+// Below 512 rows fewer and larger eigenvalues share the roundings, and single steps it is: the error before the last rounding was 0.04 % for single
+// steps and 0.35 % for three and two at once at 10 rows, 0.05 and 0.22 at 64, 0.05 and 0.12 at 512 (64 x 9000 would take 92 us in place of 109).
+bool ns_grouped(int64_t m, int64_t n) { return m >= 512 && (m > 1024 ? m : 1024) * (n - m) >= (int64_t)6 << 20; }
 
 int ns_shape(int64_t rows, int64_t cols, NsShape* z) {
   if (rows < 0 || cols < 0 || rows > kMostSide || cols > kMostSide) return SF_ERR_SHAPE;

@@ -159,8 +159,7 @@ def _on_device(G, steps):
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6])
 def test_several_steps_at_once(steps):
-    """Matrices much wider than high (m (n - m) of 6 x 2^20 and more): three steps at once, then two at a time. The bound is that of the larger
-    ones above."""
+    """512 rows and more of a matrix much wider than high: three steps at once, then two at a time. The bound is that of the larger ones above."""
     for m, n in ((1030, 1600), (1700, 1030), (1030, 7300), (13000, 520), (40, 160000), (2100, 5200)):
         g = torch.Generator("cuda").manual_seed(m + steps)
         f = torch.arange(1, 257, device="cuda") ** -0.5
@@ -173,6 +172,18 @@ def test_several_steps_at_once(steps):
     assert not _run(G, steps).any()
     G[5, 7] = float("nan")
     assert bool(torch.isnan(_run(G, steps)).all())
+
+
+@pytest.mark.parametrize("m,n", [(10, 17703), (35, 14517), (9000, 64), (200, 9000), (511, 8000)])
+def test_few_rows_of_long_ones_keep_the_precision(m, n):
+    """Where several steps at once would lose some: the error is at most 1.5 times that of a result that is rounded only at its end."""
+    g = torch.Generator("cuda").manual_seed(m)
+    r = min(m, n, 256)
+    f = torch.arange(1, r + 1, device="cuda") ** -0.5
+    G = ((torch.randn(m, r, generator=g, device="cuda") * f) @ torch.randn(r, n, generator=g, device="cuda") + 0.3 * torch.randn(m, n, generator=g, device="cuda")).to(BF)
+    x = _on_device(G, 5)
+    once = float((x.to(torch.float32).to(BF).double() - x).norm())
+    assert float((_run(G).double() - x).norm()) < 1.5 * once
 
 
 def test_captured_replayed_on_another_stream_and_side_by_side():
