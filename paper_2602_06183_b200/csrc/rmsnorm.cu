@@ -5,9 +5,8 @@
 // Sums are in float32; S, y, dX and dgamma are rounded once each.
 //
 // Memory bounds them: 8 bytes an element forward (7 with codes) and 8 backward. A row stays in the registers of one group of threads from
-// its load to its store; the only thing that crosses warps is a row's sum. 16384 x 4096: forward 87 us (6.2 TB/s), backward 93 and 5 for the sum
-// of dgamma's parts (5.7 TB/s), each alone; the two in turn 183 (5.9 TB/s) in graph replay and 200 under the power cap of endless repetition.
-// 8192 x 4096 to E4M3 rows 44.5 (5.3 TB/s). One row of 4096: 4.1, a launch.
+// its load to its store; the only thing that crosses warps is a row's sum. 16384 x 4096: forward 82 us (6.6 TB/s), backward 93 and 5 for the sum
+// of dgamma's parts (5.7 TB/s), each alone. 8192 x 4096 to E4M3 rows 39.5 (5.9 TB/s). One row of 4096: 4.1, a launch.
 #include "fp8_fmt.cuh"
 #include "gated.cuh"
 #include "sums.cuh"
@@ -88,7 +87,7 @@ constexpr float kLeastAmax = 1.2621774483536189e-29f;      // 2^-96
 template <int V, bool kRows>
 __global__ void __launch_bounds__(1024)
 rmsnorm_kernel(const NormArgs a) {
-  __shared__ float slots[2][128];       // (of groups of more than a warp)
+  __shared__ float slots[4][128];       // (of groups of more than a warp)
   Group g;
   g.index = (int)threadIdx.x / a.tpr;
   g.lane = (int)threadIdx.x - g.index * a.tpr;
@@ -379,7 +378,8 @@ int sf_rmsnorm_fwd(const void* X, int64_t ldx, const void* residual, const void*
     return SF_ERR_UNSUPPORTED;
   SF_TRY(check_arch());
   const RowPlan p = fwd_plan(T, D);
-  const int groups = p.tpr >= 128 ? 1 : 128 / p.tpr;
+  // CTAs of 256 threads: with 128 the rate at which CTAs start was in the way (8192 x 4096 46.3 us instead of 42.6, to E4M3 46.1 instead of 39.5)
+  const int groups = p.tpr >= 256 ? 1 : 256 / p.tpr;
   NormArgs a{};
   a.X = (const uint16_t*)X; a.R = (const uint16_t*)residual; a.gamma = (const uint16_t*)gamma; a.ldx = ldx; a.T = T;
   a.sum = (uint16_t*)sum; a.Y = (uint16_t*)Y; a.codes = (uint8_t*)codes; a.scales = (float*)scales; a.rstd = (float*)rstd;
