@@ -5,8 +5,8 @@
 // Sums are in float32; S, y, dX and dgamma are rounded once each.
 //
 // Memory bounds them: 8 bytes an element forward (7 with codes) and 8 backward. A row stays in the registers of one group of threads from
-// its load to its store; the only thing that crosses warps is a row's sum. 16384 x 4096: forward 82 us (6.6 TB/s), backward 93 and 5 for the sum
-// of dgamma's parts (5.7 TB/s), each alone. 8192 x 4096 to E4M3 rows 39.5 (5.9 TB/s). One row of 4096: 4.1, a launch.
+// its load to its store; the only thing that crosses warps is a row's sum. 16384 x 4096: forward 82 us (6.6 TB/s), backward 84 (6.4 TB/s) with the sum of dgamma's parts,
+// each alone. 8192 x 4096 to E4M3 rows 39.5 (5.9 TB/s). One row of 4096: 4.1, a launch.
 #include "fp8_fmt.cuh"
 #include "gated.cuh"
 #include "sums.cuh"
@@ -340,11 +340,13 @@ RowPlan fwd_plan(int64_t T, int64_t D) {
   const int v = T <= sm_count_now() && vecs <= 1024 ? 1 : T <= sm_count_now() && vecs <= 2048 ? 2 : vecs <= 64 ? 2 : 4;
   return RowPlan{v, whole_warps((vecs + v - 1) / v)};
 }
-// Backward: up to 512 threads to a row, of one, two or four vectors each; a row of more than 16384 elements takes up to 1024.
+// Backward: up to 512 threads to a row, of one, two or four vectors each; a row of more than 16384 elements takes up to 1024. Four vectors make
+// more rows of a CTA and fewer barriers a byte, two start and end sooner: 2 / 4 vectors, us: 16384 x 4096 91.4 / 84.3, 4096 x 8192 51.6 / 46.9, 8192 x 4096
+// 49.3 / 47.1; 8192 x 2048 27.8 / 28.5, 2000 x 4096 15.4 / 15.9, 1000 x 1408 7.7 / 8.3.
 RowPlan bwd_plan(int64_t T, int64_t D) {
   const int vecs = (int)(D / 8);
   if (vecs <= 32) return RowPlan{1, vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32};
-  const int v = T <= kBwdCtas && vecs <= 512 ? 1 : vecs <= 1024 ? 2 : 4;
+  const int v = T <= kBwdCtas && vecs <= 512 ? 1 : vecs > 1024 || (vecs >= 512 && T >= 4096) ? 4 : 2;
   return RowPlan{v, whole_warps((vecs + v - 1) / v)};
 }
 
@@ -427,14 +429,14 @@ int sf_rmsnorm_bwd(const void* dY, const void* sum, const void* gamma, const voi
   NormBwdArgs a{};
   a.dY = (const uint16_t*)dY; a.S = (const uint16_t*)sum; a.gamma = (const uint16_t*)gamma; a.dS = (const uint16_t*)dS; a.rstd = (const float*)rstd;
   a.T = T; a.dX = (uint16_t*)dX; a.dgamma = (uint16_t*)dgamma; a.parts = (float*)workspace; a.D = (int)D; a.tpr = p.tpr;
-  const int threads = groups * p.tpr, stages = p.v < 4 ? 4 : threads > 512 ? 1 : 2;
+  const int threads = groups * p.tpr, stages = p.v == 1 ? 4 : p.v == 2 ? 3 : threads > 512 ? 1 : 2;
   const size_t smem = (size_t)stages * 3 * p.v * threads * 16;
-  auto kern = p.v == 1 ? rmsnorm_bwd_kernel<1, 4> : p.v == 2 ? rmsnorm_bwd_kernel<2, 4> : stages == 2 ? rmsnorm_bwd_kernel<4, 2> : rmsnorm_bwd_kernel<4, 1>;
+  auto kern = p.v == 1 ? rmsnorm_bwd_kernel<1, 4> : p.v == 2 ? rmsnorm_bwd_kernel<2, 3> : stages == 2 ? rmsnorm_bwd_kernel<4, 2> : rmsnorm_bwd_kernel<4, 1>;
   static std::atomic<bool> attr_done[64]{};
   int dev = 0;
   SF_CUDA_TRY(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64 || !attr_done[dev]) {
-    for (auto k : {rmsnorm_bwd_kernel<1, 4>, rmsnorm_bwd_kernel<2, 4>, rmsnorm_bwd_kernel<4, 2>, rmsnorm_bwd_kernel<4, 1>})
+    for (auto k : {rmsnorm_bwd_kernel<1, 4>, rmsnorm_bwd_kernel<2, 3>, rmsnorm_bwd_kernel<4, 2>, rmsnorm_bwd_kernel<4, 1>})
       SF_CUDA_TRY(cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kBwdSmem));
     if (dev >= 0 && dev < 64) attr_done[dev] = true;
   }

@@ -15,7 +15,7 @@ pytestmark = pytest.mark.gpu
 BF, U16, F32E = torch.bfloat16, 2.0 ** -8, 2.0 ** -16
 
 SHAPES = [(1, 8), (1, 4096), (2, 1032), (5, 64), (3, 32768), (149, 256), (150, 264), (300, 512), (333, 1024), (1000, 1408), (160, 4104),
-          (160, 8192), (150, 16384), (152, 32760)]
+          (160, 8192), (150, 16384), (152, 32760), (4100, 4104)]
 
 
 def _case(T, D, seed=0):
