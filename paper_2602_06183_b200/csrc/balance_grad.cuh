@@ -16,11 +16,18 @@ struct Softmax { float p[kMostExperts], lse; };
 __device__ __forceinline__ Softmax softmax_of(const float* __restrict__ l, int E) {
   Softmax s;
   float top = -INFINITY;
+  if ((E & 3) == 0) {                  // rows on 16-byte boundaries
 #pragma unroll
-  for (int e = 0; e < kMostExperts; ++e) {
-    s.p[e] = e < E ? __ldg(l + e) : -INFINITY;
-    top = fmaxf(top, s.p[e]);
+    for (int e = 0; e < kMostExperts; e += 4) {
+      const float4 v = e < E ? __ldg(reinterpret_cast<const float4*>(l + e)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      s.p[e] = v.x; s.p[e + 1] = v.y; s.p[e + 2] = v.z; s.p[e + 3] = v.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < kMostExperts; ++e) s.p[e] = e < E ? __ldg(l + e) : -INFINITY;
   }
+#pragma unroll
+  for (int e = 0; e < kMostExperts; ++e) top = fmaxf(top, s.p[e]);
   const float from = top == -INFINITY ? 0.f : top;         // (a row of -infinities is NaN: 0 / 0)
   float sum = 0.f;
 #pragma unroll

@@ -6,11 +6,12 @@
 //   dX      = dX_in + dl means,   dmeans = dl^T X          (l = X means^T)
 // A token whose expert lies outside [0, E) (padding) is left out of all sums and has dl = 0. n_e is counted, not differentiated.
 //
-// Forward: 4 E + 4 bytes a token, one launch; the CTA that finishes last adds up what the others left. Backward: 6 bytes an element of X
+// Forward: 4 E + 4 bytes a token, one launch; the CTA that finishes last adds up what the others left (one token
+// 2.6 us, 16384 of 16 experts 5.7, a million 27.9 in graph replay). Backward: 6 bytes an element of X
 // (X and dX_in in, dX out) and 4 T D E flops, one launch and one that adds up the CTAs' partial sums of dmeans.
 //
 // Memory bounds the backward pass only if the products stay out of its way: as float32 multiply-adds they took 417 us where the bytes take 62 (16384
-// tokens, D 4096, E 16; now 72 alone, 5.6 TB/s, both calls 87). Sixteen experts are one side of a warp's m16n8k16 product, so both run there: dX = dl means with the means'
+// tokens, D 4096, E 16; now 72 alone, 5.6 TB/s, both calls 85). Sixteen experts are one side of a warp's m16n8k16 product, so both run there: dX = dl means with the means'
 // fragments of a warp's 64 columns in 16 registers, dmeans = dl^T X with its sums in 32. dl is a sum of two bf16 numbers (16 bits), X and
 // the means are bf16 as they come, sums are in float32.
 #include "balance_grad.cuh"
@@ -27,98 +28,125 @@ namespace {
 using namespace ptx;
 
 constexpr int64_t kMostTokens = (int64_t)1 << 28, kMostCols = (int64_t)1 << 20;
-constexpr int kLossCtas = 148, kLossThreads = 256;
+constexpr int kLossCtas = 296, kLossThreads = 256, kLossWarps = kLossThreads / 32;
 constexpr size_t kHead = 256, kDone = 128;                 // status word; the word that counts the CTAs that have finished
 
-// (z in double: a masked row's log-sum-exp may be the lowest float32, whose square is none)
-struct LossPart { float p[kMostExperts]; double z; int n[kMostExperts]; };
+// What a CTA adds up. (z in double: a masked row's log-sum-exp may be the lowest float32, whose square is none)
+struct LossPart { float p[kMostExperts]; int n[kMostExperts]; double z; };
 
+// Sixteen sums over a warp's lanes in sixteen shuffles: half of them change hands at every step. The sum of value e is in lanes 2 e and 2 e + 1.
+__device__ __forceinline__ float sixteen_sums(float (&v)[kMostExperts], int lane) {
+#pragma unroll
+  for (int h = 8; h > 0; h >>= 1) {
+    const bool up = lane & 2 * h;
+#pragma unroll
+    for (int i = 0; i < h; ++i) {
+      const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, 2 * h);
+    }
+  }
+  return v[0] + __shfl_xor_sync(0xFFFFFFFFu, v[0], 1);
+}
+
+// One launch: a CTA's sums go to memory, and the one that finishes last adds them up in their order. (A single CTA keeps them.)
 __global__ void __launch_bounds__(kLossThreads)
 balance_loss_kernel(const float* __restrict__ logits, const int* __restrict__ expert, int64_t T, int E, float cb, float cz, float* __restrict__ loss,
                     int* __restrict__ counts, LossPart* __restrict__ parts, unsigned* __restrict__ done) {
-  __shared__ LossPart warps[kLossThreads / 32];
-  __shared__ int last;
+  __shared__ LossPart warps[kLossWarps];
+  __shared__ double sums[kLossWarps][kMostExperts + 1];
+  __shared__ int nums[kLossWarps][kMostExperts], last;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_trigger();
-  LossPart a{};
-  for (int64_t t = (int64_t)blockIdx.x * kLossThreads + threadIdx.x; t < T; t += (int64_t)gridDim.x * kLossThreads) {
-    const int ex = __ldg(expert + t);
-    if ((unsigned)ex >= (unsigned)E) continue;
+  float p[kMostExperts];
+#pragma unroll
+  for (int e = 0; e < kMostExperts; ++e) p[e] = 0.f;
+  double z = 0;
+  int n = 0;                           // of expert `lane`
+  for (int64_t t0 = (int64_t)blockIdx.x * kLossThreads; t0 < T; t0 += (int64_t)gridDim.x * kLossThreads) {
+    const int64_t t = t0 + threadIdx.x;
+    const int ex = t < T ? __ldg(expert + t) : -1;
+    const bool counts_here = (unsigned)ex < (unsigned)E;
+#pragma unroll
+    for (int e = 0; e < kMostExperts; ++e) {
+      const unsigned all = __ballot_sync(0xFFFFFFFFu, counts_here && ex == e);
+      if (lane == e) n += __popc(all);
+    }
+    if (!counts_here) continue;
     const Softmax s = softmax_of(logits + t * E, E);
-    a.z = fma((double)s.lse, (double)s.lse, a.z);
+    z = fma((double)s.lse, (double)s.lse, z);
 #pragma unroll
-    for (int e = 0; e < kMostExperts; ++e) {
-      a.p[e] += s.p[e];
-      a.n[e] += ex == e;
-    }
+    for (int e = 0; e < kMostExperts; ++e) p[e] += s.p[e];
   }
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float mine = sixteen_sums(p, lane);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    a.z += __shfl_xor_sync(0xFFFFFFFFu, a.z, o);
-#pragma unroll
-    for (int e = 0; e < kMostExperts; ++e) {
-      a.p[e] += __shfl_xor_sync(0xFFFFFFFFu, a.p[e], o);
-      a.n[e] += __shfl_xor_sync(0xFFFFFFFFu, a.n[e], o);
-    }
-  }
-  if (lane == 0) warps[warp] = a;
+  for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, o);
+  if ((lane & 1) == 0) warps[warp].p[lane >> 1] = mine;
+  if (lane < kMostExperts) warps[warp].n[lane] = n;
+  if (lane == 0) warps[warp].z = z;
   __syncthreads();
-  // the warps' sums, in their order: a value to a lane
-  if (warp == 0) {
-    LossPart& out = parts[blockIdx.x];
-    double z = 0;
-    float p = 0.f;
-    int n = 0;
+  // the warps' sums, in their order: p and z a value to a lane (z in the sixteenth), n beside
+  double a = 0;
+  n = 0;
+  if (warp == 0 && lane <= kMostExperts) {
+    float f = 0.f;
 #pragma unroll
-    for (int w = 0; w < kLossThreads / 32; ++w) {
-      if (lane == 16) z += warps[w].z;
-      if (lane < 16) { p += warps[w].p[lane]; n += warps[w].n[lane]; }
+    for (int w = 0; w < kLossWarps; ++w) {
+      if (lane < kMostExperts) { f += warps[w].p[lane]; n += warps[w].n[lane]; }
+      else a += warps[w].z;
     }
-    if (lane == 16) out.z = z;
-    if (lane < 16) { out.p[lane] = p; out.n[lane] = n; }
+    if (lane < kMostExperts) a = f;
+    if (gridDim.x > 1) {
+      LossPart& out = parts[blockIdx.x];
+      if (lane < kMostExperts) { out.p[lane] = f; out.n[lane] = n; }
+      else out.z = a;
+    }
+  }
+  if (gridDim.x > 1) {
+    if (warp == 0) {
+      __threadfence();
+      __syncwarp();
+      if (lane == 0) last = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;      // (and back to 0 with the last one)
+    }
+    __syncthreads();
+    if (!last) return;                 // (the whole CTA)
     __threadfence();
-    __syncwarp();
-    if (lane == 0) last = atomicInc(done, gridDim.x - 1) == gridDim.x - 1;      // (and back to 0 with the last one)
-  }
-  __syncthreads();
-  if (!last) return;                   // (the whole CTA)
-  __threadfence();
-  // one expert to a lane, z in lane 16; every eighth part to a warp, then the warps' sums in their order
-  __shared__ double sums[kLossThreads / 32][17];
-  __shared__ int nums[kLossThreads / 32][16];
-  double p = 0;
-  int n = 0;
-  if (lane < 17) {
-#pragma unroll 4
-    for (int i = warp; i < (int)gridDim.x; i += kLossThreads / 32) {
-      p += lane < 16 ? (double)__ldcg(&parts[i].p[lane]) : __ldcg(&parts[i].z);
-      if (lane < 16) n += __ldcg(&parts[i].n[lane]);
+    // every eighth part to a warp, then the warps' sums in their order
+    a = 0;
+    n = 0;
+    if (lane <= kMostExperts) {
+#pragma unroll 8
+      for (int i = warp; i < (int)gridDim.x; i += kLossWarps) {
+        a += lane < kMostExperts ? (double)__ldcg(&parts[i].p[lane]) : __ldcg(&parts[i].z);
+        if (lane < kMostExperts) n += __ldcg(&parts[i].n[lane]);
+      }
+      sums[warp][lane] = a;
+      if (lane < kMostExperts) nums[warp][lane] = n;
     }
-    sums[warp][lane] = p;
-    if (lane < 16) nums[warp][lane] = n;
+    __syncthreads();
+    if (warp == 0 && lane <= kMostExperts) {
+#pragma unroll
+      for (int w = 1; w < kLossWarps; ++w) {
+        a += sums[w][lane];
+        if (lane < kMostExperts) n += nums[w][lane];
+      }
+    }
   }
-  __syncthreads();
   if (warp != 0) return;
-  if (lane < 17)
-    for (int w = 1; w < kLossThreads / 32; ++w) {
-      p += sums[w][lane];
-      if (lane < 16) n += nums[w][lane];
-    }
-  long long all = n;
+  int all = lane < kMostExperts ? n : 0;
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o, 16);
   all = __shfl_sync(0xFFFFFFFFu, all, 0);
   const double inv = all > 0 ? 1.0 / (double)all : 0.0;
-  double b = lane < 16 ? ((double)n * inv) * (p * inv) * E : 0.0;
+  double b = lane < kMostExperts ? ((double)n * inv) * (a * inv) * E : 0.0;
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) b += __shfl_xor_sync(0xFFFFFFFFu, b, o, 16);
-  const double z = __shfl_sync(0xFFFFFFFFu, p, 16) * inv;
+  const double zm = __shfl_sync(0xFFFFFFFFu, a, kMostExperts) * inv;
   if (lane < E) counts[lane] = n;
   if (lane == 0) {
-    loss[0] = (float)((double)cb * b + (double)cz * z);
+    loss[0] = (float)((double)cb * b + (double)cz * zm);
     loss[1] = (float)b;
-    loss[2] = (float)z;
+    loss[2] = (float)zm;
   }
 }
 
