@@ -189,6 +189,17 @@ struct NormBwdArgs {
   int D, tpr;
 };
 
+// Eight elements of dX: of dY, S, gamma and dS, with the row's r and its mean of q n.
+__device__ __forceinline__ uint4 row_gradient(const uint4& d, const uint4& x, const uint4& w, const uint4& e, float r, float m) {
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t dw = word(d, i), xw = word(x, i), ww = word(w, i), ew = word(e, i);
+    o[i] = pack2(fmaf(r, fmaf(-lo32(xw) * r, m, lo32(dw) * lo32(ww)), lo32(ew)), fmaf(r, fmaf(-hi32(xw) * r, m, hi32(dw) * hi32(ww)), hi32(ew)));
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
 __device__ __forceinline__ void copy_async(uint32_t saddr, const uint4* p) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(saddr), "l"(p) : "memory");
 }
@@ -280,13 +291,7 @@ rmsnorm_bwd_kernel(const NormBwdArgs a) {
         if (!here || c >= vecs) continue;
         const uint4 d = mine[j * blockDim.x], x = mine[(V + j) * blockDim.x],
                     e = adds ? mine[(2 * V + j) * blockDim.x] : make_uint4(0u, 0u, 0u, 0u);
-        uint32_t o[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t dw = word(d, i), xw = word(x, i), ww = word(w[j], i), ew = word(e, i);
-          o[i] = pack2(fmaf(r, fmaf(-lo32(xw) * r, m, lo32(dw) * lo32(ww)), lo32(ew)), fmaf(r, fmaf(-hi32(xw) * r, m, hi32(dw) * hi32(ww)), hi32(ew)));
-        }
-        out[c] = make_uint4(o[0], o[1], o[2], o[3]);
+        out[c] = row_gradient(d, x, w[j], e, r, m);
       }
     }
     r = r_next;
@@ -330,6 +335,103 @@ rmsnorm_bwd_kernel(const NormBwdArgs a) {
   }
 }
 
+// Both gradients of a short batch in one launch. dgamma needs no sum along a row, only r, so the first CTAs take 32 columns of all rows each and the
+// others the rows; dY and S are read twice, the second time from the L2. 8 x 4096: 2.6 us; 1999 x 1408: 6.7, 3.4 TB/s of what HBM would have to
+// move. (Two CTAs of 512 threads to an SM: with the registers for one 2000 x 4096 took 17.5 us instead of 14.4.)
+constexpr int kOnceCols = 32, kOnceRows = 2;
+template <int V>
+__global__ void __launch_bounds__(512, 2)
+rmsnorm_bwd_once_kernel(const NormBwdArgs a, int col_ctas) {
+  __shared__ float shared[8 * 128];    // columns: 32 of up to 16 warps; rows: as in the other kernels
+  const int threads = (int)blockDim.x;
+  pdl_wait();
+  pdl_trigger();
+  if ((int)blockIdx.x < col_ctas) {
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, c = (int)blockIdx.x * (kOnceCols / 8) + (lane & 3);
+    float dg[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[i] = 0.f;
+    if (c < a.D >> 3) {
+      const int64_t step = threads >> 2;
+      for (int64_t t = threadIdx.x >> 2; t < a.T; t += kOnceRows * step) {
+        uint4 d[kOnceRows], x[kOnceRows];
+        float r[kOnceRows];
+#pragma unroll
+        for (int k = 0; k < kOnceRows; ++k) {
+          const int64_t u = t + k * step;
+          d[k] = x[k] = make_uint4(0u, 0u, 0u, 0u);
+          r[k] = 0.f;
+          if (u < a.T) {
+            d[k] = __ldg(reinterpret_cast<const uint4*>(a.dY + u * a.D) + c);
+            x[k] = __ldg(reinterpret_cast<const uint4*>(a.S + u * a.D) + c);
+            r[k] = __ldg(a.rstd + u);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kOnceRows; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            dg[2 * i] = fmaf(lo32(word(d[k], i)), lo32(word(x[k], i)) * r[k], dg[2 * i]);
+            dg[2 * i + 1] = fmaf(hi32(word(d[k], i)), hi32(word(x[k], i)) * r[k], dg[2 * i + 1]);
+          }
+      }
+    }
+    // eight rows of a warp, then the warps in their order
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int o = 16; o >= 4; o >>= 1) dg[i] += __shfl_xor_sync(0xFFFFFFFFu, dg[i], o);
+      if (lane < 4) shared[warp * kOnceCols + lane * 8 + i] = dg[i];
+    }
+    __syncthreads();
+    const int col = (int)blockIdx.x * kOnceCols + (int)threadIdx.x;
+    if (threadIdx.x >= kOnceCols || col >= a.D) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int w = 0; w < threads >> 5; ++w) s += shared[w * kOnceCols + threadIdx.x];
+    a.dgamma[col] = float_to_bf16_bits(s);
+    return;
+  }
+  Group g;
+  g.index = (int)threadIdx.x / a.tpr;
+  g.lane = (int)threadIdx.x - g.index * a.tpr;
+  g.size = a.tpr;
+  g.slots = shared + (a.tpr > 32 ? g.index : 0) * 128;
+  g.turn = 0;
+  const int64_t row = (int64_t)((int)blockIdx.x - col_ctas) * (threads / a.tpr) + g.index;
+  const bool here = row < a.T;
+  const int vecs = here ? a.D >> 3 : 0;
+  const uint4 *dy = reinterpret_cast<const uint4*>(a.dY + row * a.D), *s = reinterpret_cast<const uint4*>(a.S + row * a.D),
+              *ds = reinterpret_cast<const uint4*>(a.dS + row * a.D), *gamma = reinterpret_cast<const uint4*>(a.gamma);
+  const float r = here ? __ldg(a.rstd + row) : 0.f;
+  uint4 d[V], x[V], e[V], w[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int c = g.lane + j * a.tpr;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    d[j] = c < vecs ? __ldg(dy + c) : zero;
+    x[j] = c < vecs ? __ldg(s + c) : zero;
+    w[j] = c < vecs ? __ldg(gamma + c) : zero;
+    e[j] = c < vecs && a.dS ? load_once(ds + c) : zero;
+  }
+  float c1 = 0.f, none = 0.f;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      c1 = fmaf(lo32(word(d[j], i)) * (lo32(word(x[j], i)) * r), lo32(word(w[j], i)), c1);
+      c1 = fmaf(hi32(word(d[j], i)) * (hi32(word(x[j], i)) * r), hi32(word(w[j], i)), c1);
+    }
+  g.reduce<false>(c1, none);
+  const float m = c1 * (1.f / (float)a.D);
+  uint4* out = reinterpret_cast<uint4*>(a.dX + row * a.D);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int c = g.lane + j * a.tpr;
+    if (c < vecs) out[c] = row_gradient(d[j], x[j], w[j], e[j], r, m);
+  }
+}
+
 // Vectors of a row to a thread, and threads to a row. Few rows: as many threads as there are vectors, for latency. Many: several vectors,
 // whose loads are under way at once, and as many rows to an SM. Rows of less than a warp's 32 vectors share it.
 struct RowPlan { int v, tpr; };
@@ -342,11 +444,22 @@ RowPlan fwd_plan(int64_t T, int64_t D) {
 }
 // Backward: up to 512 threads to a row, of one, two or four vectors each; a row of more than 16384 elements takes up to 1024. Four vectors make
 // more rows of a CTA and fewer barriers a byte, two start and end sooner: 2 / 4 vectors, us: 16384 x 4096 91.4 / 84.3, 4096 x 8192 51.6 / 46.9, 8192 x 4096
-// 49.3 / 47.1; 8192 x 2048 27.8 / 28.5, 2000 x 4096 15.4 / 15.9, 1000 x 1408 7.7 / 8.3.
+// 49.3 / 47.1; 8192 x 2048 27.8 / 28.5.
 RowPlan bwd_plan(int64_t T, int64_t D) {
   const int vecs = (int)(D / 8);
   if (vecs <= 32) return RowPlan{1, vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32};
-  const int v = T <= kBwdCtas && vecs <= 512 ? 1 : vecs > 1024 || (vecs >= 512 && T >= 4096) ? 4 : 2;
+  const int v = vecs > 1024 || (vecs >= 512 && T >= 4096) ? 4 : 2;
+  return RowPlan{v, whole_warps((vecs + v - 1) / v)};
+}
+
+// Up to where one launch does: as long as what its two kinds of CTAs read twice comes from the L2 the second time and a column's rows are not
+// many. Two launches / one, us in graph replay: 8 x 4096 4.6 / 2.6, 300 x 8192 10.3 / 6.7, 1999 x 1408 9.2 / 6.7, 4096 x 1408 13.4 / 11.3, 2000 x 4096
+// 15.4 / 14.4, 2000 x 64 4.6 / 4.6; 4096 x 4096 28.5 / 29.2, 2000 x 8192 30.0 / 30.0, 4096 x 512 7.7 / 9.8, 128 x 16384 10.8 / 10.8.
+bool bwd_once(int64_t T, int64_t D) { return D <= 8192 && T * D <= (int64_t)1 << 23 && (T <= 2048 || T <= 3 * D); }
+RowPlan once_plan(int64_t T, int64_t D) {
+  const int vecs = (int)(D / 8);
+  if (vecs <= 32) return RowPlan{1, vecs <= 8 ? 8 : vecs <= 16 ? 16 : 32};
+  const int v = vecs <= 64 || (T <= sm_count_now() && vecs <= 512) ? 1 : 2;
   return RowPlan{v, whole_warps((vecs + v - 1) / v)};
 }
 
@@ -420,15 +533,28 @@ int sf_rmsnorm_bwd(const void* dY, const void* sum, const void* gamma, const voi
       !apart({{dgamma, d2}, parts}, {{dY, td}, {dS, td}}))
     return SF_ERR_UNSUPPORTED;
   SF_TRY(check_arch());
+  NormBwdArgs a{};
+  a.dY = (const uint16_t*)dY; a.S = (const uint16_t*)sum; a.gamma = (const uint16_t*)gamma; a.dS = (const uint16_t*)dS; a.rstd = (const float*)rstd;
+  a.T = T; a.dX = (uint16_t*)dX; a.dgamma = (uint16_t*)dgamma; a.parts = (float*)workspace; a.D = (int)D;
+  if (bwd_once(T, D)) {
+    const RowPlan p = once_plan(T, D);
+    const int most = T > kBwdCtas ? 512 : 256, groups = p.tpr >= most ? 1 : most / p.tpr;
+    const int64_t cols = dgamma ? (D + kOnceCols - 1) / kOnceCols : 0, rows = dX ? (T + groups - 1) / groups : 0;      // CTAs
+    a.tpr = p.tpr;
+    auto launch = [&](int64_t c, int64_t r) {
+      return launch_pdl(p.v == 1 ? rmsnorm_bwd_once_kernel<1> : rmsnorm_bwd_once_kernel<2>, dim3((unsigned)(c + r)), (unsigned)(groups * p.tpr), 0, s, a, (int)c);
+    };
+    if (dX != dY || !cols) return launch(cols, rows);
+    SF_TRY(launch(cols, 0));                               // the columns' sums first: dX takes dY's place
+    return launch(0, rows);
+  }
   const RowPlan p = bwd_plan(T, D);
   const int ctas = bwd_ctas(T);
   const int64_t rows = (T + ctas - 1) / ctas;              // of a CTA
   int groups = p.tpr > 512 ? 1 : 512 / p.tpr;
   if (groups > rows) groups = (int)rows;
   while (groups * p.tpr % 32) ++groups;                    // whole warps
-  NormBwdArgs a{};
-  a.dY = (const uint16_t*)dY; a.S = (const uint16_t*)sum; a.gamma = (const uint16_t*)gamma; a.dS = (const uint16_t*)dS; a.rstd = (const float*)rstd;
-  a.T = T; a.dX = (uint16_t*)dX; a.dgamma = (uint16_t*)dgamma; a.parts = (float*)workspace; a.D = (int)D; a.tpr = p.tpr;
+  a.tpr = p.tpr;
   const int threads = groups * p.tpr, stages = p.v == 1 ? 4 : p.v == 2 ? 3 : threads > 512 ? 1 : 2;
   const size_t smem = (size_t)stages * 3 * p.v * threads * 16;
   auto kern = p.v == 1 ? rmsnorm_bwd_kernel<1, 4> : p.v == 2 ? rmsnorm_bwd_kernel<2, 3> : stages == 2 ? rmsnorm_bwd_kernel<4, 2> : rmsnorm_bwd_kernel<4, 1>;

@@ -16,6 +16,8 @@ BF, U16, F32E = torch.bfloat16, 2.0 ** -8, 2.0 ** -16
 
 SHAPES = [(1, 8), (1, 4096), (2, 1032), (5, 64), (3, 32768), (149, 256), (150, 264), (300, 512), (333, 1024), (1000, 1408), (160, 4104),
           (160, 8192), (150, 16384), (152, 32760), (4100, 4104)]
+# and of the backward pass: short batches, which one launch takes, and the first ones that take two
+BACKWARD = [(148, 1408), (149, 1408), (2048, 8), (2049, 8), (6000, 40), (2049, 264), (2500, 520), (3097, 1032), (1024, 8192), (1025, 8192), (3, 8200), (1, 8200)]
 
 
 def _case(T, D, seed=0):
@@ -73,6 +75,28 @@ def test_forward_and_backward(T, D):
     assert torch.equal(again_x, out["dX"].t) and torch.equal(again_g, dg.t)
     for g in [*out.values(), rstd, dg, codes, scales, ws]:
         g.check()
+
+
+@pytest.mark.parametrize("T,D", BACKWARD)
+def test_backward_of_short_and_long_batches(T, D):
+    _, S, gamma, dY, dS = _case(T, D, 6)
+    rstd = np.random.default_rng(T).uniform(0.1, 3, size=(T, 1)).astype(np.float32).astype(np.float64)
+    dX, dgamma = around.rmsnorm_bwd(dY, S, rstd, gamma, dS)
+    sd, G, r, dx, dg = _dev(S), _dev(gamma), torch.from_numpy(rstd[:, 0].astype(np.float32)).cuda(), Guarded((T, D), BF), Guarded((D,), BF)
+    b.sf_rmsnorm_bwd(_dev(dY), sd, G, r, dS=_dev(dS), dX=dx.t, dgamma=dg.t)
+    # bounds as above
+    n, q = S * rstd, dY * gamma
+    size = np.abs(dS) + rstd * (np.abs(q) + np.abs(n) * np.mean(np.abs(q * n), axis=1, keepdims=True))
+    _near(dx.t, dX, U16 * np.abs(dX) + 2 * F32E * size)
+    _near(dg.t, dgamma, U16 * np.abs(dgamma) + (T / 296 + 64) * 2.0 ** -23 * np.sum(np.abs(dY * n), axis=0))
+    # one of the two alone, and in place: the same bits
+    alone = b.sf_rmsnorm_bwd(_dev(dY), sd, G, r, dS=_dev(dS), dX=torch.empty_like(sd))[0]
+    dgs = b.sf_rmsnorm_bwd(_dev(dY), sd, G, r, dgamma=torch.empty_like(G))[1]
+    place = _dev(dY)
+    both = b.sf_rmsnorm_bwd(place, sd, G, r, dS=_dev(dS), dX=place, dgamma=torch.empty_like(G))[1]
+    assert torch.equal(alone, dx.t) and torch.equal(place, dx.t) and torch.equal(dgs, dg.t) and torch.equal(both, dg.t)
+    dx.check()
+    dg.check()
 
 
 @pytest.mark.parametrize("T,D", [(3, 264), (200, 1408)])
