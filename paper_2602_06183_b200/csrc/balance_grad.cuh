@@ -48,6 +48,7 @@ struct BalanceArgs {
   const float* dloss;
   const uint16_t* means;
   float* parts;                        // [gridDim.y][E][D]
+  uint16_t* dmeans;                    // instead of parts: the runs of a slab are a cluster, which adds them up itself
   int* status;
   int64_t T, rows;                     // rows: tokens of a CTA, a multiple of kTile
   int D, E;
@@ -82,6 +83,13 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t saddr, uint32_t (&v)[
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Four floats of shared memory of the cluster's CTA `rank`, at this CTA's address `saddr`.
+__device__ __forceinline__ float4 ld_cluster(uint32_t saddr, uint32_t rank) {
+  float4 v;
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, %5;\n\tld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n\t}\n"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(saddr), "r"(rank) : "memory");
+  return v;
 }
 // Where the half `h` (8 experts) of a token's dl lies: neighbouring rows of 32 bytes, halves exchanged in every other four rows, so that eight
 // rows of a half touch all banks once.
@@ -254,6 +262,32 @@ balance_grad_kernel(const __grid_constant__ BalanceMaps maps, const BalanceArgs 
       }
     }
     __syncwarp();
+  }
+  if (a.dmeans) {
+    if (lane == 0) bulk_wait_all();
+    __syncwarp();
+    // [16 experts][64 columns] of the warp, in its ring's place
+    if (works) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<float2*>(ring + ((lane >> 2) + h * 8) * 256 + (j * 8 + (lane & 3) * 2) * 4) = make_float2(dm[j][2 * h], dm[j][2 * h + 1]);
+    }
+    cluster_sync_all();
+    const int runs = (int)gridDim.y;
+    for (int i = (int)blockIdx.y * 32 * kWarps + (int)threadIdx.x; i < a.E * (kSlab / 4); i += runs * 32 * kWarps) {
+      const int e = i / (kSlab / 4), c = i % (kSlab / 4) * 4, to = (int)blockIdx.x * kSlab + c;
+      if (to >= a.D) continue;
+      const uint32_t from = smem_u32(smem) + (uint32_t)((c >> 6) * kRing * 2 * kTileBytes + e * 256 + (c & 63) * 4);
+      float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < runs; ++k) {
+        const float4 v = ld_cluster(from, (uint32_t)k);
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+      *reinterpret_cast<uint2*>(a.dmeans + (int64_t)e * a.D + to) = make_uint2(pack2(s.x, s.y), pack2(s.z, s.w));
+    }
+    cluster_sync_all();                // (the others have read this CTA's sums)
   }
   if (a.parts && works && ok) {
 #pragma unroll

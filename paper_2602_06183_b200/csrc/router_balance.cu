@@ -8,7 +8,7 @@
 //
 // Forward: 4 E + 4 bytes a token, one launch; the CTA that finishes last adds up what the others left (one token
 // 2.6 us, 16384 of 16 experts 5.7, a million 27.9 in graph replay). Backward: 6 bytes an element of X
-// (X and dX_in in, dX out) and 4 T D E flops, one launch and one that adds up the CTAs' partial sums of dmeans.
+// (X and dX_in in, dX out) and 4 T D E flops, one launch and one that adds up the CTAs' partial sums of dmeans (short batches: one).
 //
 // Memory bounds the backward pass only if the products stay out of its way: as float32 multiply-adds they took 417 us where the bytes take 62 (16384
 // tokens, D 4096, E 16; now 72 alone, 5.6 TB/s, both calls 85). Sixteen experts are one side of a warp's m16n8k16 product, so both run there: dX = dl means with the means'
@@ -159,6 +159,14 @@ int64_t balance_runs(int64_t T, int64_t D) {
   return runs < tiles ? runs : tiles;
 }
 
+// Short batches, of a tile to a run: the runs of a slab are a cluster, which adds up its sums itself, and one launch is all. Two launches / one, us, from the
+// host (in graph replay), E 5: 33 x 1408 11.5 / 9.6 (7.2 / 7.2), 256 x 4096 11.4 / 9.3 (7.7 / 7.7), 100 x 8192 11.5 / 9.5 (8.2 / 7.7). Two tiles to a run cost
+// more than the launch: 400 x 4096 7.7 / 9.2 in graph replay; and so do clusters that do not all fit at once (256 x 8192, sixteen of eight CTAs: 8.7 / 14.4).
+bool balance_joins(int64_t T, int64_t D) {
+  const int64_t tiles = (T + kTile - 1) / kTile, slabs = (D + kSlab - 1) / kSlab;
+  return tiles == 1 || (tiles <= 8 && tiles * slabs <= 64);
+}
+
 int balance_shape(int64_t T, int64_t D, int E) {
   return T < 0 || T > kMostTokens || D <= 0 || D % 8 || D > kMostCols || E < 1 || E > kMostExperts ? SF_ERR_SHAPE : SF_OK;
 }
@@ -223,10 +231,12 @@ int sf_router_balance_bwd(const void* logits, const void* expert, const void* co
   BalanceArgs a{};
   a.logits = (const float*)logits; a.expert = (const int*)expert; a.counts = (const int*)counts; a.dloss = (const float*)dloss;
   a.means = (const uint16_t*)means;
-  a.parts = dmeans ? (float*)((uint8_t*)workspace + kHead) : nullptr;
   a.status = (int*)workspace;
   a.adds = dX && dX_in; a.writes = dX != nullptr;
   a.T = T; a.D = (int)D; a.E = E; a.cb = balance_coef; a.cz = z_coef;
+  const bool joins = dmeans && balance_joins(T, D);
+  a.parts = dmeans && !joins ? (float*)((uint8_t*)workspace + kHead) : nullptr;
+  a.dmeans = joins ? (uint16_t*)dmeans : nullptr;
   int64_t runs = balance_runs(T, D);
   a.rows = ((T + runs - 1) / runs + kTile - 1) / kTile * kTile;
   runs = (T + a.rows - 1) / a.rows;
@@ -241,8 +251,21 @@ int sf_router_balance_bwd(const void* logits, const void* expert, const void* co
     SF_CUDA_TRY(cudaFuncSetAttribute(balance_grad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kGradSmem));
     if (dev >= 0 && dev < 64) attr_done[dev] = true;
   }
-  SF_TRY(launch_pdl(balance_grad_kernel, dim3((unsigned)((D + kSlab - 1) / kSlab), (unsigned)runs), 32 * kWarps, (size_t)kGradSmem, s, maps, a));
-  if (!dmeans) return SF_OK;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((D + kSlab - 1) / kSlab), (unsigned)runs);
+  cfg.blockDim = dim3(32 * kWarps);
+  cfg.dynamicSmemBytes = kGradSmem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = attr[1].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.y = joins ? (unsigned)runs : 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  SF_CUDA_TRY(cudaLaunchKernelEx(&cfg, balance_grad_kernel, maps, a));
+  if (!dmeans || joins) return SF_OK;
   return launch_sum_parts(a.parts, (int)runs, (int64_t)E * D, dmeans, s);
 }
 

@@ -70,7 +70,9 @@ def test_every_number_of_experts(E):
     _check(X, means, logits, expert, 0.02, 0.003, dX_in=around.rne_bf16(r.normal(size=X.shape) * 1e-4), dloss=3.0)
 
 
-@pytest.mark.parametrize("T,D", [(1, 8), (3, 1032), (31, 64), (32, 72), (33, 512), (255, 520), (257, 1408), (2000, 256), (5000, 4096), (40000, 24)])
+@pytest.mark.parametrize("T,D", [(1, 8), (3, 1032), (31, 64), (32, 72), (33, 512), (255, 520), (257, 1408), (2000, 256), (5000, 4096), (40000, 24),
+                                 # one launch up to eight tiles of 32 tokens and 64 CTAs, and two beyond
+                                 (256, 520), (224, 1024), (256, 4096), (256, 4104), (160, 6144), (40, 16384), (2, 80000)])
 def test_sizes(T, D):
     X, means, logits, expert, r = _case(T, D, 6)
     dX, dm = _check(X, means, logits, expert, 0.02, 0.003)
@@ -87,6 +89,12 @@ def test_sizes(T, D):
     want = b.sf_router_balance_bwd(L, ex, n, 0.02, 0.003, _dev(X), _dev(means), dX_in=add, dX=x)[0].clone()
     b.sf_router_balance_bwd(L, ex, n, 0.02, 0.003, _dev(X), _dev(means), dX_in=add, dX=add)
     assert torch.equal(add, want)
+
+
+@pytest.mark.parametrize("E", [1, 2, 7, 13, 16])
+def test_every_number_of_experts_of_a_short_batch(E):
+    X, means, logits, expert, r = _case(200, 584, E)
+    _check(X, means, logits, expert, 0.02, 0.003, dX_in=around.rne_bf16(r.normal(size=X.shape) * 1e-4), dloss=3.0)
 
 
 def test_tokens_that_are_left_out_may_hold_anything():
