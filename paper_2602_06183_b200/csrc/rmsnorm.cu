@@ -409,7 +409,7 @@ rmsnorm_bwd_once_kernel(const NormBwdArgs a, int col_ctas) {
   for (int j = 0; j < V; ++j) {
     const int c = g.lane + j * a.tpr;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    d[j] = c < vecs ? __ldg(dy + c) : zero;
+    d[j] = c < vecs ? load_once(dy + c) : zero;            // (dX may take its place, or dS's)
     x[j] = c < vecs ? __ldg(s + c) : zero;
     w[j] = c < vecs ? __ldg(gamma + c) : zero;
     e[j] = c < vecs && a.dS ? load_once(ds + c) : zero;
