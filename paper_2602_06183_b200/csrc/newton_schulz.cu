@@ -42,7 +42,7 @@ struct NsShape {
 // Several steps at once save 6 m^2 (n - m) flops and the passes over X, and cost six more products of the small side, which halves of tiles and
 // single rounds leave half used; with fewer rows they are launches, and the passes count. Single steps / three and two at once, us:
 // 512 x 4096 119 / 125, 512 x 9000 173 / 149; 1024 x 4096 194 / 215, 1024 x 8192 252 / 242; 1400 x 5600 320 / 335, 1400 x 11200
-// 467 / 399; 2048 x 3072 277 / 288, 2048 x 6144 423 / 345; 3000 x 4500 965 / 970, 3000 x 9000 1611 / 1243; 4096 x 4096 1189 / 1336, 4096 x 6144 1615 / 1526,
+// 467 / 399; 2048 x 6144 423 / 345; 3000 x 4500 965 / 970, 3000 x 9000 1611 / 1243; 4096 x 4096 1189 / 1336, 4096 x 6144 1615 / 1526,
 // 4096 x 16384 3844 / 2219.
 // Below 512 rows fewer and larger eigenvalues share the roundings, and single steps it is: the error before the last rounding was 0.04 % for single
 // steps and 0.35 % for three and two at once at 10 rows, 0.05 and 0.22 at 64, 0.05 and 0.12 at 512 (64 x 9000 would take 92 us in place of 109).
