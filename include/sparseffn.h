@@ -422,7 +422,8 @@ SF_API int sf_gemm_fp4_gated(const void* A, const void* a_scales, const void* Bg
  *       sum    bf16 [T, D]   S. May be `residual` itself, or X (with ldx == D)
  *       Y      bf16 [T, D]   y
  *       codes  uint8 [T, D]  y as E4M3 codes. With scales (float32 [T]): scales[t] = top / 448, top = max(the row's largest |y|, 2^-96), code =
- *                            e4m3(y * (448 / top)), for sf_gemm_fp8_rows. With scales NULL: code = e4m3(y * scale), as sf_fp8_quantize
+ *                            e4m3(y * (448 / top)), for sf_gemm_fp8_rows; above 2^-96 r falls out of it, and the code is exactly that of
+ *                            448 S gamma / max |S gamma|, ties to even. With scales NULL: code = e4m3(y * scale), as sf_fp8_quantize
  *       rstd   float32 [T]   r, for the backward pass
  *     The squares are summed in float32. An infinity makes its own element NaN and the others of its row 0, a NaN its whole row; the scale
  *     of a row with either is NaN, and so are its codes.

@@ -6,7 +6,7 @@
 //
 // Memory bounds them: 8 bytes an element forward (7 with codes) and 8 backward. A row stays in the registers of one group of threads from
 // its load to its store; the only thing that crosses warps is a row's sum. 16384 x 4096: forward 82 us (6.6 TB/s), backward 84 (6.4 TB/s) with the sum of dgamma's parts,
-// each alone. 8192 x 4096 to E4M3 rows 39.5 (5.9 TB/s). One row of 4096: 4.1, a launch.
+// each alone. 8192 x 4096 to E4M3 rows 41 (5.7 TB/s). One row of 4096: 4.1, a launch.
 #include "fp8_fmt.cuh"
 #include "gated.cuh"
 #include "sums.cuh"
@@ -70,6 +70,12 @@ struct Group {
   }
 };
 
+// The nearest number of 22 bits (Veltkamp's splitting).
+__device__ __forceinline__ float to_22_bits(float q) {
+  const float c = __fmul_rn(q, 5.f);
+  return __fsub_rn(c, __fsub_rn(c, q));
+}
+
 struct NormArgs {
   const uint16_t *X, *R, *gamma;
   int64_t ldx, T;
@@ -82,11 +88,59 @@ struct NormArgs {
 
 // Smallest magnitude that a row's scale is made for: a row of zeros has codes of 0 and a scale that is not 0.
 constexpr float kLeastAmax = 1.2621774483536189e-29f;      // 2^-96
+// A row's largest |S gamma|, down to which it is exact in float32, and so are those of 2^-10 of it, which have the last codes.
+constexpr float kLeastProduct = 7.888609052210118e-31f;    // 2^-100
+
+// A row's own scale takes its largest |y| to 448, and a code is that of 448 S gamma / max |S gamma|: r falls out. S gamma has 16 bits, 448 times it 19, so
+// a quotient that is not half-way between two codes (five bits) is 2^-21 of it away at least. As S gamma times the rounded inverse it is off by 2^-23 of
+// it; rounded to 22 bits, what is half-way is exactly that again, and goes to the even code. (7 in 100 000 of normal rows are. As y * (448 / top), rounded
+// three times, the last bit decided; divided instead, 8192 x 4096 took 51.4 us.) top: the largest |S gamma|. Returns the inverse.
+__device__ __forceinline__ float row_scale(float r, float top, float* to) {
+  const float y_top = max_nan(top * r, kLeastAmax), scale = __fdiv_rn(y_top, 448.f);
+  if (to) *to = scale;
+  return y_top > kLeastAmax ? __fdiv_rn(448.f, top) : __fdiv_rn(r, scale);        // (or NaN)
+}
+__device__ __forceinline__ uint2 row_codes(const uint4& s, const uint4& w, float inv) {
+  uint32_t b[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    b[i] = e4m3x2(to_22_bits(lo32(word(s, i)) * lo32(word(w, i)) * inv), to_22_bits(hi32(word(s, i)) * hi32(word(w, i)) * inv));
+  return make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
+}
+__device__ __forceinline__ uint4 sum_of(const uint4& s, const uint4& t) {
+  return make_uint4(pack2(lo32(s.x) + lo32(t.x), hi32(s.x) + hi32(t.x)), pack2(lo32(s.y) + lo32(t.y), hi32(s.y) + hi32(t.y)),
+                    pack2(lo32(s.z) + lo32(t.z), hi32(s.z) + hi32(t.z)), pack2(lo32(s.w) + lo32(t.w), hi32(s.w) + hi32(t.w)));
+}
+// The same once more for the rows of a warp, or of a group of several, of which one (far) has a |S gamma| that leaves float32's range or comes near its
+// lower end: S is taken times a power of two near r. It is rare, so it reads S again, and is not inlined: 8192 x 4096 took 45.3 us with S kept for
+// it, 42.8 so, 42.2 with nothing of it.
+__device__ __noinline__ void far_row(const NormArgs* a, Group g, int64_t row, int vecs, float r, bool far) {
+  const uint4 *x = reinterpret_cast<const uint4*>(a->sum ? a->sum + row * a->D : a->X + row * a->ldx),
+              *t = reinterpret_cast<const uint4*>(a->R + row * a->D), *gamma = reinterpret_cast<const uint4*>(a->gamma);
+  const bool adds = !a->sum && a->R;
+  const float p = far && r > 0.f && r < INFINITY ? __uint_as_float(__float_as_uint(r) & 0x7F800000u) : 1.f;
+  auto scaled = [&](int c) {
+    uint4 s = load_once(x + c);
+    if (adds) s = sum_of(s, load_once(t + c));
+    return make_uint4(pack2(lo32(s.x) * p, hi32(s.x) * p), pack2(lo32(s.y) * p, hi32(s.y) * p), pack2(lo32(s.z) * p, hi32(s.z) * p),
+                      pack2(lo32(s.w) * p, hi32(s.w) * p));
+  };
+  float top = 0.f, none = 0.f;
+  for (int c = g.lane; c < vecs; c += g.size) {
+    const uint4 s = scaled(c), w = __ldg(gamma + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      top = max_nan(top, max_nan(fabsf(lo32(word(s, i)) * lo32(word(w, i))), fabsf(hi32(word(s, i)) * hi32(word(w, i)))));
+  }
+  g.reduce<true>(none, top);
+  const float inv = row_scale(r / p, top, vecs && g.lane == 0 ? a->scales + row : nullptr);
+  for (int c = g.lane; c < vecs; c += g.size) reinterpret_cast<uint2*>(a->codes + row * a->D)[c] = row_codes(scaled(c), __ldg(gamma + c), inv);
+}
 
 // kRows: codes with a scale to every row.
 template <int V, bool kRows>
 __global__ void __launch_bounds__(1024)
-rmsnorm_kernel(const NormArgs a) {
+rmsnorm_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float slots[4][128];       // (of groups of more than a warp)
   Group g;
   g.index = (int)threadIdx.x / a.tpr;
@@ -117,12 +171,7 @@ rmsnorm_kernel(const NormArgs a) {
         t[j] = c < vecs ? load_once(r + c) : make_uint4(0u, 0u, 0u, 0u);
       }
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        s[j].x = pack2(lo32(s[j].x) + lo32(t[j].x), hi32(s[j].x) + hi32(t[j].x));
-        s[j].y = pack2(lo32(s[j].y) + lo32(t[j].y), hi32(s[j].y) + hi32(t[j].y));
-        s[j].z = pack2(lo32(s[j].z) + lo32(t[j].z), hi32(s[j].z) + hi32(t[j].z));
-        s[j].w = pack2(lo32(s[j].w) + lo32(t[j].w), hi32(s[j].w) + hi32(t[j].w));
-      }
+      for (int j = 0; j < V; ++j) s[j] = sum_of(s[j], t[j]);
     }
   }
   if (a.sum) {
@@ -152,29 +201,48 @@ rmsnorm_kernel(const NormArgs a) {
     l = lo32(word(v, i)) * rstd * lo32(word(w, i));
     h = hi32(word(v, i)) * rstd * hi32(word(w, i));
   };
-  float inv = a.scale;
-  if (kRows) {                         // a row's own scale: its largest magnitude becomes 448
-    top = max_nan(top * rstd, kLeastAmax);
-    inv = __fdiv_rn(448.f, top);
-    if (here && g.lane == 0) a.scales[row] = __fdiv_rn(top, 448.f);
-  }
-  uint4* y = reinterpret_cast<uint4*>(a.Y + row * a.D);
-  uint2* q = reinterpret_cast<uint2*>(a.codes + row * a.D);
+  if (a.Y) {
+    uint4* y = reinterpret_cast<uint4*>(a.Y + row * a.D);
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int c = g.lane + j * a.tpr;
-    if (c >= vecs) continue;
-    const uint4 w = __ldg(gamma + c);
-    uint32_t o[4], b[4];
+    for (int j = 0; j < V; ++j) {
+      const int c = g.lane + j * a.tpr;
+      if (c >= vecs) continue;
+      const uint4 w = __ldg(gamma + c);
+      uint32_t o[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float l, h;
-      normed(s[j], w, i, l, h);
-      o[i] = pack2(l, h);
-      b[i] = e4m3x2(__fmul_rn(l, inv), __fmul_rn(h, inv));
+      for (int i = 0; i < 4; ++i) {
+        float l, h;
+        normed(s[j], w, i, l, h);
+        o[i] = pack2(l, h);
+      }
+      y[c] = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    if (a.Y) y[c] = make_uint4(o[0], o[1], o[2], o[3]);
-    if (a.codes) q[c] = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
+  }
+  uint2* q = reinterpret_cast<uint2*>(a.codes + row * a.D);
+  if (kRows) {
+    const float inv = row_scale(rstd, top, here && g.lane == 0 ? a.scales + row : nullptr);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = g.lane + j * a.tpr;
+      if (c < vecs) q[c] = row_codes(s[j], __ldg(gamma + c), inv);
+    }
+    const bool far = here && !(top >= kLeastProduct && top < INFINITY);
+    if (__any_sync(0xFFFFFFFFu, far)) far_row(&a, g, row, vecs, rstd, far);
+  } else if (a.codes) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      const int c = g.lane + j * a.tpr;
+      if (c >= vecs) continue;
+      const uint4 w = __ldg(gamma + c);
+      uint32_t b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float l, h;
+        normed(s[j], w, i, l, h);
+        b[i] = e4m3x2(__fmul_rn(l, a.scale), __fmul_rn(h, a.scale));
+      }
+      q[c] = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
+    }
   }
 }
 
