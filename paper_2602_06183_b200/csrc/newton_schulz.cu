@@ -11,18 +11,19 @@
 //     float32 from both. This alone takes the error at rank 8 from 2.6 % to 0.03 %, and costs no product;
 //   - the diagonals of A and B, which are far larger than the rest, are held apart in float32 and multiplied in the epilogues:
 //     A = D + A', A^2 = D^2 + D A' + A' D + A'^2, B X = diag(B) X + B' X. A matrix of 512 x 2048: 0.3 % to 0.05 %.
-// Then the final rounding to bf16 (0.17 %) is the largest error.
+// What the roundings leave with five steps of the usual quintic: 0.02 to 0.15 % where G is of full rank, 0.3 % usually and 1 % at most where it is of low
+// rank or has rows that are copies, whose roundings are alike. The final rounding to bf16 is 0.17 %.
 //
-// Several steps at once, where X is wide: a step multiplies X by a polynomial of A, so what X becomes after g steps is Q X with Q a product of
-// polynomials of the first A, and the A of the next step is A B^2 (B = a I + b A + c A^2): all of them symmetric, of the small side, and
-// commuting. Then X is read and written once for g steps, 3 m^2 n + (4 g - 3) m^3 flops in place of 3 g m^2 n + g m^3 (m <= n; halves of the
-// symmetric products). What rounding leaves in A where it has no eigenvalue grows 11.9 times with a step, so A is made anew from X after three
-// steps, then after every two, and A is held in two terms for what is added elementwise. (Five steps at once: errors of 0.4 to 6 %.)
+// A wide matrix could take g steps at once by products of the small side: X becomes Q X, Q a product of polynomials of the first A, and the next A
+// is A B^2. Five steps of 4096 x 16384 took 2400 us so (single steps: 3980). It is not done: where G has components, a^g X is cancelled by what is held
+// in fp16, and errors were 3 to 20 times those of single steps for matrices far from full rank (equal rows 1.8 %, ten steps of copied rows
+// 5 %). Second terms of Q and of all matrices in the products mend that and cost what is saved; two steps at once in the first group only save a tenth, and
+// leave 4 % after ten steps.
 //
 // Launches: norm (partial sums in double), conversion (with the transposition of a high G), then PK_GRAM, PK_SYMM and PK_APPLY of
-// pair_product.cuh: three for a single step, 4 g - 1 for g at once. Half of the tiles of the symmetric ones are computed. Small sides of up
-// to 128 are one launch (newton_small.cuh). Five steps, back to back: 1021 x 253 97 us (17 launches, each its latency), 2048 x 2048 241 (0.71 PFLOP/s:
-// products of 11 to 19 us whose tiles take 7 to 9), 4096 x 16384 2450 (1.06 PFLOP/s of 2.6 TFLOP; 2130 in graph replay; power cap).
+// pair_product.cuh for every step. Half of the tiles of the symmetric ones are computed. Small sides of up to 128 are one launch
+// (newton_small.cuh). Five steps, back to back: 1021 x 253 97 us (17 launches, each its latency), 2048 x 2048 243 (0.71 PFLOP/s: products of 11
+// to 19 us whose tiles take 7 to 9), 4096 x 16384 3980 (1.12 PFLOP/s of 4.5 TFLOP; power cap).
 #include "newton_small.cuh"
 
 namespace sf {
@@ -34,19 +35,9 @@ constexpr int64_t kMostSide = 1 << 24, kMostSmall = 1 << 16;
 
 struct NsShape {
   int64_t m, n, ldm, ldn, mp;          // small and large side, leading dimensions, m in whole tiles
-  bool high, grouped;                  // G has more rows than columns; several steps at once
-  int matrices;                        // symmetric ones
-  size_t sums, sym[5], second, diag[5], x[4], total;      // (second: that term of the first matrix)
+  bool high;                           // G has more rows than columns
+  size_t sums, sym[2], diag[2], x[4], total;              // A and B; X and the next one, two terms each
 };
-
-// Several steps at once save 6 m^2 (n - m) flops and the passes over X, and cost six more products of the small side, which halves of tiles and
-// single rounds leave half used; with fewer rows they are launches, and the passes count. Single steps / three and two at once, us:
-// 512 x 4096 119 / 125, 512 x 9000 173 / 149; 1024 x 4096 194 / 215, 1024 x 8192 252 / 242; 1400 x 5600 320 / 335, 1400 x 11200
-// 467 / 399; 2048 x 6144 423 / 345; 3000 x 4500 965 / 970, 3000 x 9000 1611 / 1243; 4096 x 4096 1189 / 1336, 4096 x 6144 1615 / 1526,
-// 4096 x 16384 3844 / 2219.
-// Below 512 rows fewer and larger eigenvalues share the roundings, and single steps it is: the error before the last rounding was 0.04 % for single
-// steps and 0.35 % for three and two at once at 10 rows, 0.05 and 0.22 at 64, 0.05 and 0.12 at 512 (64 x 9000 would take 92 us in place of 109).
-bool ns_grouped(int64_t m, int64_t n) { return m >= 512 && (m > 1024 ? m : 1024) * (n - m) >= (int64_t)6 << 20; }
 
 int ns_shape(int64_t rows, int64_t cols, NsShape* z) {
   if (rows < 0 || cols < 0 || rows > kMostSide || cols > kMostSide) return SF_ERR_SHAPE;
@@ -58,16 +49,13 @@ int ns_shape(int64_t rows, int64_t cols, NsShape* z) {
   z->ldm = up8(z->m);
   z->ldn = up8(z->n);
   z->mp = ceil_div(z->m, 256) * 256;
-  z->grouped = ns_grouped(z->m, z->n);
-  z->matrices = z->grouped ? 5 : 2;
   size_t o = kStatus + kScalars;
   auto take = [&](size_t bytes) { const size_t r = o; o += (bytes + 255) & ~(size_t)255; return r; };
   z->sums = take(8 * kNormCtas);
-  for (int i = 0; i < z->matrices; ++i) {
+  for (int i = 0; i < 2; ++i) {
     z->sym[i] = take(2 * (size_t)z->m * (size_t)z->ldm);
     z->diag[i] = take(4 * (size_t)z->mp);
   }
-  z->second = z->grouped ? take(2 * (size_t)z->m * (size_t)z->ldm) : z->sym[0];
   for (int i = 0; i < 4; ++i) z->x[i] = take(2 * (size_t)z->m * (size_t)z->ldn);
   z->total = o;
   return SF_OK;
@@ -364,81 +352,50 @@ int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_
   p.ns.scale = scale / 16384.f;
   p.ns.transposed = z.high;
   const bool direct = aligned16(O) && ldo % 8 == 0;
-  // exponents: of A 14, of a product that is `most` at most, so that it stays below 2^15
-  auto exponent = [](double most) { return 14 - (int)std::ceil(std::log2(std::fmax(most, 1.0))); };
-  struct Sym { int at, e, two; };      // number of the matrix, exponent, whether it has two terms (the first may)
-  auto matrix = [&](const Sym& x) { return SymMatrix{(const float*)(w + z.diag[x.at]), std::ldexp(1.f, -x.e), x.two}; };
-  auto map = [&](CUtensorMap* m, const Sym& x, int term) { return make_tmap_store(m, w + (term && x.two ? z.second : z.sym[x.at]), z.m, z.m, z.ldm); };
-  auto target = [&](NsPairArgs& q, const Sym& x) {
-    q.ns.diag_out = (float*)(w + z.diag[x.at]);
-    q.ns.up = std::ldexp(1.f, x.e);
-    q.ns.two_out = x.two;
-  };
-  // out = c0 I + c1 x + c2 x y
-  auto product = [&](const Sym& x, const Sym& y, float c0, float c1, float c2, const Sym& out) {
+  // exponents: of A 14, of B so that it stays below 2^15
+  const int e_b = 14 - (int)std::ceil(std::log2(std::fmax(p_most, 1.0)));
+  uint8_t *const A = w + z.sym[0], *const B = w + z.sym[1];
+  float *const diag_a = (float*)(w + z.diag[0]), *const diag_b = (float*)(w + z.diag[1]);
+  for (int step = 0; step < steps; ++step) {
+    const uint8_t *xh = w + z.x[2 * (step & 1)], *xl = w + z.x[2 * (step & 1) + 1];
+    uint8_t *yh = w + z.x[2 * (~step & 1)], *yl = w + z.x[2 * (~step & 1) + 1];
     NsPairArgs q = p;
-    q.ns.m1 = matrix(x);
-    q.ns.m2 = matrix(y);
-    q.ns.same = x.at == y.at;
-    q.ns.c0 = c0; q.ns.c1 = c1; q.ns.c2 = c2;
-    target(q, out);
-    q.ns.down = std::ldexp(1.f, -x.e - y.e);
-    q.nkb = q.nkb0 = k_blocks(FMT_F16, z.m);
-    return launch_best<PK_SYMM, FMT_F16>(q, s, [&](CUtensorMap* m, int bn) {
-      SF_TRY(make_tmap_2d(&m[0], w + z.sym[x.at], z.m, z.m, z.ldm, 64, 128, true));
-      SF_TRY(make_tmap_2d(&m[1], w + z.sym[y.at], z.m, z.m, z.ldm, 64, bn / 2, true));
-      SF_TRY(map(&m[2], out, 0));
-      SF_TRY(map(&m[3], out, 1));
-      SF_TRY(map(&m[4], x, 0));
-      SF_TRY(map(&m[5], x, 1));
-      return map(&m[6], y, 0);
-    });
-  };
-  int groups = 0;
-  for (int done = 0; done < steps; ++groups) {
-    const int most = !z.grouped ? 1 : done == 0 ? 3 : 2, g = steps - done < most ? steps - done : most;
-    const uint8_t *xh = w + z.x[2 * (groups & 1)], *xl = w + z.x[2 * (groups & 1) + 1];
-    uint8_t *yh = w + z.x[2 * (~groups & 1)], *yl = w + z.x[2 * (~groups & 1) + 1];
-    const Sym A{0, 14, g > 1};
-    NsPairArgs q = p;
-    q.ns.first = done == 0 ? first : nullptr;
-    target(q, A);
-    q.ns.down = std::ldexp(1.f, -28);
+    q.ns.first = step == 0 ? first : nullptr;
+    q.ns.diag_out = diag_a;
+    q.ns.up = 0x1p14f;
+    q.ns.down = 0x1p-28f;
     q.nkb = q.nkb0 = k_blocks(FMT_F16, z.n);
     SF_TRY((launch_best<PK_GRAM, FMT_F16>(q, s, [&](CUtensorMap* m, int bn) {
       SF_TRY(make_tmap_2d(&m[0], xh, z.m, z.n, z.ldn, 64, 128, true));
       SF_TRY(make_tmap_2d(&m[1], xh, z.m, z.n, z.ldn, 64, bn / 2, true));
-      SF_TRY(map(&m[2], A, 0));
-      return map(&m[3], A, 1);
+      return make_tmap_store(&m[2], A, z.m, z.m, z.ldm);
     })));
-    Sym Q{-1, 0, 0};
-    double q_most = 1;
-    for (int k = 0; k < g; ++k) {
-      // matrices 1 to 3 hold B and Q in turn (with k == 2 the first B is no longer needed), 4 holds A B
-      const Sym B{k == 1 ? 2 : 1, exponent(p_most), 0}, AB{4, exponent(1.5625 * p_most), 0};
-      SF_TRY(product(A, A, a, b, c, B));
-      if (k < g - 1) {
-        SF_TRY(product(A, B, 0.f, 0.f, 1.f, AB));
-        SF_TRY(product(AB, B, 0.f, 0.f, 1.f, A));
-      }
-      q_most *= p_most;
-      const Sym next{k == 1 ? 3 : 2, exponent(q_most), 0};
-      if (k > 0) SF_TRY(product(Q, B, 0.f, 0.f, 1.f, next));
-      Q = k == 0 ? B : next;
-    }
-    done += g;
     q = p;
-    q.ns.first = groups == 0 ? first : nullptr;
-    q.ns.last = done == steps;
+    q.ns.a = a; q.ns.b = b; q.ns.c = c;
+    q.ns.diag_in = diag_a;
+    q.ns.diag_out = diag_b;
+    q.ns.up = std::ldexp(1.f, e_b);
+    q.ns.down = 0x1p-28f;
+    q.ns.down1 = 0x1p-14f;
+    q.nkb = q.nkb0 = k_blocks(FMT_F16, z.m);
+    SF_TRY((launch_best<PK_SYMM, FMT_F16>(q, s, [&](CUtensorMap* m, int bn) {
+      SF_TRY(make_tmap_2d(&m[0], A, z.m, z.m, z.ldm, 64, 128, true));
+      SF_TRY(make_tmap_2d(&m[1], A, z.m, z.m, z.ldm, 64, bn / 2, true));
+      SF_TRY(make_tmap_store(&m[2], B, z.m, z.m, z.ldm));
+      return make_tmap_store(&m[3], A, z.m, z.m, z.ldm);
+    })));
+    q = p;
+    q.ns.first = step == 0 ? first : nullptr;
+    q.ns.last = step == steps - 1;
     q.ns.out = direct ? nullptr : (uint16_t*)O;
     q.ns.ldo = ldo;
-    q.ns.two_terms = groups > 0 || f32;
-    q.ns.diag_in = (const float*)(w + z.diag[Q.at]);
-    q.ns.down = std::ldexp(1.f, -Q.e);
+    q.ns.two_terms = step > 0 || f32;
+    q.ns.diag_in = diag_b;
+    q.ns.down = std::ldexp(1.f, -e_b);
     q.N[0] = (int)z.n;
     q.nkb = q.nkb0 = k_blocks(FMT_F16, z.m);
     SF_TRY((launch_best<PK_APPLY, FMT_F16>(q, s, [&](CUtensorMap* m, int) {
-      SF_TRY(make_tmap_2d(&m[0], w + z.sym[Q.at], z.m, z.m, z.ldm, 64, 128, true));
+      SF_TRY(make_tmap_2d(&m[0], B, z.m, z.m, z.ldm, 64, 128, true));
       SF_TRY(make_tmap_2d(&m[1], xh, z.m, z.n, z.ldn, 64, 64, true));
       SF_TRY(make_tmap_store(&m[2], xh, z.m, z.n, z.ldn));
       SF_TRY(make_tmap_store(&m[3], xl, z.m, z.n, z.ldn));

@@ -13,8 +13,8 @@
 // and the three of an orthogonalised update (see newton_schulz.cu), of which the first two are symmetric: tiles on and below the
 // diagonal are computed, what lies below it is stored twice.
 //   PK_GRAM  A = X X^T                                      off the diagonal in fp16, the diagonal in float32
-//   PK_SYMM  c0 I + c1 M1 + c2 M1 M2                        of symmetric matrices that commute, the diagonals' parts in float32
-//   PK_APPLY X' = Q X                                       the diagonal's part in float32
+//   PK_SYMM  B = a I + b A + c A^2                          the same of a symmetric A, the diagonals' parts in float32
+//   PK_APPLY X' = B X                                       the diagonal's part in float32
 //
 // CTA = 10 warps: TMA producer, MMA issuer, two sets of four epilogue warps that share a tile's columns. Every wait is bounded
 // (see gemm_tc.cu): on expiry the CTA raises the status word and leaves.
@@ -65,7 +65,7 @@ struct PairCfg {
   static constexpr int kBBlocks = kBN / 128;                                     // row blocks of B's scales
   static constexpr int kScaleBytes = kTiles * 512 * (1 + kBBlocks);
   static constexpr int kStageBytes = kABytes + kBBytes + kScaleBytes;
-  static constexpr int kEpiWarpBytes = kKind == PK_SYMM ? 12288 : kWide ? 8192 : 4096;
+  static constexpr int kEpiWarpBytes = kWide ? 8192 : 4096;
   static constexpr int kRoom = (kPairSmemMax - 2048 - 8 * kEpiWarpBytes) / kStageBytes;
   static constexpr int kStages = kRoom < 8 ? kRoom : 8;
   static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kEpiWarpBytes + 1024;
@@ -75,7 +75,7 @@ struct PairCfg {
   static constexpr uint32_t kScaleACols = kTiles * 4, kScaleCols = kScaleACols * (1 + kBBlocks);    // of one stage
   static constexpr int kEpiBars = kKind == PK_APPLY || kKind == PK_SYMM ? 16 : 8;
   static constexpr int kMaps = kKind == PK_DW ? 9 : kKind == PK_DX ? 5 : kKind == PK_NT ? (kFp4 ? 5 : 3)
-                             : kKind == PK_FWD ? (kFp4 ? 7 : 4) : kKind == PK_GRAM ? 4 : kKind == PK_SYMM ? 7 : 6;
+                             : kKind == PK_FWD ? (kFp4 ? 7 : 4) : kKind == PK_GRAM ? 3 : kKind == PK_SYMM ? 4 : 6;
   static_assert(kBN == 256 || (kFp4 && kBN == 128), "tile width");
   static_assert(kMode == PM_FULL || !kFp4 || (kMode == PM_SPLIT && kBN == 128), "4-bit operands: widths of whole row blocks of scales");
   static_assert(!kFp4 || kKind == PK_NT || (kKind == PK_FWD && kBN == 256), "4-bit operands: K-major, whole row blocks of scales");
@@ -101,22 +101,15 @@ struct PairArgs {
   int beside, first_late, late_rounds;
   int* status;
 };
-// The products of an orthogonalised update. A matrix is held as a power of two times itself, in fp16, in one term or two; a symmetric one
+// The products of an orthogonalised update. A matrix is held as a power of two times itself, in fp16, X in one term or two; a symmetric one
 // without its diagonal, which is apart in float32 (see newton_schulz.cu). up: 2^e of the result; down: 2^-e of the operands together.
-struct SymMatrix {
-  const float* diag;
-  float down;                          // 2^-e
-  int two;                             // terms: the second factor has one
-};
 struct NsArgs {
   const float* first;                // the first step's X is to be multiplied by *first (NULL: 1)
-  SymMatrix m1, m2;                  // PK_SYMM: the factors
-  int same;                          // ... which are one and the same
-  float c0, c1, c2;                  // ... c0 I + c1 M1 + c2 M1 M2
-  const float* diag_in;              // PK_APPLY: the diagonal of the matrix that is applied
+  float a, b, c;                     // PK_SYMM
+  const float* diag_in;              // PK_SYMM, PK_APPLY: the diagonal of the symmetric operand
   float* diag_out;                   // PK_GRAM, PK_SYMM
   float up, down;
-  int two_out;                       // PK_GRAM, PK_SYMM: the result has two terms
+  float down1;                       // PK_SYMM: 2^-e of A
   int two_terms;                     // PK_APPLY: X has
   int last, transposed;              // PK_APPLY: the result is written as bf16 times `scale`, and as its transpose
   float scale;
@@ -272,21 +265,20 @@ __device__ __forceinline__ void column_put(uint8_t* b, int lane, const uint32_t 
   for (int i = 0; i < 32; ++i)
     *reinterpret_cast<uint16_t*>(b + i * 64 + (((lane >> 3) ^ ((i >> 1) & 3)) << 4) + (lane & 7) * 2) = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
 }
-struct NsRow { float scale, d1, d2; };
+struct NsRow { float scale, d; };
 // What a row of a tile needs (arrays are padded to whole tiles).
 template <int kKind>
 __device__ __forceinline__ NsRow ns_begin(const NsPairArgs& args, int row) {
-  NsRow r{1.f, 0.f, 0.f};
+  NsRow r{1.f, 0.f};
   if (kKind != PK_SYMM && args.ns.first) r.scale = __ldcg(args.ns.first);
-  if (kKind == PK_SYMM) { r.d1 = __ldcg(args.ns.m1.diag + row); r.d2 = __ldcg(args.ns.m2.diag + row); }
-  if (kKind == PK_APPLY) r.d1 = __ldcg(args.ns.diag_in + row);
+  if (kKind != PK_GRAM) r.d = __ldcg(args.ns.diag_in + row);
   return r;
 }
-// A chunk of 32 x 32 sums of a symmetric result, this lane's row of it: as it lies and mirrored, one term or two, to b, a half of the warp's
-// buffer, and from there to the matrix. PK_SYMM: b holds the factors' chunks (ns_fetch), and the result takes their place; dcol: the second
-// factor's diagonal at this lane's column.
+// A chunk of 32 x 32 sums of a symmetric result, this lane's row of it: as it lies and mirrored to b, a half of the warp's buffer, and from there to
+// the matrix. PK_SYMM: b holds A's chunk (ns_fetch), and the result takes its place; dcol: A's diagonal at this lane's column.
 template <int kKind>
-__device__ __forceinline__ bool ns_symmetric(const NsPairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* b, float dcol, uint64_t* loaded, uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
+__device__ __forceinline__ bool ns_symmetric(const NsPairArgs& args, const CUtensorMap* maps, const NsRow& r, uint32_t (&v)[32], uint8_t* b, float dcol,
+                                             uint64_t* loaded, uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
   const bool on_diag = row == col;
   const float up = args.ns.up;
   float d = 0.f;
@@ -299,30 +291,20 @@ __device__ __forceinline__ bool ns_symmetric(const NsPairArgs& args, const CUten
       v[i] = __float_as_uint(x * up);
     }
   } else {
-    const float c1 = args.ns.c1, c2 = args.ns.c2, down = args.ns.down, down1 = args.ns.m1.down, down2 = args.ns.m2.down;
-    const bool same = args.ns.same, two1 = args.ns.m1.two;
+    const float nb = args.ns.b, nc = args.ns.c, down = args.ns.down, down1 = args.ns.down1;
     if (!mbar_wait_warp(loaded, phase, abort_flag)) return false;
-    uint32_t h1[16], l1[16], h2[16];
-    row_get(b, lane, h1);
-    if (two1) row_get(b + 2048, lane, l1);
-    if (!same) row_get(b + 4096, lane, h2);
+    uint32_t held[16];
+    row_get(b, lane, held);
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
-      float2 x = from_f16x2(h1[q]);
-      if (two1) { const float2 y = from_f16x2(l1[q]); x.x += y.x; x.y += y.y; }
-      x.x *= down1; x.y *= down1;
-      float2 z = x;
-      if (!same) {
-        z = from_f16x2(h2[q]);
-        z.x *= down2; z.y *= down2;
-      }
-      const float a[2] = {x.x, x.y}, c[2] = {z.x, z.y};
+      const float2 h = from_f16x2(held[q]);
+      const float x[2] = {h.x * down1, h.y * down1};
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int i = 2 * q + u;
         const float p = __uint_as_float(v[i]) * down;
-        float o = fmaf(c2, fmaf(r.d1, c[u], fmaf(a[u], __shfl_sync(0xFFFFFFFFu, dcol, i), p)), c1 * a[u]);
-        if (on_diag && i == lane) { d = fmaf(c2, fmaf(r.d1, r.d2, p), fmaf(c1, r.d1, args.ns.c0)); o = 0.f; }
+        float o = fmaf(nc, fmaf(r.d, x[u], fmaf(x[u], __shfl_sync(0xFFFFFFFFu, dcol, i), p)), nb * x[u]);
+        if (on_diag && i == lane) { d = fmaf(nc, fmaf(r.d, r.d, p), fmaf(nb, r.d, args.ns.a)); o = 0.f; }
         v[i] = __float_as_uint(o * up);
       }
     }
@@ -333,31 +315,18 @@ __device__ __forceinline__ bool ns_symmetric(const NsPairArgs& args, const CUten
   uint32_t w[16];
 #pragma unroll
   for (int i = 0; i < 16; ++i) w[i] = f16x2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-  auto store = [&](const CUtensorMap* m) {
-    row_bf16(b, lane, w);
-    if (!on_diag) column_put(b + 2048, lane, w);
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      tma_store_2d(m, b, col, row);
-      if (!on_diag) tma_store_2d(m, b + 2048, row, col);
-      bulk_commit();
-    }
-  };
-  store(&maps[2]);
-  if (args.ns.two_out) {
-    if (lane == 0) bulk_wait_read<0>();
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float2 h = from_f16x2(w[i]);
-      w[i] = f16x2(__uint_as_float(v[2 * i]) - h.x, __uint_as_float(v[2 * i + 1]) - h.y);
-    }
-    store(&maps[3]);
+  row_bf16(b, lane, w);
+  if (!on_diag) column_put(b + 2048, lane, w);
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    tma_store_2d(&maps[2], b, col, row);
+    if (!on_diag) tma_store_2d(&maps[2], b + 2048, row, col);
+    bulk_commit();
   }
   return true;
 }
-// A chunk of Q X, with what ns_fetch brought to b, a half of the warp's buffer.
+// A chunk of B X, with what ns_fetch brought to b, a half of the warp's buffer.
 __device__ __forceinline__ bool ns_apply(const NsPairArgs& args, const CUtensorMap* maps, const NsRow& r, const uint32_t (&v)[32], uint8_t* b, uint64_t* loaded,
                                          uint32_t phase, volatile int* abort_flag, int col, int row, int lane) {
   if (!mbar_wait_warp(loaded, phase, abort_flag)) return false;
@@ -370,8 +339,8 @@ __device__ __forceinline__ bool ns_apply(const NsPairArgs& args, const CUtensorM
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float2 h = from_f16x2(w[i]), l = from_f16x2(lo[i]);
-    const float y0 = r.scale * fmaf(r.d1, h.x + l.x, __uint_as_float(v[2 * i]) * args.ns.down);
-    const float y1 = r.scale * fmaf(r.d1, h.y + l.y, __uint_as_float(v[2 * i + 1]) * args.ns.down);
+    const float y0 = r.scale * fmaf(r.d, h.x + l.x, __uint_as_float(v[2 * i]) * args.ns.down);
+    const float y1 = r.scale * fmaf(r.d, h.y + l.y, __uint_as_float(v[2 * i + 1]) * args.ns.down);
     if (args.ns.last) {
       w[i] = bf16x2(y0 * args.ns.scale, y1 * args.ns.scale);
     } else {
@@ -609,12 +578,12 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
       put_chunk_end(m, bufs + buf * kBufBytes, col, row, lane);
       buf ^= 1u;
     };
-    // PK_APPLY: a chunk of X, both terms, into one of the two halves of the warp's buffer; PK_SYMM: the factors' chunks
+    // Into one of the two halves of the warp's buffer: a chunk of X, both terms (PK_APPLY), or of A (PK_SYMM)
     float ns_dcol[2] = {0.f, 0.f};
     auto ns_fetch = [&](int ch, int n0, int row, uint32_t h) {
       const int col = n0 + ch * 32;
       if constexpr (kKind == PK_SYMM) {
-        const float d = __ldcg(args.ns.m2.diag + col + lane);
+        const float d = __ldcg(args.ns.diag_in + col + lane);
         if (h) ns_dcol[1] = d;
         else ns_dcol[0] = d;
       }
@@ -628,10 +597,8 @@ pair_product_kernel(const __grid_constant__ PairMaps<PairCfg<kKind, kBN, kFmt, k
             tma_load_2d(b, &maps.m[2], bar, col, row);
             if (args.ns.two_terms) tma_load_2d(b + 2048, &maps.m[3], bar, col, row);
           } else {
-            mbar_arrive_expect_tx(bar, 2048u * (1u + (args.ns.m1.two ? 1u : 0u) + (args.ns.same ? 0u : 1u)));
-            tma_load_2d(b, &maps.m[4], bar, col, row);
-            if (args.ns.m1.two) tma_load_2d(b + 2048, &maps.m[5], bar, col, row);
-            if (!args.ns.same) tma_load_2d(b + 4096, &maps.m[6], bar, col, row);
+            mbar_arrive_expect_tx(bar, 2048u);
+            tma_load_2d(b, &maps.m[3], bar, col, row);
           }
         }
         __syncwarp();
