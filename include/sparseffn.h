@@ -431,7 +431,8 @@ SF_API int sf_gemm_fp4_gated(const void* A, const void* a_scales, const void* Bg
  *       n = S r,  q = dY gamma,  dX = dS + r (q - n mean(q n)) [T, D] (of X and of the residual alike),  dgamma = sum over t of dY n [D], bf16.
  *     Either output may be NULL. dX may be dY or dS itself. With T == 0 dgamma is zero. The same call gives the same bits.
  * Outputs that otherwise share a byte with one another or with an input are refused (SF_ERR_UNSUPPORTED), and so is a negative or NaN eps.
- * workspace (needed with dgamma): sf_rmsnorm_bwd_workspace_size bytes; no status word, nothing to be zeroed. */
+ * workspace (needed with dgamma): sf_rmsnorm_bwd_workspace_size bytes, nothing to be zeroed; the first 256, in which other calls have their status
+ * word, are not touched, so that one buffer can be lent to all of them in turn. */
 SF_API int sf_rmsnorm_fwd(const void* X, int64_t ldx, const void* residual, const void* gamma, int64_t T, int64_t D, float eps, void* sum,
                           void* Y, void* codes, void* scales, float scale, void* rstd, void* stream);
 SF_API int sf_rmsnorm_bwd_workspace_size(int64_t T, int64_t D, size_t* bytes);

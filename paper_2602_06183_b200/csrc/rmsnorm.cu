@@ -22,6 +22,7 @@ namespace {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 28;
 constexpr int64_t kMaxWidth = 32768;
+constexpr size_t kHead = 256;           // of a workspace: the status word of other calls and what they count there, left alone
 constexpr int kBwdCtas = 148;          // of the backward pass, at most: each leaves one row of partial sums of dgamma
 
 // Past the L1: every element is read once. (Not the read-only path: the sum may be written where an input lies.)
@@ -575,7 +576,7 @@ int sf_rmsnorm_fwd(const void* X, int64_t ldx, const void* residual, const void*
 int sf_rmsnorm_bwd_workspace_size(int64_t T, int64_t D, size_t* bytes) {
   SF_TRY(norm_shape(T, D));
   if (!bytes) return SF_ERR_NULL;
-  *bytes = 4 * (size_t)bwd_ctas(T) * (size_t)D;
+  *bytes = kHead + 4 * (size_t)bwd_ctas(T) * (size_t)D;
   return SF_OK;
 }
 
@@ -603,7 +604,8 @@ int sf_rmsnorm_bwd(const void* dY, const void* sum, const void* gamma, const voi
   SF_TRY(check_arch());
   NormBwdArgs a{};
   a.dY = (const uint16_t*)dY; a.S = (const uint16_t*)sum; a.gamma = (const uint16_t*)gamma; a.dS = (const uint16_t*)dS; a.rstd = (const float*)rstd;
-  a.T = T; a.dX = (uint16_t*)dX; a.dgamma = (uint16_t*)dgamma; a.parts = (float*)workspace; a.D = (int)D;
+  a.T = T; a.dX = (uint16_t*)dX; a.dgamma = (uint16_t*)dgamma; a.D = (int)D;
+  a.parts = dgamma ? (float*)((uint8_t*)workspace + kHead) : nullptr;
   if (bwd_once(T, D)) {
     const RowPlan p = once_plan(T, D);
     const int most = T > kBwdCtas ? 512 : 256, groups = p.tpr >= most ? 1 : most / p.tpr;
@@ -636,7 +638,7 @@ int sf_rmsnorm_bwd(const void* dY, const void* sum, const void* gamma, const voi
   }
   SF_TRY(launch_pdl(kern, dim3((unsigned)ctas), (unsigned)threads, smem, s, a));
   if (!dgamma || ctas == 1) return SF_OK;
-  return launch_sum_parts((const float*)workspace, ctas, D, dgamma, s);
+  return launch_sum_parts(a.parts, ctas, D, dgamma, s);
 }
 
 }  // extern "C"
