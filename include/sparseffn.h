@@ -425,8 +425,9 @@ SF_API int sf_gemm_fp4_gated(const void* A, const void* a_scales, const void* Bg
  *                            e4m3(y * (448 / top)), for sf_gemm_fp8_rows; above 2^-96 r falls out of it, and the code is exactly that of
  *                            448 S gamma / max |S gamma|, ties to even. With scales NULL: code = e4m3(y * scale), as sf_fp8_quantize
  *       rstd   float32 [T]   r, for the backward pass
- *     The squares are summed in float32. An infinity makes its own element NaN and the others of its row 0, a NaN its whole row; the scale
- *     of a row with either is NaN, and so are its codes.
+ *     The squares are summed in float32, whose range they can leave: a row with |S| near 2^62 and above has r = 0 and y = 0 everywhere; with eps 0 one
+ *     of 2^-62 and below loses bits of r, and one of 2^-75 and below has r infinite and y NaN or infinite. An infinity makes its own element NaN and
+ *     the others of its row 0, a NaN its whole row; the scale of a row with either is NaN, and so are its codes.
  * sf_rmsnorm_bwd:  dY bf16 [T, D], S and r of the forward call, dS the gradient that comes to S from elsewhere (bf16 [T, D] or NULL):
  *       n = S r,  q = dY gamma,  dX = dS + r (q - n mean(q n)) [T, D] (of X and of the residual alike),  dgamma = sum over t of dY n [D], bf16.
  *     Either output may be NULL. dX may be dY or dS itself. With T == 0 dgamma is zero. The same call gives the same bits.
@@ -485,7 +486,8 @@ SF_API int sf_router_balance_bwd(const void* logits, const void* expert, const v
  * nothing (ten steps, low rank: 1 to 5 %, and tens of percent for a handful of rows), and with the quintic's slope in the others ((4, -8, 3.5), which is
  * steep, five steps, equal rows: up to 16 %). The same call gives the same bits.
  * `workspace`: sf_orthogonalize_workspace_size() bytes, the first 256 the status word as everywhere. Outputs that share a byte with the
- * input are refused (SF_ERR_UNSUPPORTED). */
+ * input are refused (SF_ERR_UNSUPPORTED); a matrix with a leading dimension counts from its first byte to its last, what lies between its rows
+ * included. */
 typedef enum sf_type { SF_BF16 = 0, SF_F32 = 1 } sf_type;
 SF_API int sf_orthogonalize_workspace_size(int64_t rows, int64_t cols, size_t* bytes);
 SF_API int sf_orthogonalize(const void* G, int type, int64_t rows, int64_t cols, int64_t ldg, int steps, float a, float b, float c, float scale,
