@@ -1,7 +1,7 @@
 // All steps of a small orthogonalised update in one launch (see newton_schulz.cu for the iteration, its roundings and its scales).
 //
 // A product of small matrices on CTA pairs is latency: 64 x 512 took 17 launches, 62 us, and 27.5 in one (16 x 16 53 / 16, 64 x 4000 78 / 42,
-// 128 x 512 69 / 52, 128 x 2000 78 / 68; graph replay). Here one cluster of up to 16 CTAs keeps X from the
+// 128 x 512 69 / 52, 128 x 2000 78 / 68; graph replay, four calls to a graph). Here one cluster of up to 16 CTAs keeps X from the
 // first step to the last, every CTA some of its columns: in float32 in the registers of the warps that make them, as fp16 operand in
 // shared memory. What has to cross goes through distributed shared memory, with two cluster barriers a step: the partial sums of A = X X^T
 // over a CTA's columns are sent to the CTAs that add them up, a part each, in the order of the senders; these send the sums to all, and every CTA

@@ -28,7 +28,7 @@ constexpr int64_t kFewTokens = 128;
 inline bool gated_by_few(int fmt, int64_t T, int nkb) { return T <= 64 || (T <= kFewTokens && nkb > (fmt == FMT_BF16 ? 16 : 8)); }
 
 // E4M3 rows: the same, but the pairs' half-empty tiles win where a short reduction leaves little to split and few columns fill the chip either
-// way. Few tokens / pairs, us, in graph replay: 65 to 128 tokens of 8192 x 1024 6.2 to 7.6 / 5.9, of 512 x 512 4.9 to 6.8 / 3.9; but of 16384 x 512
+// way. Few tokens / pairs, us, in graph replay of several calls: 65 to 128 tokens of 8192 x 1024 6.2 to 7.6 / 5.9, of 512 x 512 4.9 to 6.8 / 3.9; but of 16384 x 512
 // 5.5 to 7.4 / 7.2, of 2048 x 2048 4.9 to 5.9 / 7.4, of 8192 x 8192 13.9 to 15.9 / 17.1.
 inline bool rows_by_few(int64_t T, int64_t N, int nkb) { return T <= 64 || (T <= kFewTokens && (nkb > 8 || N > 8192)); }
 

@@ -5,8 +5,9 @@
 // Sums are in float32; S, y, dX and dgamma are rounded once each.
 //
 // Memory bounds them: 8 bytes an element forward (7 with codes) and 8 backward. A row stays in the registers of one group of threads from
-// its load to its store; the only thing that crosses warps is a row's sum. 16384 x 4096: forward 82 us (6.6 TB/s), backward 84 (6.4 TB/s) with the sum of dgamma's parts,
-// each alone. 8192 x 4096 to E4M3 rows 41 (5.7 TB/s). One row of 4096: 4.1, a launch.
+// its load to its store; the only thing that crosses warps is a row's sum. In graph replay (here and below four calls to a graph): 16384 x 4096 forward
+// 82 us (6.6 TB/s), backward 84 (6.4 TB/s) with the sum of dgamma's parts; 8192 x 4096 to E4M3 rows 40.4 (5.8 TB/s); one row of 4096 2.6, a launch. 4096 x
+// 32768 backward 277 (3.9 TB/s): a row's vectors are too many for a second stage of the ring.
 #include "fp8_fmt.cuh"
 #include "gated.cuh"
 #include "sums.cuh"
@@ -95,7 +96,7 @@ constexpr float kLeastProduct = 7.888609052210118e-31f;    // 2^-100
 // A row's own scale takes its largest |y| to 448, and a code is that of 448 S gamma / max |S gamma|: r falls out. S gamma has 16 bits, 448 times it 19, so
 // a quotient that is not half-way between two codes (five bits) is 2^-21 of it away at least. As S gamma times the rounded inverse it is off by 2^-23 of
 // it; rounded to 22 bits, what is half-way is exactly that again, and goes to the even code. (7 in 100 000 of normal rows are. As y * (448 / top), rounded
-// three times, the last bit decided; divided instead, 8192 x 4096 took 51.4 us.) top: the largest |S gamma|. Returns the inverse.
+// three times, the last bit decided. 8192 x 4096 back to back: 41.2 us so, 42.2 in 22 bits, 51.4 with a division.) top: the largest |S gamma|. Returns the inverse.
 __device__ __forceinline__ float row_scale(float r, float top, float* to) {
   const float y_top = max_nan(top * r, kLeastAmax), scale = __fdiv_rn(y_top, 448.f);
   if (to) *to = scale;
@@ -113,8 +114,8 @@ __device__ __forceinline__ uint4 sum_of(const uint4& s, const uint4& t) {
                     pack2(lo32(s.z) + lo32(t.z), hi32(s.z) + hi32(t.z)), pack2(lo32(s.w) + lo32(t.w), hi32(s.w) + hi32(t.w)));
 }
 // The same once more for the rows of a warp, or of a group of several, of which one (far) has a |S gamma| that leaves float32's range or comes near its
-// lower end: S is taken times a power of two near r. It is rare, so it reads S again, and is not inlined: 8192 x 4096 took 45.3 us with S kept for
-// it, 42.8 so, 42.2 with nothing of it.
+// lower end: S is taken times a power of two near r. It is rare, so it reads S again, and is not inlined: 8192 x 4096 took 45.3 us back to back with S kept
+// for it, 42.8 so, 42.2 with nothing of it.
 __device__ __noinline__ void far_row(const NormArgs* a, Group g, int64_t row, int vecs, float r, bool far) {
   const uint4 *x = reinterpret_cast<const uint4*>(a->sum ? a->sum + row * a->D : a->X + row * a->ldx),
               *t = reinterpret_cast<const uint4*>(a->R + row * a->D), *gamma = reinterpret_cast<const uint4*>(a->gamma);
